@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "st_block_keep.h"
+#include "st_host.h"
 #include "st_stage_pool.h"
 #include "st_bloom_kernels.h"
 #include "st_mfma2_kernels.h"
@@ -33,9 +34,10 @@
 // memory that exists from the moment the code object is loaded, one copy per GPU.
 static __device__ __align__(256) unsigned char scratch[ST_STATIC_SCRATCH_BYTES];
 
-namespace {
+namespace st {
 
-thread_local char g_err[512] = "";
+static thread_local char g_err[512] = "";
+thread_local Timing g_timing;
 
 int fail(int code, const char* fmt, ...)
 {
@@ -46,61 +48,19 @@ int fail(int code, const char* fmt, ...)
     return code;
 }
 
-// The C ABI never lets an exception out: host allocations that fail become ST_ENOMEM.
-template <class F>
-int guarded(F&& body)
-{
-    try {
-        return body();
-    } catch (const std::bad_alloc&) {
-        return fail(ST_ENOMEM, "out of host memory");
-    } catch (...) {
-        return fail(ST_EINVAL, "unexpected failure in host code");
-    }
-}
+}  // namespace st
 
-#define ST_HIP(call)                                                                       \
-    do {                                                                                   \
-        hipError_t e_ = (call);                                                            \
-        if (e_ != hipSuccess)                                                              \
-            return fail(e_ == hipErrorOutOfMemory ? ST_ENOMEM : ST_EHIP,                   \
-                        "%s failed: %s (%s:%d)", #call, hipGetErrorString(e_), __FILE__,   \
-                        __LINE__);                                                         \
-    } while (0)
+namespace {
+
+using st::fail;
+using st::g_timing;
+using st::guarded;
+using st::TimedLaunch;
 
 // Test aid: the scorer a search of the calling thread is forced onto (0 auto, 1 wavefront dot
 // product, 2 MFMA where it applies).  Per thread, so that one thread's setting never changes
 // another thread's search.
 thread_local int g_scoring_path = 0;
-
-// Optional per-kernel timing with HIP events recorded on the caller's stream around each launch
-// (state of the calling thread: the thread that begins a measurement makes the calls and ends it).
-struct Timing {
-    bool on = false;
-    std::vector<hipEvent_t> ev;  // pairs: [2i] before, [2i+1] after launch i
-    std::vector<int> kind;       // 0 scan, 1 select, 2 rescue, 3 filter expressions
-    size_t used = 0;             // launches recorded
-    size_t dropped = 0;
-};
-thread_local Timing g_timing;
-
-struct TimedLaunch {
-    hipStream_t stream;
-    bool active;
-    size_t slot;
-    TimedLaunch(int kind, hipStream_t s) : stream(s), active(false), slot(0)
-    {
-        if (!g_timing.on) return;
-        if (2 * (g_timing.used + 1) > g_timing.ev.size()) { ++g_timing.dropped; return; }
-        slot = g_timing.used++;
-        g_timing.kind[slot] = kind;
-        active = hipEventRecord(g_timing.ev[2 * slot], stream) == hipSuccess;
-    }
-    ~TimedLaunch()
-    {
-        if (active) (void)hipEventRecord(g_timing.ev[2 * slot + 1], stream);
-    }
-};
 
 // Pinned staging slots for the per-call tables (st_stage_pool.h): a call owns its slot from
 // stage_get() until the StageHold goes out of scope, by which time a kernel behind the work that reads
@@ -677,7 +637,7 @@ struct st_bloom {
 
 extern "C" {
 
-const char* st_last_error(void) { return g_err; }
+const char* st_last_error(void) { return st::g_err; }
 
 int32_t st_version(void) { return 100; }
 
