@@ -325,6 +325,126 @@ int st_value_model(const float* dev_task_scores, int64_t n, int32_t n_tasks,
                    const int32_t* host_ops, const float* host_consts, int32_t n_ops,
                    float* dev_out, void* hip_stream);
 
+/* ------------------------------------------------------------------ cached histories
+ * Keys and values of users' event histories, resident between requests, and the operators of the attention
+ * models on either side of the search: the User Tower that makes the query embeddings (Sec. 3) and the stacked
+ * attention that re-ranks the retrieved items (Sec. 5.1).  Rows are held as items are: int8 with a scale, here one
+ * fp32 scale for each block of ST_KV_BLOCK tokens and head, for keys and values apart.
+ *
+ * A page holds one block of one sequence, all heads:
+ *   dev_k        [n_pages, n_heads, 64, d] int8        key of token t (position t % 64 of its block) is row t
+ *   dev_v        [n_pages, n_heads, d, 64] int8        value channel c of token t is at [c][slot(t)], where slot is
+ *                                                      t with its bits 5 4 3 2 1 0 in the order 3 2 5 4 1 0
+ *   dev_k_scale, dev_v_scale [n_pages, n_heads] fp32   a held integer stands for integer * scale
+ *   dev_bounds   [n_pages, n_heads, 2, d] int8         per channel the largest and the smallest key of the block
+ * The integers of positions that hold no token are ignored.  d is 64, 96, 128 or 256.  All arrays 16-byte aligned;
+ * the caller owns them.  (The slot order is the order in which a lane of the matrix instruction holds the
+ * weights that multiply the values, so that values go from memory into the product as they lie.) */
+#define ST_KV_BLOCK 64
+#define ST_KV_MAX_BLOCKS 16384  /* blocks of one sequence: 1,048,576 tokens */
+#define ST_KV_MAX_HEADS 1024
+
+typedef enum st_dtype { ST_BF16 = 0, ST_F16 = 1 } st_dtype;
+
+typedef struct st_kv_cache {
+    int8_t* dev_k;
+    int8_t* dev_v;
+    float* dev_k_scale;
+    float* dev_v_scale;
+    int8_t* dev_bounds;
+    int64_t n_pages;  /* 1 .. 2^31 - 1 */
+    int32_t n_heads;  /* heads of keys and values */
+    int32_t d;
+} st_kv_cache;
+
+/* The sequences of a call.  Block b of sequence s lies in page dev_tables[s * max_blocks + b]; sequence s holds
+ * dev_lengths[s] tokens, those of this call among them: the call's n_tok tokens (rows of queries or of new keys) are, sequence
+ * by sequence, the last n_s positions of each, n_s = dev_offsets[s + 1] - dev_offsets[s], or n_tok / n_seq for all where
+ * dev_offsets is NULL.  Lengths, offsets and page numbers are read on the device and not trusted: lengths are cut
+ * to [0, max_len], offsets to [0, n_tok] and max_tok tokens a sequence, and a block whose page is not in
+ * [0, n_pages) counts as masked (append: is skipped).  Two sequences may share pages that no append writes. */
+typedef struct st_kv_batch {
+    const int32_t* dev_tables;   /* [n_seq, max_blocks] */
+    const int32_t* dev_lengths;  /* [n_seq] */
+    const int32_t* dev_offsets;  /* [n_seq + 1], non-decreasing from 0 to n_tok, or NULL */
+    int32_t n_seq;
+    int32_t max_blocks;          /* 1 .. ST_KV_MAX_BLOCKS */
+    int32_t n_tok;
+    int32_t max_tok;             /* no sequence has more tokens in this call (n_tok / n_seq where dev_offsets is NULL) */
+    int32_t max_len;             /* no length is larger; at most 64 * max_blocks */
+} st_kv_batch;
+
+/* Writes the keys and values of the call's tokens into the cache: dev_k_new, dev_v_new are rows
+ * [n_tok, n_heads, d] of dtype, k_stride and v_stride elements apart (multiples of 8, at least n_heads * d), 16-byte
+ * aligned, finite.  Lengths are those after the append.  For each block that receives tokens, keys and values alike:
+ *   a   = largest magnitude of the block's new tokens;  o = its scale so far, 0 where it holds no older token
+ *   s   = max(o, a / 127)            older integers become rint(q * (o / s)), new ones rint(x / s) kept in
+ *                                    [-127, 127] (0 where s is 0); ties to even, all in fp32
+ * and the bounds those of the block's tokens.  A second call with the same arguments changes nothing.  A token before
+ * position 0 (n_s > length) is left out.  One kernel, asynchronous, no allocation. */
+int st_kv_append(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_k_new, int64_t k_stride,
+                 const void* dev_v_new, int64_t v_stride, int32_t dtype, void* hip_stream);
+
+/* Parity/debug export of the last n_blocks blocks of each sequence (all of them where it holds fewer; row j is block
+ * max(0, blocks - n_blocks) + j), in token order and as the values they stand for (integer * scale):
+ * dev_out_k, dev_out_v [n_seq, n_blocks, n_heads, 64, d] fp32, dev_out_bounds [n_seq, n_blocks, n_heads, 2, d] fp32, 16-byte
+ * aligned; each may be NULL.  Zeros where there is no token or block.  The batch's tokens play no part. */
+int st_kv_read(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_blocks, float* dev_out_k,
+               float* dev_out_v, float* dev_out_bounds, void* hip_stream);
+
+/* Attention of the call's tokens over the cache.  Queries have n_q_heads = G * n_heads heads, head h reads the
+ * cache's head h / G.  Token i (0-based) of the n_s tokens of a sequence of length L sees position t iff
+ * t < L (causal 0) or t < L - (n_s - 1 - i) (causal 1), its mask bit is 1, and the position's block is listed:
+ *   x_t = (q . k_t) * softmax_scale;  p = softmax of x over the positions seen;  out = sum_t p_t v_t
+ * A row that sees nothing gives out = 0 and lse = -inf.
+ *   dev_q      [n_tok, n_q_heads, d] of dtype, rows q_stride elements apart, 16-byte aligned
+ *   dev_mask   NULL, or uint64 [n_tok, mask_words], mask_words >= ceil(max_len / 64): bit t % 64 of word t / 64, the
+ *              layout of st_bloom_mask
+ *   dev_blocks NULL (all blocks), or int32 [n_tok, n_heads, n_sel]: the blocks that each token and head of the cache
+ *              reads, each once, in any order; entries out of range are ignored (st_kv_select writes them)
+ *   dev_out    [n_tok, n_q_heads, d] of dtype;  dev_lse NULL or [n_tok, n_q_heads] fp32, log sum exp of x
+ *   dev_mass_out NULL, or [n_seq, n_heads, max_blocks] fp32: for each block of the sequence
+ *              decay * dev_mass_in + the sum of p over its positions and the call's rows of that sequence and head
+ *              (dev_mass_in NULL: 0; may be dev_mass_out itself); 0 behind the sequence's last block
+ *   workspace  st_kv_attend_workspace_bytes() bytes, 256-byte aligned, scratch
+ * Sums, maxima and outputs are accumulated in fp32; the weights are rounded to 11 significant bits before they multiply the values.
+ * softmax_scale and decay are finite.  Asynchronous, no allocation; results do not vary from call to call. */
+int64_t st_kv_attend_workspace_bytes(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads,
+                                     int32_t n_sel, int32_t with_mass);
+int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_q, int64_t q_stride,
+                 int32_t dtype, int32_t n_q_heads, float softmax_scale, int32_t causal, const uint64_t* dev_mask,
+                 int32_t mask_words, const int32_t* dev_blocks, int32_t n_sel, void* dev_out, float* dev_lse,
+                 const float* dev_mass_in, float decay, float* dev_mass_out, void* dev_workspace,
+                 int64_t workspace_bytes, void* hip_stream);
+
+/* Chooses n_sel blocks for each token and head of the cache by a score that reads 2 d bytes of a block in place of its
+ * 128 d: an upper bound of the group's summed logits over the block, in the search's arithmetic.
+ *   u+[c] = sum_g max(q[g][c], 0), u-[c] = sum_g min(q[g][c], 0)   fp32, g ascending over the group's G heads
+ *   both quantised to int8 with one scale, a / 127 with a their largest magnitude (rint(u / scale), 0 where a is 0)
+ *   score_b = (float)(u+ . max_b + u- . min_b) * k_scale_b          int32 sum, one rounded fp32 multiply
+ * Candidates are the blocks in which the token sees a position (length, causal, mask: as st_kv_attend).  Of these the
+ * first `sink` blocks of the sequence and the last `recent` up to the token's last visible position always stay, then the
+ * best by (score desc, block asc).  sink + recent <= n_sel, 1 <= n_sel <= ST_KV_MAX_BLOCKS.
+ * dev_out_blocks int32 [n_tok, n_heads, n_sel]: ascending, -1 behind the last.  Finite queries.  Bit-exact. */
+int64_t st_kv_select_workspace_bytes(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads,
+                                     int32_t n_sel);
+int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_q, int64_t q_stride, int32_t dtype,
+                 int32_t n_q_heads, int32_t causal, const uint64_t* dev_mask, int32_t mask_words, int32_t n_sel,
+                 int32_t sink, int32_t recent, int32_t* dev_out_blocks, void* dev_workspace, int64_t workspace_bytes,
+                 void* hip_stream);
+
+/* Shrinks each sequence to at most `budget` blocks by the weight they drew: the score of a block is the largest of
+ * dev_mass [n_seq, n_heads, max_blocks] (finite, >= 0) over the heads; the first `sink` blocks and the last `recent` stay,
+ * then the best by (score desc, block asc).  1 <= recent, sink + recent <= budget.  Of the batch only tables, lengths
+ * and sizes are used.  What stays keeps its order and closes up:
+ *   dev_out_tables [n_seq, max_blocks] (-1 behind), dev_out_lengths [n_seq] (64 less for each block that goes),
+ *   dev_out_mass [n_seq, n_heads, max_blocks] (0 behind), dev_out_freed [n_seq, max_blocks]: the pages that go, in order (-1
+ *   behind), dev_out_n_freed [n_seq]
+ * Tables, lengths and mass may be updated in place (out = in).  One kernel, asynchronous, no allocation. */
+int st_kv_evict(const st_kv_batch* batch, const float* dev_mass, int32_t n_heads, int32_t budget, int32_t sink,
+                int32_t recent, int32_t* dev_out_tables, int32_t* dev_out_lengths, float* dev_out_mass,
+                int32_t* dev_out_freed, int32_t* dev_out_n_freed, void* hip_stream);
+
 /* Bandwidth probe for benchmarks: one kernel that reads bytes / 16 16-byte pieces of dev_src
  * (16-byte aligned) with `workgroups` workgroups of 256 threads and writes one uint32 per workgroup
  * to dev_sink ([workgroups]).  Its measured rate is the practical HBM read ceiling that the

@@ -24,6 +24,8 @@ EXPORTS = [
     "st_search_overflow_flags_offset", "st_bloom_mask_expr", "st_search_expr_workspace_bytes",
     "st_search_expr", "st_search_ivf_workspace_bytes", "st_search_ivf", "st_quantize_global", "st_value_model",
     "st_search_host_plan", "st_search_host_units", "st_stream_read", "st_search_static",
+    "st_kv_append", "st_kv_read", "st_kv_attend_workspace_bytes", "st_kv_attend", "st_kv_select_workspace_bytes",
+    "st_kv_select", "st_kv_evict",
 ]
 
 ST_OP_LEAF, ST_OP_AND, ST_OP_OR, ST_OP_NOT = 0, 1, 2, 3  # operations of a filter program
@@ -104,6 +106,20 @@ def lib() -> C.CDLL:
         L.st_stream_read.argtypes = [p, i64, p, i32, p]
         L.st_quantize_global.restype = C.c_int
         L.st_quantize_global.argtypes = [p, i64, i32, p, p, p, p, p]
+        L.st_kv_append.restype = C.c_int
+        L.st_kv_append.argtypes = [p, p, p, i64, p, i64, i32, p]
+        L.st_kv_read.restype = C.c_int
+        L.st_kv_read.argtypes = [p, p, i32, p, p, p, p]
+        L.st_kv_attend_workspace_bytes.restype = i64
+        L.st_kv_attend_workspace_bytes.argtypes = [p, p, i32, i32, i32]
+        L.st_kv_attend.restype = C.c_int
+        L.st_kv_attend.argtypes = [p, p, p, i64, i32, i32, C.c_float, i32, p, i32, p, i32, p, p, p, C.c_float, p, p, i64, p]
+        L.st_kv_select_workspace_bytes.restype = i64
+        L.st_kv_select_workspace_bytes.argtypes = [p, p, i32, i32]
+        L.st_kv_select.restype = C.c_int
+        L.st_kv_select.argtypes = [p, p, p, i64, i32, i32, i32, p, i32, i32, i32, i32, p, p, i64, p]
+        L.st_kv_evict.restype = C.c_int
+        L.st_kv_evict.argtypes = [p, p, i32, i32, i32, i32, p, p, p, p, p, p]
         _lib = L
     return _lib
 
@@ -510,3 +526,220 @@ def st_score_pairs(items, item_scale, queries, query_scale, pair_item, pair_quer
                                 _dptr(pair_item), _dptr(pair_query), n, _dptr(dots), _dptr(scores),
                                 _stream(stream)))
     return dots, scores
+
+
+# ------------------------------------------------------------------ cached histories
+
+ST_KV_BLOCK, ST_KV_MAX_BLOCKS, ST_KV_MAX_HEADS = 64, 16384, 1024
+ST_BF16, ST_F16 = 0, 1
+_KV_TYPES = {torch.bfloat16: ST_BF16, torch.float16: ST_F16}
+
+
+class _KvCacheC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "bounds")] + [
+        ("n_pages", C.c_int64), ("n_heads", C.c_int32), ("d", C.c_int32)]
+
+
+class _KvBatchC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("tables", "lengths", "offsets")] + [
+        (n, C.c_int32) for n in ("n_seq", "max_blocks", "n_tok", "max_tok", "max_len")]
+
+
+class KvCache:
+    """Pages of cached keys and values (``st_kv_cache``) on the tensors given: k int8 [pages, heads, 64, d],
+    v int8 [pages, heads, d, 64] (in slot order), k_scale and v_scale fp32 [pages, heads], bounds int8 [pages, heads, 2, d]."""
+
+    def __init__(self, k, v, k_scale, v_scale, bounds):
+        for t, dtype, name in ((k, torch.int8, "k"), (v, torch.int8, "v"), (k_scale, torch.float32, "k_scale"),
+                               (v_scale, torch.float32, "v_scale"), (bounds, torch.int8, "bounds")):
+            _need(t, dtype, name)
+        if k.dim() != 4:
+            raise ValueError("k must be [pages, heads, 64, d]")
+        n, h, b, d = k.shape
+        if b != ST_KV_BLOCK or v.shape != (n, h, d, b) or k_scale.shape != (n, h) or v_scale.shape != (n, h) or bounds.shape != (n, h, 2, d):
+            raise ValueError("shape mismatch")
+        self.k, self.v, self.k_scale, self.v_scale, self.bounds = k, v, k_scale, v_scale, bounds
+        self.n_pages, self.n_heads, self.d = n, h, d
+        self._c = _KvCacheC(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), bounds.data_ptr(), n, h, d)
+        self._p = C.cast(C.pointer(self._c), C.c_void_p)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_heads: int, d: int, device="cuda") -> "KvCache":
+        def new(shape, dtype):
+            return torch.zeros(shape, dtype=dtype, device=device)
+        return cls(new((n_pages, n_heads, ST_KV_BLOCK, d), torch.int8), new((n_pages, n_heads, d, ST_KV_BLOCK), torch.int8),
+                   new((n_pages, n_heads), torch.float32), new((n_pages, n_heads), torch.float32),
+                   new((n_pages, n_heads, 2, d), torch.int8))
+
+
+class KvBatch:
+    """The sequences of a call (``st_kv_batch``): tables int32 [n_seq, max_blocks], lengths int32 [n_seq] (the call's
+    tokens included), n_tok tokens in all; offsets int32 [n_seq + 1] where sequences have different numbers of them, with
+    max_tok a bound on one sequence's (n_tok if not given).  max_len bounds the lengths (64 * max_blocks if not given)."""
+
+    def __init__(self, tables, lengths, n_tok: int, offsets=None, max_tok: int | None = None, max_len: int | None = None):
+        _need(tables, torch.int32, "tables")
+        _need(lengths, torch.int32, "lengths")
+        if tables.dim() != 2 or lengths.numel() != tables.shape[0]:
+            raise ValueError("shape mismatch")
+        n_seq, max_blocks = tables.shape
+        if offsets is not None:
+            _need(offsets, torch.int32, "offsets")
+            if offsets.numel() != n_seq + 1:
+                raise ValueError("offsets must have one more entry than there are sequences")
+        if max_tok is None:
+            max_tok = n_tok if offsets is not None else n_tok // max(n_seq, 1)
+        if max_len is None:
+            max_len = max_blocks * ST_KV_BLOCK
+        self.tables, self.lengths, self.offsets = tables, lengths, offsets
+        self.n_seq, self.max_blocks, self.n_tok, self.max_tok, self.max_len = n_seq, max_blocks, n_tok, max_tok, max_len
+        self._c = _KvBatchC(tables.data_ptr(), lengths.data_ptr(), None if offsets is None else offsets.data_ptr(), n_seq,
+                            max_blocks, n_tok, max_tok, max_len)
+        self._p = C.cast(C.pointer(self._c), C.c_void_p)
+
+
+def _kv_rows(t: torch.Tensor, n_tok: int, d: int, name: str):
+    """Rows [n_tok, heads, d] of a 16-bit type, whole heads side by side; rows may be further apart."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _KV_TYPES):
+        raise TypeError(f"{name} must be a CUDA tensor of torch.bfloat16 or torch.float16")
+    if t.dim() != 3 or t.shape[0] != n_tok or t.shape[2] != d:
+        raise ValueError(f"{name} must be [{n_tok}, heads, {d}]")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d):
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
+    return t.stride(0) if n_tok > 1 else t.shape[1] * d, _KV_TYPES[t.dtype]
+
+
+def _kv_mask(mask, n_tok: int):
+    if mask is None:
+        return None, 0
+    _need(mask, torch.int64, "mask")
+    if mask.dim() != 2 or mask.shape[0] != n_tok:
+        raise ValueError("mask must be [n_tok, words]")
+    return C.c_void_p(mask.data_ptr()), mask.shape[1]
+
+
+def _kv_out(t, shape, dtype, name: str):
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    _need(t, dtype, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}")
+    return t
+
+
+class KvBuffers:
+    """Workspace and outputs of repeated st_kv_attend and st_kv_select calls of one shape: queries like q; n_sel: room
+    for that many selected blocks; mass: room for the blocks' weights."""
+
+    def __init__(self, cache: KvCache, batch: KvBatch, q: torch.Tensor, n_sel: int = 0, mass: bool = False):
+        n_q_heads = q.shape[1]
+        self.nbytes = st_kv_attend_workspace_bytes(cache, batch, n_q_heads, n_sel, mass)
+        self.out = torch.empty((batch.n_tok, n_q_heads, cache.d), dtype=q.dtype, device="cuda")
+        self.blocks = self.mass = None
+        if n_sel:
+            self.nbytes = max(self.nbytes, st_kv_select_workspace_bytes(cache, batch, n_q_heads, n_sel))
+            self.blocks = torch.empty((batch.n_tok, cache.n_heads, n_sel), dtype=torch.int32, device="cuda")
+        if mass:
+            self.mass = torch.empty((batch.n_seq, cache.n_heads, batch.max_blocks), dtype=torch.float32, device="cuda")
+        self.workspace = torch.empty(self.nbytes, dtype=torch.uint8, device="cuda")
+
+
+def st_kv_append(cache: KvCache, batch: KvBatch, k, v, stream=None) -> None:
+    """Writes the batch's tokens (rows [n_tok, heads, d], bf16 or fp16) behind what the sequences held."""
+    ks, dtype = _kv_rows(k, batch.n_tok, cache.d, "k")
+    vs, v_dtype = _kv_rows(v, batch.n_tok, cache.d, "v")
+    if dtype != v_dtype or k.shape[1] != cache.n_heads or v.shape[1] != cache.n_heads:
+        raise ValueError("k and v must be of one type and have the cache's heads")
+    _check(lib().st_kv_append(cache._p, batch._p, k.data_ptr(), ks, v.data_ptr(), vs, dtype, _stream(stream)))
+
+
+def st_kv_read(cache: KvCache, batch: KvBatch, n_blocks: int, stream=None):
+    """The last n_blocks blocks of each sequence as fp32 (k, v [n_seq, n_blocks, heads, 64, d], bounds [.., 2, d])."""
+    shape = (batch.n_seq, n_blocks, cache.n_heads, ST_KV_BLOCK, cache.d)
+    k = torch.empty(shape, dtype=torch.float32, device="cuda")
+    v = torch.empty(shape, dtype=torch.float32, device="cuda")
+    bounds = torch.empty((*shape[:3], 2, cache.d), dtype=torch.float32, device="cuda")
+    _check(lib().st_kv_read(cache._p, batch._p, n_blocks, k.data_ptr(), v.data_ptr(), bounds.data_ptr(), _stream(stream)))
+    return k, v, bounds
+
+
+def st_kv_attend_workspace_bytes(cache: KvCache, batch: KvBatch, n_q_heads: int, n_sel: int = 0, mass: bool = False) -> int:
+    return _check(lib().st_kv_attend_workspace_bytes(cache._p, batch._p, n_q_heads, n_sel, int(mass)))
+
+
+def st_kv_attend(cache: KvCache, batch: KvBatch, q, scale: float | None = None, causal: bool = True, mask=None,
+                 blocks=None, mass=None, decay: float = 1.0, mass_out=None, lse=None, out=None,
+                 buffers: KvBuffers | None = None, stream=None) -> torch.Tensor:
+    """Attention of q [n_tok, n_q_heads, d] over the cache; returns out, like q.  scale: 1 / sqrt(d) if not given.
+    mask int64 [n_tok, words], a bit to a position; blocks int32 [n_tok, heads, n_sel] from st_kv_select.  The blocks'
+    weights go to mass_out (or buffers.mass) where that or mass (the weights so far, times decay) is given; lse fp32
+    [n_tok, n_q_heads] is filled where given."""
+    q_stride, dtype = _kv_rows(q, batch.n_tok, cache.d, "q")
+    n_q_heads, n_sel = q.shape[1], 0
+    mask_p, words = _kv_mask(mask, batch.n_tok)
+    if blocks is not None:
+        _need(blocks, torch.int32, "blocks")
+        if blocks.dim() != 3 or blocks.shape[0] != batch.n_tok or blocks.shape[1] != cache.n_heads:
+            raise ValueError("blocks must be [n_tok, heads, n_sel]")
+        n_sel = blocks.shape[2]
+    shape = (batch.n_seq, cache.n_heads, batch.max_blocks)
+    if mass is not None:
+        mass = _kv_out(mass, shape, torch.float32, "mass")
+    with_mass = mass is not None or mass_out is not None
+    if buffers is not None:
+        out = buffers.out if out is None else out
+        if with_mass and mass_out is None:
+            mass_out = buffers.mass
+        work, nbytes = buffers.workspace, buffers.nbytes
+    else:
+        nbytes = st_kv_attend_workspace_bytes(cache, batch, n_q_heads, n_sel, with_mass)
+        work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    out = _kv_out(out, (batch.n_tok, n_q_heads, cache.d), q.dtype, "out")
+    if with_mass:
+        mass_out = _kv_out(mass_out, shape, torch.float32, "mass_out")
+    if lse is not None:
+        lse = _kv_out(lse, (batch.n_tok, n_q_heads), torch.float32, "lse")
+    _check(lib().st_kv_attend(cache._p, batch._p, q.data_ptr(), q_stride, dtype, n_q_heads,
+                              cache.d ** -0.5 if scale is None else scale, int(causal), mask_p, words,
+                              _dptr(blocks), n_sel, out.data_ptr(), _dptr(lse), _dptr(mass), decay, _dptr(mass_out),
+                              work.data_ptr(), nbytes, _stream(stream)))
+    return out
+
+
+def st_kv_select_workspace_bytes(cache: KvCache, batch: KvBatch, n_q_heads: int, n_sel: int) -> int:
+    return _check(lib().st_kv_select_workspace_bytes(cache._p, batch._p, n_q_heads, n_sel))
+
+
+def st_kv_select(cache: KvCache, batch: KvBatch, q, n_sel: int, causal: bool = True, mask=None, sink: int = 0,
+                 recent: int = 0, out=None, buffers: KvBuffers | None = None, stream=None) -> torch.Tensor:
+    """The n_sel blocks that each token and head of the cache reads: int32 [n_tok, heads, n_sel], ascending, -1 behind."""
+    q_stride, dtype = _kv_rows(q, batch.n_tok, cache.d, "q")
+    n_q_heads = q.shape[1]
+    mask_p, words = _kv_mask(mask, batch.n_tok)
+    if buffers is not None:
+        out = buffers.blocks if out is None else out
+        work, nbytes = buffers.workspace, buffers.nbytes
+    else:
+        nbytes = st_kv_select_workspace_bytes(cache, batch, n_q_heads, n_sel)
+        work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    out = _kv_out(out, (batch.n_tok, cache.n_heads, n_sel), torch.int32, "out")
+    _check(lib().st_kv_select(cache._p, batch._p, q.data_ptr(), q_stride, dtype, n_q_heads, int(causal), mask_p, words, n_sel,
+                              sink, recent, out.data_ptr(), work.data_ptr(), nbytes, _stream(stream)))
+    return out
+
+
+def st_kv_evict(batch: KvBatch, mass, budget: int, sink: int = 0, recent: int = 1, out=None, stream=None):
+    """Cuts each sequence to at most budget blocks by mass fp32 [n_seq, heads, max_blocks].  Returns (tables, lengths,
+    mass, freed, n_freed); out: the tensors to fill, of which tables, lengths and mass may be the batch's own."""
+    _need(mass, torch.float32, "mass")
+    if mass.dim() != 3 or mass.shape[0] != batch.n_seq or mass.shape[2] != batch.max_blocks:
+        raise ValueError("mass must be [n_seq, heads, max_blocks]")
+    rows = (batch.n_seq, batch.max_blocks)
+    given = out if out is not None else (None,) * 5
+    out = tuple(_kv_out(t, shape, dtype, name) for t, shape, dtype, name in zip(
+        given, (rows, (batch.n_seq,), tuple(mass.shape), rows, (batch.n_seq,)),
+        (torch.int32, torch.int32, torch.float32, torch.int32, torch.int32),
+        ("tables", "lengths", "mass", "freed", "n_freed"), strict=True))
+    _check(lib().st_kv_evict(batch._p, mass.data_ptr(), mass.shape[1], budget, sink, recent,
+                             *(t.data_ptr() for t in out), _stream(stream)))
+    return out

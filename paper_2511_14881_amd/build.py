@@ -10,7 +10,7 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(CSRC, "libsilvertorch.so")
-SOURCES = ["silvertorch.hip", "st_mfma_ks1.hip", "st_mfma_ks2.hip", "st_mfma_ks4.hip", "st_mfma_ks8.hip"]
+SOURCES = ["silvertorch.hip", "st_kv.hip", "st_mfma_ks1.hip", "st_mfma_ks2.hip", "st_mfma_ks4.hip", "st_mfma_ks8.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

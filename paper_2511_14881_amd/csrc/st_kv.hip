@@ -1,0 +1,358 @@
+// Entry points on cached histories (silvertorch.h): argument checks, launch shapes and launches.
+#include "st_host.h"
+#include "st_kv_attend_kernels.h"
+#include "st_kv_cache_kernels.h"
+#include "st_plan.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+using st::fail;
+using st::guarded;
+using st::TimedLaunch;
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+int check_batch(const st_kv_batch* b)
+{
+    if (!b) return fail(ST_EINVAL, "null argument");
+    if (b->n_seq < 0 || b->n_tok < 0 || b->max_tok < 0 || b->max_len < 0)
+        return fail(ST_EINVAL, "negative size");
+    if (b->max_blocks < 1 || b->max_blocks > ST_KV_MAX_BLOCKS)
+        return fail(ST_EINVAL, "max_blocks=%d out of range", b->max_blocks);
+    if (b->max_len > b->max_blocks * ST_KV_BLOCK)
+        return fail(ST_EINVAL, "max_len=%d exceeds %d blocks", b->max_len, b->max_blocks);
+    if (b->max_tok > b->n_tok) return fail(ST_EINVAL, "max_tok=%d exceeds n_tok=%d", b->max_tok, b->n_tok);
+    if (b->n_seq == 0 && b->n_tok != 0) return fail(ST_EINVAL, "tokens of no sequence");
+    if (!b->dev_offsets && (int64_t)b->n_seq * b->max_tok != b->n_tok)
+        return fail(ST_EINVAL, "without offsets n_tok has to be n_seq * max_tok");
+    if (b->n_seq > 0 && (!b->dev_tables || !b->dev_lengths)) return fail(ST_EINVAL, "null argument");
+    return ST_OK;
+}
+
+bool known_dim(int32_t d) { return d == 64 || d == 96 || d == 128 || d == 256; }
+
+int check_cache(const st_kv_cache* c, bool keys, bool values)
+{
+    if (!c) return fail(ST_EINVAL, "null argument");
+    if (!known_dim(c->d)) return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", c->d);
+    if (c->n_heads < 1 || c->n_heads > ST_KV_MAX_HEADS) return fail(ST_EINVAL, "n_heads=%d out of range", c->n_heads);
+    if (c->n_pages < 1 || c->n_pages > 0x7FFFFFFFll) return fail(ST_EINVAL, "n_pages=%lld out of range", (long long)c->n_pages);
+    if (!c->dev_k_scale || (keys && !c->dev_k) || (values && (!c->dev_v || !c->dev_v_scale)) || !c->dev_bounds)
+        return fail(ST_EINVAL, "null argument");
+    if (misaligned(c->dev_k) || misaligned(c->dev_v) || misaligned(c->dev_k_scale) || misaligned(c->dev_v_scale) || misaligned(c->dev_bounds))
+        return fail(ST_EINVAL, "misaligned cache (16 B)");
+    return ST_OK;
+}
+
+int check_rows(const char* name, const void* p, int64_t stride, int64_t least, int32_t n)
+{
+    if (n == 0) return ST_OK;
+    if (!p) return fail(ST_EINVAL, "null argument");
+    if (stride < least || stride % 8 != 0 || misaligned(p))
+        return fail(ST_EINVAL, "%s: rows of %lld elements, %lld apart, have to begin at multiples of 16 bytes", name, (long long)least, (long long)stride);
+    return ST_OK;
+}
+
+int check_dtype(int32_t t) { return t == ST_BF16 || t == ST_F16 ? (int)ST_OK : fail(ST_EINVAL, "unknown dtype %d", t); }
+
+int check_heads(const st_kv_cache* c, int32_t n_q_heads)
+{
+    if (n_q_heads < c->n_heads || n_q_heads % c->n_heads != 0 || n_q_heads > 64 * ST_KV_MAX_HEADS)
+        return fail(ST_EINVAL, "n_q_heads=%d is no multiple of n_heads=%d", n_q_heads, c->n_heads);
+    return ST_OK;
+}
+
+int check_mask(const uint64_t* mask, int32_t words, const st_kv_batch* b)
+{
+    if (!mask) return ST_OK;
+    if ((uintptr_t)mask & 7) return fail(ST_EINVAL, "misaligned mask (8 B)");
+    if (words < (b->max_len + 63) / 64) return fail(ST_EINVAL, "mask rows of %d words do not cover max_len=%d", words, b->max_len);
+    return ST_OK;
+}
+
+int check_grid(int64_t groups)  // (a launch has fewer than 2^32 threads)
+{
+    return groups <= 0xFFFFFFll ? (int)ST_OK : fail(ST_EINVAL, "too many rows for one call (%lld workgroups)", (long long)groups);
+}
+
+st::KvCacheView view(const st_kv_cache* c)
+{
+    return {c->dev_k, c->dev_v, c->dev_k_scale, c->dev_v_scale, c->dev_bounds, c->n_pages, c->n_heads};
+}
+st::KvBatchView view(const st_kv_batch* b)
+{
+    return {b->dev_tables, b->dev_lengths, b->dev_offsets, b->n_seq, b->max_blocks, b->n_tok, b->max_tok, b->max_len};
+}
+
+int blocks_of(int32_t tokens) { return (tokens + ST_KV_BLOCK - 1) / ST_KV_BLOCK; }
+
+// body(std::integral_constant<int, d>)
+template <class F>
+int with_dim(int32_t d, F&& body)
+{
+    switch (d) {
+    case 64: return body(std::integral_constant<int, 64>());
+    case 96: return body(std::integral_constant<int, 96>());
+    case 128: return body(std::integral_constant<int, 128>());
+    case 256: return body(std::integral_constant<int, 256>());
+    }
+    return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", d);
+}
+
+struct AttendPlan {
+    int32_t tiles, chunk, splits;
+    int64_t units;
+    int64_t o_bytes, ml_bytes, block_bytes, row_bytes;
+    int64_t groups() const { return units * tiles * splits; }  // and times heads
+    int64_t bytes() const { return o_bytes + ml_bytes + block_bytes + row_bytes; }
+};
+
+// How the blocks of a row are split over workgroups: a function of the call's sizes alone.
+AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_heads, int32_t n_sel, bool mass)
+{
+    AttendPlan p;
+    const int32_t group = n_q_heads / c->n_heads;
+    p.units = n_sel > 0 ? b->n_tok : b->n_seq;
+    p.tiles = (int32_t)(((n_sel > 0 ? 1 : (int64_t)b->max_tok) * group + 15) / 16);
+    const int32_t list = std::max(1, n_sel > 0 ? std::min(n_sel, blocks_of(b->max_len)) : blocks_of(b->max_len));
+    const int32_t entries = n_sel > 0 ? n_sel : list;
+    const int64_t pairs = std::max<int64_t>(1, p.units * p.tiles * c->n_heads);
+    const int64_t want = std::max<int64_t>(1, 4ll * st::kComputeUnits / pairs);
+    int32_t chunk = (int32_t)std::max<int64_t>(8, (list + want - 1) / want);
+    if (chunk >= list) chunk = std::max(entries, 1);
+    p.chunk = chunk;
+    p.splits = (std::max(entries, 1) + chunk - 1) / chunk;
+    const int64_t parts = p.splits > 1 ? p.units * c->n_heads * p.tiles * p.splits * 16 : 0;
+    const int64_t rows = (int64_t)b->n_tok * n_q_heads;
+    p.o_bytes = st::round_up(parts * c->d * 4, 256);
+    p.ml_bytes = st::round_up(parts * 8, 256);
+    p.block_bytes = mass ? st::round_up(rows * entries * 8, 256) : 0;
+    p.row_bytes = mass ? st::round_up(rows * 8, 256) : 0;
+    return p;
+}
+
+template <int D, bool kSelected>
+int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t stream)
+{
+    {
+        TimedLaunch t(0, stream);
+        hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected>), dim3((unsigned)(p.groups() * a.c.n_heads)), dim3(st::kKvThreads), 0, stream, a);
+    }
+    if (p.splits > 1) {
+        TimedLaunch t(1, stream);
+        const int64_t rows = (int64_t)a.b.n_tok * a.c.n_heads * a.group;
+        hipLaunchKernelGGL((st::kv_join_kernel<D, kSelected>), dim3((unsigned)((rows + 3) / 4)), dim3(st::kKvThreads), 0, stream, a);
+    }
+    return ST_OK;
+}
+
+int64_t select_stride(const st_kv_batch* b) { return st::round_up(std::max(1, blocks_of(b->max_len)), 16); }
+
+// Kernels whose dynamic LDS may pass the default limit: the limit is raised once.
+template <class K>
+int allow_lds(K kernel, int bytes)
+{
+    if (bytes > 64 * 1024) ST_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024));
+    return ST_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int st_kv_append(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_k_new, int64_t k_stride,
+                 const void* dev_v_new, int64_t v_stride, int32_t dtype, void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if ((rc = check_cache(cache, true, true)) || (rc = check_batch(batch)) || (rc = check_dtype(dtype))) return rc;
+    const int64_t width = (int64_t)cache->n_heads * cache->d;
+    if ((rc = check_rows("keys", dev_k_new, k_stride, width, batch->n_tok)) ||
+        (rc = check_rows("values", dev_v_new, v_stride, width, batch->n_tok)))
+        return rc;
+    if (batch->n_tok == 0 || batch->max_tok == 0) return ST_OK;
+    st::KvAppendArgs a = {view(cache), view(batch), dev_k_new, dev_v_new, k_stride, v_stride, dtype == ST_BF16,
+                          (batch->max_tok + ST_KV_BLOCK - 2) / ST_KV_BLOCK + 1};
+    const int64_t groups = (int64_t)batch->n_seq * a.touched * cache->n_heads;
+    if ((rc = check_grid(groups))) return rc;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    with_dim(cache->d, [&](auto d) -> int {
+        TimedLaunch t(0, stream);
+        hipLaunchKernelGGL((st::kv_append_kernel<decltype(d)::value>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        return ST_OK;
+    });
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int st_kv_read(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_blocks, float* dev_out_k,
+               float* dev_out_v, float* dev_out_bounds, void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if ((rc = check_cache(cache, true, true)) || (rc = check_batch(batch))) return rc;
+    if (n_blocks < 1 || n_blocks > ST_KV_MAX_BLOCKS) return fail(ST_EINVAL, "n_blocks=%d out of range", n_blocks);
+    if (misaligned(dev_out_k) || misaligned(dev_out_v) || misaligned(dev_out_bounds)) return fail(ST_EINVAL, "misaligned output (16 B)");
+    const int64_t groups = (int64_t)batch->n_seq * n_blocks * cache->n_heads;
+    if ((rc = check_grid(groups))) return rc;
+    if (groups == 0 || (!dev_out_k && !dev_out_v && !dev_out_bounds)) return ST_OK;
+    st::KvReadArgs a = {view(cache), view(batch), n_blocks, dev_out_k, dev_out_v, dev_out_bounds};
+    hipStream_t stream = (hipStream_t)hip_stream;
+    with_dim(cache->d, [&](auto d) -> int {
+        TimedLaunch t(0, stream);
+        hipLaunchKernelGGL((st::kv_read_kernel<decltype(d)::value>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        return ST_OK;
+    });
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int64_t st_kv_attend_workspace_bytes(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads,
+                                     int32_t n_sel, int32_t with_mass)
+{
+    int rc;
+    if (!cache || !batch) return fail(ST_EINVAL, "null argument");
+    if (!known_dim(cache->d) || cache->n_heads < 1 || cache->n_heads > ST_KV_MAX_HEADS) return fail(ST_EINVAL, "bad cache");
+    if ((rc = check_batch(batch)) || (rc = check_heads(cache, n_q_heads))) return rc;
+    if (n_sel < 0 || n_sel > ST_KV_MAX_BLOCKS) return fail(ST_EINVAL, "n_sel=%d out of range", n_sel);
+    return std::max<int64_t>(256, attend_plan(cache, batch, n_q_heads, n_sel, with_mass != 0).bytes());
+}
+
+int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_q, int64_t q_stride,
+                 int32_t dtype, int32_t n_q_heads, float softmax_scale, int32_t causal, const uint64_t* dev_mask,
+                 int32_t mask_words, const int32_t* dev_blocks, int32_t n_sel, void* dev_out, float* dev_lse,
+                 const float* dev_mass_in, float decay, float* dev_mass_out, void* dev_workspace,
+                 int64_t workspace_bytes, void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if ((rc = check_cache(cache, true, true)) || (rc = check_batch(batch)) || (rc = check_dtype(dtype)) ||
+        (rc = check_heads(cache, n_q_heads)) || (rc = check_mask(dev_mask, mask_words, batch)) ||
+        (rc = check_rows("queries", dev_q, q_stride, (int64_t)n_q_heads * cache->d, batch->n_tok)))
+        return rc;
+    if (!std::isfinite(softmax_scale) || !std::isfinite(decay)) return fail(ST_EINVAL, "softmax_scale and decay have to be finite");
+    if (dev_blocks ? n_sel < 1 || n_sel > ST_KV_MAX_BLOCKS : n_sel != 0) return fail(ST_EINVAL, "n_sel=%d out of range", n_sel);
+    if (batch->n_tok > 0 && !dev_out) return fail(ST_EINVAL, "null argument");
+    if (misaligned(dev_out) || ((uintptr_t)dev_lse & 3) || ((uintptr_t)dev_blocks & 3)) return fail(ST_EINVAL, "misaligned buffer (output 16 B)");
+    if (dev_mass_in && !dev_mass_out) return fail(ST_EINVAL, "dev_mass_in without dev_mass_out");
+    const bool mass = dev_mass_out != nullptr;
+    const AttendPlan p = attend_plan(cache, batch, n_q_heads, n_sel, mass);
+    if (p.bytes() > 0 && (!dev_workspace || workspace_bytes < p.bytes()))
+        return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)p.bytes());
+    if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
+    if ((rc = check_grid(p.groups() * cache->n_heads)) || (rc = check_grid((int64_t)batch->n_tok * n_q_heads))) return rc;
+    const int32_t entries = n_sel > 0 ? n_sel : std::max(1, blocks_of(batch->max_len));
+    char* ws = (char*)dev_workspace;
+    st::KvAttendArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
+                          softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse,
+                          p.chunk, p.splits, p.tiles, (float*)ws, (float2*)(ws + p.o_bytes),
+                          mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, entries,
+                          mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr};
+    hipStream_t stream = (hipStream_t)hip_stream;
+    if (batch->n_tok > 0 && batch->max_tok > 0)
+        with_dim(cache->d, [&](auto d) -> int {
+            return n_sel > 0 ? launch_attend<decltype(d)::value, true>(a, p, stream) : launch_attend<decltype(d)::value, false>(a, p, stream);
+        });
+    if (mass && batch->n_seq > 0) {
+        st::KvMassArgs m = {a, dev_mass_in, decay, dev_mass_out};
+        const int64_t sh = (int64_t)batch->n_seq * cache->n_heads;
+        const int chunks = (batch->max_blocks + st::kKvThreads - 1) / st::kKvThreads;
+        if ((rc = check_grid(sh * chunks))) return rc;
+        if (n_sel > 0 && (rc = allow_lds(&st::kv_mass_selected_kernel, batch->max_blocks * 4))) return rc;
+        TimedLaunch t(1, stream);
+        if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, dim3((unsigned)sh), dim3(st::kKvThreads), batch->max_blocks * 4, stream, m);
+        else hipLaunchKernelGGL(st::kv_mass_kernel, dim3((unsigned)(sh * chunks)), dim3(st::kKvThreads), 0, stream, m);
+    }
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int64_t st_kv_select_workspace_bytes(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads, int32_t n_sel)
+{
+    int rc;
+    if (!cache || !batch) return fail(ST_EINVAL, "null argument");
+    if (!known_dim(cache->d) || cache->n_heads < 1 || cache->n_heads > ST_KV_MAX_HEADS) return fail(ST_EINVAL, "bad cache");
+    if ((rc = check_batch(batch)) || (rc = check_heads(cache, n_q_heads))) return rc;
+    if (n_sel < 1 || n_sel > ST_KV_MAX_BLOCKS) return fail(ST_EINVAL, "n_sel=%d out of range", n_sel);
+    return std::max<int64_t>(256, st::round_up((int64_t)batch->n_tok * cache->n_heads * select_stride(batch) * 4, 256));
+}
+
+int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_q, int64_t q_stride, int32_t dtype,
+                 int32_t n_q_heads, int32_t causal, const uint64_t* dev_mask, int32_t mask_words, int32_t n_sel,
+                 int32_t sink, int32_t recent, int32_t* dev_out_blocks, void* dev_workspace, int64_t workspace_bytes,
+                 void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if ((rc = check_cache(cache, false, false)) || (rc = check_batch(batch)) || (rc = check_dtype(dtype)) ||
+        (rc = check_heads(cache, n_q_heads)) || (rc = check_mask(dev_mask, mask_words, batch)) ||
+        (rc = check_rows("queries", dev_q, q_stride, (int64_t)n_q_heads * cache->d, batch->n_tok)))
+        return rc;
+    if (n_sel < 1 || n_sel > ST_KV_MAX_BLOCKS) return fail(ST_EINVAL, "n_sel=%d out of range", n_sel);
+    if (sink < 0 || recent < 0 || (int64_t)sink + recent > n_sel) return fail(ST_EINVAL, "sink=%d and recent=%d exceed n_sel=%d", sink, recent, n_sel);
+    if (batch->n_tok > 0 && !dev_out_blocks) return fail(ST_EINVAL, "null argument");
+    if ((uintptr_t)dev_out_blocks & 3) return fail(ST_EINVAL, "misaligned output (4 B)");
+    const int64_t need = st_kv_select_workspace_bytes(cache, batch, n_q_heads, n_sel);
+    if (need < 0) return (int)need;
+    if (!dev_workspace || workspace_bytes < need)
+        return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+    if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
+    if (batch->n_tok == 0 || batch->max_tok == 0) return ST_OK;
+    const int32_t blocks = std::max(1, blocks_of(batch->max_len));
+    st::KvSelectArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
+                          dev_mask, mask_words, n_sel, sink, recent, (batch->max_tok + 15) / 16,
+                          (blocks + st::kKvScoreBlocks - 1) / st::kKvScoreBlocks, select_stride(batch),
+                          (uint32_t*)dev_workspace, dev_out_blocks};
+    const int64_t groups = (int64_t)batch->n_seq * cache->n_heads * a.tiles * a.chunks;
+    const int64_t rows = (int64_t)batch->n_tok * cache->n_heads;
+    if ((rc = check_grid(groups)) || (rc = check_grid(rows))) return rc;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    with_dim(cache->d, [&](auto d) -> int {
+        TimedLaunch t(0, stream);
+        hipLaunchKernelGGL((st::kv_score_kernel<decltype(d)::value>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        return ST_OK;
+    });
+    const int lds = blocks * 4;
+    if ((rc = allow_lds(&st::kv_choose_kernel, lds))) return rc;
+    {
+        TimedLaunch t(1, stream);
+        hipLaunchKernelGGL(st::kv_choose_kernel, dim3((unsigned)rows), dim3(st::kKvThreads), lds, stream, a);
+    }
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int st_kv_evict(const st_kv_batch* batch, const float* dev_mass, int32_t n_heads, int32_t budget, int32_t sink,
+                int32_t recent, int32_t* dev_out_tables, int32_t* dev_out_lengths, float* dev_out_mass,
+                int32_t* dev_out_freed, int32_t* dev_out_n_freed, void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if ((rc = check_batch(batch))) return rc;
+    if (n_heads < 1 || n_heads > ST_KV_MAX_HEADS) return fail(ST_EINVAL, "n_heads=%d out of range", n_heads);
+    if (recent < 1 || sink < 0 || (int64_t)sink + recent > budget)
+        return fail(ST_EINVAL, "budget=%d, sink=%d, recent=%d: recent is at least 1 and both fit the budget", budget, sink, recent);
+    if (batch->n_seq == 0) return ST_OK;
+    if (!dev_mass || !dev_out_tables || !dev_out_lengths || !dev_out_mass || !dev_out_freed || !dev_out_n_freed)
+        return fail(ST_EINVAL, "null argument");
+    st::KvEvictArgs a = {view(batch), dev_mass, n_heads, budget, sink, recent, dev_out_tables, dev_out_lengths, dev_out_mass,
+                         dev_out_freed, dev_out_n_freed};
+    const int lds = batch->max_blocks * 8;
+    if ((rc = allow_lds(&st::kv_evict_kernel, lds))) return rc;
+    {
+        TimedLaunch t(1, (hipStream_t)hip_stream);
+        hipLaunchKernelGGL(st::kv_evict_kernel, dim3((unsigned)batch->n_seq), dim3(st::kKvThreads), lds, (hipStream_t)hip_stream, a);
+    }
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+}  // extern "C"
