@@ -120,7 +120,7 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int32_t list = std::max(1, n_sel > 0 ? std::min(n_sel, blocks_of(b->max_len)) : blocks_of(b->max_len));
     const int32_t entries = n_sel > 0 ? n_sel : list;
     const int64_t pairs = std::max<int64_t>(1, p.units * p.tiles * c->n_heads);
-    const int64_t want = std::max<int64_t>(1, 4ll * st::kComputeUnits / pairs);
+    const int64_t want = std::max<int64_t>(1, (8ll * st::kComputeUnits + pairs - 1) / pairs);
     int32_t chunk = (int32_t)std::max<int64_t>(8, (list + want - 1) / want);
     if (chunk >= list) chunk = std::max(entries, 1);
     p.chunk = chunk;
@@ -144,7 +144,8 @@ int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t st
     if (p.splits > 1) {
         TimedLaunch t(1, stream);
         const int64_t rows = (int64_t)a.b.n_tok * a.c.n_heads * a.group;
-        hipLaunchKernelGGL((st::kv_join_kernel<D, kSelected>), dim3((unsigned)((rows + 3) / 4)), dim3(st::kKvThreads), 0, stream, a);
+        if (p.splits >= 16) hipLaunchKernelGGL((st::kv_join_kernel<D, kSelected, 4>), dim3((unsigned)rows), dim3(st::kKvThreads), 0, stream, a);
+        else hipLaunchKernelGGL((st::kv_join_kernel<D, kSelected, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(st::kKvThreads), 0, stream, a);
     }
     return ST_OK;
 }

@@ -7,8 +7,9 @@
 //
 // Integers are exact as 16-bit floats.  A query row is scaled by a power of two so that its largest magnitude is near
 // 2^14 (exact but for values 2^-38 of that), the key scale of the block and the softmax scale multiply the logits in fp32.
-// Weights are exp2(x - m + 14): 11 significant bits from 2^14 down to 2^-14 (a 16-bit float's denormals
-// come below 2^-28 of the row's largest weight), and the sum of the weights is of the unrounded ones, in fp32.
+// Weights are exp2(x - m + 8) with m a maximum that follows the row's largest logit at a distance of at most 7, so that the sums are
+// seldom rescaled: 11 significant bits from 2^15 down to 2^-14 (a 16-bit float's denormals come below 2^-22 of the row's
+// largest weight), and the sum of the weights is of the unrounded ones, in fp32.
 #pragma once
 #include "st_kv_device.h"
 
@@ -34,7 +35,8 @@ struct KvAttendArgs {
     float2* row_ml;     // [n_tok, n_q_heads]: final maximum and sum, written where block_ml is
 };
 
-constexpr float kKvLift = 14.0f;  // weights are 2^14 times themselves
+constexpr float kKvLift = 8.0f;   // weights are 2^8 times themselves,
+constexpr float kKvSlack = 7.0f;  // and the maximum they go by may lie 7 (in powers of two) below the largest logit
 
 // What a tile of 16 rows of a unit (a sequence, or a token whose blocks were selected) and a head reads.
 struct KvTile {
@@ -48,6 +50,7 @@ struct KvTile {
     int lim_all;    // all valid rows of the tile see those below this one
     int n_blocks;   // blocks that any row of the tile sees
     int n_list;     // entries to go through: blocks, or what was selected
+    int64_t tok_unit, tok_first, tok_last;  // first token of the unit; first and last token of the tile
 };
 
 template <bool kSelected>
@@ -71,6 +74,9 @@ __device__ inline KvTile kv_tile(const KvAttendArgs& a, int unit, int head, int 
     const int lim_max = tile * 16 < t.rows && mine ? max(0, a.causal ? q.len - (past - i_last) : q.len) : 0;
     t.n_blocks = (lim_max + kKvBlock - 1) / kKvBlock;
     t.n_list = kSelected ? a.n_sel : t.n_blocks;
+    t.tok_unit = kSelected ? unit : q.first;
+    t.tok_first = kSelected ? unit : (int64_t)q.first + i_first;
+    t.tok_last = kSelected ? unit : (int64_t)q.first + i_last;
     return t;
 }
 
@@ -79,6 +85,7 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
 {
     constexpr int kSteps = D / 32, kWide = D / 64, kCh = D / 16;
     constexpr bool kHalf = D % 64 != 0;
+    constexpr bool kAhead = D <= 128;  // keys of the next block and values of this one are loaded ahead (256: too few registers)
     __shared__ float s_o[4][16][D + 4];
     __shared__ float2 s_ml[4][16];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
@@ -113,8 +120,8 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
         top = max_over_16_32(top);
         int e = top > 0.0f ? ilogbf(top) : 0;
         e = min(max(e, -100), 120);
-        const float up = ldexpf(1.0f, 13 - e);
-        factor = a.scale_log2 * ldexpf(1.0f, e - 13);
+        const float up = ldexpf(a.scale_log2 < 0.0f ? -1.0f : 1.0f, 13 - e);
+        factor = fabsf(a.scale_log2) * ldexpf(1.0f, e - 13);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
 #pragma unroll
@@ -134,49 +141,70 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
             block = kSelected ? a.blocks[((int64_t)unit * a.c.n_heads + head) * a.n_sel + j] : j;
             if (block >= 0 && block < t.n_blocks) page = kv_page(a.c, a.b, t.seq, block);
         }
+        if (a.mask && page >= 0) {  // a block that no row of the tile sees is not read
+            uint64_t any = 0;
+            for (int64_t tok = t.tok_first; tok <= t.tok_last; ++tok) any |= a.mask[tok * a.mask_words + block];
+            if (any == 0) page = -1;
+        }
+        if (a.block_ml && j < je && page < 0)
+            for (int r = 0; r < 16 && tile * 16 + r < t.rows; ++r) {
+                const int row = tile * 16 + r, i = kSelected ? 0 : row / a.group;
+                a.block_ml[((t.tok_unit + i) * a.c.n_heads * a.group + head * a.group + (row - i * a.group)) * a.block_stride + j] = make_float2(0.0f, 0.0f);
+            }
         const int64_t ph_l = (int64_t)max(page, 0) * a.c.n_heads + head;
         const float ks_l = page >= 0 ? a.c.k_scale[ph_l] : 0.0f, vs_l = page >= 0 ? a.c.v_scale[ph_l] : 0.0f;
-        const int n_it = min(64, max(0, (je - j0 - w + 3) / 4));
-        for (int it = 0; it < n_it; ++it) {
-            const int pg = (int)lane_value((uint32_t)page, it);
-            const int b = (int)lane_value((uint32_t)block, it);
-            float2* bml = a.block_ml ? a.block_ml + (t.tok * a.c.n_heads * a.group + t.q_head) * a.block_stride + (j0 + 4 * it + w) : nullptr;
+        uint64_t todo = ballot(page >= 0);
+        if (todo == 0) continue;
+        int it = __builtin_ctzll(todo);
+        uint4 kw[4][kWide ? kWide : 1];
+        uint2 kh[4];
+        auto load_keys = [&](int from) {
+            const int64_t at_page = (int64_t)(int)lane_value((uint32_t)page, from) * a.c.n_heads + head;
+            const int8_t* kp = a.c.k + at_page * (D * kKvBlock) + n * D;
+#pragma unroll
+            for (int tt = 0; tt < 4; ++tt) {
+#pragma unroll
+                for (int c = 0; c < kWide; ++c) kw[tt][c] = *(const uint4*)(kp + tt * 16 * D + c * 64 + g * 16);
+                if (kHalf) kh[tt] = *(const uint2*)(kp + tt * 16 * D + kWide * 64 + g * 8);
+            }
+        };
+        if (kAhead) load_keys(it);
+        while (todo) {
+            const int cur = it;
+            todo &= todo - 1;
+            it = todo ? __builtin_ctzll(todo) : -1;
+            const int b = (int)lane_value((uint32_t)block, cur);
+            const int64_t ph = (int64_t)(int)lane_value((uint32_t)page, cur) * a.c.n_heads + head;
+            const int8_t* vp = a.c.v + ph * (D * kKvBlock) + n * kKvBlock + g * 16;
+            uint4 vw[kCh];
+            if (kAhead) {
+#pragma unroll
+                for (int c = 0; c < kCh; ++c) vw[c] = *(const uint4*)(vp + c * 16 * kKvBlock);
+            } else {
+                load_keys(cur);
+            }
             uint64_t see = ~0ull;
-            bool part = false;
-            if (pg >= 0 && (a.mask || (b + 1) * kKvBlock > t.lim_all)) {
-                part = true;
+            const bool part = a.mask || (b + 1) * kKvBlock > t.lim_all;
+            if (part) {
                 const int left = t.lim - b * kKvBlock;
                 see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
                 if (a.mask && see) see &= a.mask[t.tok * a.mask_words + b];
             }
-            if (pg < 0 || (part && ballot(see != 0) == 0)) {
-                if (bml && g == 0 && t.valid) *bml = make_float2(0.0f, 0.0f);
-                continue;
-            }
-            const int64_t ph = (int64_t)pg * a.c.n_heads + head;
-            const int8_t* kp = a.c.k + ph * (D * kKvBlock) + n * D;
-            const int8_t* vp = a.c.v + ph * (D * kKvBlock) + n * kKvBlock + g * 16;
-            const float ks = __uint_as_float(lane_value(__float_as_uint(ks_l), it)) * factor;
-            const float vs = __uint_as_float(lane_value(__float_as_uint(vs_l), it));
             float4v x[4];
 #pragma unroll
             for (int tt = 0; tt < 4; ++tt) {
                 x[tt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int c = 0; c < kWide; ++c) {
-                    const uint4 r = *(const uint4*)(kp + tt * 16 * D + c * 64 + g * 16);
-                    x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(r.x, r.y), q[2 * c], x[tt], 0, 0, 0);
-                    x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(r.z, r.w), q[2 * c + 1], x[tt], 0, 0, 0);
+                    x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(kw[tt][c].x, kw[tt][c].y), q[2 * c], x[tt], 0, 0, 0);
+                    x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(kw[tt][c].z, kw[tt][c].w), q[2 * c + 1], x[tt], 0, 0, 0);
                 }
-                if (kHalf) {
-                    const uint2 r = *(const uint2*)(kp + tt * 16 * D + kWide * 64 + g * 8);
-                    x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(r.x, r.y), q[kSteps - 1], x[tt], 0, 0, 0);
-                }
+                if (kHalf) x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(kh[tt].x, kh[tt].y), q[kSteps - 1], x[tt], 0, 0, 0);
             }
-#pragma unroll
-            for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[tt][r] *= ks;
+            if (kAhead && it >= 0) load_keys(it);  // the next block's, behind this one's products
+            // (a scale or a factor of zero gives logits of next to nothing, and -inf stays what it is)
+            const float ks = fmaxf(__uint_as_float(lane_value(__float_as_uint(ks_l), cur)) * factor, 1e-37f);
+            const float vs = __uint_as_float(lane_value(__float_as_uint(vs_l), cur));
             if (part) {
                 const uint64_t mine = see >> (g * 4);
 #pragma unroll
@@ -190,33 +218,42 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
             for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) top = fmaxf(top, x[tt][r]);
-            const float m_new = fmaxf(m, max_over_16_32(top));
-            const float base = m_new == -__builtin_inff() ? 0.0f : m_new - kKvLift;
-            const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-            m = m_new;
+            top = max_over_16_32(top) * ks;
+            if (ballot(top > m + kKvSlack) != 0) {
+                const float m_new = top > m + kKvSlack ? top : m;
+                const float alpha = m_new == m ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+                m = m_new;
+                l *= alpha;
+#pragma unroll
+                for (int c = 0; c < kCh; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[c][r] *= alpha;
+            }
+            const float base = m == -__builtin_inff() ? 0.0f : kKvLift - m;
             float sum = 0.0f;
             half8 p[2];
 #pragma unroll
             for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(x[tt][r] - base);
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tt][r], ks, base));
                     sum += e;
                     p[tt / 2][tt % 2 * 4 + r] = (_Float16)e;
                 }
-            l = l * alpha + sum;
-            if (bml) {
+            l += sum;
+            if (a.block_ml) {
                 const float all = sum_over_16_32(sum);
-                if (g == 0 && t.valid) *bml = make_float2(m, all);
+                if (g == 0 && t.valid)
+                    a.block_ml[(t.tok * a.c.n_heads * a.group + t.q_head) * a.block_stride + (j0 + 4 * cur + w)] = make_float2(m, all);
             }
 #pragma unroll
             for (int c = 0; c < kCh; ++c) {
-                const uint4 r = *(const uint4*)(vp + c * 16 * kKvBlock);
+                if (!kAhead) vw[c] = *(const uint4*)(vp + c * 16 * kKvBlock);
                 float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
-                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(r.x, r.y), p[0], y, 0, 0, 0);
-                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(r.z, r.w), p[1], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(vw[c].x, vw[c].y), p[0], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(vw[c].z, vw[c].w), p[1], y, 0, 0, 0);
 #pragma unroll
-                for (int r4 = 0; r4 < 4; ++r4) o[c][r4] = o[c][r4] * alpha + y[r4] * vs;
+                for (int r = 0; r < 4; ++r) o[c][r] = __builtin_fmaf(y[r], vs, o[c][r]);
             }
         }
     }
@@ -252,8 +289,8 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
             if (c == 0) a.part_ml[part * 16 + r] = make_float2(top, sum);
             continue;
         }
-        const KvTile tr = kv_tile<kSelected>(a, unit, head, tile, r);
-        const int64_t place = tr.tok * heads_all + tr.q_head;
+        const int of = kSelected ? 0 : row / a.group;
+        const int64_t place = (t.tok_unit + of) * heads_all + head * a.group + (row - of * a.group);
         const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
         uint32_t h[4];
 #pragma unroll
@@ -266,44 +303,67 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
     }
 }
 
-// Joins the splits of a row.  One wavefront to a row.
-template <int D, bool kSelected>
+// Joins the splits of a row: kWaves wavefronts to a row, each lane a quarter of four channels' sums over every
+// (kWaves * 256 / D)-th split.
+template <int D, bool kSelected, int kWaves>
 __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
 {
-    constexpr int kPer = D / 64 ? (D + 63) / 64 : 1;  // channels of a lane
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    constexpr int kLanes = D / 4, kTeam = kWaves * 64, kParts = kTeam / kLanes;  // (D = 96: 24 lanes, 16 of 256 idle)
+    constexpr int kRows = kKvThreads / kTeam;
+    __shared__ float4v s_y[kRows][kParts][kLanes];
+    __shared__ float s_top[kRows][kWaves];
+    __shared__ float s_sum[kRows][kParts];
+    const int team = threadIdx.x / kTeam, me = threadIdx.x % kTeam, lane = me & 63;
     const int64_t heads_all = (int64_t)a.c.n_heads * a.group;
-    const int64_t place = (int64_t)blockIdx.x * 4 + w;
-    if (place >= a.b.n_tok * heads_all) return;
-    const int tok = (int)(place / heads_all), qh = (int)(place % heads_all), head = qh / a.group;
+    const int64_t place = (int64_t)blockIdx.x * kRows + team;
+    const bool there = place < a.b.n_tok * heads_all;
+    const int tok = there ? (int)(place / heads_all) : 0, qh = there ? (int)(place % heads_all) : 0, head = qh / a.group;
     const int s = kv_seq_of(a.b, tok);
     const KvSeq q = kv_seq(a.b, s);
-    if (tok < q.first || tok >= q.first + q.count) return;
+    const bool mine = there && tok >= q.first && tok < q.first + q.count;
     const int unit = kSelected ? tok : s;
-    const int row = kSelected ? qh % a.group : (tok - q.first) * a.group + qh % a.group, tile = row / 16;
+    const int row = !mine ? 0 : kSelected ? qh % a.group : (tok - q.first) * a.group + qh % a.group, tile = row / 16;
     const KvTile t = kv_tile<kSelected>(a, unit, head, tile, row % 16);
-    const int splits = min(a.splits, max(1, (t.n_list + a.chunk - 1) / a.chunk));
+    const int splits = mine ? min(a.splits, max(1, (t.n_list + a.chunk - 1) / a.chunk)) : 0;
     const int64_t part = (((int64_t)unit * a.c.n_heads + head) * a.tiles + tile) * a.splits * 16 + row % 16;
     float top = -__builtin_inff();
-    for (int i = lane; i < splits; i += 64) top = fmaxf(top, a.part_ml[part + (int64_t)i * 16].x);
+    for (int i = me; i < splits; i += kTeam) top = fmaxf(top, a.part_ml[part + (int64_t)i * 16].x);
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-    float sum = 0.0f, y[kPer];
+    if (lane == 0) s_top[team][me >> 6] = top;
+    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) y[u] = 0.0f;
-    for (int i = 0; i < splits; ++i) {
-        const float2 ml = a.part_ml[part + (int64_t)i * 16];
-        const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
-        sum += ml.y * f;
-        const float* src = a.part_o + (part + (int64_t)i * 16) * D;
+    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_top[team][k]);
+    const int c = me % kLanes, from = me / kLanes;
+    float sum = 0.0f;
+    float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (from < kParts) {
+#pragma unroll 4
+        for (int i = from; i < splits; i += kParts) {
+            const float2 ml = a.part_ml[part + (int64_t)i * 16];
+            const float4v v = *(const float4v*)(a.part_o + (part + (int64_t)i * 16) * D + c * 4);
+            const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
+            sum = __builtin_fmaf(ml.y, f, sum);
 #pragma unroll
-        for (int u = 0; u < kPer; ++u)
-            if (u * 64 + lane < D) y[u] += src[u * 64 + lane] * f;
+            for (int u = 0; u < 4; ++u) y[u] = __builtin_fmaf(v[u], f, y[u]);
+        }
+        s_y[team][from][c] = y;
+        if (c == 0) s_sum[team][from] = sum;
+    }
+    __syncthreads();
+    if (!mine || from != 0) return;
+#pragma unroll
+    for (int k = 1; k < kParts; ++k) {
+        const float4v v = s_y[team][k][c];
+        sum += s_sum[team][k];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] += v[u];
     }
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    uint32_t h[4];
 #pragma unroll
-    for (int u = 0; u < kPer; ++u)
-        if (u * 64 + lane < D) ((uint16_t*)a.out)[place * D + u * 64 + lane] = (uint16_t)to_16_bits(y[u] * inv, a.bf16 != 0);
-    if (lane == 0) {
+    for (int u = 0; u < 4; ++u) h[u] = to_16_bits(y[u] * inv, a.bf16 != 0);
+    *(uint2*)((uint16_t*)a.out + place * D + c * 4) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+    if (c == 0) {
         if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(sum)) * 0.69314718056f;
         if (a.row_ml) a.row_ml[place] = make_float2(top, sum);
     }
