@@ -2,6 +2,7 @@
 #include "st_host.h"
 #include "st_kv_attend_kernels.h"
 #include "st_kv_cache_kernels.h"
+#include "st_kv_rows_kernels.h"
 #include "st_plan.h"
 
 #include <algorithm>
@@ -102,35 +103,48 @@ int with_dim(int32_t d, F&& body)
     return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", d);
 }
 
+#ifndef KV_RT
+#define KV_RT 1
+#define KV_W 8
+#define KV_WANT 4ll
+#endif
+constexpr int row_tiles(int d) { return d > 128 ? 1 : KV_RT; }
+constexpr int kRowWaves = KV_W;
+
 struct AttendPlan {
-    int32_t tiles, chunk, splits;
+    bool many;          // the kernel for many rows
+    int32_t tile_rows, tiles, chunk, splits, rows_pad, entries;
     int64_t units;
     int64_t o_bytes, ml_bytes, block_bytes, row_bytes;
     int64_t groups() const { return units * tiles * splits; }  // and times heads
     int64_t bytes() const { return o_bytes + ml_bytes + block_bytes + row_bytes; }
 };
 
-// How the blocks of a row are split over workgroups: a function of the call's sizes alone.
+// Which kernel, and how the blocks of a row are split over workgroups: a function of the call's sizes alone.
 AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_heads, int32_t n_sel, bool mass)
 {
     AttendPlan p;
     const int32_t group = n_q_heads / c->n_heads;
+    const int64_t rows = (n_sel > 0 ? 1 : (int64_t)b->max_tok) * group;  // of a unit and head
     p.units = n_sel > 0 ? b->n_tok : b->n_seq;
-    p.tiles = (int32_t)(((n_sel > 0 ? 1 : (int64_t)b->max_tok) * group + 15) / 16);
+    p.many = n_sel == 0 && rows > 32;
+    p.tile_rows = p.many ? row_tiles(c->d) * kRowWaves * 32 : 16;
+    p.tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
+    p.rows_pad = (int32_t)st::round_up(rows, 16);
     const int32_t list = std::max(1, n_sel > 0 ? std::min(n_sel, blocks_of(b->max_len)) : blocks_of(b->max_len));
-    const int32_t entries = n_sel > 0 ? n_sel : list;
+    p.entries = n_sel > 0 ? n_sel : list;
     const int64_t pairs = std::max<int64_t>(1, p.units * p.tiles * c->n_heads);
-    const int64_t want = std::max<int64_t>(1, (8ll * st::kComputeUnits + pairs - 1) / pairs);
+    const int64_t want = std::max<int64_t>(1, ((p.many ? KV_WANT : 8ll) * st::kComputeUnits + pairs - 1) / pairs);
     int32_t chunk = (int32_t)std::max<int64_t>(8, (list + want - 1) / want);
-    if (chunk >= list) chunk = std::max(entries, 1);
+    if (chunk >= list) chunk = p.entries;
     p.chunk = chunk;
-    p.splits = (std::max(entries, 1) + chunk - 1) / chunk;
-    const int64_t parts = p.splits > 1 ? p.units * c->n_heads * p.tiles * p.splits * 16 : 0;
-    const int64_t rows = (int64_t)b->n_tok * n_q_heads;
+    p.splits = (p.entries + chunk - 1) / chunk;
+    const int64_t uh = p.units * c->n_heads;
+    const int64_t parts = p.splits > 1 ? uh * p.splits * p.rows_pad : 0;
     p.o_bytes = st::round_up(parts * c->d * 4, 256);
     p.ml_bytes = st::round_up(parts * 8, 256);
-    p.block_bytes = mass ? st::round_up(rows * entries * 8, 256) : 0;
-    p.row_bytes = mass ? st::round_up(rows * 8, 256) : 0;
+    p.block_bytes = mass ? st::round_up(uh * p.entries * p.rows_pad * 8, 256) : 0;
+    p.row_bytes = mass ? st::round_up(uh * p.rows_pad * 8, 256) : 0;
     return p;
 }
 
@@ -139,7 +153,9 @@ int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t st
 {
     {
         TimedLaunch t(0, stream);
-        hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected>), dim3((unsigned)(p.groups() * a.c.n_heads)), dim3(st::kKvThreads), 0, stream, a);
+        const dim3 grid((unsigned)(p.groups() * a.c.n_heads));
+        if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_tiles(D), kRowWaves>), grid, dim3(kRowWaves * 64), 0, stream, a);
+        else hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected>), grid, dim3(st::kKvThreads), 0, stream, a);
     }
     if (p.splits > 1) {
         TimedLaunch t(1, stream);
@@ -247,12 +263,11 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
         return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)p.bytes());
     if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
     if ((rc = check_grid(p.groups() * cache->n_heads)) || (rc = check_grid((int64_t)batch->n_tok * n_q_heads))) return rc;
-    const int32_t entries = n_sel > 0 ? n_sel : std::max(1, blocks_of(batch->max_len));
     char* ws = (char*)dev_workspace;
     st::KvAttendArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
                           softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse,
-                          p.chunk, p.splits, p.tiles, (float*)ws, (float2*)(ws + p.o_bytes),
-                          mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, entries,
+                          p.chunk, p.splits, p.tiles, p.tile_rows, p.rows_pad, (float*)ws, (float2*)(ws + p.o_bytes),
+                          mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr};
     hipStream_t stream = (hipStream_t)hip_stream;
     if (batch->n_tok > 0 && batch->max_tok > 0)
@@ -262,12 +277,14 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     if (mass && batch->n_seq > 0) {
         st::KvMassArgs m = {a, dev_mass_in, decay, dev_mass_out};
         const int64_t sh = (int64_t)batch->n_seq * cache->n_heads;
-        const int chunks = (batch->max_blocks + st::kKvThreads - 1) / st::kKvThreads;
-        if ((rc = check_grid(sh * chunks))) return rc;
+        const int lanes = p.rows_pad > 16 ? 64 : 16, of = st::kKvThreads / lanes;
+        const int64_t groups = n_sel > 0 ? sh : sh * ((batch->max_blocks + of - 1) / of);
+        if ((rc = check_grid(groups))) return rc;
         if (n_sel > 0 && (rc = allow_lds(&st::kv_mass_selected_kernel, batch->max_blocks * 4))) return rc;
         TimedLaunch t(1, stream);
-        if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, dim3((unsigned)sh), dim3(st::kKvThreads), batch->max_blocks * 4, stream, m);
-        else hipLaunchKernelGGL(st::kv_mass_kernel, dim3((unsigned)(sh * chunks)), dim3(st::kKvThreads), 0, stream, m);
+        if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, dim3((unsigned)groups), dim3(st::kKvThreads), batch->max_blocks * 4, stream, m);
+        else if (lanes == 64) hipLaunchKernelGGL(st::kv_mass_kernel<64>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, m);
+        else hipLaunchKernelGGL(st::kv_mass_kernel<16>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, m);
     }
     ST_HIP(hipGetLastError());
     return ST_OK;

@@ -27,56 +27,65 @@ struct KvAttendArgs {
     const int32_t* blocks;  // selected ones, or null
     void* out;
     float* lse;
-    int32_t chunk, splits, tiles;
-    float* part_o;      // [unit, head, tile, split, 16, d]
-    float2* part_ml;    // [unit, head, tile, split, 16]: maximum, sum of weights
-    float2* block_ml;   // [n_tok, n_q_heads, block_stride]: maximum so far, sum of the block's weights; or null
-    int64_t block_stride;
-    float2* row_ml;     // [n_tok, n_q_heads]: final maximum and sum, written where block_ml is
+    int32_t chunk, splits, tiles, tile_rows;
+    int32_t rows_pad;    // rows of a unit and head in the workspace
+    float* part_o;       // [unit, head, split, rows_pad, d]
+    float2* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of weights
+    float2* block_ml;    // [unit, head, entries, rows_pad]: maximum so far, sum of the block's weights; or null
+    int64_t entries;     // blocks, or selected ones
+    float2* row_ml;      // [unit, head, rows_pad]: final maximum and sum, written where block_ml is
 };
 
 constexpr float kKvLift = 8.0f;   // weights are 2^8 times themselves,
 constexpr float kKvSlack = 7.0f;  // and the maximum they go by may lie 7 (in powers of two) below the largest logit
 
-// What a tile of 16 rows of a unit (a sequence, or a token whose blocks were selected) and a head reads.
+// A query row goes into the product times *up, a power of two that brings its largest magnitude near 2^14, with the sign
+// of the softmax scale; *factor times the product and a key scale is then the logit, in powers of two.
+__device__ inline void kv_query_unit(float top, float scale_log2, float* up, float* factor)
+{
+    const int e = top > 0.0f ? min(max(ilogbf(top), -100), 120) : 0;
+    *up = ldexpf(scale_log2 < 0.0f ? -1.0f : 1.0f, 13 - e);
+    *factor = fabsf(scale_log2) * ldexpf(1.0f, e - 13);
+}
+
+// What a tile of rows of a unit (a sequence, or a token whose blocks were selected) and a head reads.
 struct KvTile {
     int seq;
     int rows;       // of the unit
-    int row;        // this lane's
-    bool valid;
-    int64_t tok;    // its token
-    int q_head;
-    int lim;        // it sees positions below this one
-    int lim_all;    // all valid rows of the tile see those below this one
     int n_blocks;   // blocks that any row of the tile sees
     int n_list;     // entries to go through: blocks, or what was selected
     int64_t tok_unit, tok_first, tok_last;  // first token of the unit; first and last token of the tile
+    int past, len, group;  // a row of token i of the unit sees positions below len - past + i (causal) or len
+    bool causal;
+    __device__ int limit(int i) const { return max(0, causal ? len - past + i : len); }
+    // row -> token of the unit, and the output row [n_tok, n_q_heads] it is
+    __device__ int token(int row) const { return row / group; }
+    __device__ int64_t place(int row, int head, int64_t heads_all) const
+    {
+        const int i = row / group;
+        return (tok_unit + i) * heads_all + head * group + (row - i * group);
+    }
 };
 
 template <bool kSelected>
-__device__ inline KvTile kv_tile(const KvAttendArgs& a, int unit, int head, int tile, int n)
+__device__ inline KvTile kv_tile(const KvAttendArgs& a, int unit, int row0, int tile_rows)
 {
     KvTile t;
     t.seq = kSelected ? kv_seq_of(a.b, unit) : unit;
     const KvSeq q = kv_seq(a.b, t.seq);
     const bool mine = !kSelected || (unit >= q.first && unit < q.first + q.count);
     t.rows = kSelected ? a.group : q.count * a.group;
-    t.row = tile * 16 + n;
-    t.valid = t.row < t.rows;
-    const int last = min(tile * 16 + 15, t.rows - 1);
-    const int i = kSelected ? unit - q.first : min(t.row, max(t.rows - 1, 0)) / a.group;
-    const int i_first = kSelected ? i : tile * 16 / a.group, i_last = kSelected ? i : last / a.group;
-    t.tok = kSelected ? unit : (int64_t)q.first + i;
-    t.q_head = head * a.group + (kSelected ? t.row : t.row - i * a.group);
-    const int past = q.count - 1;
-    t.lim = t.valid && mine ? max(0, a.causal ? q.len - (past - i) : q.len) : 0;
-    t.lim_all = max(0, a.causal ? q.len - (past - i_first) : q.len);
-    const int lim_max = tile * 16 < t.rows && mine ? max(0, a.causal ? q.len - (past - i_last) : q.len) : 0;
-    t.n_blocks = (lim_max + kKvBlock - 1) / kKvBlock;
-    t.n_list = kSelected ? a.n_sel : t.n_blocks;
+    t.group = a.group;
+    t.causal = a.causal != 0;
+    t.len = mine ? q.len : 0;
+    // (a unit of one token: that token is its token 0)
+    t.past = kSelected ? q.count - 1 - (unit - q.first) : q.count - 1;
     t.tok_unit = kSelected ? unit : q.first;
-    t.tok_first = kSelected ? unit : (int64_t)q.first + i_first;
-    t.tok_last = kSelected ? unit : (int64_t)q.first + i_last;
+    const int i_first = row0 / a.group, i_last = max(0, min(row0 + tile_rows, t.rows) - 1) / a.group;
+    t.tok_first = t.tok_unit + i_first;
+    t.tok_last = t.tok_unit + i_last;
+    t.n_blocks = row0 < t.rows ? (t.limit(i_last) + kKvBlock - 1) / kKvBlock : 0;
+    t.n_list = kSelected ? a.n_sel : t.n_blocks;
     return t;
 }
 
@@ -95,8 +104,15 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
     const int tile = (int)(at % a.tiles);
     at /= a.tiles;
     const int head = (int)(at % a.c.n_heads), unit = (int)(at / a.c.n_heads);
-    const KvTile t = kv_tile<kSelected>(a, unit, head, tile, n);
-    if (tile * 16 >= t.rows) return;
+    const int row0 = tile * 16;
+    const KvTile t = kv_tile<kSelected>(a, unit, row0, 16);
+    if (row0 >= t.rows) return;
+    const int64_t uh = (int64_t)unit * a.c.n_heads + head, heads_all = (int64_t)a.c.n_heads * a.group;
+    const int row = row0 + n;
+    const bool valid = row < t.rows;
+    const int64_t place = valid ? t.place(row, head, heads_all) : 0;
+    const int64_t tok = place / heads_all;
+    const int lim = valid ? t.limit(t.token(row)) : 0, lim_all = t.limit(t.token(row0));
     const int jb = split * a.chunk, je = min(jb + a.chunk, t.n_list);
     if (split > 0 && jb >= je) return;
     const bool bf16 = a.bf16 != 0;
@@ -107,21 +123,18 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
     {
         float f[kSteps][8];
         float top = 0.0f;
-        const uint16_t* src = (const uint16_t*)a.q + t.tok * a.q_stride + (int64_t)t.q_head * D;
+        const uint16_t* src = (const uint16_t*)a.q + tok * a.q_stride + (place - tok * heads_all) * D;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
             const int ch = k < 2 * kWide ? k / 2 * 64 + g * 16 + k % 2 * 8 : kWide * 64 + g * 8;
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (t.valid) v = *(const uint4*)(src + ch);
+            if (valid) v = *(const uint4*)(src + ch);
             eight_floats(v, bf16, f[k]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[k][j]));
         }
-        top = max_over_16_32(top);
-        int e = top > 0.0f ? ilogbf(top) : 0;
-        e = min(max(e, -100), 120);
-        const float up = ldexpf(a.scale_log2 < 0.0f ? -1.0f : 1.0f, 13 - e);
-        factor = fabsf(a.scale_log2) * ldexpf(1.0f, e - 13);
+        float up;
+        kv_query_unit(max_over_16_32(top), a.scale_log2, &up, &factor);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
 #pragma unroll
@@ -138,19 +151,16 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
         const int j = j0 + 4 * lane + w;
         int block = -1, page = -1;
         if (j < je) {
-            block = kSelected ? a.blocks[((int64_t)unit * a.c.n_heads + head) * a.n_sel + j] : j;
+            block = kSelected ? a.blocks[uh * a.n_sel + j] : j;
             if (block >= 0 && block < t.n_blocks) page = kv_page(a.c, a.b, t.seq, block);
         }
         if (a.mask && page >= 0) {  // a block that no row of the tile sees is not read
             uint64_t any = 0;
-            for (int64_t tok = t.tok_first; tok <= t.tok_last; ++tok) any |= a.mask[tok * a.mask_words + block];
+            for (int64_t i = t.tok_first; i <= t.tok_last; ++i) any |= a.mask[i * a.mask_words + block];
             if (any == 0) page = -1;
         }
         if (a.block_ml && j < je && page < 0)
-            for (int r = 0; r < 16 && tile * 16 + r < t.rows; ++r) {
-                const int row = tile * 16 + r, i = kSelected ? 0 : row / a.group;
-                a.block_ml[((t.tok_unit + i) * a.c.n_heads * a.group + head * a.group + (row - i * a.group)) * a.block_stride + j] = make_float2(0.0f, 0.0f);
-            }
+            for (int r = 0; r < 16; ++r) a.block_ml[(uh * a.entries + j) * a.rows_pad + row0 + r] = make_float2(0.0f, 0.0f);
         const int64_t ph_l = (int64_t)max(page, 0) * a.c.n_heads + head;
         const float ks_l = page >= 0 ? a.c.k_scale[ph_l] : 0.0f, vs_l = page >= 0 ? a.c.v_scale[ph_l] : 0.0f;
         uint64_t todo = ballot(page >= 0);
@@ -184,11 +194,11 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
                 load_keys(cur);
             }
             uint64_t see = ~0ull;
-            const bool part = a.mask || (b + 1) * kKvBlock > t.lim_all;
+            const bool part = a.mask || (b + 1) * kKvBlock > lim_all;
             if (part) {
-                const int left = t.lim - b * kKvBlock;
+                const int left = lim - b * kKvBlock;
                 see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
-                if (a.mask && see) see &= a.mask[t.tok * a.mask_words + b];
+                if (a.mask && see) see &= a.mask[tok * a.mask_words + b];
             }
             float4v x[4];
 #pragma unroll
@@ -243,8 +253,7 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
             l += sum;
             if (a.block_ml) {
                 const float all = sum_over_16_32(sum);
-                if (g == 0 && t.valid)
-                    a.block_ml[(t.tok * a.c.n_heads * a.group + t.q_head) * a.block_stride + (j0 + 4 * cur + w)] = make_float2(m, all);
+                if (g == 0) a.block_ml[(uh * a.entries + j0 + 4 * cur + w) * a.rows_pad + row] = make_float2(m, all);
             }
 #pragma unroll
             for (int c = 0; c < kCh; ++c) {
@@ -264,8 +273,7 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
 #pragma unroll
     for (int c = 0; c < kCh; ++c) *(float4v*)&s_o[w][n][c * 16 + g * 4] = o[c];
     __syncthreads();
-    const int64_t part = ((int64_t)(unit * (int64_t)a.c.n_heads + head) * a.tiles + tile) * a.splits + split;
-    const int64_t heads_all = (int64_t)a.c.n_heads * a.group;
+    const int64_t part = (uh * a.splits + split) * a.rows_pad + row0;
     for (int i = threadIdx.x; i < 16 * (D / 4); i += kKvThreads) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
         float top = -__builtin_inff();
@@ -282,15 +290,13 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
 #pragma unroll
             for (int u = 0; u < 4; ++u) y[u] += v[u] * f;
         }
-        const int row = tile * 16 + r;
-        if (row >= t.rows) continue;
+        if (row0 + r >= t.rows) continue;
         if (a.splits > 1) {
-            *(float4v*)(a.part_o + (part * 16 + r) * D + c) = y;
-            if (c == 0) a.part_ml[part * 16 + r] = make_float2(top, sum);
+            *(float4v*)(a.part_o + (part + r) * D + c) = y;
+            if (c == 0) a.part_ml[part + r] = make_float2(top, sum);
             continue;
         }
-        const int of = kSelected ? 0 : row / a.group;
-        const int64_t place = (t.tok_unit + of) * heads_all + head * a.group + (row - of * a.group);
+        const int64_t place = t.place(row0 + r, head, heads_all);
         const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
         uint32_t h[4];
 #pragma unroll
@@ -298,7 +304,7 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
         *(uint2*)((uint16_t*)a.out + place * D + c) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
         if (c == 0) {
             if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(sum)) * 0.69314718056f;
-            if (a.row_ml) a.row_ml[place] = make_float2(top, sum);
+            if (a.row_ml) a.row_ml[uh * a.rows_pad + row0 + r] = make_float2(top, sum);
         }
     }
 }
@@ -322,12 +328,13 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     const KvSeq q = kv_seq(a.b, s);
     const bool mine = there && tok >= q.first && tok < q.first + q.count;
     const int unit = kSelected ? tok : s;
-    const int row = !mine ? 0 : kSelected ? qh % a.group : (tok - q.first) * a.group + qh % a.group, tile = row / 16;
-    const KvTile t = kv_tile<kSelected>(a, unit, head, tile, row % 16);
+    const int row = !mine ? 0 : kSelected ? qh % a.group : (tok - q.first) * a.group + qh % a.group;
+    const KvTile t = kv_tile<kSelected>(a, unit, row / a.tile_rows * a.tile_rows, a.tile_rows);
+    const int64_t uh = (int64_t)unit * a.c.n_heads + head, stride = a.rows_pad;
     const int splits = mine ? min(a.splits, max(1, (t.n_list + a.chunk - 1) / a.chunk)) : 0;
-    const int64_t part = (((int64_t)unit * a.c.n_heads + head) * a.tiles + tile) * a.splits * 16 + row % 16;
+    const int64_t part = uh * a.splits * stride + row;
     float top = -__builtin_inff();
-    for (int i = me; i < splits; i += kTeam) top = fmaxf(top, a.part_ml[part + (int64_t)i * 16].x);
+    for (int i = me; i < splits; i += kTeam) top = fmaxf(top, a.part_ml[part + i * stride].x);
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
     if (lane == 0) s_top[team][me >> 6] = top;
     __syncthreads();
@@ -339,8 +346,8 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     if (from < kParts) {
 #pragma unroll 4
         for (int i = from; i < splits; i += kParts) {
-            const float2 ml = a.part_ml[part + (int64_t)i * 16];
-            const float4v v = *(const float4v*)(a.part_o + (part + (int64_t)i * 16) * D + c * 4);
+            const float2 ml = a.part_ml[part + i * stride];
+            const float4v v = *(const float4v*)(a.part_o + (part + i * stride) * D + c * 4);
             const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
             sum = __builtin_fmaf(ml.y, f, sum);
 #pragma unroll
@@ -365,7 +372,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     *(uint2*)((uint16_t*)a.out + place * D + c * 4) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
     if (c == 0) {
         if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(sum)) * 0.69314718056f;
-        if (a.row_ml) a.row_ml[place] = make_float2(top, sum);
+        if (a.row_ml) a.row_ml[uh * stride + row] = make_float2(top, sum);
     }
 }
 
@@ -381,31 +388,31 @@ __device__ inline float kv_weight(float2 block, float2 row)
     return row.y != 0.0f && block.y != 0.0f ? block.y * __builtin_amdgcn_exp2f(block.x - row.x) / row.y : 0.0f;
 }
 
-// Weights of the blocks, summed over the rows of a sequence and head, in the order of the rows.  A thread to a block.
+// Weights of the blocks, summed over the rows of a sequence and head: kLanes lanes to a block, each every kLanes-th row.
+template <int kLanes>
 __global__ __launch_bounds__(kKvThreads) void kv_mass_kernel(KvMassArgs a)
 {
-    const int nb = a.t.b.max_blocks, chunks = (nb + kKvThreads - 1) / kKvThreads;
+    constexpr int kBlocks = kKvThreads / kLanes;
+    const int nb = a.t.b.max_blocks, chunks = (nb + kBlocks - 1) / kBlocks;
     const int chunk = blockIdx.x % chunks, sh = blockIdx.x / chunks;
-    const int head = sh % a.t.c.n_heads, s = sh / a.t.c.n_heads;
-    const int b = chunk * kKvThreads + threadIdx.x;
-    if (b >= nb) return;
+    const int s = sh / a.t.c.n_heads, lane = threadIdx.x % kLanes;
+    const int b = chunk * kBlocks + threadIdx.x / kLanes;
     const KvSeq q = kv_seq(a.t.b, s);
-    const int64_t to = (int64_t)sh * nb + b;
-    if (b * kKvBlock >= q.len) {
-        a.out[to] = 0.0f;
-        return;
-    }
+    const bool held = b < nb && b * kKvBlock < q.len;
     float sum = 0.0f;
-    const int heads_all = a.t.c.n_heads * a.t.group;
-    for (int i = 0; i < q.count; ++i) {
-        const int lim = a.t.causal ? q.len - (q.count - 1 - i) : q.len;
-        if (b * kKvBlock >= lim) continue;  // (nothing was written there)
-        for (int h = 0; h < a.t.group; ++h) {
-            const int64_t place = (int64_t)(q.first + i) * heads_all + head * a.t.group + h;
-            sum += kv_weight(a.t.block_ml[place * a.t.block_stride + b], a.t.row_ml[place]);
-        }
+    if (held) {
+        // (nothing was written for rows that end before the block)
+        int first = 0;
+        if (a.t.causal) first = max(0, b * kKvBlock - (q.len - q.count)) * a.t.group;
+        const float2* block = a.t.block_ml + ((int64_t)sh * a.t.entries + b) * a.t.rows_pad;
+        const float2* row = a.t.row_ml + (int64_t)sh * a.t.rows_pad;
+        for (int r = first + lane; r < q.count * a.t.group; r += kLanes) sum += kv_weight(block[r], row[r]);
     }
-    a.out[to] = (a.in ? a.in[to] * a.decay : 0.0f) + sum;
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane != 0 || b >= nb) return;
+    const int64_t to = (int64_t)sh * nb + b;
+    a.out[to] = held ? (a.in ? a.in[to] * a.decay : 0.0f) + sum : 0.0f;
 }
 
 // The same where blocks were selected: token after token, each adds to the blocks it read.
@@ -418,17 +425,14 @@ __global__ __launch_bounds__(kKvThreads) void kv_mass_selected_kernel(KvMassArgs
     const int held = (q.len + kKvBlock - 1) / kKvBlock;
     for (int b = threadIdx.x; b < held; b += kKvThreads) acc[b] = 0.0f;
     __syncthreads();
-    const int heads_all = a.t.c.n_heads * a.t.group;
     for (int i = 0; i < q.count; ++i) {
-        const int64_t tok = q.first + i;
+        const int64_t th = (int64_t)(q.first + i) * a.t.c.n_heads + head;
         for (int j = threadIdx.x; j < a.t.n_sel; j += kKvThreads) {
-            const int b = a.t.blocks[(tok * a.t.c.n_heads + head) * a.t.n_sel + j];
+            const int b = a.t.blocks[th * a.t.n_sel + j];
             if (b < 0 || b >= held) continue;
             float sum = 0.0f;
-            for (int h = 0; h < a.t.group; ++h) {
-                const int64_t place = tok * heads_all + head * a.t.group + h;
-                sum += kv_weight(a.t.block_ml[place * a.t.block_stride + j], a.t.row_ml[place]);
-            }
+            for (int h = 0; h < a.t.group; ++h)
+                sum += kv_weight(a.t.block_ml[(th * a.t.n_sel + j) * a.t.rows_pad + h], a.t.row_ml[th * a.t.rows_pad + h]);
             acc[b] += sum;
         }
         __syncthreads();

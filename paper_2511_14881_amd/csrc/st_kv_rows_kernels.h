@@ -1,0 +1,299 @@
+// Attention of many rows of a sequence (candidates, a prompt's chunk) over its cached history.
+//
+// Bound by the matrix units and the vector units beside them: 4 d operations to a row and token for the products, some five
+// vector instructions to a weight.  A workgroup's wavefronts hold kTiles tiles of 32 rows each; a block's integers are turned into
+// 16-bit floats once for all of them, on their way into the LDS (two blocks deep, the next one's integers in flight behind the
+// products), and a fragment that is read from there serves every tile of the wavefront.  As in the kernel for few rows a lane
+// holds one row's logits, and weights go from one product to the other as they lie.  The value scale
+// of a block is part of its weights (relative to a reference that follows the scales at a distance), so that the products
+// accumulate into the outputs.
+#pragma once
+#include "st_kv_attend_kernels.h"
+
+namespace st {
+
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+__device__ inline float max_over_32(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
+
+template <int D, int kTiles, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel(KvAttendArgs a)
+{
+    constexpr int kThreads = kWaves * 64, kRows = kWaves * kTiles * 32, kSteps = D / 16, kCh = D / 32;
+    constexpr int kKeyBytes = 2 * D + 16, kValBytes = 2 * kKvBlock + 16;  // rows of the LDS, an odd number of 16 bytes apart
+    constexpr int kPieces = (4 * D + kThreads - 1) / kThreads;            // 16 bytes of keys, and of values, of a thread
+    __shared__ __align__(16) char s_k[2][kKvBlock * kKeyBytes];
+    __shared__ __align__(16) char s_v[2][D * kValBytes];
+    __shared__ uint64_t s_any[kWaves][64];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 31, h = lane >> 5;
+    int64_t at = blockIdx.x;
+    const int split = (int)(at % a.splits);
+    at /= a.splits;
+    const int tile = (int)(at % a.tiles);
+    at /= a.tiles;
+    const int head = (int)(at % a.c.n_heads), unit = (int)(at / a.c.n_heads);
+    const int row0 = tile * kRows;
+    const KvTile t = kv_tile<false>(a, unit, row0, kRows);
+    if (row0 >= t.rows) return;
+    const int jb = split * a.chunk, je = min(jb + a.chunk, t.n_list);
+    if (split > 0 && jb >= je) return;
+    const int64_t uh = (int64_t)unit * a.c.n_heads + head, heads_all = (int64_t)a.c.n_heads * a.group;
+    const bool bf16 = a.bf16 != 0;
+
+    int row[kTiles], lim[kTiles];
+    int64_t tok[kTiles];
+    half8 q[kTiles][kSteps];
+    float factor[kTiles], m[kTiles], l[kTiles];
+    float16v o[kTiles][kCh];
+#pragma unroll
+    for (int rt = 0; rt < kTiles; ++rt) {
+        row[rt] = row0 + (w * kTiles + rt) * 32 + n;
+        const bool valid = row[rt] < t.rows;
+        const int64_t place = valid ? t.place(row[rt], head, heads_all) : 0;
+        tok[rt] = place / heads_all;
+        lim[rt] = valid ? t.limit(t.token(row[rt])) : 0;
+        const uint16_t* src = (const uint16_t*)a.q + tok[rt] * a.q_stride + (place - tok[rt] * heads_all) * D + h * 8;
+        uint4 raw[kSteps];
+        float top = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            raw[k] = make_uint4(0, 0, 0, 0);
+            if (valid) raw[k] = *(const uint4*)(src + k * 16);
+        }
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            float f[8];
+            eight_floats(raw[k], bf16, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
+        }
+        float up;
+        kv_query_unit(max_over_32(top), a.scale_log2, &up, &factor[rt]);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            float f[8];
+            eight_floats(raw[k], bf16, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[rt][k][j] = (_Float16)(f[j] * up);
+        }
+        m[rt] = -__builtin_inff();
+        l[rt] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kCh; ++c) o[rt][c] = float16v(0.0f);
+    }
+    const int row_w = row0 + w * kTiles * 32;
+    const bool busy = row_w < t.rows;                               // this wavefront has rows at all
+    const int lim_all = busy ? t.limit(t.token(row_w)) : 0;         // its rows see at least the positions below this one
+    float v_unit = 0.0f;                                            // outputs are in units of this value scale
+    int buf = 0;
+
+    for (int j0 = jb; j0 < je; j0 += 64) {
+        // up to 64 blocks: page and scales, one to a lane (the same in all wavefronts)
+        const int j = j0 + lane;
+        int page = j < je ? kv_page(a.c, a.b, t.seq, j) : -1;
+        if (a.mask) {  // a block that no row of the tile sees is not read
+            uint64_t any = 0;
+            if (page >= 0)
+                for (int64_t i = t.tok_first + w; i <= t.tok_last; i += kWaves) any |= a.mask[i * a.mask_words + j];
+            __syncthreads();
+            s_any[w][lane] = any;
+            __syncthreads();
+            for (int i = 0; i < kWaves; ++i) any |= s_any[i][lane];
+            if (any == 0) page = -1;
+        }
+        const uint64_t all = ballot(j < je);
+        uint64_t todo = ballot(page >= 0);
+        if (a.block_ml)
+            for (uint64_t dead = all & ~todo; dead; dead &= dead - 1)
+                for (int r = tid; r < kRows && row0 + r < a.rows_pad; r += kThreads)
+                    a.block_ml[(uh * a.entries + j0 + __builtin_ctzll(dead)) * a.rows_pad + row0 + r] = make_float2(0.0f, 0.0f);
+        if (todo == 0) continue;
+        const int64_t ph_l = (int64_t)max(page, 0) * a.c.n_heads + head;
+        const float ks_l = page >= 0 ? a.c.k_scale[ph_l] : 0.0f, vs_l = page >= 0 ? a.c.v_scale[ph_l] : 0.0f;
+        uint4 kraw[kPieces], vraw[kPieces];
+        auto load = [&](int from) {
+            const int64_t ph = (int64_t)(int)lane_value((uint32_t)page, from) * a.c.n_heads + head;
+            const uint4* kp = (const uint4*)(a.c.k + ph * (D * kKvBlock));
+            const uint4* vp = (const uint4*)(a.c.v + ph * (D * kKvBlock));
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                if (4 * D % kThreads == 0 || i * kThreads + tid < 4 * D) {
+                    kraw[i] = kp[i * kThreads + tid];
+                    vraw[i] = vp[i * kThreads + tid];
+                }
+        };
+        int it = __builtin_ctzll(todo);
+        load(it);
+        while (todo) {
+            const int cur = it, b = j0 + cur;
+            todo &= todo - 1;
+            it = todo ? __builtin_ctzll(todo) : -1;
+            // the scale of the values against the reference; integers under a scale of zero are zeros
+            const float vs = __uint_as_float(lane_value(__float_as_uint(vs_l), cur));
+            float rho = 1.0f, rho_inv = 1.0f;
+            const bool empty = vs == 0.0f;
+            if (!empty) {
+                rho = vs / v_unit;
+                if (!(rho >= 0.00390625f && rho <= 1.875f)) {
+                    if (v_unit != 0.0f) {
+                        const float f = v_unit / vs;
+#pragma unroll
+                        for (int rt = 0; rt < kTiles; ++rt)
+#pragma unroll
+                            for (int c = 0; c < kCh; ++c) o[rt][c] *= f;
+                    }
+                    v_unit = vs;
+                    rho = 1.0f;
+                }
+                rho_inv = 1.0f / rho;
+            }
+            char* const bk = s_k[buf];
+            char* const bv = s_v[buf];
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int p = i * kThreads + tid;
+                if (4 * D % kThreads == 0 || p < 4 * D) {
+                    char* kd = bk + p / (D / 16) * kKeyBytes + p % (D / 16) * 32;
+                    *(half8*)kd = eight_halves(kraw[i].x, kraw[i].y);
+                    *(half8*)(kd + 16) = eight_halves(kraw[i].z, kraw[i].w);
+                    // four neighbouring tokens to a word: half of the 8 that a lane's fragment of 16 tokens holds
+                    const int g = p & 3;
+                    char* vd = bv + p / 4 * kValBytes + (g & 1) * 16 + (g >> 1) * 8;
+                    const uint32_t some = empty ? 0u : ~0u;
+                    *(uint2*)vd = halves_of_bytes(vraw[i].x & some);
+                    *(uint2*)(vd + 32) = halves_of_bytes(vraw[i].y & some);
+                    *(uint2*)(vd + 64) = halves_of_bytes(vraw[i].z & some);
+                    *(uint2*)(vd + 96) = halves_of_bytes(vraw[i].w & some);
+                }
+            }
+            if (it >= 0) load(it);
+            __syncthreads();
+            buf ^= 1;
+            if (!busy) continue;
+
+            uint64_t see[kTiles];
+            const bool part = a.mask || (b + 1) * kKvBlock > lim_all;
+            bool none = false;
+            if (part) {
+                uint64_t some = 0;
+#pragma unroll
+                for (int rt = 0; rt < kTiles; ++rt) {
+                    const int left = lim[rt] - b * kKvBlock;
+                    see[rt] = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
+                    if (a.mask && see[rt]) see[rt] &= a.mask[tok[rt] * a.mask_words + b];
+                    some |= see[rt];
+                }
+                none = ballot(some != 0) == 0;
+            }
+            if (none) {
+                if (a.block_ml && h == 0)
+#pragma unroll
+                    for (int rt = 0; rt < kTiles; ++rt)
+                        if (row[rt] < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row[rt]] = make_float2(0.0f, 0.0f);
+                continue;
+            }
+            float16v x[kTiles][2];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+                for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = float16v(0.0f);
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) {
+                    const half8 f = *(const half8*)(bk + (tt * 32 + n) * kKeyBytes + k * 32 + h * 16);
+#pragma unroll
+                    for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[rt][k], x[rt][tt], 0, 0, 0);
+                }
+            }
+            const float ks_b = __uint_as_float(lane_value(__float_as_uint(ks_l), cur));
+            const float rho_log = __builtin_amdgcn_logf(rho);
+            half8 p[kTiles][4];
+#pragma unroll
+            for (int rt = 0; rt < kTiles; ++rt) {
+                const float ks = fmaxf(ks_b * factor[rt], 1e-37f);
+                if (part) {
+                    const uint64_t mine = see[rt] >> (h * 4);
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!((mine >> (tt * 32 + (i >> 2) * 8 + (i & 3))) & 1)) x[rt][tt][i] = -__builtin_inff();
+                }
+                float top = x[rt][0][0];
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, x[rt][tt][i]);
+                top = max_over_32(top) * ks;
+                if (ballot(top > m[rt] + kKvSlack) != 0) {
+                    const float m_new = top > m[rt] + kKvSlack ? top : m[rt];
+                    const float alpha = m_new == m[rt] ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - m_new);
+                    m[rt] = m_new;
+                    l[rt] *= alpha;
+#pragma unroll
+                    for (int c = 0; c < kCh; ++c) o[rt][c] *= alpha;
+                }
+                const float base = m[rt] == -__builtin_inff() ? 0.0f : kKvLift + rho_log - m[rt];
+                float sum = 0.0f;
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][tt][i], ks, base));
+                        sum += e;
+                        p[rt][tt * 2 + (i >> 3)][i & 7] = (_Float16)e;
+                    }
+                sum *= rho_inv;
+                l[rt] += sum;
+                if (a.block_ml) {
+                    const float both = sum + __shfl_xor(sum, 32);
+                    if (h == 0 && row[rt] < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row[rt]] = make_float2(m[rt], both);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kCh; ++c)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const half8 f = *(const half8*)(bv + (c * 32 + n) * kValBytes + u * 32 + h * 16);
+#pragma unroll
+                    for (int rt = 0; rt < kTiles; ++rt) o[rt][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[rt][u], o[rt][c], 0, 0, 0);
+                }
+        }
+    }
+
+#pragma unroll
+    for (int rt = 0; rt < kTiles; ++rt) {
+        const float sum = l[rt] + __shfl_xor(l[rt], 32);
+        if (row[rt] >= t.rows) continue;
+        if (a.splits > 1) {
+            const int64_t part = (uh * a.splits + split) * a.rows_pad + row[rt];
+#pragma unroll
+            for (int c = 0; c < kCh; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float4v y;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) y[u] = o[rt][c][4 * i + u] * v_unit;
+                    *(float4v*)(a.part_o + part * D + c * 32 + i * 8 + h * 4) = y;
+                }
+            if (h == 0) a.part_ml[part] = make_float2(m[rt], sum);
+            continue;
+        }
+        const int64_t place = t.place(row[rt], head, heads_all);
+        const float inv = sum > 0.0f || sum != sum ? v_unit / sum : 0.0f;
+#pragma unroll
+        for (int c = 0; c < kCh; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t r[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) r[u] = to_16_bits(o[rt][c][4 * i + u] * inv, bf16);
+                *(uint2*)((uint16_t*)a.out + place * D + c * 32 + i * 8 + h * 4) = make_uint2(r[0] | r[1] << 16, r[2] | r[3] << 16);
+            }
+        if (h == 0) {
+            if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (m[rt] - kKvLift + log2f(sum)) * 0.69314718056f;
+            if (a.row_ml) a.row_ml[uh * a.rows_pad + row[rt]] = make_float2(m[rt], sum);
+        }
+    }
+}
+
+}  // namespace st
