@@ -106,10 +106,10 @@ int with_dim(int32_t d, F&& body)
 #ifndef KV_RT
 #define KV_RT 1
 #define KV_W 8
-#define KV_WANT 4ll
+#define KV_WANT 1ll
 #endif
 constexpr int row_tiles(int d) { return d > 128 ? 1 : KV_RT; }
-constexpr int kRowWaves = KV_W;
+constexpr int row_waves(int d) { return d > 128 ? 4 : KV_W; }
 
 struct AttendPlan {
     bool many;          // the kernel for many rows
@@ -128,7 +128,7 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int64_t rows = (n_sel > 0 ? 1 : (int64_t)b->max_tok) * group;  // of a unit and head
     p.units = n_sel > 0 ? b->n_tok : b->n_seq;
     p.many = n_sel == 0 && rows > 32;
-    p.tile_rows = p.many ? row_tiles(c->d) * kRowWaves * 32 : 16;
+    p.tile_rows = p.many ? row_tiles(c->d) * row_waves(c->d) * 32 : 16;
     p.tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
     p.rows_pad = (int32_t)st::round_up(rows, 16);
     const int32_t list = std::max(1, n_sel > 0 ? std::min(n_sel, blocks_of(b->max_len)) : blocks_of(b->max_len));
@@ -154,7 +154,7 @@ int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t st
     {
         TimedLaunch t(0, stream);
         const dim3 grid((unsigned)(p.groups() * a.c.n_heads));
-        if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_tiles(D), kRowWaves>), grid, dim3(kRowWaves * 64), 0, stream, a);
+        if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_tiles(D), row_waves(D)>), grid, dim3(row_waves(D) * 64), 0, stream, a);
         else hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected>), grid, dim3(st::kKvThreads), 0, stream, a);
     }
     if (p.splits > 1) {

@@ -10,6 +10,9 @@
 #pragma once
 #include "st_kv_attend_kernels.h"
 
+#ifndef KV_SCHED
+#define KV_SCHED
+#endif
 namespace st {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
@@ -81,11 +84,8 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
 #pragma unroll
         for (int c = 0; c < kCh; ++c) o[rt][c] = float16v(0.0f);
     }
-    const int row_w = row0 + w * kTiles * 32;
-    const bool busy = row_w < t.rows;                               // this wavefront has rows at all
-    const int lim_all = busy ? t.limit(t.token(row_w)) : 0;         // its rows see at least the positions below this one
-    float v_unit = 0.0f;                                            // outputs are in units of this value scale
-    int buf = 0;
+    const int lim_all = t.limit(t.token(min(row0 + w * kTiles * 32, t.rows - 1)));  // its rows see at least the positions below this one
+    float v_unit = 0.0f;                                                            // outputs are in units of this value scale
 
     for (int j0 = jb; j0 < je; j0 += 64) {
         // up to 64 blocks: page and scales, one to a lane (the same in all wavefronts)
@@ -111,28 +111,63 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
         const int64_t ph_l = (int64_t)max(page, 0) * a.c.n_heads + head;
         const float ks_l = page >= 0 ? a.c.k_scale[ph_l] : 0.0f, vs_l = page >= 0 ? a.c.v_scale[ph_l] : 0.0f;
         uint4 kraw[kPieces], vraw[kPieces];
-        auto load = [&](int from) {
-            const int64_t ph = (int64_t)(int)lane_value((uint32_t)page, from) * a.c.n_heads + head;
-            const uint4* kp = (const uint4*)(a.c.k + ph * (D * kKvBlock));
-            const uint4* vp = (const uint4*)(a.c.v + ph * (D * kKvBlock));
+        auto load = [&](const int8_t* from, int block, uint4* raw) {
+            const int64_t ph = (int64_t)(int)lane_value((uint32_t)page, block) * a.c.n_heads + head;
+            const uint4* src = (const uint4*)(from + ph * (D * kKvBlock));
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
-                if (4 * D % kThreads == 0 || i * kThreads + tid < 4 * D) {
-                    kraw[i] = kp[i * kThreads + tid];
-                    vraw[i] = vp[i * kThreads + tid];
-                }
+                if (4 * D % kThreads == 0 || i * kThreads + tid < 4 * D) raw[i] = src[i * kThreads + tid];
         };
-        int it = __builtin_ctzll(todo);
-        load(it);
-        while (todo) {
-            const int cur = it, b = j0 + cur;
-            todo &= todo - 1;
-            it = todo ? __builtin_ctzll(todo) : -1;
-            // the scale of the values against the reference; integers under a scale of zero are zeros
+        auto put_keys = [&](int buf) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int p = i * kThreads + tid;
+                if (4 * D % kThreads == 0 || p < 4 * D) {
+                    char* to = s_k[buf] + p / (D / 16) * kKeyBytes + p % (D / 16) * 32;
+                    *(half8*)to = eight_halves(kraw[i].x, kraw[i].y);
+                    *(half8*)(to + 16) = eight_halves(kraw[i].z, kraw[i].w);
+                }
+            }
+        };
+        auto put_values = [&](int buf, int block) {
+            // (integers under a scale of zero are zeros)
+            const uint32_t some = lane_value(__float_as_uint(vs_l), block) << 1 ? ~0u : 0u;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int p = i * kThreads + tid;
+                if (4 * D % kThreads == 0 || p < 4 * D) {
+                    // four neighbouring tokens to a word: half of the 8 that a lane's fragment of 16 tokens holds
+                    char* to = s_v[buf] + p / 4 * kValBytes + (p & 1) * 16 + (p >> 1 & 1) * 8;
+                    *(uint2*)to = halves_of_bytes(vraw[i].x & some);
+                    *(uint2*)(to + 32) = halves_of_bytes(vraw[i].y & some);
+                    *(uint2*)(to + 64) = halves_of_bytes(vraw[i].z & some);
+                    *(uint2*)(to + 96) = halves_of_bytes(vraw[i].w & some);
+                }
+            }
+        };
+        auto products = [&](int buf, float16v (&x)[kTiles][2]) {
+            const char* bk = s_k[buf] + n * kKeyBytes + h * 16;
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+                for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = float16v(0.0f);
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) {
+                    const half8 f = *(const half8*)(bk + tt * 32 * kKeyBytes + k * 32);
+#pragma unroll
+                    for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[rt][k], x[rt][tt], 0, 0, 0);
+                }
+            }
+        };
+        // One block: x holds its products with the keys; next is filled with those of the block behind it.
+        auto step = [&](int buf, int cur, int next, int third, float16v (&x)[kTiles][2], float16v (&xn)[kTiles][2]) {
+            const int b = j0 + cur;
+            load(a.c.k, third, kraw);
+            load(a.c.v, next, vraw);
+            // the scale of the values against the reference
             const float vs = __uint_as_float(lane_value(__float_as_uint(vs_l), cur));
             float rho = 1.0f, rho_inv = 1.0f;
-            const bool empty = vs == 0.0f;
-            if (!empty) {
+            if (vs != 0.0f) {
                 rho = vs / v_unit;
                 if (!(rho >= 0.00390625f && rho <= 1.875f)) {
                     if (v_unit != 0.0f) {
@@ -147,116 +182,123 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
                 }
                 rho_inv = 1.0f / rho;
             }
-            char* const bk = s_k[buf];
-            char* const bv = s_v[buf];
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int p = i * kThreads + tid;
-                if (4 * D % kThreads == 0 || p < 4 * D) {
-                    char* kd = bk + p / (D / 16) * kKeyBytes + p % (D / 16) * 32;
-                    *(half8*)kd = eight_halves(kraw[i].x, kraw[i].y);
-                    *(half8*)(kd + 16) = eight_halves(kraw[i].z, kraw[i].w);
-                    // four neighbouring tokens to a word: half of the 8 that a lane's fragment of 16 tokens holds
-                    const int g = p & 3;
-                    char* vd = bv + p / 4 * kValBytes + (g & 1) * 16 + (g >> 1) * 8;
-                    const uint32_t some = empty ? 0u : ~0u;
-                    *(uint2*)vd = halves_of_bytes(vraw[i].x & some);
-                    *(uint2*)(vd + 32) = halves_of_bytes(vraw[i].y & some);
-                    *(uint2*)(vd + 64) = halves_of_bytes(vraw[i].z & some);
-                    *(uint2*)(vd + 96) = halves_of_bytes(vraw[i].w & some);
-                }
-            }
-            if (it >= 0) load(it);
-            __syncthreads();
-            buf ^= 1;
-            if (!busy) continue;
-
-            uint64_t see[kTiles];
-            const bool part = a.mask || (b + 1) * kKvBlock > lim_all;
-            bool none = false;
-            if (part) {
-                uint64_t some = 0;
+            if (a.mask || (b + 1) * kKvBlock > lim_all) {
 #pragma unroll
                 for (int rt = 0; rt < kTiles; ++rt) {
                     const int left = lim[rt] - b * kKvBlock;
-                    see[rt] = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
-                    if (a.mask && see[rt]) see[rt] &= a.mask[tok[rt] * a.mask_words + b];
-                    some |= see[rt];
-                }
-                none = ballot(some != 0) == 0;
-            }
-            if (none) {
-                if (a.block_ml && h == 0)
+                    uint64_t see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
+                    if (a.mask && see) see &= a.mask[tok[rt] * a.mask_words + b];
+                    see >>= h * 4;
 #pragma unroll
-                    for (int rt = 0; rt < kTiles; ++rt)
-                        if (row[rt] < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row[rt]] = make_float2(0.0f, 0.0f);
-                continue;
-            }
-            float16v x[kTiles][2];
+                    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-#pragma unroll
-                for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = float16v(0.0f);
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    const half8 f = *(const half8*)(bk + (tt * 32 + n) * kKeyBytes + k * 32 + h * 16);
-#pragma unroll
-                    for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[rt][k], x[rt][tt], 0, 0, 0);
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t yes = (uint32_t)((int)((uint32_t)(see >> (tt * 32)) << (31 - ((i >> 2) * 8 + (i & 3)))) >> 31);
+                            x[rt][tt][i] = __uint_as_float((__float_as_uint(x[rt][tt][i]) & yes) | (0xFF800000u & ~yes));
+                        }
                 }
             }
             const float ks_b = __uint_as_float(lane_value(__float_as_uint(ks_l), cur));
             const float rho_log = __builtin_amdgcn_logf(rho);
-            half8 p[kTiles][4];
+            float ks[kTiles];
+            bool far = false;
+            float top[kTiles];
 #pragma unroll
             for (int rt = 0; rt < kTiles; ++rt) {
-                const float ks = fmaxf(ks_b * factor[rt], 1e-37f);
-                if (part) {
-                    const uint64_t mine = see[rt] >> (h * 4);
-#pragma unroll
-                    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (!((mine >> (tt * 32 + (i >> 2) * 8 + (i & 3))) & 1)) x[rt][tt][i] = -__builtin_inff();
-                }
-                float top = x[rt][0][0];
+                ks[rt] = fmaxf(ks_b * factor[rt], 1e-37f);
+                top[rt] = x[rt][0][0];
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, x[rt][tt][i]);
-                top = max_over_32(top) * ks;
-                if (ballot(top > m[rt] + kKvSlack) != 0) {
-                    const float m_new = top > m[rt] + kKvSlack ? top : m[rt];
+                    for (int i = 0; i < 16; ++i) top[rt] = fmaxf(top[rt], x[rt][tt][i]);
+                top[rt] = max_over_32(top[rt]) * ks[rt];
+                far = far || top[rt] > m[rt] + kKvSlack;
+            }
+            if (ballot(far) != 0) {
+#pragma unroll
+                for (int rt = 0; rt < kTiles; ++rt) {
+                    const float m_new = top[rt] > m[rt] + kKvSlack ? top[rt] : m[rt];
                     const float alpha = m_new == m[rt] ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - m_new);
                     m[rt] = m_new;
                     l[rt] *= alpha;
 #pragma unroll
                     for (int c = 0; c < kCh; ++c) o[rt][c] *= alpha;
                 }
+            }
+            products(buf ^ 1, xn);
+            half8 p[kTiles][4];
+            float sums[kTiles];
+#pragma unroll
+            for (int rt = 0; rt < kTiles; ++rt) {
                 const float base = m[rt] == -__builtin_inff() ? 0.0f : kKvLift + rho_log - m[rt];
                 float sum = 0.0f;
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][tt][i], ks, base));
+                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][tt][i], ks[rt], base));
                         sum += e;
                         p[rt][tt * 2 + (i >> 3)][i & 7] = (_Float16)e;
                     }
-                sum *= rho_inv;
-                l[rt] += sum;
-                if (a.block_ml) {
-                    const float both = sum + __shfl_xor(sum, 32);
-                    if (h == 0 && row[rt] < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row[rt]] = make_float2(m[rt], both);
-                }
+                sums[rt] = sum * rho_inv;
+                l[rt] += sums[rt];
             }
+            const char* bv = s_v[buf] + n * kValBytes + h * 16;
 #pragma unroll
             for (int c = 0; c < kCh; ++c)
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    const half8 f = *(const half8*)(bv + (c * 32 + n) * kValBytes + u * 32 + h * 16);
+                    const half8 f = *(const half8*)(bv + c * 32 * kValBytes + u * 32);
 #pragma unroll
                     for (int rt = 0; rt < kTiles; ++rt) o[rt][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[rt][u], o[rt][c], 0, 0, 0);
                 }
+            put_keys(buf);
+            put_values(buf ^ 1, next);
+            KV_SCHED
+            if (a.block_ml)
+#pragma unroll
+                for (int rt = 0; rt < kTiles; ++rt) {
+                    const float both = sums[rt] + __shfl_xor(sums[rt], 32);
+                    if (h == 0 && row[rt] < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row[rt]] = make_float2(m[rt], both);
+                }
+            __syncthreads();
+        };
+        // the walk over the blocks to do: the last one again where there is none
+        auto after = [&](int* it) {
+            if (todo) {
+                *it = __builtin_ctzll(todo);
+                todo &= todo - 1;
+                return 1;
+            }
+            return 0;
+        };
+        float16v xa[kTiles][2], xb[kTiles][2];
+        int left = __builtin_popcountll(todo);
+        int first = 0, second, third;
+        after(&first);
+        second = first;
+        after(&second);
+        third = second;
+        after(&third);
+        __syncthreads();  // (the LDS may still be read for the blocks of the round before)
+        load(a.c.k, first, kraw);
+        load(a.c.v, first, vraw);
+        put_keys(0);
+        put_values(0, first);
+        load(a.c.k, second, kraw);
+        put_keys(1);
+        __syncthreads();
+        products(0, xa);
+        for (; left > 0; left -= 2) {
+            step(0, first, second, third, xa, xb);
+            first = second;
+            second = third;
+            after(&third);
+            if (left == 1) break;
+            step(1, first, second, third, xb, xa);
+            first = second;
+            second = third;
+            after(&third);
         }
     }
 
