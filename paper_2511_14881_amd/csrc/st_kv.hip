@@ -172,7 +172,7 @@ int64_t select_stride(const st_kv_batch* b) { return st::round_up(std::max(1, bl
 template <class K>
 int allow_lds(K kernel, int bytes)
 {
-    if (bytes > 64 * 1024) ST_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024));
+    if (bytes > 32 * 1024) ST_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024));
     return ST_OK;
 }
 
@@ -193,7 +193,7 @@ int st_kv_append(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     if (batch->n_tok == 0 || batch->max_tok == 0) return ST_OK;
     st::KvAppendArgs a = {view(cache), view(batch), dev_k_new, dev_v_new, k_stride, v_stride, dtype == ST_BF16,
                           (batch->max_tok + ST_KV_BLOCK - 2) / ST_KV_BLOCK + 1};
-    const int64_t groups = (int64_t)batch->n_seq * a.touched * cache->n_heads;
+    const int64_t groups = 2ll * batch->n_seq * a.touched * cache->n_heads;
     if ((rc = check_grid(groups))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
     with_dim(cache->d, [&](auto d) -> int {
@@ -214,7 +214,7 @@ int st_kv_read(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_blo
     if ((rc = check_cache(cache, true, true)) || (rc = check_batch(batch))) return rc;
     if (n_blocks < 1 || n_blocks > ST_KV_MAX_BLOCKS) return fail(ST_EINVAL, "n_blocks=%d out of range", n_blocks);
     if (misaligned(dev_out_k) || misaligned(dev_out_v) || misaligned(dev_out_bounds)) return fail(ST_EINVAL, "misaligned output (16 B)");
-    const int64_t groups = (int64_t)batch->n_seq * n_blocks * cache->n_heads;
+    const int64_t groups = 2ll * batch->n_seq * n_blocks * cache->n_heads;
     if ((rc = check_grid(groups))) return rc;
     if (groups == 0 || (!dev_out_k && !dev_out_v && !dev_out_bounds)) return ST_OK;
     st::KvReadArgs a = {view(cache), view(batch), n_blocks, dev_out_k, dev_out_v, dev_out_bounds};
@@ -323,24 +323,42 @@ int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
     if (batch->n_tok == 0 || batch->max_tok == 0) return ST_OK;
     const int32_t blocks = std::max(1, blocks_of(batch->max_len));
+    // One token to a sequence: the workgroup that scores also chooses, as long as its blocks are few enough to be read by one
+    // (or there are as many sequences and heads as compute units anyway).
+    const int64_t pairs = (int64_t)batch->n_seq * cache->n_heads;
+    const bool one = batch->max_tok == 1 && (blocks <= 1024 || pairs >= st::kComputeUnits);
     st::KvSelectArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
-                          dev_mask, mask_words, n_sel, sink, recent, (batch->max_tok + 15) / 16,
-                          (blocks + st::kKvScoreBlocks - 1) / st::kKvScoreBlocks, select_stride(batch),
+                          dev_mask, mask_words, n_sel, sink, recent, (batch->max_tok + 15) / 16, 1, 1, select_stride(batch),
                           (uint32_t*)dev_workspace, dev_out_blocks};
-    const int64_t groups = (int64_t)batch->n_seq * cache->n_heads * a.tiles * a.chunks;
+    if (!one) {
+        // rounds of 256 blocks to a workgroup: as many as still leave two workgroups to a compute unit
+        const int all = (blocks + st::kKvScoreBlocks - 1) / st::kKvScoreBlocks;
+        const int64_t want = std::max<int64_t>(1, 2ll * st::kComputeUnits / std::max<int64_t>(1, pairs * a.tiles));
+        a.chunks = (int32_t)std::min<int64_t>(all, want);
+        a.rounds = (all + a.chunks - 1) / a.chunks;
+    }
+    const int64_t groups = pairs * a.tiles * a.chunks;
     const int64_t rows = (int64_t)batch->n_tok * cache->n_heads;
     if ((rc = check_grid(groups)) || (rc = check_grid(rows))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
-    with_dim(cache->d, [&](auto d) -> int {
+    const int lds = (int)select_stride(batch) * 4;
+    rc = with_dim(cache->d, [&](auto d) -> int {
+        constexpr int D = decltype(d)::value;
+        int rc2;
+        if (one && (rc2 = allow_lds(&st::kv_score_kernel<D, true>, lds))) return rc2;
         TimedLaunch t(0, stream);
-        hipLaunchKernelGGL((st::kv_score_kernel<decltype(d)::value>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        if (one) hipLaunchKernelGGL((st::kv_score_kernel<D, true>), dim3((unsigned)groups), dim3(st::kKvThreads), lds, stream, a);
+        else hipLaunchKernelGGL((st::kv_score_kernel<D, false>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
         return ST_OK;
     });
-    const int lds = blocks * 4;
-    if ((rc = allow_lds(&st::kv_choose_kernel, lds))) return rc;
-    {
+    if (rc != ST_OK) return rc;
+    if (!one) {
+        if (blocks > 512 && (rc = allow_lds(&st::kv_choose_kernel, lds))) return rc;
         TimedLaunch t(1, stream);
-        hipLaunchKernelGGL(st::kv_choose_kernel, dim3((unsigned)rows), dim3(st::kKvThreads), lds, stream, a);
+        const dim3 waves((unsigned)((rows + 3) / 4));
+        if (blocks <= 128) hipLaunchKernelGGL(st::kv_choose_wave_kernel<2>, waves, dim3(st::kKvThreads), 0, stream, a);
+        else if (blocks <= 512) hipLaunchKernelGGL(st::kv_choose_wave_kernel<8>, waves, dim3(st::kKvThreads), 0, stream, a);
+        else hipLaunchKernelGGL(st::kv_choose_kernel, dim3((unsigned)rows), dim3(st::kKvThreads), lds, stream, a);
     }
     ST_HIP(hipGetLastError());
     return ST_OK;
@@ -366,7 +384,7 @@ int st_kv_evict(const st_kv_batch* batch, const float* dev_mass, int32_t n_heads
     if ((rc = allow_lds(&st::kv_evict_kernel, lds))) return rc;
     {
         TimedLaunch t(1, (hipStream_t)hip_stream);
-        hipLaunchKernelGGL(st::kv_evict_kernel, dim3((unsigned)batch->n_seq), dim3(st::kKvThreads), lds, (hipStream_t)hip_stream, a);
+        hipLaunchKernelGGL(st::kv_evict_kernel, dim3((unsigned)batch->n_seq), dim3(st::kKvEvictThreads), lds, (hipStream_t)hip_stream, a);
     }
     ST_HIP(hipGetLastError());
     return ST_OK;
