@@ -530,6 +530,17 @@ def st_score_pairs(items, item_scale, queries, query_scale, pair_item, pair_quer
 
 # ------------------------------------------------------------------ cached histories
 
+# The current stream as a number: torch.cuda.current_stream() builds an object first, which takes longer than a launch.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _kv_stream(stream):
+    if stream is not None or _raw_stream is None or _raw_device is None:
+        return _stream(stream)
+    return _raw_stream(_raw_device())
+
+
 ST_KV_BLOCK, ST_KV_MAX_BLOCKS, ST_KV_MAX_HEADS = 64, 16384, 1024
 ST_BF16, ST_F16 = 0, 1
 _KV_TYPES = {torch.bfloat16: ST_BF16, torch.float16: ST_F16}
@@ -619,8 +630,6 @@ def _kv_mask(mask, n_tok: int):
 
 
 def _kv_out(t, shape, dtype, name: str):
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device="cuda")
     _need(t, dtype, name)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {list(shape)}")
@@ -650,16 +659,16 @@ def st_kv_append(cache: KvCache, batch: KvBatch, k, v, stream=None) -> None:
     vs, v_dtype = _kv_rows(v, batch.n_tok, cache.d, "v")
     if dtype != v_dtype or k.shape[1] != cache.n_heads or v.shape[1] != cache.n_heads:
         raise ValueError("k and v must be of one type and have the cache's heads")
-    _check(lib().st_kv_append(cache._p, batch._p, k.data_ptr(), ks, v.data_ptr(), vs, dtype, _stream(stream)))
+    _check(lib().st_kv_append(cache._p, batch._p, k.data_ptr(), ks, v.data_ptr(), vs, dtype, _kv_stream(stream)))
 
 
 def st_kv_read(cache: KvCache, batch: KvBatch, n_blocks: int, stream=None):
     """The last n_blocks blocks of each sequence as fp32 (k, v [n_seq, n_blocks, heads, 64, d], bounds [.., 2, d])."""
     shape = (batch.n_seq, n_blocks, cache.n_heads, ST_KV_BLOCK, cache.d)
-    k = torch.empty(shape, dtype=torch.float32, device="cuda")
-    v = torch.empty(shape, dtype=torch.float32, device="cuda")
-    bounds = torch.empty((*shape[:3], 2, cache.d), dtype=torch.float32, device="cuda")
-    _check(lib().st_kv_read(cache._p, batch._p, n_blocks, k.data_ptr(), v.data_ptr(), bounds.data_ptr(), _stream(stream)))
+    k = cache.k_scale.new_empty(shape)
+    v = cache.k_scale.new_empty(shape)
+    bounds = cache.k_scale.new_empty((*shape[:3], 2, cache.d))
+    _check(lib().st_kv_read(cache._p, batch._p, n_blocks, k.data_ptr(), v.data_ptr(), bounds.data_ptr(), _kv_stream(stream)))
     return k, v, bounds
 
 
@@ -694,15 +703,18 @@ def st_kv_attend(cache: KvCache, batch: KvBatch, q, scale: float | None = None, 
     else:
         nbytes = st_kv_attend_workspace_bytes(cache, batch, n_q_heads, n_sel, with_mass)
         work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
-    out = _kv_out(out, (batch.n_tok, n_q_heads, cache.d), q.dtype, "out")
+    if out is None:
+        out = q.new_empty((batch.n_tok, n_q_heads, cache.d))
+    else:
+        _kv_out(out, (batch.n_tok, n_q_heads, cache.d), q.dtype, "out")
     if with_mass:
-        mass_out = _kv_out(mass_out, shape, torch.float32, "mass_out")
+        mass_out = torch.empty_like(mass) if mass_out is None else _kv_out(mass_out, shape, torch.float32, "mass_out")
     if lse is not None:
         lse = _kv_out(lse, (batch.n_tok, n_q_heads), torch.float32, "lse")
     _check(lib().st_kv_attend(cache._p, batch._p, q.data_ptr(), q_stride, dtype, n_q_heads,
                               cache.d ** -0.5 if scale is None else scale, int(causal), mask_p, words,
                               _dptr(blocks), n_sel, out.data_ptr(), _dptr(lse), _dptr(mass), decay, _dptr(mass_out),
-                              work.data_ptr(), nbytes, _stream(stream)))
+                              work.data_ptr(), nbytes, _kv_stream(stream)))
     return out
 
 
@@ -722,9 +734,12 @@ def st_kv_select(cache: KvCache, batch: KvBatch, q, n_sel: int, causal: bool = T
     else:
         nbytes = st_kv_select_workspace_bytes(cache, batch, n_q_heads, n_sel)
         work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
-    out = _kv_out(out, (batch.n_tok, cache.n_heads, n_sel), torch.int32, "out")
+    if out is None:
+        out = batch.lengths.new_empty((batch.n_tok, cache.n_heads, n_sel))
+    else:
+        _kv_out(out, (batch.n_tok, cache.n_heads, n_sel), torch.int32, "out")
     _check(lib().st_kv_select(cache._p, batch._p, q.data_ptr(), q_stride, dtype, n_q_heads, int(causal), mask_p, words, n_sel,
-                              sink, recent, out.data_ptr(), work.data_ptr(), nbytes, _stream(stream)))
+                              sink, recent, out.data_ptr(), work.data_ptr(), nbytes, _kv_stream(stream)))
     return out
 
 
@@ -734,12 +749,16 @@ def st_kv_evict(batch: KvBatch, mass, budget: int, sink: int = 0, recent: int = 
     _need(mass, torch.float32, "mass")
     if mass.dim() != 3 or mass.shape[0] != batch.n_seq or mass.shape[2] != batch.max_blocks:
         raise ValueError("mass must be [n_seq, heads, max_blocks]")
-    rows = (batch.n_seq, batch.max_blocks)
-    given = out if out is not None else (None,) * 5
-    out = tuple(_kv_out(t, shape, dtype, name) for t, shape, dtype, name in zip(
-        given, (rows, (batch.n_seq,), tuple(mass.shape), rows, (batch.n_seq,)),
-        (torch.int32, torch.int32, torch.float32, torch.int32, torch.int32),
-        ("tables", "lengths", "mass", "freed", "n_freed"), strict=True))
-    _check(lib().st_kv_evict(batch._p, mass.data_ptr(), mass.shape[1], budget, sink, recent,
-                             *(t.data_ptr() for t in out), _stream(stream)))
+    if out is None:
+        out = (torch.empty_like(batch.tables), torch.empty_like(batch.lengths), torch.empty_like(mass),
+               torch.empty_like(batch.tables), torch.empty_like(batch.lengths))
+    else:
+        rows = (batch.n_seq, batch.max_blocks)
+        for t, shape, dtype, name in zip(out, (rows, (batch.n_seq,), mass.shape, rows, (batch.n_seq,)),
+                                         (torch.int32, torch.int32, torch.float32, torch.int32, torch.int32),
+                                         ("tables", "lengths", "mass", "freed", "n_freed"), strict=True):
+            _kv_out(t, shape, dtype, name)
+    t, n, m, f, nf = out
+    _check(lib().st_kv_evict(batch._p, mass.data_ptr(), mass.shape[1], budget, sink, recent, t.data_ptr(), n.data_ptr(),
+                             m.data_ptr(), f.data_ptr(), nf.data_ptr(), _kv_stream(stream)))
     return out

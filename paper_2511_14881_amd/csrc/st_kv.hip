@@ -103,6 +103,12 @@ int with_dim(int32_t d, F&& body)
     return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", d);
 }
 
+#ifndef KV_ONE
+#define KV_ONE 512
+#endif
+#ifndef KV_CHUNK
+#define KV_CHUNK 16
+#endif
 #ifndef KV_RT
 #define KV_RT 1
 #define KV_W 8
@@ -111,12 +117,14 @@ int with_dim(int32_t d, F&& body)
 constexpr int row_tiles(int d) { return d > 128 ? 1 : KV_RT; }
 constexpr int row_waves(int d) { return d > 128 ? 4 : KV_W; }
 
+constexpr int kDies = 8;  // of the chip, each with an L2 of its own
+
 struct AttendPlan {
     bool many;          // the kernel for many rows
-    int32_t tile_rows, tiles, chunk, splits, rows_pad, entries;
+    int32_t tile_rows, tiles, chunk, splits, rows_pad, entries, dies;
     int64_t units;
+    int64_t grid;       // workgroups
     int64_t o_bytes, ml_bytes, block_bytes, row_bytes;
-    int64_t groups() const { return units * tiles * splits; }  // and times heads
     int64_t bytes() const { return o_bytes + ml_bytes + block_bytes + row_bytes; }
 };
 
@@ -135,10 +143,14 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     p.entries = n_sel > 0 ? n_sel : list;
     const int64_t pairs = std::max<int64_t>(1, p.units * p.tiles * c->n_heads);
     const int64_t want = std::max<int64_t>(1, ((p.many ? KV_WANT : 8ll) * st::kComputeUnits + pairs - 1) / pairs);
-    int32_t chunk = (int32_t)std::max<int64_t>(8, (list + want - 1) / want);
+    int32_t chunk = (int32_t)std::max<int64_t>(KV_CHUNK, (list + want - 1) / want);
     if (chunk >= list) chunk = p.entries;
     p.chunk = chunk;
     p.splits = (p.entries + chunk - 1) / chunk;
+    // Parts that read the same blocks go to one die, where the sequences and heads are enough to keep all dies alike.
+    const int64_t sh = (int64_t)b->n_seq * c->n_heads, per = (int64_t)p.tiles * p.splits * (n_sel > 0 ? b->max_tok : 1);
+    p.dies = per > p.splits && (sh % kDies == 0 || sh >= 8 * kDies) ? kDies : 1;
+    p.grid = st::round_up(sh, p.dies) * per;
     const int64_t uh = p.units * c->n_heads;
     const int64_t parts = p.splits > 1 ? uh * p.splits * p.rows_pad : 0;
     p.o_bytes = st::round_up(parts * c->d * 4, 256);
@@ -153,7 +165,7 @@ int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t st
 {
     {
         TimedLaunch t(0, stream);
-        const dim3 grid((unsigned)(p.groups() * a.c.n_heads));
+        const dim3 grid((unsigned)p.grid);
         if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_tiles(D), row_waves(D)>), grid, dim3(row_waves(D) * 64), 0, stream, a);
         else hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected>), grid, dim3(st::kKvThreads), 0, stream, a);
     }
@@ -262,11 +274,11 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     if (p.bytes() > 0 && (!dev_workspace || workspace_bytes < p.bytes()))
         return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)p.bytes());
     if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
-    if ((rc = check_grid(p.groups() * cache->n_heads)) || (rc = check_grid((int64_t)batch->n_tok * n_q_heads))) return rc;
+    if ((rc = check_grid(p.grid)) || (rc = check_grid((int64_t)batch->n_tok * n_q_heads))) return rc;
     char* ws = (char*)dev_workspace;
     st::KvAttendArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
                           softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse,
-                          p.chunk, p.splits, p.tiles, p.tile_rows, p.rows_pad, (float*)ws, (float2*)(ws + p.o_bytes),
+                          p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, p.rows_pad, (float*)ws, (float2*)(ws + p.o_bytes),
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr};
     hipStream_t stream = (hipStream_t)hip_stream;
@@ -345,10 +357,11 @@ int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     rc = with_dim(cache->d, [&](auto d) -> int {
         constexpr int D = decltype(d)::value;
         int rc2;
-        if (one && (rc2 = allow_lds(&st::kv_score_kernel<D, true>, lds))) return rc2;
+        constexpr int kOneThreads = KV_ONE;
+        if (one && (rc2 = allow_lds(&st::kv_score_kernel<D, true, kOneThreads>, lds))) return rc2;
         TimedLaunch t(0, stream);
-        if (one) hipLaunchKernelGGL((st::kv_score_kernel<D, true>), dim3((unsigned)groups), dim3(st::kKvThreads), lds, stream, a);
-        else hipLaunchKernelGGL((st::kv_score_kernel<D, false>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        if (one) hipLaunchKernelGGL((st::kv_score_kernel<D, true, kOneThreads>), dim3((unsigned)groups), dim3(kOneThreads), lds, stream, a);
+        else hipLaunchKernelGGL((st::kv_score_kernel<D, false, st::kKvThreads>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
         return ST_OK;
     });
     if (rc != ST_OK) return rc;

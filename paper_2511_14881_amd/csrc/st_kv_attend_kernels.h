@@ -27,7 +27,7 @@ struct KvAttendArgs {
     const int32_t* blocks;  // selected ones, or null
     void* out;
     float* lse;
-    int32_t chunk, splits, tiles, tile_rows;
+    int32_t chunk, splits, tiles, tile_rows, dies;
     int32_t rows_pad;    // rows of a unit and head in the workspace
     float* part_o;       // [unit, head, split, rows_pad, d]
     float2* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of weights
@@ -67,11 +67,45 @@ struct KvTile {
     }
 };
 
+// Which part of the work a workgroup does.  The parts of one sequence and head that read the same blocks (tiles of rows, tokens whose
+// blocks were selected) follow one another on one of the chip's 8 dies, whose L2 serves them: workgroups are handed to the dies in turn.
+struct KvPlace {
+    int seq, head, unit, tile, split;  // unit < 0: none
+};
 template <bool kSelected>
-__device__ inline KvTile kv_tile(const KvAttendArgs& a, int unit, int row0, int tile_rows)
+__device__ inline KvPlace kv_place(const KvAttendArgs& a)
+{
+    const uint32_t per = (uint32_t)a.tiles * a.splits * (kSelected ? a.b.max_tok : 1);
+    uint32_t pair, item;
+    if (a.dies > 1) {
+        const uint32_t k = blockIdx.x / a.dies;
+        pair = k / per * a.dies + blockIdx.x % a.dies;
+        item = k % per;
+    } else {
+        pair = blockIdx.x / per;
+        item = blockIdx.x % per;
+    }
+    KvPlace p;
+    p.seq = pair / a.c.n_heads;
+    p.head = pair % a.c.n_heads;
+    p.unit = p.seq;
+    p.tile = item % a.tiles;
+    item /= a.tiles;
+    p.split = item % a.splits;
+    if (p.seq >= a.b.n_seq) p.unit = -1;
+    else if (kSelected) {
+        const KvSeq q = kv_seq(a.b, p.seq);
+        const int i = item / a.splits;
+        p.unit = i < q.count ? q.first + i : -1;
+    }
+    return p;
+}
+
+template <bool kSelected>
+__device__ inline KvTile kv_tile(const KvAttendArgs& a, int seq, int unit, int row0, int tile_rows)
 {
     KvTile t;
-    t.seq = kSelected ? kv_seq_of(a.b, unit) : unit;
+    t.seq = seq;
     const KvSeq q = kv_seq(a.b, t.seq);
     const bool mine = !kSelected || (unit >= q.first && unit < q.first + q.count);
     t.rows = kSelected ? a.group : q.count * a.group;
@@ -98,14 +132,10 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
     __shared__ float s_o[4][16][D + 4];
     __shared__ float2 s_ml[4][16];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    int64_t at = blockIdx.x;
-    const int split = (int)(at % a.splits);
-    at /= a.splits;
-    const int tile = (int)(at % a.tiles);
-    at /= a.tiles;
-    const int head = (int)(at % a.c.n_heads), unit = (int)(at / a.c.n_heads);
-    const int row0 = tile * 16;
-    const KvTile t = kv_tile<kSelected>(a, unit, row0, 16);
+    const KvPlace at = kv_place<kSelected>(a);
+    if (at.unit < 0) return;
+    const int split = at.split, head = at.head, unit = at.unit, row0 = at.tile * 16;
+    const KvTile t = kv_tile<kSelected>(a, at.seq, unit, row0, 16);
     if (row0 >= t.rows) return;
     const int64_t uh = (int64_t)unit * a.c.n_heads + head, heads_all = (int64_t)a.c.n_heads * a.group;
     const int row = row0 + n;
@@ -329,7 +359,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     const bool mine = there && tok >= q.first && tok < q.first + q.count;
     const int unit = kSelected ? tok : s;
     const int row = !mine ? 0 : kSelected ? qh % a.group : (tok - q.first) * a.group + qh % a.group;
-    const KvTile t = kv_tile<kSelected>(a, unit, row / a.tile_rows * a.tile_rows, a.tile_rows);
+    const KvTile t = kv_tile<kSelected>(a, s, unit, row / a.tile_rows * a.tile_rows, a.tile_rows);
     const int64_t uh = (int64_t)unit * a.c.n_heads + head, stride = a.rows_pad;
     const int splits = mine ? min(a.splits, max(1, (t.n_list + a.chunk - 1) / a.chunk)) : 0;
     const int64_t part = uh * a.splits * stride + row;

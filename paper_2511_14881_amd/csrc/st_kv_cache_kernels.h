@@ -370,15 +370,18 @@ template <int kPer, class Emit>
 __device__ inline int kv_pick_wave(const uint32_t (&keys)[kPer], int want, Emit emit)
 {
     uint32_t t = 0;
+    bool ends = false;  // exactly `want` keys are t or larger
 #pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = 31; bit >= 0 && !ends; --bit) {
         const uint32_t c = t | 1u << bit;
         int count = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) count += __builtin_popcountll(ballot(keys[i] >= c));
         if (count >= want) t = c;
+        ends = count == want;
     }
-    // t is the want-th key; 0: there are fewer
+    if (ends) --t;
+    // those above t are in, and as many of those equal to t as are left to be had; t = 0: there are no more than wanted
     uint32_t over = 0, same = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -386,7 +389,7 @@ __device__ inline int kv_pick_wave(const uint32_t (&keys)[kPer], int want, Emit 
         same += t != 0 && keys[i] == t;
     }
     const uint32_t over_all = lane_value(wave_scan_add(over), 63);
-    const uint32_t need = t ? (uint32_t)want - over_all : 0u;
+    const uint32_t need = t && !ends ? (uint32_t)want - over_all : 0u;
     const uint32_t same_before = wave_scan_add(same) - same;
     uint32_t left = same_before < need ? min(need - same_before, same) : 0u;
     const uint32_t inc = wave_scan_add(over + left);
@@ -422,10 +425,10 @@ constexpr int kKvScoreBlocks = 256;  // blocks of a workgroup's round
 
 // Queries of up to 16 tokens as int8 [token][2 d], each the group's positive parts and its negative ones, into the LDS.
 // A thread to eight channels of a token.
-template <int D>
+template <int D, int kThreads>
 __device__ inline void kv_query_bytes(const KvSelectArgs& a, int64_t tok0, int tokens, int head, int8_t* out, int out_stride, uint32_t* tops)
 {
-    constexpr int kGroups = D / 8, kItems = (16 * kGroups + kKvThreads - 1) / kKvThreads;
+    constexpr int kGroups = D / 8, kItems = (16 * kGroups + kThreads - 1) / kThreads;
     const int tid = threadIdx.x;
     const bool bf16 = a.bf16 != 0;
     if (tid < 16) tops[tid] = 0;
@@ -433,7 +436,7 @@ __device__ inline void kv_query_bytes(const KvSelectArgs& a, int64_t tok0, int t
     float u[kItems][16];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-        const int item = i * kKvThreads + tid, t = item / kGroups, c = item % kGroups * 8;
+        const int item = i * kThreads + tid, t = item / kGroups, c = item % kGroups * 8;
         if (t >= tokens) continue;
         const uint16_t* q = (const uint16_t*)a.q + (tok0 + t) * a.q_stride + (int64_t)head * a.group * D + c;
 #pragma unroll
@@ -461,7 +464,7 @@ __device__ inline void kv_query_bytes(const KvSelectArgs& a, int64_t tok0, int t
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-        const int item = i * kKvThreads + tid, t = item / kGroups, c = item % kGroups * 8;
+        const int item = i * kThreads + tid, t = item / kGroups, c = item % kGroups * 8;
         if (t >= 16) continue;
         uint32_t w[4] = {0, 0, 0, 0};
         if (t < tokens) {
@@ -478,8 +481,8 @@ __device__ inline void kv_query_bytes(const KvSelectArgs& a, int64_t tok0, int t
 // Keys of (token, head, block): one int8 product of 16 blocks' bounds with 16 tokens' queries to an instruction.
 // Bound by the bounds, read once for every 16 tokens of a sequence.  kOne: sequences have one token each, and the workgroup that
 // has formed the keys of all blocks chooses among them in its LDS.
-template <int D, bool kOne>
-__global__ __launch_bounds__(kKvThreads) void kv_score_kernel(KvSelectArgs a)
+template <int D, bool kOne, int kThreads>
+__global__ __launch_bounds__(kThreads) void kv_score_kernel(KvSelectArgs a)
 {
     constexpr int kSteps = 2 * D / 64, kStride = 2 * D + 16, kAt = D > 128 ? 2 : 4;  // (tiles of 16 blocks at a time)
     extern __shared__ uint32_t keys[];
@@ -505,11 +508,11 @@ __global__ __launch_bounds__(kKvThreads) void kv_score_kernel(KvSelectArgs a)
     const int64_t tok = tok0 + (valid ? n : 0);
     const int lim = valid ? max(0, a.causal ? q.len - (q.count - 1 - i) : q.len) : 0;
     const int seen = (lim + kKvBlock - 1) / kKvBlock;  // blocks of this token
-    kv_query_bytes<D>(a, tok0, tokens, head, s_u, kStride, s_top);
+    kv_query_bytes<D, kThreads>(a, tok0, tokens, head, s_u, kStride, s_top);
     int4v u[kSteps];
 #pragma unroll
     for (int c = 0; c < kSteps; ++c) u[c] = *(const int4v*)(s_u + n * kStride + c * 64 + g * 16);
-    for (int bw = b0 + w * 64; bw < b1; bw += 256) {
+    for (int bw = b0 + w * 64; bw < b1; bw += kThreads) {
         // 64 blocks: page and scale, one to a lane
         const int mine = bw + lane;
         const int page_l = mine < b1 ? kv_page(a.c, a.b, s, mine) : -1;
@@ -517,12 +520,16 @@ __global__ __launch_bounds__(kKvThreads) void kv_score_kernel(KvSelectArgs a)
 #pragma unroll
         for (int t0 = 0; t0 < 4; t0 += kAt) {
             int4v row[kAt][kSteps];
+            uint64_t word[kAt][4];
 #pragma unroll
             for (int t = 0; t < kAt; ++t) {
                 const int page = __shfl(page_l, (t0 + t) * 16 + n);
                 const int8_t* src = a.c.bounds + ((int64_t)max(page, 0) * a.c.n_heads + head) * (2 * D) + g * 16;
 #pragma unroll
                 for (int c = 0; c < kSteps; ++c) row[t][c] = *(const int4v*)(src + c * 64);
+                if (a.mask)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) word[t][r] = a.mask[tok * a.mask_words + min(bw + (t0 + t) * 16 + g * 4 + r, held - 1)];
             }
 #pragma unroll
             for (int t = 0; t < kAt; ++t) {
@@ -537,10 +544,8 @@ __global__ __launch_bounds__(kKvThreads) void kv_score_kernel(KvSelectArgs a)
                     const float scale = __shfl(ks_l, from);
                     bool can = __shfl(page_l, from) >= 0 && bb < seen;
                     if (a.mask && can) {
-                        uint64_t word = a.mask[tok * a.mask_words + bb];
                         const int left = lim - bb * kKvBlock;
-                        if (left < 64) word &= (1ull << left) - 1;
-                        can = word != 0;
+                        can = (left < 64 ? word[t][r] & ((1ull << left) - 1) : word[t][r]) != 0;
                     }
                     const uint32_t k = min(max(score_bits(__fmul_rn((float)acc[r], scale)), 1u), 0xFFFFFFFEu);
                     key[r] = !can ? 0u : bb < a.sink || bb >= seen - a.recent ? 0xFFFFFFFFu : k;
@@ -556,11 +561,11 @@ __global__ __launch_bounds__(kKvThreads) void kv_score_kernel(KvSelectArgs a)
         }
     }
     if (!kOne) return;
-    __shared__ KvPick<kKvThreads> pick;
+    __shared__ KvPick<kThreads> pick;
     int32_t* out = a.out + (tok0 * a.c.n_heads + head) * a.n_sel;
     __syncthreads();
-    const int got = kv_pick<kKvThreads>(keys, held, a.n_sel, &pick, [&](int b, int rank) { out[rank] = b; });
-    for (int b = got + threadIdx.x; b < a.n_sel; b += kKvThreads) out[b] = -1;
+    const int got = kv_pick<kThreads>(keys, held, a.n_sel, &pick, [&](int b, int rank) { out[rank] = b; });
+    for (int b = got + threadIdx.x; b < a.n_sel; b += kThreads) out[b] = -1;
 }
 
 __global__ __launch_bounds__(kKvThreads) void kv_choose_kernel(KvSelectArgs a)

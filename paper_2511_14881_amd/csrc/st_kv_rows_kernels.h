@@ -29,14 +29,10 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
     __shared__ __align__(16) char s_v[2][D * kValBytes];
     __shared__ uint64_t s_any[kWaves][64];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 31, h = lane >> 5;
-    int64_t at = blockIdx.x;
-    const int split = (int)(at % a.splits);
-    at /= a.splits;
-    const int tile = (int)(at % a.tiles);
-    at /= a.tiles;
-    const int head = (int)(at % a.c.n_heads), unit = (int)(at / a.c.n_heads);
-    const int row0 = tile * kRows;
-    const KvTile t = kv_tile<false>(a, unit, row0, kRows);
+    const KvPlace at = kv_place<false>(a);
+    if (at.unit < 0) return;
+    const int split = at.split, head = at.head, unit = at.unit, row0 = at.tile * kRows;
+    const KvTile t = kv_tile<false>(a, at.seq, unit, row0, kRows);
     if (row0 >= t.rows) return;
     const int jb = split * a.chunk, je = min(jb + a.chunk, t.n_list);
     if (split > 0 && jb >= je) return;
