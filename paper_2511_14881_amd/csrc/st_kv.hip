@@ -103,27 +103,22 @@ int with_dim(int32_t d, F&& body)
     return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", d);
 }
 
-#ifndef KV_ONE
-#define KV_ONE 512
+#ifndef KV_MULT
+#define KV_MULT 2
 #endif
-#ifndef KV_CHUNK
-#define KV_CHUNK 16
-#endif
-#ifndef KV_RT
-#define KV_RT 1
-#define KV_W 8
-#define KV_WANT 1ll
-#endif
-constexpr int row_tiles(int d) { return d > 128 ? 1 : KV_RT; }
-constexpr int row_waves(int d) { return d > 128 ? 4 : KV_W; }
-
+constexpr int kFewRows = 48;       // of a sequence and head: up to here tiles of 16 that read the cache themselves (64 rows: 38.5 us
+                                  // against 36.7, 40 rows: 35.5 against 36.3; 4 x 8192 tokens, 8 heads of 128)
+constexpr int row_waves(int d) { return d > 128 ? 4 : 8; }  // of the kernel for many rows (256: 512 registers to a lane)
+constexpr int kManyRows = 2048;   // tiles that fill the chip with a wavefront each
+constexpr int kLeastChunk = 16;   // blocks of a split, at least: it takes as long to start as to read four
+constexpr double kSplitStart = 4.0, kSplitJoin = 6.0;  // start of a workgroup, and joining splits, in blocks
 constexpr int kDies = 8;  // of the chip, each with an L2 of its own
 
 struct AttendPlan {
     bool many;          // the kernel for many rows
-    int32_t tile_rows, tiles, chunk, splits, rows_pad, entries, dies;
+    int32_t tile_rows, tiles, chunk, splits, rows_pad, entries, dies, waves;
     int64_t units;
-    int64_t grid;       // workgroups
+    int64_t parts, grid;  // workgroups to a split, and in all
     int64_t o_bytes, ml_bytes, block_bytes, row_bytes;
     int64_t bytes() const { return o_bytes + ml_bytes + block_bytes + row_bytes; }
 };
@@ -135,22 +130,39 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int32_t group = n_q_heads / c->n_heads;
     const int64_t rows = (n_sel > 0 ? 1 : (int64_t)b->max_tok) * group;  // of a unit and head
     p.units = n_sel > 0 ? b->n_tok : b->n_seq;
-    p.many = n_sel == 0 && rows > 32;
-    p.tile_rows = p.many ? row_tiles(c->d) * row_waves(c->d) * 32 : 16;
+    p.many = n_sel == 0 && rows > kFewRows;
+    p.tile_rows = p.many ? row_waves(c->d) * 32 : 16;
     p.tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
     p.rows_pad = (int32_t)st::round_up(rows, 16);
     const int32_t list = std::max(1, n_sel > 0 ? std::min(n_sel, blocks_of(b->max_len)) : blocks_of(b->max_len));
     p.entries = n_sel > 0 ? n_sel : list;
     const int64_t pairs = std::max<int64_t>(1, p.units * p.tiles * c->n_heads);
-    const int64_t want = std::max<int64_t>(1, ((p.many ? KV_WANT : 8ll) * st::kComputeUnits + pairs - 1) / pairs);
-    int32_t chunk = (int32_t)std::max<int64_t>(KV_CHUNK, (list + want - 1) / want);
+    p.waves = pairs >= kManyRows ? 1 : 4;
+    // Workgroups that the chip holds at a time (registers and LDS), and splits of a row's blocks: one round of workgroups where
+    // there are few rows (each split is long enough to pay for its start), two where sequences of different lengths
+    // would leave a single round to the longest, and for a lone sequence what wastes least of its last round.
+    const int64_t slots = (int64_t)st::kComputeUnits * (p.many ? 1 : c->d <= 64 ? 4 : c->d <= 96 ? 3 : 2);
+    int64_t splits = 1;
+    if (p.waves == 1 && !p.many) splits = 1;
+    else if (pairs * 4 <= slots) splits = slots / pairs;
+    else if (b->n_seq > 1 && n_sel == 0) splits = (KV_MULT * slots + pairs - 1) / pairs;
+    else {
+        double best = 1e30;
+        for (int64_t s = 1; s <= 16; ++s) {
+            const double rounds = (double)((pairs * s + slots - 1) / slots);
+            const double cost = rounds * ((double)((list + s - 1) / s) + kSplitStart) + (s > 1 ? kSplitJoin : 0.0);
+            if (cost < best) best = cost, splits = s;
+        }
+    }
+    int32_t chunk = (int32_t)std::max<int64_t>(kLeastChunk, (list + splits - 1) / splits);
     if (chunk >= list) chunk = p.entries;
     p.chunk = chunk;
     p.splits = (p.entries + chunk - 1) / chunk;
     // Parts that read the same blocks go to one die, where the sequences and heads are enough to keep all dies alike.
-    const int64_t sh = (int64_t)b->n_seq * c->n_heads, per = (int64_t)p.tiles * p.splits * (n_sel > 0 ? b->max_tok : 1);
-    p.dies = per > p.splits && (sh % kDies == 0 || sh >= 8 * kDies) ? kDies : 1;
-    p.grid = st::round_up(sh, p.dies) * per;
+    const int64_t sh = (int64_t)b->n_seq * c->n_heads, per = (int64_t)p.tiles * (n_sel > 0 ? b->max_tok : 1);
+    p.dies = per > 1 && (sh % kDies == 0 || sh >= 8 * kDies) ? kDies : 1;
+    p.parts = st::round_up(sh, p.dies) * per;
+    p.grid = p.parts * p.splits;
     const int64_t uh = p.units * c->n_heads;
     const int64_t parts = p.splits > 1 ? uh * p.splits * p.rows_pad : 0;
     p.o_bytes = st::round_up(parts * c->d * 4, 256);
@@ -166,8 +178,9 @@ int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t st
     {
         TimedLaunch t(0, stream);
         const dim3 grid((unsigned)p.grid);
-        if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_tiles(D), row_waves(D)>), grid, dim3(row_waves(D) * 64), 0, stream, a);
-        else hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected>), grid, dim3(st::kKvThreads), 0, stream, a);
+        if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_waves(D)>), grid, dim3(row_waves(D) * 64), 0, stream, a);
+        else if (p.waves == 1) hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected, 1>), grid, dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected, 4>), grid, dim3(256), 0, stream, a);
     }
     if (p.splits > 1) {
         TimedLaunch t(1, stream);
@@ -278,7 +291,7 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     char* ws = (char*)dev_workspace;
     st::KvAttendArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
                           softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse,
-                          p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, p.rows_pad, (float*)ws, (float2*)(ws + p.o_bytes),
+                          p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)p.parts, p.rows_pad, (float*)ws, (float2*)(ws + p.o_bytes),
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr};
     hipStream_t stream = (hipStream_t)hip_stream;
@@ -357,7 +370,7 @@ int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     rc = with_dim(cache->d, [&](auto d) -> int {
         constexpr int D = decltype(d)::value;
         int rc2;
-        constexpr int kOneThreads = KV_ONE;
+        constexpr int kOneThreads = 512;
         if (one && (rc2 = allow_lds(&st::kv_score_kernel<D, true, kOneThreads>, lds))) return rc2;
         TimedLaunch t(0, stream);
         if (one) hipLaunchKernelGGL((st::kv_score_kernel<D, true, kOneThreads>), dim3((unsigned)groups), dim3(kOneThreads), lds, stream, a);

@@ -28,6 +28,7 @@ struct KvAttendArgs {
     void* out;
     float* lse;
     int32_t chunk, splits, tiles, tile_rows, dies;
+    uint32_t parts;      // workgroups to a split
     int32_t rows_pad;    // rows of a unit and head in the workspace
     float* part_o;       // [unit, head, split, rows_pad, d]
     float2* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of weights
@@ -48,6 +49,20 @@ __device__ inline void kv_query_unit(float top, float scale_log2, float* up, flo
     *factor = fabsf(scale_log2) * ldexpf(1.0f, e - 13);
 }
 
+// A row of a unit and head: its token and its head of queries.
+struct KvRow {
+    int64_t tok;
+    int q_head, i;  // i: token of the unit
+};
+__device__ inline KvRow kv_row(int row, int64_t tok_unit, int head, int group)
+{
+    KvRow r;
+    r.i = (int)((uint32_t)row / (uint32_t)group);
+    r.tok = tok_unit + r.i;
+    r.q_head = head * group + row - r.i * group;
+    return r;
+}
+
 // What a tile of rows of a unit (a sequence, or a token whose blocks were selected) and a head reads.
 struct KvTile {
     int seq;
@@ -58,45 +73,42 @@ struct KvTile {
     int past, len, group;  // a row of token i of the unit sees positions below len - past + i (causal) or len
     bool causal;
     __device__ int limit(int i) const { return max(0, causal ? len - past + i : len); }
-    // row -> token of the unit, and the output row [n_tok, n_q_heads] it is
-    __device__ int token(int row) const { return row / group; }
-    __device__ int64_t place(int row, int head, int64_t heads_all) const
-    {
-        const int i = row / group;
-        return (tok_unit + i) * heads_all + head * group + (row - i * group);
-    }
+    __device__ int token(int row) const { return (int)((uint32_t)row / (uint32_t)group); }  // of the unit
 };
 
-// Which part of the work a workgroup does.  The parts of one sequence and head that read the same blocks (tiles of rows, tokens whose
-// blocks were selected) follow one another on one of the chip's 8 dies, whose L2 serves them: workgroups are handed to the dies in turn.
+// Which part of the work a workgroup does.  The first splits of all rows come first, so that the last workgroups to start
+// are those with what long sequences have left.  Parts of one sequence and head that read the same blocks (tiles of rows, tokens
+// whose blocks were selected) follow one another on one of the chip's 8 dies, whose L2 serves them: workgroups are handed to
+// the dies in turn.
 struct KvPlace {
     int seq, head, unit, tile, split;  // unit < 0: none
 };
 template <bool kSelected>
 __device__ inline KvPlace kv_place(const KvAttendArgs& a)
 {
-    const uint32_t per = (uint32_t)a.tiles * a.splits * (kSelected ? a.b.max_tok : 1);
+    const uint32_t per = (uint32_t)a.tiles * (kSelected ? a.b.max_tok : 1);
+    const uint32_t split = blockIdx.x / a.parts, at = blockIdx.x - split * a.parts;
     uint32_t pair, item;
     if (a.dies > 1) {
-        const uint32_t k = blockIdx.x / a.dies;
-        pair = k / per * a.dies + blockIdx.x % a.dies;
-        item = k % per;
+        const uint32_t k = at / a.dies;
+        pair = k / per;
+        item = k - pair * per;
+        pair = pair * a.dies + (at - k * a.dies);
     } else {
-        pair = blockIdx.x / per;
-        item = blockIdx.x % per;
+        pair = at / per;
+        item = at - pair * per;
     }
     KvPlace p;
     p.seq = pair / a.c.n_heads;
-    p.head = pair % a.c.n_heads;
-    p.unit = p.seq;
-    p.tile = item % a.tiles;
-    item /= a.tiles;
-    p.split = item % a.splits;
-    if (p.seq >= a.b.n_seq) p.unit = -1;
-    else if (kSelected) {
-        const KvSeq q = kv_seq(a.b, p.seq);
-        const int i = item / a.splits;
-        p.unit = i < q.count ? q.first + i : -1;
+    p.head = pair - p.seq * a.c.n_heads;
+    p.unit = p.seq < a.b.n_seq ? p.seq : -1;
+    p.split = split;
+    const int i = item / a.tiles;
+    p.tile = item - i * a.tiles;
+    if (kSelected && p.unit >= 0) {
+        int first, count;
+        kv_tokens(a.b, p.seq, &first, &count);
+        p.unit = i < count ? first + i : -1;
     }
     return p;
 }
@@ -115,7 +127,7 @@ __device__ inline KvTile kv_tile(const KvAttendArgs& a, int seq, int unit, int r
     // (a unit of one token: that token is its token 0)
     t.past = kSelected ? q.count - 1 - (unit - q.first) : q.count - 1;
     t.tok_unit = kSelected ? unit : q.first;
-    const int i_first = row0 / a.group, i_last = max(0, min(row0 + tile_rows, t.rows) - 1) / a.group;
+    const int i_first = t.token(row0), i_last = t.token(max(0, min(row0 + tile_rows, t.rows) - 1));
     t.tok_first = t.tok_unit + i_first;
     t.tok_last = t.tok_unit + i_last;
     t.n_blocks = row0 < t.rows ? (t.limit(i_last) + kKvBlock - 1) / kKvBlock : 0;
@@ -123,29 +135,47 @@ __device__ inline KvTile kv_tile(const KvAttendArgs& a, int seq, int unit, int r
     return t;
 }
 
-template <int D, bool kSelected>
-__global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a)
+// kWaves wavefronts share the blocks of 16 rows and join what they found in the LDS (one: nothing to join, for calls that
+// fill the chip with rows alone).
+template <int D, bool kSelected, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void kv_attend_kernel(KvAttendArgs a)
 {
     constexpr int kSteps = D / 32, kWide = D / 64, kCh = D / 16;
     constexpr bool kHalf = D % 64 != 0;
     constexpr bool kAhead = D <= 128;  // keys of the next block and values of this one are loaded ahead (256: too few registers)
-    __shared__ float s_o[4][16][D + 4];
-    __shared__ float2 s_ml[4][16];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+    __shared__ float s_o[kWaves][16][D + 4];
+    __shared__ float2 s_ml[kWaves][16];
+    const int lane = threadIdx.x & 63, w = kWaves == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const KvPlace at = kv_place<kSelected>(a);
     if (at.unit < 0) return;
-    const int split = at.split, head = at.head, unit = at.unit, row0 = at.tile * 16;
-    const KvTile t = kv_tile<kSelected>(a, at.seq, unit, row0, 16);
-    if (row0 >= t.rows) return;
+    const int split = at.split, head = at.head, unit = at.unit, row0 = at.tile * 16, jb = split * a.chunk;
     const int64_t uh = (int64_t)unit * a.c.n_heads + head, heads_all = (int64_t)a.c.n_heads * a.group;
-    const int row = row0 + n;
-    const bool valid = row < t.rows;
-    const int64_t place = valid ? t.place(row, head, heads_all) : 0;
-    const int64_t tok = place / heads_all;
-    const int lim = valid ? t.limit(t.token(row)) : 0, lim_all = t.limit(t.token(row0));
-    const int jb = split * a.chunk, je = min(jb + a.chunk, t.n_list);
-    if (split > 0 && jb >= je) return;
     const bool bf16 = a.bf16 != 0;
+    // A workgroup's life is short, so what it reads first is asked for at once: the first blocks (pages, or the
+    // list of what was selected), the queries, the length.
+    const int32_t* list = kSelected ? a.blocks + uh * a.n_sel : a.b.tables + (int64_t)at.seq * a.b.max_blocks;
+    const int first_entry = list[min(jb + kWaves * lane + w, (kSelected ? a.n_sel : a.b.max_blocks) - 1)];
+    const int row = row0 + n;
+    bool valid;
+    KvRow of;
+    uint4 raw[kSteps];
+    {
+        int first = unit, rows = a.group;
+        if (!kSelected) kv_tokens(a.b, at.seq, &first, &rows), rows *= a.group;
+        if (row0 >= rows) return;
+        valid = row < rows;
+        of = kv_row(valid ? row : row0, first, head, a.group);
+        const uint16_t* src = (const uint16_t*)a.q + of.tok * a.q_stride + of.q_head * D;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const int ch = k < 2 * kWide ? k / 2 * 64 + g * 16 + k % 2 * 8 : kWide * 64 + g * 8;
+            raw[k] = *(const uint4*)(src + ch);
+        }
+    }
+    const KvTile t = kv_tile<kSelected>(a, at.seq, unit, row0, 16);
+    const int lim = valid ? t.limit(of.i) : 0, lim_all = t.limit(t.token(row0));
+    const int je = min(jb + a.chunk, t.n_list);
+    if (split > 0 && jb >= je) return;
 
     // queries: eight channels of each 32 to a lane, in the order in which it holds those of a key
     half8 q[kSteps];
@@ -153,15 +183,14 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
     {
         float f[kSteps][8];
         float top = 0.0f;
-        const uint16_t* src = (const uint16_t*)a.q + tok * a.q_stride + (place - tok * heads_all) * D;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-            const int ch = k < 2 * kWide ? k / 2 * 64 + g * 16 + k % 2 * 8 : kWide * 64 + g * 8;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (valid) v = *(const uint4*)(src + ch);
-            eight_floats(v, bf16, f[k]);
+            eight_floats(raw[k], bf16, f[k]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[k][j]));
+            for (int j = 0; j < 8; ++j) {
+                f[k][j] = valid ? f[k][j] : 0.0f;
+                top = fmaxf(top, fabsf(f[k][j]));
+            }
         }
         float up;
         kv_query_unit(max_over_16_32(top), a.scale_log2, &up, &factor);
@@ -176,13 +205,14 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
 #pragma unroll
     for (int c = 0; c < kCh; ++c) o[c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (int j0 = jb; j0 < je; j0 += 256) {
+    for (int j0 = jb; j0 < je; j0 += 64 * kWaves) {
         // up to 64 blocks of this wavefront: page and scales, one to a lane
-        const int j = j0 + 4 * lane + w;
+        const int j = j0 + kWaves * lane + w;
         int block = -1, page = -1;
         if (j < je) {
-            block = kSelected ? a.blocks[uh * a.n_sel + j] : j;
-            if (block >= 0 && block < t.n_blocks) page = kv_page(a.c, a.b, t.seq, block);
+            const int entry = j0 == jb ? first_entry : list[j];
+            block = kSelected ? entry : j;
+            if (block >= 0 && block < t.n_blocks) page = kSelected ? kv_page(a.c, a.b, t.seq, block) : kv_page_of(a.c, entry);
         }
         if (a.mask && page >= 0) {  // a block that no row of the tile sees is not read
             uint64_t any = 0;
@@ -228,7 +258,7 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
             if (part) {
                 const int left = lim - b * kKvBlock;
                 see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
-                if (a.mask && see) see &= a.mask[tok * a.mask_words + b];
+                if (a.mask && see) see &= a.mask[of.tok * a.mask_words + b];
             }
             float4v x[4];
 #pragma unroll
@@ -250,8 +280,7 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
 #pragma unroll
                 for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (!((mine >> (tt * 16 + r)) & 1)) x[tt][r] = -__builtin_inff();
+                    for (int r = 0; r < 4; ++r) x[tt][r] = kv_seen(x[tt][r], (uint32_t)(mine >> (tt / 2 * 32)), tt % 2 * 16 + r);
             }
             float top = x[0][0];
 #pragma unroll
@@ -283,7 +312,7 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
             l += sum;
             if (a.block_ml) {
                 const float all = sum_over_16_32(sum);
-                if (g == 0) a.block_ml[(uh * a.entries + j0 + 4 * cur + w) * a.rows_pad + row] = make_float2(m, all);
+                if (g == 0) a.block_ml[(uh * a.entries + j0 + kWaves * cur + w) * a.rows_pad + row] = make_float2(m, all);
             }
 #pragma unroll
             for (int c = 0; c < kCh; ++c) {
@@ -298,21 +327,21 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
     }
     l = sum_over_16_32(l);
 
-    // the four wavefronts' states into one
+    // the wavefronts' states into one
     if (g == 0) s_ml[w][n] = make_float2(m, l);
 #pragma unroll
     for (int c = 0; c < kCh; ++c) *(float4v*)&s_o[w][n][c * 16 + g * 4] = o[c];
     __syncthreads();
     const int64_t part = (uh * a.splits + split) * a.rows_pad + row0;
-    for (int i = threadIdx.x; i < 16 * (D / 4); i += kKvThreads) {
+    for (int i = threadIdx.x; i < 16 * (D / 4); i += kWaves * 64) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
         float top = -__builtin_inff();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) top = fmaxf(top, s_ml[k][r].x);
+        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[k][r].x);
         float sum = 0.0f;
         float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kWaves; ++k) {
             const float2 ml = s_ml[k][r];
             const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
             const float4v v = *(const float4v*)&s_o[k][r][c];
@@ -321,12 +350,13 @@ __global__ __launch_bounds__(kKvThreads, 2) void kv_attend_kernel(KvAttendArgs a
             for (int u = 0; u < 4; ++u) y[u] += v[u] * f;
         }
         if (row0 + r >= t.rows) continue;
-        if (a.splits > 1) {
+        if (t.n_list > a.chunk) {
             *(float4v*)(a.part_o + (part + r) * D + c) = y;
             if (c == 0) a.part_ml[part + r] = make_float2(top, sum);
             continue;
         }
-        const int64_t place = t.place(row0 + r, head, heads_all);
+        const KvRow to = kv_row(row0 + r, t.tok_unit, head, a.group);
+        const int64_t place = to.tok * heads_all + to.q_head;
         const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
         uint32_t h[4];
 #pragma unroll
@@ -356,12 +386,13 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     const int tok = there ? (int)(place / heads_all) : 0, qh = there ? (int)(place % heads_all) : 0, head = qh / a.group;
     const int s = kv_seq_of(a.b, tok);
     const KvSeq q = kv_seq(a.b, s);
-    const bool mine = there && tok >= q.first && tok < q.first + q.count;
+    bool mine = there && tok >= q.first && tok < q.first + q.count;
     const int unit = kSelected ? tok : s;
     const int row = !mine ? 0 : kSelected ? qh % a.group : (tok - q.first) * a.group + qh % a.group;
     const KvTile t = kv_tile<kSelected>(a, s, unit, row / a.tile_rows * a.tile_rows, a.tile_rows);
     const int64_t uh = (int64_t)unit * a.c.n_heads + head, stride = a.rows_pad;
-    const int splits = mine ? min(a.splits, max(1, (t.n_list + a.chunk - 1) / a.chunk)) : 0;
+    mine = mine && t.n_list > a.chunk;  // (a row in one split has its output already)
+    const int splits = mine ? (t.n_list + a.chunk - 1) / a.chunk : 0;
     const int64_t part = uh * a.splits * stride + row;
     float top = -__builtin_inff();
     for (int i = me; i < splits; i += kTeam) top = fmaxf(top, a.part_ml[part + i * stride].x);

@@ -37,17 +37,21 @@ struct KvSeq {
 };
 
 // What a device array says is cut to what the call allows.
+__device__ inline void kv_tokens(const KvBatchView& b, int s, int* first, int* count)
+{
+    if (b.offsets) {
+        *first = max(0, min(b.offsets[s], b.n_tok));
+        *count = max(0, min(min(b.offsets[s + 1], b.n_tok) - *first, b.max_tok));
+    } else {
+        *first = s * b.max_tok;
+        *count = b.max_tok;
+    }
+}
 __device__ inline KvSeq kv_seq(const KvBatchView& b, int s)
 {
     KvSeq r;
     r.len = max(0, min(b.lengths[s], b.max_len));
-    if (b.offsets) {
-        r.first = max(0, min(b.offsets[s], b.n_tok));
-        r.count = max(0, min(min(b.offsets[s + 1], b.n_tok) - r.first, b.max_tok));
-    } else {
-        r.first = s * b.max_tok;
-        r.count = b.max_tok;
-    }
+    kv_tokens(b, s, &r.first, &r.count);
     return r;
 }
 
@@ -65,10 +69,10 @@ __device__ inline int kv_seq_of(const KvBatchView& b, int tok)
 }
 
 // Page of block b, -1 where the table names none.
+__device__ inline int kv_page_of(const KvCacheView& c, int entry) { return entry >= 0 && (int64_t)entry < c.n_pages ? entry : -1; }
 __device__ inline int kv_page(const KvCacheView& c, const KvBatchView& b, int s, int block)
 {
-    const int p = b.tables[(int64_t)s * b.max_blocks + block];
-    return p >= 0 && (int64_t)p < c.n_pages ? p : -1;
+    return kv_page_of(c, b.tables[(int64_t)s * b.max_blocks + block]);
 }
 
 // Slot of token t of a block in a row of values: bits 5 4 3 2 1 0 of t in the order 3 2 5 4 1 0.
@@ -121,15 +125,44 @@ __device__ inline half8 eight_halves(uint32_t lo, uint32_t hi)
     return __builtin_bit_cast(half8, make_uint4(a.x, a.y, b.x, b.y));
 }
 
-__device__ inline float max_over_16_32(float v)  // over the lanes that share lane % 16
+// Steps over the lanes that share lane % 16 (or lane % 32), with moves between registers in place of the LDS: a swap of
+// rows of 16 (halves of 32) lanes of a value with itself leaves one partner's value in the one result, the other's in the other.
+__device__ inline float2 both_of_16(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float2 both_of_32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_over_32(float v)
+{
+    const float2 r = both_of_32(v);
+    return fmaxf(r.x, r.y);
+}
+__device__ inline float sum_over_32(float v)
+{
+    const float2 r = both_of_32(v);
+    return r.x + r.y;
+}
+__device__ inline float max_over_16_32(float v)
+{
+    const float2 r = both_of_16(v);
+    return max_over_32(fmaxf(r.x, r.y));
 }
 __device__ inline float sum_over_16_32(float v)
 {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    const float2 r = both_of_16(v);
+    return sum_over_32(r.x + r.y);
+}
+
+// x where the bit is 1, -inf where it is 0.
+__device__ inline float kv_seen(float x, uint32_t bits, int bit)
+{
+    const uint32_t yes = (uint32_t)((int)(bits << (31 - bit)) >> 31);
+    return __uint_as_float((__float_as_uint(x) & yes) | (0xFF800000u & ~yes));
 }
 
 }  // namespace st

@@ -10,25 +10,20 @@
 #pragma once
 #include "st_kv_attend_kernels.h"
 
-#ifndef KV_SCHED
-#define KV_SCHED
-#endif
 namespace st {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-__device__ inline float max_over_32(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
-
-template <int D, int kTiles, int kWaves>
-__global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel(KvAttendArgs a)
+template <int D, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_kernel(KvAttendArgs a)
 {
-    constexpr int kThreads = kWaves * 64, kRows = kWaves * kTiles * 32, kSteps = D / 16, kCh = D / 32;
+    constexpr int kTiles = 1, kThreads = kWaves * 64, kRows = kWaves * kTiles * 32, kSteps = D / 16, kCh = D / 32;
     constexpr int kKeyBytes = 2 * D + 16, kValBytes = 2 * kKvBlock + 16;  // rows of the LDS, an odd number of 16 bytes apart
     constexpr int kPieces = (4 * D + kThreads - 1) / kThreads;            // 16 bytes of keys, and of values, of a thread
     __shared__ __align__(16) char s_k[2][kKvBlock * kKeyBytes];
     __shared__ __align__(16) char s_v[2][D * kValBytes];
     __shared__ uint64_t s_any[kWaves][64];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const KvPlace at = kv_place<false>(a);
     if (at.unit < 0) return;
     const int split = at.split, head = at.head, unit = at.unit, row0 = at.tile * kRows;
@@ -48,10 +43,10 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
     for (int rt = 0; rt < kTiles; ++rt) {
         row[rt] = row0 + (w * kTiles + rt) * 32 + n;
         const bool valid = row[rt] < t.rows;
-        const int64_t place = valid ? t.place(row[rt], head, heads_all) : 0;
-        tok[rt] = place / heads_all;
-        lim[rt] = valid ? t.limit(t.token(row[rt])) : 0;
-        const uint16_t* src = (const uint16_t*)a.q + tok[rt] * a.q_stride + (place - tok[rt] * heads_all) * D + h * 8;
+        const KvRow of = kv_row(valid ? row[rt] : row0, t.tok_unit, head, a.group);
+        tok[rt] = of.tok;
+        lim[rt] = valid ? t.limit(of.i) : 0;
+        const uint16_t* src = (const uint16_t*)a.q + of.tok * a.q_stride + of.q_head * D + h * 8;
         uint4 raw[kSteps];
         float top = 0.0f;
 #pragma unroll
@@ -80,6 +75,7 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
 #pragma unroll
         for (int c = 0; c < kCh; ++c) o[rt][c] = float16v(0.0f);
     }
+    const bool busy = row0 + w * kTiles * 32 < t.rows;  // this wavefront has rows; all help with the blocks
     const int lim_all = t.limit(t.token(min(row0 + w * kTiles * 32, t.rows - 1)));  // its rows see at least the positions below this one
     float v_unit = 0.0f;                                                            // outputs are in units of this value scale
 
@@ -188,10 +184,7 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
 #pragma unroll
                     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const uint32_t yes = (uint32_t)((int)((uint32_t)(see >> (tt * 32)) << (31 - ((i >> 2) * 8 + (i & 3)))) >> 31);
-                            x[rt][tt][i] = __uint_as_float((__float_as_uint(x[rt][tt][i]) & yes) | (0xFF800000u & ~yes));
-                        }
+                        for (int i = 0; i < 16; ++i) x[rt][tt][i] = kv_seen(x[rt][tt][i], (uint32_t)(see >> (tt * 32)), (i >> 2) * 8 + (i & 3));
                 }
             }
             const float ks_b = __uint_as_float(lane_value(__float_as_uint(ks_l), cur));
@@ -250,11 +243,10 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
                 }
             put_keys(buf);
             put_values(buf ^ 1, next);
-            KV_SCHED
             if (a.block_ml)
 #pragma unroll
                 for (int rt = 0; rt < kTiles; ++rt) {
-                    const float both = sums[rt] + __shfl_xor(sums[rt], 32);
+                    const float both = sum_over_32(sums[rt]);
                     if (h == 0 && row[rt] < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row[rt]] = make_float2(m[rt], both);
                 }
             __syncthreads();
@@ -276,7 +268,6 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
         after(&second);
         third = second;
         after(&third);
-        __syncthreads();  // (the LDS may still be read for the blocks of the round before)
         load(a.c.k, first, kraw);
         load(a.c.v, first, vraw);
         put_keys(0);
@@ -284,7 +275,21 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
         load(a.c.k, second, kraw);
         put_keys(1);
         __syncthreads();
-        products(0, xa);
+        if (busy) products(0, xa);
+        __syncthreads();  // (the first step writes other keys where these were)
+        // (loops of their own: with the choice inside the step its products and its stores are no longer interleaved)
+        if (!busy) {
+            for (int buf = 0; left > 0; --left, buf ^= 1) {
+                load(a.c.k, third, kraw);
+                load(a.c.v, second, vraw);
+                put_keys(buf);
+                put_values(buf ^ 1, second);
+                second = third;
+                after(&third);
+                __syncthreads();
+            }
+            continue;
+        }
         for (; left > 0; left -= 2) {
             step(0, first, second, third, xa, xb);
             first = second;
@@ -300,9 +305,9 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
 
 #pragma unroll
     for (int rt = 0; rt < kTiles; ++rt) {
-        const float sum = l[rt] + __shfl_xor(l[rt], 32);
+        const float sum = sum_over_32(l[rt]);
         if (row[rt] >= t.rows) continue;
-        if (a.splits > 1) {
+        if (t.n_list > a.chunk) {
             const int64_t part = (uh * a.splits + split) * a.rows_pad + row[rt];
 #pragma unroll
             for (int c = 0; c < kCh; ++c)
@@ -316,7 +321,8 @@ __global__ __launch_bounds__(kWaves * 64, kWaves / 4) void kv_attend_rows_kernel
             if (h == 0) a.part_ml[part] = make_float2(m[rt], sum);
             continue;
         }
-        const int64_t place = t.place(row[rt], head, heads_all);
+        const KvRow to = kv_row(row[rt], t.tok_unit, head, a.group);
+        const int64_t place = to.tok * heads_all + to.q_head;
         const float inv = sum > 0.0f || sum != sum ? v_unit / sum : 0.0f;
 #pragma unroll
         for (int c = 0; c < kCh; ++c)
