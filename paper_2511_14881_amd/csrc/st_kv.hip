@@ -103,9 +103,6 @@ int with_dim(int32_t d, F&& body)
     return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", d);
 }
 
-#ifndef KV_MULT
-#define KV_MULT 2
-#endif
 constexpr int kFewRows = 48;       // of a sequence and head: up to here tiles of 16 that read the cache themselves (64 rows: 38.5 us
                                   // against 36.7, 40 rows: 35.5 against 36.3; 4 x 8192 tokens, 8 heads of 128)
 constexpr int row_waves(int d) { return d > 128 ? 4 : 8; }  // of the kernel for many rows (256: 512 registers to a lane)
@@ -145,7 +142,7 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     int64_t splits = 1;
     if (p.waves == 1 && !p.many) splits = 1;
     else if (pairs * 4 <= slots) splits = slots / pairs;
-    else if (b->n_seq > 1 && n_sel == 0) splits = (KV_MULT * slots + pairs - 1) / pairs;
+    else if (b->n_seq > 1 && n_sel == 0) splits = (slots + pairs - 1) / pairs;
     else {
         double best = 1e30;
         for (int64_t s = 1; s <= 16; ++s) {
@@ -293,23 +290,24 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
                           softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse,
                           p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)p.parts, p.rows_pad, (float*)ws, (float2*)(ws + p.o_bytes),
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
-                          mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr};
+                          mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr, dev_mass_in, decay, dev_mass_out};
     hipStream_t stream = (hipStream_t)hip_stream;
     if (batch->n_tok > 0 && batch->max_tok > 0)
         with_dim(cache->d, [&](auto d) -> int {
             return n_sel > 0 ? launch_attend<decltype(d)::value, true>(a, p, stream) : launch_attend<decltype(d)::value, false>(a, p, stream);
         });
-    if (mass && batch->n_seq > 0) {
-        st::KvMassArgs m = {a, dev_mass_in, decay, dev_mass_out};
+    // (one workgroup to each sequence and head writes the weights itself, unless there are no tokens)
+    const bool whole = n_sel == 0 && !p.many && p.tiles == 1 && p.splits == 1 && !batch->dev_offsets;
+    if (mass && batch->n_seq > 0 && !(whole && batch->max_tok > 0)) {
         const int64_t sh = (int64_t)batch->n_seq * cache->n_heads;
         const int lanes = p.rows_pad > 16 ? 64 : 16, of = st::kKvThreads / lanes;
         const int64_t groups = n_sel > 0 ? sh : sh * ((batch->max_blocks + of - 1) / of);
         if ((rc = check_grid(groups))) return rc;
         if (n_sel > 0 && (rc = allow_lds(&st::kv_mass_selected_kernel, batch->max_blocks * 4))) return rc;
         TimedLaunch t(1, stream);
-        if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, dim3((unsigned)groups), dim3(st::kKvThreads), batch->max_blocks * 4, stream, m);
-        else if (lanes == 64) hipLaunchKernelGGL(st::kv_mass_kernel<64>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, m);
-        else hipLaunchKernelGGL(st::kv_mass_kernel<16>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, m);
+        if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, dim3((unsigned)groups), dim3(st::kKvThreads), batch->max_blocks * 4, stream, a);
+        else if (lanes == 64) hipLaunchKernelGGL(st::kv_mass_kernel<64>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        else hipLaunchKernelGGL(st::kv_mass_kernel<16>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
     }
     ST_HIP(hipGetLastError());
     return ST_OK;
@@ -379,11 +377,12 @@ int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     });
     if (rc != ST_OK) return rc;
     if (!one) {
-        if (blocks > 512 && (rc = allow_lds(&st::kv_choose_kernel, lds))) return rc;
+        if (blocks > 1024 && (rc = allow_lds(&st::kv_choose_kernel, lds))) return rc;
         TimedLaunch t(1, stream);
         const dim3 waves((unsigned)((rows + 3) / 4));
-        if (blocks <= 128) hipLaunchKernelGGL(st::kv_choose_wave_kernel<2>, waves, dim3(st::kKvThreads), 0, stream, a);
+        if (blocks <= 256) hipLaunchKernelGGL(st::kv_choose_wave_kernel<4>, waves, dim3(st::kKvThreads), 0, stream, a);
         else if (blocks <= 512) hipLaunchKernelGGL(st::kv_choose_wave_kernel<8>, waves, dim3(st::kKvThreads), 0, stream, a);
+        else if (blocks <= 1024) hipLaunchKernelGGL(st::kv_choose_wave_kernel<16>, waves, dim3(st::kKvThreads), 0, stream, a);
         else hipLaunchKernelGGL(st::kv_choose_kernel, dim3((unsigned)rows), dim3(st::kKvThreads), lds, stream, a);
     }
     ST_HIP(hipGetLastError());

@@ -35,7 +35,17 @@ struct KvAttendArgs {
     float2* block_ml;    // [unit, head, entries, rows_pad]: maximum so far, sum of the block's weights; or null
     int64_t entries;     // blocks, or selected ones
     float2* row_ml;      // [unit, head, rows_pad]: final maximum and sum, written where block_ml is
+    const float* mass_in;
+    float decay;
+    float* mass_out;     // [n_seq, n_heads, max_blocks] or null
 };
+
+__device__ inline float kv_weight(float2 block, float2 row)
+{
+    return row.y != 0.0f && block.y != 0.0f ? block.y * __builtin_amdgcn_exp2f(block.x - row.x) / row.y : 0.0f;
+}
+// Whether the workgroup that has all rows and blocks of a sequence and head writes its blocks' weights too.
+__device__ inline bool kv_whole(const KvAttendArgs& a, int n_list) { return a.tiles == 1 && a.tile_rows == 16 && n_list <= a.chunk; }
 
 constexpr float kKvLift = 8.0f;   // weights are 2^8 times themselves,
 constexpr float kKvSlack = 7.0f;  // and the maximum they go by may lie 7 (in powers of two) below the largest logit
@@ -144,7 +154,7 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
     constexpr bool kHalf = D % 64 != 0;
     constexpr bool kAhead = D <= 128;  // keys of the next block and values of this one are loaded ahead (256: too few registers)
     __shared__ float s_o[kWaves][16][D + 4];
-    __shared__ float2 s_ml[kWaves][16];
+    __shared__ float2 s_ml[kWaves][16], s_fin[16];
     const int lane = threadIdx.x & 63, w = kWaves == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const KvPlace at = kv_place<kSelected>(a);
     if (at.unit < 0) return;
@@ -365,7 +375,20 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
         if (c == 0) {
             if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(sum)) * 0.69314718056f;
             if (a.row_ml) a.row_ml[uh * a.rows_pad + row0 + r] = make_float2(top, sum);
+            s_fin[r] = make_float2(top, sum);
         }
+    }
+    if (kSelected || !a.mass_out || !kv_whole(a, t.n_list)) return;
+    __syncthreads();
+    const int nb = a.b.max_blocks, held = (t.len + kKvBlock - 1) / kKvBlock;
+    const int64_t to = uh * nb;
+    for (int b = threadIdx.x; b < nb; b += kWaves * 64) {
+        float sum = 0.0f;
+        if (b < t.n_list) {
+            const float2* block = a.block_ml + (uh * a.entries + b) * a.rows_pad;
+            for (int r = 0; r < t.rows; ++r) sum += kv_weight(block[r], s_fin[r]);
+        }
+        a.mass_out[to + b] = b < held ? (a.mass_in ? a.mass_in[to + b] * a.decay : 0.0f) + sum : 0.0f;
     }
 }
 
@@ -437,70 +460,59 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     }
 }
 
-struct KvMassArgs {
-    KvAttendArgs t;
-    const float* in;
-    float decay;
-    float* out;
-};
-
-__device__ inline float kv_weight(float2 block, float2 row)
-{
-    return row.y != 0.0f && block.y != 0.0f ? block.y * __builtin_amdgcn_exp2f(block.x - row.x) / row.y : 0.0f;
-}
-
 // Weights of the blocks, summed over the rows of a sequence and head: kLanes lanes to a block, each every kLanes-th row.
 template <int kLanes>
-__global__ __launch_bounds__(kKvThreads) void kv_mass_kernel(KvMassArgs a)
+__global__ __launch_bounds__(kKvThreads) void kv_mass_kernel(KvAttendArgs a)
 {
     constexpr int kBlocks = kKvThreads / kLanes;
-    const int nb = a.t.b.max_blocks, chunks = (nb + kBlocks - 1) / kBlocks;
+    const int nb = a.b.max_blocks, chunks = (nb + kBlocks - 1) / kBlocks;
     const int chunk = blockIdx.x % chunks, sh = blockIdx.x / chunks;
-    const int s = sh / a.t.c.n_heads, lane = threadIdx.x % kLanes;
+    const int s = sh / a.c.n_heads, lane = threadIdx.x % kLanes;
     const int b = chunk * kBlocks + threadIdx.x / kLanes;
-    const KvSeq q = kv_seq(a.t.b, s);
+    const KvSeq q = kv_seq(a.b, s);
+    if (kLanes == 16 && q.count > 0 && kv_whole(a, kv_tile<false>(a, s, s, 0, 16).n_list)) return;  // (written already)
     const bool held = b < nb && b * kKvBlock < q.len;
     float sum = 0.0f;
     if (held) {
         // (nothing was written for rows that end before the block)
         int first = 0;
-        if (a.t.causal) first = max(0, b * kKvBlock - (q.len - q.count)) * a.t.group;
-        const float2* block = a.t.block_ml + ((int64_t)sh * a.t.entries + b) * a.t.rows_pad;
-        const float2* row = a.t.row_ml + (int64_t)sh * a.t.rows_pad;
-        for (int r = first + lane; r < q.count * a.t.group; r += kLanes) sum += kv_weight(block[r], row[r]);
+        if (a.causal) first = max(0, b * kKvBlock - (q.len - q.count)) * a.group;
+        const float2* block = a.block_ml + ((int64_t)sh * a.entries + b) * a.rows_pad;
+        const float2* row = a.row_ml + (int64_t)sh * a.rows_pad;
+        for (int r = first + lane; r < q.count * a.group; r += kLanes) sum += kv_weight(block[r], row[r]);
     }
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if (lane != 0 || b >= nb) return;
     const int64_t to = (int64_t)sh * nb + b;
-    a.out[to] = held ? (a.in ? a.in[to] * a.decay : 0.0f) + sum : 0.0f;
+    a.mass_out[to] = held ? (a.mass_in ? a.mass_in[to] * a.decay : 0.0f) + sum : 0.0f;
 }
 
 // The same where blocks were selected: token after token, each adds to the blocks it read.
-__global__ __launch_bounds__(kKvThreads) void kv_mass_selected_kernel(KvMassArgs a)
+__global__ __launch_bounds__(kKvThreads) void kv_mass_selected_kernel(KvAttendArgs a)
 {
     extern __shared__ float acc[];
-    const int nb = a.t.b.max_blocks;
-    const int head = blockIdx.x % a.t.c.n_heads, s = blockIdx.x / a.t.c.n_heads;
-    const KvSeq q = kv_seq(a.t.b, s);
+    const int nb = a.b.max_blocks;
+    const int head = blockIdx.x % a.c.n_heads, s = blockIdx.x / a.c.n_heads;
+    const KvSeq q = kv_seq(a.b, s);
     const int held = (q.len + kKvBlock - 1) / kKvBlock;
     for (int b = threadIdx.x; b < held; b += kKvThreads) acc[b] = 0.0f;
     __syncthreads();
     for (int i = 0; i < q.count; ++i) {
-        const int64_t th = (int64_t)(q.first + i) * a.t.c.n_heads + head;
-        for (int j = threadIdx.x; j < a.t.n_sel; j += kKvThreads) {
-            const int b = a.t.blocks[th * a.t.n_sel + j];
+        const int64_t th = (int64_t)(q.first + i) * a.c.n_heads + head;
+        for (int j = threadIdx.x; j < a.n_sel; j += kKvThreads) {
+            const int b = a.blocks[th * a.n_sel + j];
             if (b < 0 || b >= held) continue;
             float sum = 0.0f;
-            for (int h = 0; h < a.t.group; ++h)
-                sum += kv_weight(a.t.block_ml[(th * a.t.n_sel + j) * a.t.rows_pad + h], a.t.row_ml[th * a.t.rows_pad + h]);
+            for (int h = 0; h < a.group; ++h)
+                sum += kv_weight(a.block_ml[(th * a.n_sel + j) * a.rows_pad + h], a.row_ml[th * a.rows_pad + h]);
             acc[b] += sum;
         }
         __syncthreads();
     }
     const int64_t to = (int64_t)blockIdx.x * nb;
     for (int b = threadIdx.x; b < nb; b += kKvThreads)
-        a.out[to + b] = b < held ? (a.in ? a.in[to + b] * a.decay : 0.0f) + acc[b] : 0.0f;
+        a.mass_out[to + b] = b < held ? (a.mass_in ? a.mass_in[to + b] * a.decay : 0.0f) + acc[b] : 0.0f;
 }
 
 }  // namespace st

@@ -237,11 +237,14 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvReadArgs a)
     if (!values) {
         const float sc = n ? a.c.k_scale[ph] : 0.0f;
         if (a.k) {
+            constexpr int kLoads = D * kKvBlock / 4 / kKvThreads;
             const uint32_t* src = (const uint32_t*)(a.c.k + ph * (D * kKvBlock));
             float4v* dst = (float4v*)(a.k + out * (D * kKvBlock));
-#pragma unroll 4
-            for (int i = tid; i < D * kKvBlock / 4; i += kKvThreads)
-                __builtin_nontemporal_store(i / (D / 4) < n ? kv_floats(src[i], sc) : zero, dst + i);
+            uint32_t w[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) w[i] = src[i * kKvThreads + tid];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) __builtin_nontemporal_store((i * kKvThreads + tid) / (D / 4) < n ? kv_floats(w[i], sc) : zero, dst + i * kKvThreads + tid);
         }
         if (a.bounds)
             for (int i = tid; i < 2 * D; i += kKvThreads) a.bounds[out * (2 * D) + i] = n ? (float)a.c.bounds[ph * (2 * D) + i] * sc : 0.0f;
@@ -252,8 +255,13 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvReadArgs a)
     const float sc = n ? a.c.v_scale[ph] : 0.0f;
     const uint32_t* src = (const uint32_t*)(a.c.v + ph * (D * kKvBlock));
     __shared__ uint32_t tile[D * (kKvBlock / 4 + 1)];
-    if (n)
-        for (int i = tid; i < D * kKvBlock / 4; i += kKvThreads) tile[i / 16 * 17 + i % 16] = src[i];
+    if (n) {
+#pragma unroll
+        for (int i = 0; i < D * kKvBlock / 4 / kKvThreads; ++i) {
+            const int at = i * kKvThreads + tid;
+            tile[at / 16 * 17 + at % 16] = src[at];
+        }
+    }
     __syncthreads();
     float* dst = a.v + out * (D * kKvBlock);
     for (int i = tid; i < 16 * (D / 4); i += kKvThreads) {
@@ -263,7 +271,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvReadArgs a)
         for (int u = 0; u < 4; ++u) f[u] = n ? kv_floats(tile[(c + u) * 17 + word], sc) : zero;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            __builtin_nontemporal_store(t0 + t < n ? float4v{f[0][t], f[1][t], f[2][t], f[3][t]} : zero, (float4v*)(dst + (t0 + t) * D + c));
+            __builtin_nontemporal_store((t0 + t < n ? float4v{f[0][t], f[1][t], f[2][t], f[3][t]} : zero), (float4v*)(dst + (t0 + t) * D + c));
     }
 }
 
@@ -365,31 +373,50 @@ __device__ inline int kv_pick(const uint32_t* keys, int n, int want, KvPick<kThr
     return (int)total;
 }
 
-// The same for up to 64 * kPer keys by one wavefront, lane l holding keys l * kPer ..: the want-th key is found bit by bit.
+// The same for up to 64 * kPer keys by one wavefront, lane l holding keys l * kPer ..: the want-th key is found bit by bit, from
+// the first in which keys differ that are neither 0 nor the largest number (those are always in) down to where it is alone.
 template <int kPer, class Emit>
 __device__ inline int kv_pick_wave(const uint32_t (&keys)[kPer], int want, Emit emit)
 {
-    uint32_t t = 0;
-    bool ends = false;  // exactly `want` keys are t or larger
-#pragma unroll 1
-    for (int bit = 31; bit >= 0 && !ends; --bit) {
-        const uint32_t c = t | 1u << bit;
-        int count = 0;
+    // (counted in the lanes and summed across them: ballots would go through the scalar unit one by one)
+    auto all = [](uint32_t v) { return (int)lane_value(wave_scan_add(v), 63); };
+    uint32_t ones = 0, zeros = 0, over = 0, same = 0, mine = 0, open = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) count += __builtin_popcountll(ballot(keys[i] >= c));
-        if (count >= want) t = c;
-        ends = count == want;
+    for (int i = 0; i < kPer; ++i) {
+        const bool is_open = keys[i] != 0 && keys[i] != 0xFFFFFFFFu;
+        ones |= is_open ? keys[i] : 0u;
+        zeros |= is_open ? ~keys[i] : 0u;
+        mine += keys[i] == 0xFFFFFFFFu;
+        open += is_open;
     }
-    if (ends) --t;
-    // those above t are in, and as many of those equal to t as are left to be had; t = 0: there are no more than wanted
-    uint32_t over = 0, same = 0;
+    const int sure = all(mine), some = all(open);
+    ones = lane_value(wave_or_u32(ones), 63);
+    zeros = lane_value(wave_or_u32(zeros), 63);
+    const uint32_t differ = ones & zeros;
+    const int top = 31 - __builtin_clz(differ | 1u);
+    uint32_t t;
+    if (sure >= want) t = 0xFFFFFFFFu;
+    else if (sure + some <= want) t = 1;  // no more than wanted: all of them
+    else {
+        t = differ ? ones & ~((2u << top) - 1u) : ones;  // what all of them share
+#pragma unroll 1
+        for (int bit = differ ? top : -1; bit >= 0; --bit) {
+            const uint32_t c = t | 1u << bit;
+            mine = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) mine += keys[i] >= c;
+            const int count = all(mine);
+            if (count >= want) t = c;
+            if (count == want) break;
+        }
+    }
+    // those above t are in, and of those equal to t the first that are left to be had
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         over += keys[i] > t;
-        same += t != 0 && keys[i] == t;
+        same += keys[i] == t;
     }
-    const uint32_t over_all = lane_value(wave_scan_add(over), 63);
-    const uint32_t need = t && !ends ? (uint32_t)want - over_all : 0u;
+    const uint32_t need = (uint32_t)max(want - all(over), 0);
     const uint32_t same_before = wave_scan_add(same) - same;
     uint32_t left = same_before < need ? min(need - same_before, same) : 0u;
     const uint32_t inc = wave_scan_add(over + left);
@@ -404,6 +431,27 @@ __device__ inline int kv_pick_wave(const uint32_t (&keys)[kPer], int want, Emit 
         if (in) emit(i, (int)rank++);
     }
     return (int)lane_value(inc, 63);
+}
+
+// One wavefront's keys from a row that is a multiple of 16 long, and the blocks it chooses.
+template <int kPer>
+__device__ inline void kv_choose_row(const uint32_t* row, int n, int want, int32_t* out)
+{
+    static_assert(kPer % 4 == 0, "whole loads");
+    const int lane = threadIdx.x & 63;
+    uint32_t keys[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; i += 4) {
+        const int b = lane * kPer + i;
+        uint4 k = make_uint4(0, 0, 0, 0);
+        if (b < n) k = *(const uint4*)(row + b);
+        keys[i] = k.x;
+        keys[i + 1] = b + 1 < n ? k.y : 0u;
+        keys[i + 2] = b + 2 < n ? k.z : 0u;
+        keys[i + 3] = b + 3 < n ? k.w : 0u;
+    }
+    const int got = kv_pick_wave<kPer>(keys, want, [&](int i, int rank) { out[rank] = lane * kPer + i; });
+    for (int i = got + lane; i < want; i += 64) out[i] = -1;
 }
 
 // ---------------------------------------------------------------- selection of blocks
@@ -478,6 +526,42 @@ __device__ inline void kv_query_bytes(const KvSelectArgs& a, int64_t tok0, int t
     __syncthreads();
 }
 
+// The same for one token, a thread to a channel; the other 15 rows are zeros.
+template <int D, int kThreads>
+__device__ inline void kv_query_bytes_of_one(const KvSelectArgs& a, int64_t tok, int head, int8_t* out, int out_stride, uint32_t* tops)
+{
+    static_assert(D <= kThreads, "a thread to a channel");
+    const int tid = threadIdx.x;
+    const bool bf16 = a.bf16 != 0;
+    float pos = 0.0f, neg = 0.0f;
+    if (tid < D) {
+        const uint16_t* q = (const uint16_t*)a.q + tok * a.q_stride + (int64_t)head * a.group * D + tid;
+        for (int h = 0; h < a.group; h += 4) {
+            uint32_t raw[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) raw[k] = h + k < a.group ? q[(h + k) * D] : 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = bf16 ? bf16_float(raw[k]) : f16_float(raw[k]);
+                pos = __fadd_rn(pos, fmaxf(f, 0.0f));
+                neg = __fadd_rn(neg, fminf(f, 0.0f));
+            }
+        }
+    }
+    for (int i = tid; i < 16 * out_stride / 4; i += kThreads) ((uint32_t*)out)[i] = 0;
+    const uint32_t top = wave_max_u32(__float_as_uint(fmaxf(pos, -neg)));  // (floats from 0 up order as their bits)
+    if (tid < 16) tops[tid] = 0;
+    __syncthreads();
+    if (lane_id() == 63 && tid < D + 63) atomicMax(&tops[0], top);
+    __syncthreads();
+    if (tid < D) {
+        const float unit = __fdiv_rn(__uint_as_float(tops[0]), 127.0f);
+        out[tid] = (int8_t)kv_quant(pos, unit);
+        out[D + tid] = (int8_t)kv_quant(neg, unit);
+    }
+    __syncthreads();
+}
+
 // Keys of (token, head, block): one int8 product of 16 blocks' bounds with 16 tokens' queries to an instruction.
 // Bound by the bounds, read once for every 16 tokens of a sequence.  kOne: sequences have one token each, and the workgroup that
 // has formed the keys of all blocks chooses among them in its LDS.
@@ -488,7 +572,7 @@ __global__ __launch_bounds__(kThreads) void kv_score_kernel(KvSelectArgs a)
     extern __shared__ uint32_t keys[];
     __shared__ __align__(16) int8_t s_u[16 * kStride];
     __shared__ uint32_t s_top[16];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     int64_t at = blockIdx.x;
     const int chunk = (int)(at % a.chunks);
     at /= a.chunks;
@@ -508,15 +592,17 @@ __global__ __launch_bounds__(kThreads) void kv_score_kernel(KvSelectArgs a)
     const int64_t tok = tok0 + (valid ? n : 0);
     const int lim = valid ? max(0, a.causal ? q.len - (q.count - 1 - i) : q.len) : 0;
     const int seen = (lim + kKvBlock - 1) / kKvBlock;  // blocks of this token
-    kv_query_bytes<D, kThreads>(a, tok0, tokens, head, s_u, kStride, s_top);
+    // 64 blocks of a wavefront's round, one to a lane; the page is asked for a round ahead
+    const int32_t* table = a.b.tables + (int64_t)s * a.b.max_blocks;
+    int entry = b0 < b1 ? table[min(b0 + w * 64 + lane, b1 - 1)] : -1;
+    if (kOne) kv_query_bytes_of_one<D, kThreads>(a, tok0, head, s_u, kStride, s_top);
+    else kv_query_bytes<D, kThreads>(a, tok0, tokens, head, s_u, kStride, s_top);
     int4v u[kSteps];
 #pragma unroll
     for (int c = 0; c < kSteps; ++c) u[c] = *(const int4v*)(s_u + n * kStride + c * 64 + g * 16);
     for (int bw = b0 + w * 64; bw < b1; bw += kThreads) {
-        // 64 blocks: page and scale, one to a lane
-        const int mine = bw + lane;
-        const int page_l = mine < b1 ? kv_page(a.c, a.b, s, mine) : -1;
-        const float ks_l = page_l >= 0 ? a.c.k_scale[(int64_t)page_l * a.c.n_heads + head] : 0.0f;
+        const int page_l = bw + lane < b1 ? kv_page_of(a.c, entry) : -1;
+        const float ks_l = a.c.k_scale[(int64_t)max(page_l, 0) * a.c.n_heads + head];  // (not used where there is no page)
 #pragma unroll
         for (int t0 = 0; t0 < 4; t0 += kAt) {
             int4v row[kAt][kSteps];
@@ -533,6 +619,7 @@ __global__ __launch_bounds__(kThreads) void kv_score_kernel(KvSelectArgs a)
             }
 #pragma unroll
             for (int t = 0; t < kAt; ++t) {
+                if (t0 + t == 0) entry = table[min(bw + kThreads + lane, b1 - 1)];
                 const int bt = bw + (t0 + t) * 16;
                 int4v acc = {0, 0, 0, 0};
 #pragma unroll
@@ -564,6 +651,12 @@ __global__ __launch_bounds__(kThreads) void kv_score_kernel(KvSelectArgs a)
     __shared__ KvPick<kThreads> pick;
     int32_t* out = a.out + (tok0 * a.c.n_heads + head) * a.n_sel;
     __syncthreads();
+    if (held <= 1024) {  // (one wavefront without a barrier: 2 us less than all of them at 1024 blocks)
+        if (w != 0) return;
+        if (held <= 256) kv_choose_row<4>(keys, held, a.n_sel, out);
+        else kv_choose_row<16>(keys, held, a.n_sel, out);
+        return;
+    }
     const int got = kv_pick<kThreads>(keys, held, a.n_sel, &pick, [&](int b, int rank) { out[rank] = b; });
     for (int b = got + threadIdx.x; b < a.n_sel; b += kThreads) out[b] = -1;
 }
@@ -588,19 +681,14 @@ __global__ __launch_bounds__(kKvThreads) void kv_choose_kernel(KvSelectArgs a)
 template <int kPer>
 __global__ __launch_bounds__(kKvThreads) void kv_choose_wave_kernel(KvSelectArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t th = (int64_t)blockIdx.x * (kKvThreads / 64) + (threadIdx.x >> 6);
+    const int64_t th = (int64_t)blockIdx.x * (kKvThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (th >= (int64_t)a.b.n_tok * a.c.n_heads) return;
     const int tok = (int)(th / a.c.n_heads);
     const KvSeq q = kv_seq(a.b, kv_seq_of(a.b, tok));
     int32_t* out = a.out + th * a.n_sel;
     int n = (q.len + kKvBlock - 1) / kKvBlock;
     if (tok < q.first || tok >= q.first + q.count) n = 0;  // a token of no sequence
-    uint32_t keys[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) keys[i] = lane * kPer + i < n ? a.keys[th * a.key_stride + lane * kPer + i] : 0u;
-    const int got = kv_pick_wave<kPer>(keys, a.n_sel, [&](int i, int rank) { out[rank] = lane * kPer + i; });
-    for (int i = got + lane; i < a.n_sel; i += 64) out[i] = -1;
+    kv_choose_row<kPer>(a.keys + th * a.key_stride, n, a.n_sel, out);
 }
 
 // ---------------------------------------------------------------- eviction
