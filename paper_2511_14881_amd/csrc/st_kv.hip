@@ -103,8 +103,9 @@ int with_dim(int32_t d, F&& body)
     return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", d);
 }
 
-constexpr int kFewRows = 48;       // of a sequence and head: up to here tiles of 16 that read the cache themselves (64 rows: 38.5 us
-                                  // against 36.7, 40 rows: 35.5 against 36.3; 4 x 8192 tokens, 8 heads of 128)
+// Rows of a sequence and head up to which tiles of 16 read the cache themselves.  4 x 8192 tokens, 8 heads of 128: 40 rows 35.5 us
+// against 36.3 of the kernel for many rows, 64 rows 38.5 against 36.7; 4 heads of 256: 128 rows 61 against 79, 256 rows 104 against 85.
+constexpr int few_rows(int d) { return d > 128 ? 160 : 48; }
 constexpr int row_waves(int d) { return d > 128 ? 4 : 8; }  // of the kernel for many rows (256: 512 registers to a lane)
 constexpr int kManyRows = 2048;   // tiles that fill the chip with a wavefront each
 constexpr int kLeastChunk = 16;   // blocks of a split, at least: it takes as long to start as to read four
@@ -127,7 +128,7 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int32_t group = n_q_heads / c->n_heads;
     const int64_t rows = (n_sel > 0 ? 1 : (int64_t)b->max_tok) * group;  // of a unit and head
     p.units = n_sel > 0 ? b->n_tok : b->n_seq;
-    p.many = n_sel == 0 && rows > kFewRows;
+    p.many = n_sel == 0 && rows > few_rows(c->d);
     p.tile_rows = p.many ? row_waves(c->d) * 32 : 16;
     p.tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
     p.rows_pad = (int32_t)st::round_up(rows, 16);
@@ -163,7 +164,7 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int64_t uh = p.units * c->n_heads;
     const int64_t parts = p.splits > 1 ? uh * p.splits * p.rows_pad : 0;
     p.o_bytes = st::round_up(parts * c->d * 4, 256);
-    p.ml_bytes = st::round_up(parts * 8, 256);
+    p.ml_bytes = st::round_up(parts * 16, 256);
     p.block_bytes = mass ? st::round_up(uh * p.entries * p.rows_pad * 8, 256) : 0;
     p.row_bytes = mass ? st::round_up(uh * p.rows_pad * 8, 256) : 0;
     return p;
@@ -175,7 +176,8 @@ int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t st
     {
         TimedLaunch t(0, stream);
         const dim3 grid((unsigned)p.grid);
-        if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_waves(D)>), grid, dim3(row_waves(D) * 64), 0, stream, a);
+        if (p.many && a.exact) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_waves(D), true>), grid, dim3(row_waves(D) * 64), 0, stream, a);
+        else if (p.many) hipLaunchKernelGGL((st::kv_attend_rows_kernel<D, row_waves(D), false>), grid, dim3(row_waves(D) * 64), 0, stream, a);
         else if (p.waves == 1) hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected, 1>), grid, dim3(64), 0, stream, a);
         else hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected, 4>), grid, dim3(256), 0, stream, a);
     }
@@ -287,8 +289,8 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     if ((rc = check_grid(p.grid)) || (rc = check_grid((int64_t)batch->n_tok * n_q_heads))) return rc;
     char* ws = (char*)dev_workspace;
     st::KvAttendArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
-                          softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse,
-                          p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)p.parts, p.rows_pad, (float*)ws, (float2*)(ws + p.o_bytes),
+                          softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse, mass || dev_lse,
+                          p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)p.parts, p.rows_pad, (float*)ws, (float4*)(ws + p.o_bytes),
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr, dev_mass_in, decay, dev_mass_out};
     hipStream_t stream = (hipStream_t)hip_stream;

@@ -9,7 +9,8 @@
 // 2^14 (exact but for values 2^-38 of that), the key scale of the block and the softmax scale multiply the logits in fp32.
 // Weights are exp2(x - m + 8) with m a maximum that follows the row's largest logit at a distance of at most 7, so that the sums are
 // seldom rescaled: 11 significant bits from 2^15 down to 2^-14 (a 16-bit float's denormals come below 2^-22 of the row's
-// largest weight), and the sum of the weights is of the unrounded ones, in fp32.
+// largest weight).  Outputs are divided by the fp32 sum of the weights as rounded, so that a row that one token dominates is
+// not off by that token's rounding; lse and the blocks' weights go by the sum of the unrounded ones, formed where they are asked for.
 #pragma once
 #include "st_kv_device.h"
 
@@ -27,11 +28,12 @@ struct KvAttendArgs {
     const int32_t* blocks;  // selected ones, or null
     void* out;
     float* lse;
+    int32_t exact;       // lse or the blocks' weights are asked for
     int32_t chunk, splits, tiles, tile_rows, dies;
     uint32_t parts;      // workgroups to a split
     int32_t rows_pad;    // rows of a unit and head in the workspace
     float* part_o;       // [unit, head, split, rows_pad, d]
-    float2* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of weights
+    float4* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of rounded weights, sum of weights
     float2* block_ml;    // [unit, head, entries, rows_pad]: maximum so far, sum of the block's weights; or null
     int64_t entries;     // blocks, or selected ones
     float2* row_ml;      // [unit, head, rows_pad]: final maximum and sum, written where block_ml is
@@ -154,7 +156,8 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
     constexpr bool kHalf = D % 64 != 0;
     constexpr bool kAhead = D <= 128;  // keys of the next block and values of this one are loaded ahead (256: too few registers)
     __shared__ float s_o[kWaves][16][D + 4];
-    __shared__ float2 s_ml[kWaves][16], s_fin[16];
+    __shared__ float4 s_ml[kWaves][16];
+    __shared__ float2 s_fin[16];
     const int lane = threadIdx.x & 63, w = kWaves == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const KvPlace at = kv_place<kSelected>(a);
     if (at.unit < 0) return;
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
             for (int j = 0; j < 8; ++j) q[k][j] = (_Float16)(f[k][j] * up);
     }
 
-    float m = -__builtin_inff(), l = 0.0f;
+    float m = -__builtin_inff(), l = 0.0f, l_exact = 0.0f;
     float4v o[kCh];
 #pragma unroll
     for (int c = 0; c < kCh; ++c) o[c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
@@ -303,26 +306,31 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
                 const float alpha = m_new == m ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
                 m = m_new;
                 l *= alpha;
+                l_exact *= alpha;
 #pragma unroll
                 for (int c = 0; c < kCh; ++c)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[c][r] *= alpha;
             }
             const float base = m == -__builtin_inff() ? 0.0f : kKvLift - m;
-            float sum = 0.0f;
             half8 p[2];
 #pragma unroll
             for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tt][r], ks, base));
-                    sum += e;
-                    p[tt / 2][tt % 2 * 4 + r] = (_Float16)e;
+                    x[tt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tt][r], ks, base));
+                    p[tt / 2][tt % 2 * 4 + r] = (_Float16)x[tt][r];
                 }
-            l += sum;
-            if (a.block_ml) {
-                const float all = sum_over_16_32(sum);
-                if (g == 0) a.block_ml[(uh * a.entries + j0 + kWaves * cur + w) * a.rows_pad + row] = make_float2(m, all);
+            l = add_halves(p[0], add_halves(p[1], l));
+            if (a.exact) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int tt = 0; tt < 4; ++tt) sum += (x[tt][0] + x[tt][1]) + (x[tt][2] + x[tt][3]);
+                l_exact += sum;
+                if (a.block_ml) {
+                    const float all = sum_over_16_32(sum);
+                    if (g == 0) a.block_ml[(uh * a.entries + j0 + kWaves * cur + w) * a.rows_pad + row] = make_float2(m, all);
+                }
             }
 #pragma unroll
             for (int c = 0; c < kCh; ++c) {
@@ -336,9 +344,10 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
         }
     }
     l = sum_over_16_32(l);
+    l_exact = sum_over_16_32(l_exact);
 
     // the wavefronts' states into one
-    if (g == 0) s_ml[w][n] = make_float2(m, l);
+    if (g == 0) s_ml[w][n] = make_float4(m, l, l_exact, 0.0f);
 #pragma unroll
     for (int c = 0; c < kCh; ++c) *(float4v*)&s_o[w][n][c * 16 + g * 4] = o[c];
     __syncthreads();
@@ -348,21 +357,22 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
         float top = -__builtin_inff();
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[k][r].x);
-        float sum = 0.0f;
+        float sum = 0.0f, exact = 0.0f;
         float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) {
-            const float2 ml = s_ml[k][r];
+            const float4 ml = s_ml[k][r];
             const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
             const float4v v = *(const float4v*)&s_o[k][r][c];
             sum += ml.y * f;
+            exact += ml.z * f;
 #pragma unroll
             for (int u = 0; u < 4; ++u) y[u] += v[u] * f;
         }
         if (row0 + r >= t.rows) continue;
         if (t.n_list > a.chunk) {
             *(float4v*)(a.part_o + (part + r) * D + c) = y;
-            if (c == 0) a.part_ml[part + r] = make_float2(top, sum);
+            if (c == 0) a.part_ml[part + r] = make_float4(top, sum, exact, 0.0f);
             continue;
         }
         const KvRow to = kv_row(row0 + r, t.tok_unit, head, a.group);
@@ -373,9 +383,9 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
         for (int u = 0; u < 4; ++u) h[u] = to_16_bits(y[u] * inv, bf16);
         *(uint2*)((uint16_t*)a.out + place * D + c) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
         if (c == 0) {
-            if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(sum)) * 0.69314718056f;
-            if (a.row_ml) a.row_ml[uh * a.rows_pad + row0 + r] = make_float2(top, sum);
-            s_fin[r] = make_float2(top, sum);
+            if (a.lse) a.lse[place] = exact == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(exact)) * 0.69314718056f;
+            if (a.row_ml) a.row_ml[uh * a.rows_pad + row0 + r] = make_float2(top, exact);
+            s_fin[r] = make_float2(top, exact);
         }
     }
     if (kSelected || !a.mass_out || !kv_whole(a, t.n_list)) return;
@@ -401,7 +411,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     constexpr int kRows = kKvThreads / kTeam;
     __shared__ float4v s_y[kRows][kParts][kLanes];
     __shared__ float s_top[kRows][kWaves];
-    __shared__ float s_sum[kRows][kParts];
+    __shared__ float2 s_sum[kRows][kParts];
     const int team = threadIdx.x / kTeam, me = threadIdx.x % kTeam, lane = me & 63;
     const int64_t heads_all = (int64_t)a.c.n_heads * a.group;
     const int64_t place = (int64_t)blockIdx.x * kRows + team;
@@ -425,27 +435,29 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_top[team][k]);
     const int c = me % kLanes, from = me / kLanes;
-    float sum = 0.0f;
+    float sum = 0.0f, exact = 0.0f;
     float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
     if (from < kParts) {
 #pragma unroll 4
         for (int i = from; i < splits; i += kParts) {
-            const float2 ml = a.part_ml[part + i * stride];
+            const float4 ml = a.part_ml[part + i * stride];
             const float4v v = *(const float4v*)(a.part_o + (part + i * stride) * D + c * 4);
             const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
             sum = __builtin_fmaf(ml.y, f, sum);
+            exact = __builtin_fmaf(ml.z, f, exact);
 #pragma unroll
             for (int u = 0; u < 4; ++u) y[u] = __builtin_fmaf(v[u], f, y[u]);
         }
         s_y[team][from][c] = y;
-        if (c == 0) s_sum[team][from] = sum;
+        if (c == 0) s_sum[team][from] = make_float2(sum, exact);
     }
     __syncthreads();
     if (!mine || from != 0) return;
 #pragma unroll
     for (int k = 1; k < kParts; ++k) {
         const float4v v = s_y[team][k][c];
-        sum += s_sum[team][k];
+        sum += s_sum[team][k].x;
+        exact += s_sum[team][k].y;
 #pragma unroll
         for (int u = 0; u < 4; ++u) y[u] += v[u];
     }
@@ -455,8 +467,8 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     for (int u = 0; u < 4; ++u) h[u] = to_16_bits(y[u] * inv, a.bf16 != 0);
     *(uint2*)((uint16_t*)a.out + place * D + c * 4) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
     if (c == 0) {
-        if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(sum)) * 0.69314718056f;
-        if (a.row_ml) a.row_ml[uh * stride + row] = make_float2(top, sum);
+        if (a.lse) a.lse[place] = exact == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(exact)) * 0.69314718056f;
+        if (a.row_ml) a.row_ml[uh * stride + row] = make_float2(top, exact);
     }
 }
 

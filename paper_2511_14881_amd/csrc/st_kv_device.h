@@ -158,6 +158,16 @@ __device__ inline float sum_over_16_32(float v)
     return sum_over_32(r.x + r.y);
 }
 
+// sum + the eight 16-bit floats, in fp32.
+__device__ inline float add_halves(const half8& p, float sum)
+{
+    const half2v one = {(_Float16)1.0f, (_Float16)1.0f};
+    sum = __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 0, 1), one, sum, false);
+    sum = __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 2, 3), one, sum, false);
+    sum = __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 4, 5), one, sum, false);
+    return __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 6, 7), one, sum, false);
+}
+
 // x where the bit is 1, -inf where it is 0.
 __device__ inline float kv_seen(float x, uint32_t bits, int bit)
 {

@@ -14,7 +14,8 @@ namespace st {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-template <int D, int kWaves>
+// kExact: lse or the blocks' weights are asked for.
+template <int D, int kWaves, bool kExact>
 __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_kernel(KvAttendArgs a)
 {
     constexpr int kTiles = 1, kThreads = kWaves * 64, kRows = kWaves * kTiles * 32, kSteps = D / 16, kCh = D / 32;
@@ -37,7 +38,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
     int row[kTiles], lim[kTiles];
     int64_t tok[kTiles];
     half8 q[kTiles][kSteps];
-    float factor[kTiles], m[kTiles], l[kTiles];
+    float factor[kTiles], m[kTiles], l[kTiles], l_exact[kTiles];
     float16v o[kTiles][kCh];
 #pragma unroll
     for (int rt = 0; rt < kTiles; ++rt) {
@@ -72,6 +73,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
         }
         m[rt] = -__builtin_inff();
         l[rt] = 0.0f;
+        l_exact[rt] = 0.0f;
 #pragma unroll
         for (int c = 0; c < kCh; ++c) o[rt][c] = float16v(0.0f);
     }
@@ -210,6 +212,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                     const float alpha = m_new == m[rt] ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - m_new);
                     m[rt] = m_new;
                     l[rt] *= alpha;
+                    if (kExact) l_exact[rt] *= alpha;
 #pragma unroll
                     for (int c = 0; c < kCh; ++c) o[rt][c] *= alpha;
                 }
@@ -226,11 +229,15 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][tt][i], ks[rt], base));
-                        sum += e;
+                        if (kExact) sum += e;
                         p[rt][tt * 2 + (i >> 3)][i & 7] = (_Float16)e;
                     }
+                float rounded = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) rounded = add_halves(p[rt][u], rounded);
+                l[rt] = __builtin_fmaf(rounded, rho_inv, l[rt]);
                 sums[rt] = sum * rho_inv;
-                l[rt] += sums[rt];
+                l_exact[rt] += sums[rt];
             }
             const char* bv = s_v[buf] + n * kValBytes + h * 16;
 #pragma unroll
@@ -243,7 +250,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                 }
             put_keys(buf);
             put_values(buf ^ 1, next);
-            if (a.block_ml)
+            if (kExact && a.block_ml)
 #pragma unroll
                 for (int rt = 0; rt < kTiles; ++rt) {
                     const float both = sum_over_32(sums[rt]);
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
 
 #pragma unroll
     for (int rt = 0; rt < kTiles; ++rt) {
-        const float sum = sum_over_32(l[rt]);
+        const float sum = sum_over_32(l[rt]), exact = kExact ? sum_over_32(l_exact[rt]) : 0.0f;
         if (row[rt] >= t.rows) continue;
         if (t.n_list > a.chunk) {
             const int64_t part = (uh * a.splits + split) * a.rows_pad + row[rt];
@@ -318,7 +325,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                     for (int u = 0; u < 4; ++u) y[u] = o[rt][c][4 * i + u] * v_unit;
                     *(float4v*)(a.part_o + part * D + c * 32 + i * 8 + h * 4) = y;
                 }
-            if (h == 0) a.part_ml[part] = make_float2(m[rt], sum);
+            if (h == 0) a.part_ml[part] = make_float4(m[rt], sum, exact, 0.0f);
             continue;
         }
         const KvRow to = kv_row(row[rt], t.tok_unit, head, a.group);
@@ -333,9 +340,9 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                 for (int u = 0; u < 4; ++u) r[u] = to_16_bits(o[rt][c][4 * i + u] * inv, bf16);
                 *(uint2*)((uint16_t*)a.out + place * D + c * 32 + i * 8 + h * 4) = make_uint2(r[0] | r[1] << 16, r[2] | r[3] << 16);
             }
-        if (h == 0) {
-            if (a.lse) a.lse[place] = sum == 0.0f ? -__builtin_inff() : (m[rt] - kKvLift + log2f(sum)) * 0.69314718056f;
-            if (a.row_ml) a.row_ml[uh * a.rows_pad + row[rt]] = make_float2(m[rt], sum);
+        if (kExact && h == 0) {
+            if (a.lse) a.lse[place] = exact == 0.0f ? -__builtin_inff() : (m[rt] - kKvLift + log2f(exact)) * 0.69314718056f;
+            if (a.row_ml) a.row_ml[uh * a.rows_pad + row[rt]] = make_float2(m[rt], exact);
         }
     }
 }
