@@ -211,6 +211,42 @@ def test_not_a_number_stays_in_its_row():
     assert torch.equal(out, clean)
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("group", [1, 4])
+def test_not_a_number_stays_in_its_row_of_few(group, bad):
+    rng = np.random.default_rng(17)
+    host = R.Host(rng, [900, 200], 2, 128)
+    q = queries(rng, 2, 2 * group, 128, "f16")
+    clean = st.st_kv_attend(host.cache(st), host.batch(st, 2), q.cuda())
+    q[1, group, 77] = bad
+    out = st.st_kv_attend(host.cache(st), host.batch(st, 2), q.cuda())
+    assert out[1, group].isnan().all()
+    out[1, group], clean[1, group] = 0, 0
+    assert torch.equal(out, clean)
+
+
+@pytest.mark.parametrize("n_q,group", [(1, 1), (1, 4), (2, 2), (4, 1)])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_up_to_four_rows(n_q, group, d):
+    """Few rows: one large weight among many small ones, values of one sign."""
+    rng = np.random.default_rng(18 + d)
+    lens = [64 * 30 + 7, 500, 3]
+    host = R.Host(rng, lens, 2, d)
+    host.v = np.abs(host.v.astype(np.int32)).clip(0, 127).astype(np.int8)
+    n_tok = n_q * len(lens)
+    q = queries(rng, n_tok, 2 * group, d, "f16", 0.01)
+    for s, n in enumerate(lens):  # the first row of each sequence finds one key 11 nats above the others
+        page, at = host.tables[s, n // 2 // 64], n // 2 % 64
+        key = host.k[page, 0, at].astype(np.float64) * host.ks[page, 0]
+        q[s * n_q, 0] = torch.from_numpy(11 * d ** 0.5 * key / (key @ key)).half()
+    lse = torch.zeros((n_tok, 2 * group), device="cuda")
+    out = st.st_kv_attend(host.cache(st), host.batch(st, n_tok), q.cuda(), causal=False, lse=lse)
+    want, want_lse, _, reach = R.attend(host, q, d ** -0.5, False)
+    check_out(out, want, reach, host, "f16")
+    tol = (2 * (d + 8) * reach + max(lens) / 16 + 64 + 4 * np.abs(want_lse)) * 2.0 ** -23
+    assert np.all(np.abs(lse.cpu().numpy() - want_lse) <= tol)
+
+
 def test_rows_inside_wider_rows():
     rng = np.random.default_rng(8)
     host = R.Host(rng, [300, 200], 2, 64)
