@@ -227,8 +227,9 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
             block = kSelected ? entry : j;
             if (block >= 0 && block < t.n_blocks) page = kSelected ? kv_page(a.c, a.b, t.seq, block) : kv_page_of(a.c, entry);
         }
+        uint64_t any = ~0ull;
         if (a.mask && page >= 0) {  // a block that no row of the tile sees is not read
-            uint64_t any = 0;
+            any = 0;
             for (int64_t i = t.tok_first; i <= t.tok_last; ++i) any |= a.mask[i * a.mask_words + block];
             if (any == 0) page = -1;
         }
@@ -251,7 +252,14 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
                 if (kHalf) kh[tt] = *(const uint2*)(kp + tt * 16 * D + kWide * 64 + g * 8);
             }
         };
+        // a block's word of the mask: rows of one token have what was read above
+        uint64_t word = ~0ull;
+        auto load_word = [&](int from) {
+            if (kSelected) word = (uint64_t)lane_value((uint32_t)(any >> 32), from) << 32 | lane_value((uint32_t)any, from);
+            else if (a.mask) word = a.mask[of.tok * a.mask_words + j0 + kWaves * from + w];
+        };
         if (kAhead) load_keys(it);
+        load_word(it);
         while (todo) {
             const int cur = it;
             todo &= todo - 1;
@@ -271,7 +279,7 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
             if (part) {
                 const int left = lim - b * kKvBlock;
                 see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
-                if (a.mask && see) see &= a.mask[of.tok * a.mask_words + b];
+                see &= word;
             }
             float4v x[4];
 #pragma unroll
@@ -284,7 +292,10 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
                 }
                 if (kHalf) x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(kh[tt].x, kh[tt].y), q[kSteps - 1], x[tt], 0, 0, 0);
             }
-            if (kAhead && it >= 0) load_keys(it);  // the next block's, behind this one's products
+            if (it >= 0) {  // the next block's, behind this one's products
+                if (kAhead) load_keys(it);
+                load_word(it);
+            }
             // (a scale or a factor of zero gives logits of next to nothing, and -inf stays what it is)
             const float ks = fmaxf(__uint_as_float(lane_value(__float_as_uint(ks_l), cur)) * factor, 1e-37f);
             const float vs = __uint_as_float(lane_value(__float_as_uint(vs_l), cur));
