@@ -103,12 +103,24 @@ int with_dim(int32_t d, F&& body)
     return fail(ST_EINVAL, "d=%d must be 64, 96, 128 or 256", d);
 }
 
-// Rows of a sequence and head up to which tiles of 16 read the cache themselves.  4 x 8192 tokens, 8 heads of 128: 40 rows 35.5 us
-// against 36.3 of the kernel for many rows, 64 rows 38.5 against 36.7; 4 heads of 256: 128 rows 61 against 79, 256 rows 104 against 85.
-constexpr int few_rows(int d) { return d > 128 ? 160 : 48; }
+// Rows of a sequence and head up to which tiles of 16 read the cache themselves, as against tiles of 256 (d = 256: 128) rows that
+// share it.  8 x 16384 tokens, 4 heads, us: d = 64, 96 rows 43 against 52, 192 rows 66 against 58; d = 96, 96 rows 53 against 62,
+// 128 rows 68 against 63; d = 128, 64 rows 56.2 against 55.3, 96 rows 72 against 58; d = 256, 80 rows 114 against 129, 128 rows
+// 204 against 136.  Where all is little, the shared tiles leave most of the chip idle: one sequence of 4000 tokens, 192 rows,
+// d = 64 14 against 18, d = 128 19 against 26, d = 256 27 against 39.
+constexpr int64_t kLittle = 512;  // blocks of all sequences and heads
+constexpr int few_rows(int d, int64_t blocks) { return blocks <= kLittle ? 256 : d > 128 ? 96 : d > 96 ? 64 : 128; }
 constexpr int row_waves(int d) { return d > 128 ? 4 : 8; }  // of the kernel for many rows (256: 512 registers to a lane)
 constexpr int kManyRows = 2048;   // tiles that fill the chip with a wavefront each
-constexpr int kLeastChunk = 16;   // blocks of a split, at least: it takes as long to start as to read four
+// Blocks of a split, at least: one for each wavefront that takes blocks by itself, two where the workgroup takes them together.
+// 1500 tokens, 4 heads: 16 rows, d = 128, 13.2 us against 15.8 with splits of 16 blocks; d = 256, 15.2 against 23.6; 256 rows,
+// d = 128, 23.0 against 45.5.  A list of up to whole_list blocks is not split, joining would take longer: 700 tokens, 16 rows,
+// d = 128, 11.2 us against 13.2.
+constexpr int least_chunk(bool many) { return many ? 2 : 4; }
+constexpr int whole_list(int d) { return d > 128 ? 8 : 16; }
+// Many rows: a block takes about this long in microseconds; joining splits this long, and the partial outputs' way out and in.
+constexpr double rows_block_us(int d) { return d > 128 ? 3.0 : 1.7; }
+constexpr double kRowsJoinUs = 3.0, kRowsJoinBytes = 5e6;  // of a microsecond
 constexpr double kSplitStart = 4.0, kSplitJoin = 6.0;  // start of a workgroup, and joining splits, in blocks
 constexpr int kDies = 8;  // of the chip, each with an L2 of its own
 
@@ -116,7 +128,7 @@ struct AttendPlan {
     bool many;          // the kernel for many rows
     int32_t tile_rows, tiles, chunk, splits, rows_pad, entries, dies, waves;
     int64_t units;
-    int64_t parts, grid;  // workgroups to a split, and in all
+    int64_t grid;
     int64_t o_bytes, ml_bytes, block_bytes, row_bytes;
     int64_t bytes() const { return o_bytes + ml_bytes + block_bytes + row_bytes; }
 };
@@ -128,16 +140,16 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int32_t group = n_q_heads / c->n_heads;
     const int64_t rows = (n_sel > 0 ? 1 : (int64_t)b->max_tok) * group;  // of a unit and head
     p.units = n_sel > 0 ? b->n_tok : b->n_seq;
-    p.many = n_sel == 0 && rows > few_rows(c->d);
+    const int32_t list = std::max(1, n_sel > 0 ? std::min(n_sel, blocks_of(b->max_len)) : blocks_of(b->max_len));
+    p.many = n_sel == 0 && rows > few_rows(c->d, (int64_t)b->n_seq * c->n_heads * list);
     p.tile_rows = p.many ? row_waves(c->d) * 32 : 16;
     p.tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
     p.rows_pad = (int32_t)st::round_up(rows, 16);
-    const int32_t list = std::max(1, n_sel > 0 ? std::min(n_sel, blocks_of(b->max_len)) : blocks_of(b->max_len));
     p.entries = n_sel > 0 ? n_sel : list;
     const int64_t pairs = std::max<int64_t>(1, p.units * p.tiles * c->n_heads);
     p.waves = pairs >= kManyRows ? 1 : 4;
     // Workgroups that the chip holds at a time (registers and LDS), and splits of a row's blocks: one round of workgroups where
-    // there are few rows (each split is long enough to pay for its start), two where sequences of different lengths
+    // there are few rows (as long as a split has work for its wavefronts), two where sequences of different lengths
     // would leave a single round to the longest, and for a lone sequence what wastes least of its last round.
     const int64_t slots = (int64_t)st::kComputeUnits * (p.many ? 1 : c->d <= 64 ? 4 : c->d <= 96 ? 3 : 2);
     int64_t splits = 1;
@@ -152,15 +164,23 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
             if (cost < best) best = cost, splits = s;
         }
     }
-    int32_t chunk = (int32_t)std::max<int64_t>(kLeastChunk, (list + splits - 1) / splits);
-    if (chunk >= list) chunk = p.entries;
+    int32_t chunk = (int32_t)std::max<int64_t>(least_chunk(p.many), (list + splits - 1) / splits);
+    bool whole = chunk >= list;
+    if (p.many) {
+        const double parts = (double)(rows * b->n_seq * c->n_heads) * ((list + chunk - 1) / chunk);
+        whole = whole || (list - chunk) * rows_block_us(c->d) < kRowsJoinUs + parts * c->d * 8 / kRowsJoinBytes;
+    } else {
+        whole = whole || list <= whole_list(c->d);
+    }
+    if (whole) chunk = p.entries;
     p.chunk = chunk;
     p.splits = (p.entries + chunk - 1) / chunk;
-    // Parts that read the same blocks go to one die, where the sequences and heads are enough to keep all dies alike.
+    // Parts that read the same blocks go to one die, where sequences, heads and splits are enough to keep all dies alike (one
+    // sequence of 100000 tokens, 4 heads of 128, 64 rows: 48 us against 72).
     const int64_t sh = (int64_t)b->n_seq * c->n_heads, per = (int64_t)p.tiles * (n_sel > 0 ? b->max_tok : 1);
-    p.dies = per > 1 && (sh % kDies == 0 || sh >= 8 * kDies) ? kDies : 1;
-    p.parts = st::round_up(sh, p.dies) * per;
-    p.grid = p.parts * p.splits;
+    const int64_t keys = sh * p.splits;
+    p.dies = per > 1 && (keys % kDies == 0 || keys >= 8 * kDies) ? kDies : 1;
+    p.grid = st::round_up(keys, p.dies) * per;
     const int64_t uh = p.units * c->n_heads;
     const int64_t parts = p.splits > 1 ? uh * p.splits * p.rows_pad : 0;
     p.o_bytes = st::round_up(parts * c->d * 4, 256);
@@ -290,7 +310,7 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     char* ws = (char*)dev_workspace;
     st::KvAttendArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
                           softmax_scale * 1.44269504089f, dev_mask, mask_words, n_sel, dev_blocks, dev_out, dev_lse, mass || dev_lse,
-                          p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)p.parts, p.rows_pad, (float*)ws, (float4*)(ws + p.o_bytes),
+                          p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)(batch->n_seq * cache->n_heads), p.rows_pad, (float*)ws, (float4*)(ws + p.o_bytes),
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr, dev_mass_in, decay, dev_mass_out};
     hipStream_t stream = (hipStream_t)hip_stream;

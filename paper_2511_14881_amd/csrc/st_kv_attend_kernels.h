@@ -30,7 +30,7 @@ struct KvAttendArgs {
     float* lse;
     int32_t exact;       // lse or the blocks' weights are asked for
     int32_t chunk, splits, tiles, tile_rows, dies;
-    uint32_t parts;      // workgroups to a split
+    uint32_t pairs;      // of sequences and heads
     int32_t rows_pad;    // rows of a unit and head in the workspace
     float* part_o;       // [unit, head, split, rows_pad, d]
     float4* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of rounded weights, sum of weights
@@ -99,22 +99,16 @@ template <bool kSelected>
 __device__ inline KvPlace kv_place(const KvAttendArgs& a)
 {
     const uint32_t per = (uint32_t)a.tiles * (kSelected ? a.b.max_tok : 1);
-    const uint32_t split = blockIdx.x / a.parts, at = blockIdx.x - split * a.parts;
-    uint32_t pair, item;
-    if (a.dies > 1) {
-        const uint32_t k = at / a.dies;
-        pair = k / per;
-        item = k - pair * per;
-        pair = pair * a.dies + (at - k * a.dies);
-    } else {
-        pair = at / per;
-        item = at - pair * per;
-    }
+    const uint32_t k = blockIdx.x / a.dies;
+    uint32_t key = k / per;  // split and pair
+    const uint32_t item = k - key * per;
+    key = key * a.dies + (blockIdx.x - k * a.dies);
     KvPlace p;
+    p.split = key / a.pairs;
+    const uint32_t pair = key - p.split * a.pairs;
     p.seq = pair / a.c.n_heads;
     p.head = pair - p.seq * a.c.n_heads;
-    p.unit = p.seq < a.b.n_seq ? p.seq : -1;
-    p.split = split;
+    p.unit = p.split < a.splits ? p.seq : -1;
     const int i = item / a.tiles;
     p.tile = item - i * a.tiles;
     if (kSelected && p.unit >= 0) {
@@ -154,7 +148,11 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
 {
     constexpr int kSteps = D / 32, kWide = D / 64, kCh = D / 16;
     constexpr bool kHalf = D % 64 != 0;
-    constexpr bool kAhead = D <= 128;  // keys of the next block and values of this one are loaded ahead (256: too few registers)
+    // Values of a block are loaded before its keys' products, the next block's keys right behind these.  d = 256 has registers for
+    // half of that: its second half of the values takes the place of keys that were used (left to the compiler, the
+    // values' loads ended up one behind the other, each with a wait: 193 us against 107 for 8 x 16000 tokens, 4 heads, 64 rows).
+    constexpr bool kBoth = D <= 128;
+    constexpr int kFirst = kBoth ? kCh : kCh / 2;
     __shared__ float s_o[kWaves][16][D + 4];
     __shared__ float4 s_ml[kWaves][16];
     __shared__ float2 s_fin[16];
@@ -240,16 +238,17 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
         uint64_t todo = ballot(page >= 0);
         if (todo == 0) continue;
         int it = __builtin_ctzll(todo);
+        const uint32_t key_at = n * D + g * 16, val_at = n * kKvBlock + g * 16;
         uint4 kw[4][kWide ? kWide : 1];
         uint2 kh[4];
         auto load_keys = [&](int from) {
             const int64_t at_page = (int64_t)(int)lane_value((uint32_t)page, from) * a.c.n_heads + head;
-            const int8_t* kp = a.c.k + at_page * (D * kKvBlock) + n * D;
+            const int8_t* kp = a.c.k + at_page * (D * kKvBlock);
 #pragma unroll
             for (int tt = 0; tt < 4; ++tt) {
 #pragma unroll
-                for (int c = 0; c < kWide; ++c) kw[tt][c] = *(const uint4*)(kp + tt * 16 * D + c * 64 + g * 16);
-                if (kHalf) kh[tt] = *(const uint2*)(kp + tt * 16 * D + kWide * 64 + g * 8);
+                for (int c = 0; c < kWide; ++c) kw[tt][c] = *(const uint4*)(kp + tt * 16 * D + c * 64 + key_at);
+                if (kHalf) kh[tt] = *(const uint2*)(kp + tt * 16 * D + kWide * 64 + (key_at - g * 8));
             }
         };
         // a block's word of the mask: rows of one token have what was read above
@@ -258,7 +257,7 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
             if (kSelected) word = (uint64_t)lane_value((uint32_t)(any >> 32), from) << 32 | lane_value((uint32_t)any, from);
             else if (a.mask) word = a.mask[of.tok * a.mask_words + j0 + kWaves * from + w];
         };
-        if (kAhead) load_keys(it);
+        if (kBoth) load_keys(it);
         load_word(it);
         while (todo) {
             const int cur = it;
@@ -266,14 +265,14 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
             it = todo ? __builtin_ctzll(todo) : -1;
             const int b = (int)lane_value((uint32_t)block, cur);
             const int64_t ph = (int64_t)(int)lane_value((uint32_t)page, cur) * a.c.n_heads + head;
-            const int8_t* vp = a.c.v + ph * (D * kKvBlock) + n * kKvBlock + g * 16;
+            const int8_t* vp = a.c.v + ph * (D * kKvBlock);
             uint4 vw[kCh];
-            if (kAhead) {
+            auto load_values = [&](int from, int to) {
 #pragma unroll
-                for (int c = 0; c < kCh; ++c) vw[c] = *(const uint4*)(vp + c * 16 * kKvBlock);
-            } else {
-                load_keys(cur);
-            }
+                for (int c = from; c < to; ++c) vw[c] = *(const uint4*)(vp + c * 16 * kKvBlock + val_at);
+            };
+            if (!kBoth) load_keys(cur);
+            load_values(0, kFirst);
             uint64_t see = ~0ull;
             const bool part = a.mask || (b + 1) * kKvBlock > lim_all;
             if (part) {
@@ -291,9 +290,14 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
                     x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(kw[tt][c].z, kw[tt][c].w), q[2 * c + 1], x[tt], 0, 0, 0);
                 }
                 if (kHalf) x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(kh[tt].x, kh[tt].y), q[kSteps - 1], x[tt], 0, 0, 0);
+                if (!kBoth) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_values(kFirst + tt * (kCh - kFirst) / 4, kFirst + (tt + 1) * (kCh - kFirst) / 4);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            if (it >= 0) {  // the next block's, behind this one's products
-                if (kAhead) load_keys(it);
+            if (it >= 0) {
+                if (kBoth) load_keys(it);
                 load_word(it);
             }
             // (a scale or a factor of zero gives logits of next to nothing, and -inf stays what it is)
@@ -345,7 +349,6 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
             }
 #pragma unroll
             for (int c = 0; c < kCh; ++c) {
-                if (!kAhead) vw[c] = *(const uint4*)(vp + c * 16 * kKvBlock);
                 float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
                 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(vw[c].x, vw[c].y), p[0], y, 0, 0, 0);
                 y = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_halves(vw[c].z, vw[c].w), p[1], y, 0, 0, 0);

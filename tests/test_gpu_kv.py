@@ -211,6 +211,38 @@ def test_not_a_number_stays_in_its_row():
     assert torch.equal(out, clean)
 
 
+MANY = [  # tiles of 256 (d = 256: 128) rows, whole and cut short, with and without splits
+    ("bf16", 128, 2, 2, [1030, 64], None, 150, False, None),
+    ("f16", 96, 1, 5, [640, 2000, 0, 333], [0, 60, 130, 130, 131], 0, True, "half"),
+    ("bf16", 64, 1, 1, [5, 400], None, 300, True, None),
+    ("f16", 256, 1, 3, [700, 130], None, 100, True, "sparse"),
+    ("bf16", 256, 2, 4, [130, 1], None, 70, False, None),
+    ("f16", 128, 1, 4, [4000], None, 80, True, "sparse"),
+    ("bf16", 96, 3, 1, [64, 65, 150], None, 257, False, "half"),
+]
+
+
+@pytest.mark.parametrize("with_mass", [False, True])
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_many_rows_match_plain(case, with_mass, monkeypatch):
+    monkeypatch.setitem(globals(), "CASES", MANY)
+    test_attention_matches_plain(case, with_mass)
+
+
+@pytest.mark.parametrize("d", [64, 256])
+def test_not_a_number_stays_in_its_row_of_many(d):
+    rng = np.random.default_rng(27)
+    host = R.Host(rng, [900], 1, d)
+    q = queries(rng, 100, 3, d, "bf16")
+    clean = st.st_kv_attend(host.cache(st), host.batch(st, 100), q.cuda(), causal=False)
+    q[2, 1, 5], q[99, 2, 0] = float("nan"), float("inf")
+    out = st.st_kv_attend(host.cache(st), host.batch(st, 100), q.cuda(), causal=False)
+    for row in ((2, 1), (99, 2)):
+        assert out[row].isnan().all()
+        out[row], clean[row] = 0, 0
+    assert torch.equal(out, clean)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("group", [1, 4])
 def test_not_a_number_stays_in_its_row_of_few(group, bad):
