@@ -1,12 +1,19 @@
 // Attention of many rows of a sequence (candidates, a prompt's chunk) over its cached history.
 //
 // Bound by the matrix units and the vector units beside them: 4 d operations to a row and token for the products, some five
-// vector instructions to a weight.  A workgroup's wavefronts hold kTiles tiles of 32 rows each; a block's integers are turned into
-// 16-bit floats once for all of them, on their way into the LDS (two blocks deep, the next one's integers in flight behind the
-// products), and a fragment that is read from there serves every tile of the wavefront.  As in the kernel for few rows a lane
-// holds one row's logits, and weights go from one product to the other as they lie.  The value scale
-// of a block is part of its weights (relative to a reference that follows the scales at a distance), so that the products
-// accumulate into the outputs.
+// vector instructions to a weight.  A workgroup's wavefronts hold 32 rows each; a block's integers are turned into 16-bit floats
+// once for all of them, on their way into the LDS (two blocks deep, the next one's integers in flight behind the products).
+// As in the kernel for few rows a lane holds one row's logits, and weights go from one product to the other as they lie.  The
+// products of the next block's keys stand beside the exponentials of this one's weights.  The value scale of a block is part of
+// its weights (relative to a reference that follows the scales at a distance), so that the products accumulate into the outputs.
+//
+// 500 candidates to each of 16 histories of 1024 to 4096 tokens, 2 query heads to each of 4 heads of 128: 133 us, 655 TFLOP/s;
+// with histories of one length 843 (a large product of matrices in 16 bits reaches 1390), since one round of workgroups lasts
+// as long as the longest history.  2047 tokens over 15001, 5 query heads to each of 3 heads of 96, under a mask: 265 us and 19 to
+// join.  With one part left out, 133 us become 131 (exponentials), 120 (stores to the LDS), 127 (loads), 106 or 104 (either product):
+// the parts hide behind each other about as far as two wavefronts of a SIMD let them.  256 rows to a workgroup of 8 wavefronts
+// rather than 128 to one of 4: 132 against 152; two tiles of 32 rows to a wavefront, 4 wavefronts: 219; products and weights
+// in turn on the two wavefronts of a SIMD, with a barrier between: 154.
 #pragma once
 #include "st_kv_attend_kernels.h"
 
@@ -14,11 +21,11 @@ namespace st {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-// kExact: lse or the blocks' weights are asked for.
+// kExact: lse or the blocks' weights are asked for (the case above: 16 us more for both).
 template <int D, int kWaves, bool kExact>
 __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_kernel(KvAttendArgs a)
 {
-    constexpr int kTiles = 1, kThreads = kWaves * 64, kRows = kWaves * kTiles * 32, kSteps = D / 16, kCh = D / 32;
+    constexpr int kThreads = kWaves * 64, kRows = kWaves * 32, kSteps = D / 16, kCh = D / 32;
     constexpr int kKeyBytes = 2 * D + 16, kValBytes = 2 * kKvBlock + 16;  // rows of the LDS, an odd number of 16 bytes apart
     constexpr int kPieces = (4 * D + kThreads - 1) / kThreads;            // 16 bytes of keys, and of values, of a thread
     __shared__ __align__(16) char s_k[2][kKvBlock * kKeyBytes];
@@ -35,51 +42,43 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
     const int64_t uh = (int64_t)unit * a.c.n_heads + head, heads_all = (int64_t)a.c.n_heads * a.group;
     const bool bf16 = a.bf16 != 0;
 
-    int row[kTiles], lim[kTiles];
-    int64_t tok[kTiles];
-    half8 q[kTiles][kSteps];
-    float factor[kTiles], m[kTiles], l[kTiles], l_exact[kTiles];
-    float16v o[kTiles][kCh];
+    const int row = row0 + w * 32 + n;
+    const bool valid = row < t.rows;
+    const KvRow of = kv_row(valid ? row : row0, t.tok_unit, head, a.group);
+    const int lim = valid ? t.limit(of.i) : 0;
+    half8 q[kSteps];
+    float factor;
+    const uint16_t* src = (const uint16_t*)a.q + of.tok * a.q_stride + of.q_head * D + h * 8;
+    uint4 raw[kSteps];
+    float top = 0.0f;
 #pragma unroll
-    for (int rt = 0; rt < kTiles; ++rt) {
-        row[rt] = row0 + (w * kTiles + rt) * 32 + n;
-        const bool valid = row[rt] < t.rows;
-        const KvRow of = kv_row(valid ? row[rt] : row0, t.tok_unit, head, a.group);
-        tok[rt] = of.tok;
-        lim[rt] = valid ? t.limit(of.i) : 0;
-        const uint16_t* src = (const uint16_t*)a.q + of.tok * a.q_stride + of.q_head * D + h * 8;
-        uint4 raw[kSteps];
-        float top = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            raw[k] = make_uint4(0, 0, 0, 0);
-            if (valid) raw[k] = *(const uint4*)(src + k * 16);
-        }
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            float f[8];
-            eight_floats(raw[k], bf16, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
-        }
-        float up;
-        kv_query_unit(max_over_32(top), a.scale_log2, &up, &factor[rt]);
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            float f[8];
-            eight_floats(raw[k], bf16, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[rt][k][j] = (_Float16)(f[j] * up);
-        }
-        m[rt] = -__builtin_inff();
-        l[rt] = 0.0f;
-        l_exact[rt] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < kCh; ++c) o[rt][c] = float16v(0.0f);
+    for (int k = 0; k < kSteps; ++k) {
+        raw[k] = make_uint4(0, 0, 0, 0);
+        if (valid) raw[k] = *(const uint4*)(src + k * 16);
     }
-    const bool busy = row0 + w * kTiles * 32 < t.rows;  // this wavefront has rows; all help with the blocks
-    const int lim_all = t.limit(t.token(min(row0 + w * kTiles * 32, t.rows - 1)));  // its rows see at least the positions below this one
-    float v_unit = 0.0f;                                                            // outputs are in units of this value scale
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+        float f[8];
+        eight_floats(raw[k], bf16, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
+    }
+    float up;
+    kv_query_unit(max_over_32(top), a.scale_log2, &up, &factor);
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+        float f[8];
+        eight_floats(raw[k], bf16, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[k][j] = (_Float16)(f[j] * up);
+    }
+    float m = -__builtin_inff(), l = 0.0f, l_exact = 0.0f;
+    float16v o[kCh];
+#pragma unroll
+    for (int c = 0; c < kCh; ++c) o[c] = float16v(0.0f);
+    const bool busy = row0 + w * 32 < t.rows;                              // this wavefront has rows; all help with the blocks
+    const int lim_all = t.limit(t.token(min(row0 + w * 32, t.rows - 1)));  // its rows see at least the positions below this one
+    float v_unit = 0.0f;                                                   // outputs are in units of this value scale
 
     for (int j0 = jb; j0 < je; j0 += 64) {
         // up to 64 blocks: page and scales, one to a lane (the same in all wavefronts)
@@ -139,22 +138,20 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                 }
             }
         };
-        auto products = [&](int buf, float16v (&x)[kTiles][2]) {
+        auto products = [&](int buf, float16v (&x)[2]) {
             const char* bk = s_k[buf] + n * kKeyBytes + h * 16;
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
-#pragma unroll
-                for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = float16v(0.0f);
+                x[tt] = float16v(0.0f);
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) {
                     const half8 f = *(const half8*)(bk + tt * 32 * kKeyBytes + k * 32);
-#pragma unroll
-                    for (int rt = 0; rt < kTiles; ++rt) x[rt][tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[rt][k], x[rt][tt], 0, 0, 0);
+                    x[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[k], x[tt], 0, 0, 0);
                 }
             }
         };
         // One block: x holds its products with the keys; next is filled with those of the block behind it.
-        auto step = [&](int buf, int cur, int next, int third, float16v (&x)[kTiles][2], float16v (&xn)[kTiles][2]) {
+        auto step = [&](int buf, int cur, int next, int third, float16v (&x)[2], float16v (&xn)[2]) {
             const int b = j0 + cur;
             load(a.c.k, third, kraw);
             load(a.c.v, next, vraw);
@@ -167,9 +164,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                     if (v_unit != 0.0f) {
                         const float f = v_unit / vs;
 #pragma unroll
-                        for (int rt = 0; rt < kTiles; ++rt)
-#pragma unroll
-                            for (int c = 0; c < kCh; ++c) o[rt][c] *= f;
+                        for (int c = 0; c < kCh; ++c) o[c] *= f;
                     }
                     v_unit = vs;
                     rho = 1.0f;
@@ -177,85 +172,64 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                 rho_inv = 1.0f / rho;
             }
             if (a.mask || (b + 1) * kKvBlock > lim_all) {
-#pragma unroll
-                for (int rt = 0; rt < kTiles; ++rt) {
-                    const int left = lim[rt] - b * kKvBlock;
-                    uint64_t see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
-                    if (a.mask && see) see &= a.mask[tok[rt] * a.mask_words + b];
-                    see >>= h * 4;
-#pragma unroll
-                    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[rt][tt][i] = kv_seen(x[rt][tt][i], (uint32_t)(see >> (tt * 32)), (i >> 2) * 8 + (i & 3));
-                }
-            }
-            const float ks_b = __uint_as_float(lane_value(__float_as_uint(ks_l), cur));
-            const float rho_log = __builtin_amdgcn_logf(rho);
-            float ks[kTiles];
-            bool far = false;
-            float top[kTiles];
-#pragma unroll
-            for (int rt = 0; rt < kTiles; ++rt) {
-                ks[rt] = fmaxf(ks_b * factor[rt], 1e-37f);
-                top[rt] = x[rt][0][0];
+                const int left = lim - b * kKvBlock;
+                uint64_t see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
+                if (a.mask && see) see &= a.mask[of.tok * a.mask_words + b];
+                see >>= h * 4;
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) top[rt] = fmaxf(top[rt], x[rt][tt][i]);
-                top[rt] = max_over_32(top[rt]) * ks[rt];
-                far = far || top[rt] > m[rt] + kKvSlack;
+                    for (int i = 0; i < 16; ++i) x[tt][i] = kv_seen(x[tt][i], (uint32_t)(see >> (tt * 32)), (i >> 2) * 8 + (i & 3));
             }
-            if (ballot(far) != 0) {
+            const float ks = fmaxf(__uint_as_float(lane_value(__float_as_uint(ks_l), cur)) * factor, 1e-37f);
+            const float rho_log = __builtin_amdgcn_logf(rho);
+            float top = x[0][0];
 #pragma unroll
-                for (int rt = 0; rt < kTiles; ++rt) {
-                    const float m_new = top[rt] > m[rt] + kKvSlack ? top[rt] : m[rt];
-                    const float alpha = m_new == m[rt] ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - m_new);
-                    m[rt] = m_new;
-                    l[rt] *= alpha;
-                    if (kExact) l_exact[rt] *= alpha;
+            for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                    for (int c = 0; c < kCh; ++c) o[rt][c] *= alpha;
-                }
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[tt][i]);
+            top = max_over_32(top) * ks;
+            if (ballot(top > m + kKvSlack) != 0) {
+                const float m_new = top > m + kKvSlack ? top : m;
+                const float alpha = m_new == m ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+                m = m_new;
+                l *= alpha;
+                if (kExact) l_exact *= alpha;
+#pragma unroll
+                for (int c = 0; c < kCh; ++c) o[c] *= alpha;
             }
             products(buf ^ 1, xn);
-            half8 p[kTiles][4];
-            float sums[kTiles];
+            half8 p[4];
+            const float base = m == -__builtin_inff() ? 0.0f : kKvLift + rho_log - m;
+            float sum = 0.0f;
 #pragma unroll
-            for (int rt = 0; rt < kTiles; ++rt) {
-                const float base = m[rt] == -__builtin_inff() ? 0.0f : kKvLift + rho_log - m[rt];
-                float sum = 0.0f;
+            for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                for (int tt = 0; tt < 2; ++tt)
+                for (int i = 0; i < 16; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tt][i], ks, base));
+                    if (kExact) sum += e;
+                    p[tt * 2 + (i >> 3)][i & 7] = (_Float16)e;
+                }
+            float rounded = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][tt][i], ks[rt], base));
-                        if (kExact) sum += e;
-                        p[rt][tt * 2 + (i >> 3)][i & 7] = (_Float16)e;
-                    }
-                float rounded = 0.0f;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) rounded = add_halves(p[rt][u], rounded);
-                l[rt] = __builtin_fmaf(rounded, rho_inv, l[rt]);
-                sums[rt] = sum * rho_inv;
-                l_exact[rt] += sums[rt];
-            }
+            for (int u = 0; u < 4; ++u) rounded = add_halves(p[u], rounded);
+            l = __builtin_fmaf(rounded, rho_inv, l);
+            const float sums = sum * rho_inv;
+            l_exact += sums;
             const char* bv = s_v[buf] + n * kValBytes + h * 16;
 #pragma unroll
             for (int c = 0; c < kCh; ++c)
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const half8 f = *(const half8*)(bv + c * 32 * kValBytes + u * 32);
-#pragma unroll
-                    for (int rt = 0; rt < kTiles; ++rt) o[rt][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[rt][u], o[rt][c], 0, 0, 0);
+                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[u], o[c], 0, 0, 0);
                 }
             put_keys(buf);
             put_values(buf ^ 1, next);
-            if (kExact && a.block_ml)
-#pragma unroll
-                for (int rt = 0; rt < kTiles; ++rt) {
-                    const float both = sum_over_32(sums[rt]);
-                    if (h == 0 && row[rt] < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row[rt]] = make_float2(m[rt], both);
-                }
+            if (kExact && a.block_ml) {
+                const float both = sum_over_32(sums);
+                if (h == 0 && row < t.rows) a.block_ml[(uh * a.entries + b) * a.rows_pad + row] = make_float2(m, both);
+            }
             __syncthreads();
         };
         // the walk over the blocks to do: the last one again where there is none
@@ -267,7 +241,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
             }
             return 0;
         };
-        float16v xa[kTiles][2], xb[kTiles][2];
+        float16v xa[2], xb[2];
         int left = __builtin_popcountll(todo);
         int first = 0, second, third;
         after(&first);
@@ -310,40 +284,37 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
         }
     }
 
-#pragma unroll
-    for (int rt = 0; rt < kTiles; ++rt) {
-        const float sum = sum_over_32(l[rt]), exact = kExact ? sum_over_32(l_exact[rt]) : 0.0f;
-        if (row[rt] >= t.rows) continue;
-        if (t.n_list > a.chunk) {
-            const int64_t part = (uh * a.splits + split) * a.rows_pad + row[rt];
-#pragma unroll
-            for (int c = 0; c < kCh; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float4v y;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) y[u] = o[rt][c][4 * i + u] * v_unit;
-                    *(float4v*)(a.part_o + part * D + c * 32 + i * 8 + h * 4) = y;
-                }
-            if (h == 0) a.part_ml[part] = make_float4(m[rt], sum, exact, 0.0f);
-            continue;
-        }
-        const KvRow to = kv_row(row[rt], t.tok_unit, head, a.group);
-        const int64_t place = to.tok * heads_all + to.q_head;
-        const float inv = sum > 0.0f || sum != sum ? v_unit / sum : 0.0f;
+    const float sum = sum_over_32(l), exact = kExact ? sum_over_32(l_exact) : 0.0f;
+    if (row >= t.rows) return;
+    if (t.n_list > a.chunk) {
+        const int64_t part = (uh * a.splits + split) * a.rows_pad + row;
 #pragma unroll
         for (int c = 0; c < kCh; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                uint32_t r[4];
+                float4v y;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) r[u] = to_16_bits(o[rt][c][4 * i + u] * inv, bf16);
-                *(uint2*)((uint16_t*)a.out + place * D + c * 32 + i * 8 + h * 4) = make_uint2(r[0] | r[1] << 16, r[2] | r[3] << 16);
+                for (int u = 0; u < 4; ++u) y[u] = o[c][4 * i + u] * v_unit;
+                *(float4v*)(a.part_o + part * D + c * 32 + i * 8 + h * 4) = y;
             }
-        if (kExact && h == 0) {
-            if (a.lse) a.lse[place] = exact == 0.0f ? -__builtin_inff() : (m[rt] - kKvLift + log2f(exact)) * 0.69314718056f;
-            if (a.row_ml) a.row_ml[uh * a.rows_pad + row[rt]] = make_float2(m[rt], exact);
+        if (h == 0) a.part_ml[part] = make_float4(m, sum, exact, 0.0f);
+        return;
+    }
+    const KvRow to = kv_row(row, t.tok_unit, head, a.group);  // (kept through the walk it would cost registers: 140 us against 133)
+    const int64_t place = to.tok * heads_all + to.q_head;
+    const float inv = sum > 0.0f || sum != sum ? v_unit / sum : 0.0f;
+#pragma unroll
+    for (int c = 0; c < kCh; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t r[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) r[u] = to_16_bits(o[c][4 * i + u] * inv, bf16);
+            *(uint2*)((uint16_t*)a.out + place * D + c * 32 + i * 8 + h * 4) = make_uint2(r[0] | r[1] << 16, r[2] | r[3] << 16);
         }
+    if (kExact && h == 0) {
+        if (a.lse) a.lse[place] = exact == 0.0f ? -__builtin_inff() : (m - kKvLift + log2f(exact)) * 0.69314718056f;
+        if (a.row_ml) a.row_ml[uh * a.rows_pad + row] = make_float2(m, exact);
     }
 }
 
