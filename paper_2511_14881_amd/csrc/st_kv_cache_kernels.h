@@ -219,7 +219,7 @@ __device__ inline float4v kv_floats(uint32_t w, float sc)
 }
 
 // One workgroup to a page, head and kind.  Bound by the floats it writes, which go past the caches (as fast as if they did not).
-// 3 x 4097 tokens, 8 heads of 128: 20 us, 75 MB in and out.
+// 3 x 4097 tokens, 8 heads of 128: 20 us, 130 MB in and out, 6.5 TB/s.
 template <int D>
 __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvReadArgs a)
 {

@@ -7,7 +7,7 @@
 // products of the next block's keys stand beside the exponentials of this one's weights.  The value scale of a block is part of
 // its weights (relative to a reference that follows the scales at a distance), so that the products accumulate into the outputs.
 //
-// 500 candidates to each of 16 histories of 1024 to 4096 tokens, 2 query heads to each of 4 heads of 128: 133 us, 655 TFLOP/s;
+// 500 candidates to each of 16 histories of 1216 to 4096 tokens, 2 query heads to each of 4 heads of 128: 133 us, 655 TFLOP/s;
 // with histories of one length 843 (a large product of matrices in 16 bits reaches 1390), since one round of workgroups lasts
 // as long as the longest history.  2047 tokens over 15001, 5 query heads to each of 3 heads of 96, under a mask: 265 us and 19 to
 // join.  With one part left out, 133 us become 131 (exponentials), 120 (stores to the LDS), 127 (loads), 106 or 104 (either product):
