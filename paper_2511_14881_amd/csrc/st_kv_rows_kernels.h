@@ -9,8 +9,8 @@
 //
 // 500 candidates to each of 16 histories of 1216 to 4096 tokens, 2 query heads to each of 4 heads of 128: 133 us, 655 TFLOP/s;
 // with histories of one length 843 (a large product of matrices in 16 bits reaches 1390), since one round of workgroups lasts
-// as long as the longest history.  2047 tokens over 15001, 5 query heads to each of 3 heads of 96, under a mask: 265 us and 19 to
-// join.  With one part left out, 133 us become 131 (exponentials), 120 (stores to the LDS), 127 (loads), 106 or 104 (either product):
+// as long as the longest history.  2047 tokens over 15001, 5 query heads to each of 3 heads of 96, under a mask: 264 us and 19 to
+// join.  With one part left out, 138 us (on another card) become 131 (exponentials), 120 (stores to the LDS), 127 (loads), 106 or 104 (either product):
 // the parts hide behind each other about as far as two wavefronts of a SIMD let them.  256 rows to a workgroup of 8 wavefronts
 // rather than 128 to one of 4: 132 against 152; two tiles of 32 rows to a wavefront, 4 wavefronts: 219; products and weights
 // in turn on the two wavefronts of a SIMD, with a barrier between: 154.
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
             const float vs = __uint_as_float(lane_value(__float_as_uint(vs_l), cur));
             float rho = 1.0f, rho_inv = 1.0f;
             if (vs != 0.0f) {
-                rho = vs / v_unit;
+                rho = vs * __builtin_amdgcn_rcpf(v_unit);  // (an ulp or two off; exact divisions: 137 us against 134)
                 if (!(rho >= 0.00390625f && rho <= 1.875f)) {
                     if (v_unit != 0.0f) {
                         const float f = v_unit / vs;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                     v_unit = vs;
                     rho = 1.0f;
                 }
-                rho_inv = 1.0f / rho;
+                rho_inv = __builtin_amdgcn_rcpf(rho);
             }
             if (a.mask || (b + 1) * kKvBlock > lim_all) {
                 const int left = lim - b * kKvBlock;
