@@ -335,7 +335,7 @@ int st_value_model(const float* dev_task_scores, int64_t n, int32_t n_tasks,
  *   dev_k        [n_pages, n_heads, 64, d] int8        key of token t (position t % 64 of its block) is row t
  *   dev_v        [n_pages, n_heads, d, 64] int8        value channel c of token t is at [c][slot(t)], where slot is
  *                                                      t with its bits 5 4 3 2 1 0 in the order 3 2 5 4 1 0
- *   dev_k_scale, dev_v_scale [n_pages, n_heads] fp32   a held integer stands for integer * scale
+ *   dev_k_scale, dev_v_scale [n_pages, n_heads] fp32   a held integer stands for integer * scale (>= 0, finite)
  *   dev_bounds   [n_pages, n_heads, 2, d] int8         per channel the largest and the smallest key of the block
  * The integers of positions that hold no token are ignored.  d is 64, 96, 128 or 256.  All arrays 16-byte aligned;
  * the caller owns them.  (The slot order is the order in which a lane of the matrix instruction holds the

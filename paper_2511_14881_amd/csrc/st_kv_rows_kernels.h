@@ -5,9 +5,10 @@
 // once for all of them, on their way into the LDS (two blocks deep, the next one's integers in flight behind the products).
 // As in the kernel for few rows a lane holds one row's logits, and weights go from one product to the other as they lie.  The
 // products of the next block's keys stand beside the exponentials of this one's weights.  The value scale of a block is part of
-// its weights (relative to a reference that follows the scales at a distance), so that the products accumulate into the outputs.
+// its weights, relative to a reference that each row has for itself and that follows the scales of the blocks it sees at a distance, so
+// that the products accumulate into the outputs.
 //
-// 500 candidates to each of 16 histories of 1216 to 4096 tokens, 2 query heads to each of 4 heads of 128: 133 us, 655 TFLOP/s;
+// 500 candidates to each of 16 histories of 1216 to 4096 tokens, 2 query heads to each of 4 heads of 128: 132 us, 660 TFLOP/s;
 // with histories of one length 843 (a large product of matrices in 16 bits reaches 1390), since one round of workgroups lasts
 // as long as the longest history.  2047 tokens over 15001, 5 query heads to each of 3 heads of 96, under a mask: 264 us and 19 to
 // join.  With one part left out, 138 us (on another card) become 131 (exponentials), 120 (stores to the LDS), 127 (loads), 106 or 104 (either product):
@@ -20,6 +21,14 @@
 namespace st {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
+
+// A block's value scale over the row's reference is part of its weights between these two; beyond them the reference moves to the
+// block's.  The least: weights are still of 11 significant bits down to 2^-20 of the row's largest, and rounding takes at
+// most 2^-31 of the largest from the sum for each lighter token.  The most: a weight of 2^15 stays a 16-bit number.  The reference does
+// not fall below kFall of the largest that the row has met (a smaller scale counts as that, off by 2^-73 of the largest
+// value): outputs of 2^20 tokens stay below 2^124.  (A reference to each row rather than to the wavefront: 131.7 us against 130.6, 292
+// against 284 with a mask.)
+constexpr float kRhoLeast = 0.25f, kRhoMost = 1.875f, kFall = 0x1p-80f;
 
 // kExact: lse or the blocks' weights are asked for (the case above: 16 us more for both).
 template <int D, int kWaves, bool kExact>
@@ -78,7 +87,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
     for (int c = 0; c < kCh; ++c) o[c] = float16v(0.0f);
     const bool busy = row0 + w * 32 < t.rows;                              // this wavefront has rows; all help with the blocks
     const int lim_all = t.limit(t.token(min(row0 + w * 32, t.rows - 1)));  // its rows see at least the positions below this one
-    float v_unit = 0.0f;                                                   // outputs are in units of this value scale
+    float v_unit = 0.0f, v_top = 0.0f;                                     // outputs are in units of this value scale; the largest it was
 
     for (int j0 = jb; j0 < je; j0 += 64) {
         // up to 64 blocks: page and scales, one to a lane (the same in all wavefronts)
@@ -155,22 +164,11 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
             const int b = j0 + cur;
             load(a.c.k, third, kraw);
             load(a.c.v, next, vraw);
-            // the scale of the values against the reference
+            // the scale of the values against the row's reference, which follows the blocks that the row sees
             const float vs = __uint_as_float(lane_value(__float_as_uint(vs_l), cur));
-            float rho = 1.0f, rho_inv = 1.0f;
-            if (vs != 0.0f) {
-                rho = vs * __builtin_amdgcn_rcpf(v_unit);  // (an ulp or two off; exact divisions: 137 us against 134)
-                if (!(rho >= 0.00390625f && rho <= 1.875f)) {
-                    if (v_unit != 0.0f) {
-                        const float f = v_unit / vs;
-#pragma unroll
-                        for (int c = 0; c < kCh; ++c) o[c] *= f;
-                    }
-                    v_unit = vs;
-                    rho = 1.0f;
-                }
-                rho_inv = __builtin_amdgcn_rcpf(rho);
-            }
+            const float ratio = vs != 0.0f ? vs * __builtin_amdgcn_rcpf(v_unit) : 1.0f;  // (an ulp or two off; exact divisions: 137 us against 134)
+            float rho = fminf(fmaxf(ratio, kRhoLeast), kRhoMost);
+            float rho_inv = __builtin_amdgcn_rcpf(rho), rho_log = __builtin_amdgcn_logf(rho);
             if (a.mask || (b + 1) * kKvBlock > lim_all) {
                 const int left = lim - b * kKvBlock;
                 uint64_t see = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
@@ -182,13 +180,23 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
                     for (int i = 0; i < 16; ++i) x[tt][i] = kv_seen(x[tt][i], (uint32_t)(see >> (tt * 32)), (i >> 2) * 8 + (i & 3));
             }
             const float ks = fmaxf(__uint_as_float(lane_value(__float_as_uint(ks_l), cur)) * factor, 1e-37f);
-            const float rho_log = __builtin_amdgcn_logf(rho);
             float top = x[0][0];
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, x[tt][i]);
             top = max_over_32(top) * ks;
+            if (ballot(top > -__builtin_inff() && ratio != rho) != 0) {
+                const bool moves = top > -__builtin_inff() && ratio != rho;
+                if (moves) v_top = fmaxf(v_top, v_unit);
+                const float to = vs < v_top * kFall ? v_top * kFall : vs, f = moves ? v_unit / to : 1.0f;
+#pragma unroll
+                for (int c = 0; c < kCh; ++c) o[c] *= f;
+                v_unit = moves ? to : v_unit;
+                rho = moves ? 1.0f : rho;
+                rho_inv = moves ? 1.0f : rho_inv;
+                rho_log = moves ? 0.0f : rho_log;
+            }
             if (ballot(top > m + kKvSlack) != 0) {
                 const float m_new = top > m + kKvSlack ? top : m;
                 const float alpha = m_new == m ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
