@@ -87,6 +87,7 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
     for (int c = 0; c < kCh; ++c) o[c] = float16v(0.0f);
     const bool busy = row0 + w * 32 < t.rows;                              // this wavefront has rows; all help with the blocks
     const int lim_all = t.limit(t.token(min(row0 + w * 32, t.rows - 1)));  // its rows see at least the positions below this one
+    uint64_t far = 0;                                                      // rows of large logits (kv_far)
     float v_unit = 0.0f, v_top = 0.0f;                                     // outputs are in units of this value scale; the largest it was
 
     for (int j0 = jb; j0 < je; j0 += 64) {
@@ -179,36 +180,43 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[tt][i] = kv_seen(x[tt][i], (uint32_t)(see >> (tt * 32)), (i >> 2) * 8 + (i & 3));
             }
-            const float ks = fmaxf(__uint_as_float(lane_value(__float_as_uint(ks_l), cur)) * factor, 1e-37f);
+            float ks = fmaxf(__uint_as_float(lane_value(__float_as_uint(ks_l), cur)) * factor, 1e-37f);
             float top = x[0][0];
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, x[tt][i]);
             top = max_over_32(top) * ks;
-            if (ballot(top > -__builtin_inff() && ratio != rho) != 0) {
-                const bool moves = top > -__builtin_inff() && ratio != rho;
+            // seldom: the maximum or the reference moves, or logits are large
+            const bool rises = top - m > kKvSlack, moves = top > -__builtin_inff() && ratio != rho;
+            float shift = m == -__builtin_inff() ? 0.0f : m;
+            if ((ballot(rises || moves) | far) != 0) {
+                const float alpha = rises ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+                m = rises ? top : m;
+                shift = m == -__builtin_inff() ? 0.0f : m;
                 if (moves) v_top = fmaxf(v_top, v_unit);
-                const float to = vs < v_top * kFall ? v_top * kFall : vs, f = moves ? v_unit / to : 1.0f;
-#pragma unroll
-                for (int c = 0; c < kCh; ++c) o[c] *= f;
+                const float to = vs < v_top * kFall ? v_top * kFall : vs, f = moves ? v_unit / to * alpha : alpha;
                 v_unit = moves ? to : v_unit;
                 rho = moves ? 1.0f : rho;
                 rho_inv = moves ? 1.0f : rho_inv;
                 rho_log = moves ? 0.0f : rho_log;
-            }
-            if (ballot(top > m + kKvSlack) != 0) {
-                const float m_new = top > m + kKvSlack ? top : m;
-                const float alpha = m_new == m ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-                m = m_new;
                 l *= alpha;
                 if (kExact) l_exact *= alpha;
 #pragma unroll
-                for (int c = 0; c < kCh; ++c) o[c] *= alpha;
+                for (int c = 0; c < kCh; ++c) o[c] *= f;
+                far = ballot(kv_far(m));
+                if (far) {
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[tt][i] = __fmul_rn(x[tt][i], ks) - shift;
+                    ks = 1.0f;
+                    shift = 0.0f;
+                }
             }
+            const float base = kKvLift + rho_log - shift;
             products(buf ^ 1, xn);
             half8 p[4];
-            const float base = m == -__builtin_inff() ? 0.0f : kKvLift + rho_log - m;
             float sum = 0.0f;
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
