@@ -62,7 +62,7 @@ __device__ inline bool kv_far(float m) { return fabsf(m) >= 0x1p18f && m != -__b
 // of the softmax scale; *factor times the product and a key scale is then the logit, in powers of two.
 __device__ inline void kv_query_unit(float top, float scale_log2, float* up, float* factor)
 {
-    const int e = top > 0.0f ? min(max(ilogbf(top), -100), 120) : 0;
+    const int e = top > 0.0f ? min(max(ilogbf(top), -100), 127) : 0;
     *up = ldexpf(scale_log2 < 0.0f ? -1.0f : 1.0f, 13 - e);
     *factor = fabsf(scale_log2) * ldexpf(1.0f, e - 13);
 }

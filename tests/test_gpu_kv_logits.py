@@ -58,3 +58,19 @@ def test_equal_large_logits_share_the_weight(d, group, n_q):
                 want[s * n_q:(s + 1) * n_q, h * group:(h + 1) * group] = host.rows(s, h)[1].mean(0)
                 value[s * n_q:(s + 1) * n_q, h * group:(h + 1) * group] = 127.0 * host.vs[host.tables[s, : -(-host.lens[s] // 64)], h].max()
         W.check(out, want, W.error(host, want, np.zeros(value.shape), value, "bf16"))
+
+
+@pytest.mark.parametrize("d,group,n_q", SHAPES)
+def test_queries_up_to_the_largest_number(d, group, n_q):
+    """bf16 queries from 2^117 up to its largest finite number, with keys that bring the logits back to ordinary size."""
+    rng = np.random.default_rng(43)
+    host = R.Host(rng, [900, 300], 2, d)
+    host.ks[:] = rng.uniform(2e-38, 4e-38, host.ks.shape)
+    for size in (2e35, 4e36, 6e37):
+        q = queries(rng, 2 * n_q, 2 * group, d, "bf16", size)
+        q[0, 0, 0] = torch.finfo(torch.bfloat16).max
+        assert torch.isfinite(q).all()
+        scale = 1.0 / (size * 3e-38 * 40 * d ** 0.5)
+        out = st.st_kv_attend(host.cache(st), host.batch(st, 2 * n_q, max_len=900), q.cuda(), scale=scale, causal=False)
+        want, _, _, reach, value = W.attend(host, q, scale, False)
+        W.check(out, want, W.error(host, want, reach, value, "bf16"))
