@@ -147,6 +147,17 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
+def _on(stream, call, *args):
+    """call(*args) on a stream that need not be the current one: what it allocates is that stream's, so that nothing of it is handed
+    out before the work there is done, and its results are kept for the current stream too."""
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        got = call(*args)
+    for t in got if isinstance(got, tuple) else (got,):
+        t.record_stream(here)
+    return got
+
+
 def _need(t: torch.Tensor, dtype, name: str):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name} must be a contiguous CUDA tensor of {dtype}")
@@ -664,6 +675,8 @@ def st_kv_append(cache: KvCache, batch: KvBatch, k, v, stream=None) -> None:
 
 def st_kv_read(cache: KvCache, batch: KvBatch, n_blocks: int, stream=None):
     """The last n_blocks blocks of each sequence as fp32 (k, v [n_seq, n_blocks, heads, 64, d], bounds [.., 2, d])."""
+    if stream is not None:
+        return _on(stream, st_kv_read, cache, batch, n_blocks)
     shape = (batch.n_seq, n_blocks, cache.n_heads, ST_KV_BLOCK, cache.d)
     k = cache.k_scale.new_empty(shape)
     v = cache.k_scale.new_empty(shape)
@@ -683,6 +696,8 @@ def st_kv_attend(cache: KvCache, batch: KvBatch, q, scale: float | None = None, 
     mask int64 [n_tok, words], a bit to a position; blocks int32 [n_tok, heads, n_sel] from st_kv_select.  The blocks'
     weights go to mass_out (or buffers.mass) where that or mass (the weights so far, times decay) is given; lse fp32
     [n_tok, n_q_heads] is filled where given."""
+    if stream is not None:
+        return _on(stream, st_kv_attend, cache, batch, q, scale, causal, mask, blocks, mass, decay, mass_out, lse, out, buffers)
     q_stride, dtype = _kv_rows(q, batch.n_tok, cache.d, "q")
     n_q_heads, n_sel = q.shape[1], 0
     mask_p, words = _kv_mask(mask, batch.n_tok)
@@ -725,6 +740,8 @@ def st_kv_select_workspace_bytes(cache: KvCache, batch: KvBatch, n_q_heads: int,
 def st_kv_select(cache: KvCache, batch: KvBatch, q, n_sel: int, causal: bool = True, mask=None, sink: int = 0,
                  recent: int = 0, out=None, buffers: KvBuffers | None = None, stream=None) -> torch.Tensor:
     """The n_sel blocks that each token and head of the cache reads: int32 [n_tok, heads, n_sel], ascending, -1 behind."""
+    if stream is not None:
+        return _on(stream, st_kv_select, cache, batch, q, n_sel, causal, mask, sink, recent, out, buffers)
     q_stride, dtype = _kv_rows(q, batch.n_tok, cache.d, "q")
     n_q_heads = q.shape[1]
     mask_p, words = _kv_mask(mask, batch.n_tok)
@@ -746,6 +763,8 @@ def st_kv_select(cache: KvCache, batch: KvBatch, q, n_sel: int, causal: bool = T
 def st_kv_evict(batch: KvBatch, mass, budget: int, sink: int = 0, recent: int = 1, out=None, stream=None):
     """Cuts each sequence to at most budget blocks by mass fp32 [n_seq, heads, max_blocks].  Returns (tables, lengths,
     mass, freed, n_freed); out: the tensors to fill, of which tables, lengths and mass may be the batch's own."""
+    if stream is not None:
+        return _on(stream, st_kv_evict, batch, mass, budget, sink, recent, out)
     _need(mass, torch.float32, "mass")
     if mass.dim() != 3 or mass.shape[0] != batch.n_seq or mass.shape[2] != batch.max_blocks:
         raise ValueError("mass must be [n_seq, heads, max_blocks]")
