@@ -313,19 +313,21 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
                           p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)(batch->n_seq * cache->n_heads), p.rows_pad, (float*)ws, (float4*)(ws + p.o_bytes),
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr, dev_mass_in, decay, dev_mass_out};
+    // (one workgroup to each sequence and head writes the weights itself, unless there are no tokens)
+    const bool whole = n_sel == 0 && !p.many && p.tiles == 1 && p.splits == 1 && !batch->dev_offsets;
+    const bool sums = mass && batch->n_seq > 0 && !(whole && batch->max_tok > 0);
+    const int lanes = p.rows_pad > 16 ? 64 : 16, of = st::kKvThreads / lanes;
+    const int64_t sh = (int64_t)batch->n_seq * cache->n_heads;
+    const int64_t groups = n_sel > 0 ? sh : sh * ((batch->max_blocks + of - 1) / of);
+    // all that can be refused is, before anything is written
+    if (sums && (rc = check_grid(groups))) return rc;
+    if (sums && n_sel > 0 && (rc = allow_lds(&st::kv_mass_selected_kernel, batch->max_blocks * 4))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
     if (batch->n_tok > 0 && batch->max_tok > 0)
         with_dim(cache->d, [&](auto d) -> int {
             return n_sel > 0 ? launch_attend<decltype(d)::value, true>(a, p, stream) : launch_attend<decltype(d)::value, false>(a, p, stream);
         });
-    // (one workgroup to each sequence and head writes the weights itself, unless there are no tokens)
-    const bool whole = n_sel == 0 && !p.many && p.tiles == 1 && p.splits == 1 && !batch->dev_offsets;
-    if (mass && batch->n_seq > 0 && !(whole && batch->max_tok > 0)) {
-        const int64_t sh = (int64_t)batch->n_seq * cache->n_heads;
-        const int lanes = p.rows_pad > 16 ? 64 : 16, of = st::kKvThreads / lanes;
-        const int64_t groups = n_sel > 0 ? sh : sh * ((batch->max_blocks + of - 1) / of);
-        if ((rc = check_grid(groups))) return rc;
-        if (n_sel > 0 && (rc = allow_lds(&st::kv_mass_selected_kernel, batch->max_blocks * 4))) return rc;
+    if (sums) {
         TimedLaunch t(1, stream);
         if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, dim3((unsigned)groups), dim3(st::kKvThreads), batch->max_blocks * 4, stream, a);
         else if (lanes == 64) hipLaunchKernelGGL(st::kv_mass_kernel<64>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
