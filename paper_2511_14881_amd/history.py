@@ -35,6 +35,17 @@ class HistoryStore:
         self.mass = torch.zeros((n_users, n_heads, max_blocks), dtype=torch.float32, device="cuda")
         self.free = list(range(n_pages - 1, -1, -1))
 
+    def _known(self, users, once: bool = False) -> np.ndarray:
+        """The users as an array of indices.  once: none may be named twice, since the call writes to their histories."""
+        users = np.asarray(users)
+        if users.ndim != 1 or (users.size and users.dtype.kind not in "iu"):
+            raise ValueError("users must be whole numbers in a row")
+        if users.size and (users.min() < 0 or users.max() >= len(self.lengths)):
+            raise ValueError(f"users must be in [0, {len(self.lengths)})")
+        if once and len(np.unique(users)) != len(users):
+            raise ValueError("a user is named twice: join what belongs to one history")
+        return users
+
     def batch(self, users, counts) -> st.KvBatch:
         """The call's view of these users, counts[i] tokens of users[i] in it."""
         counts = np.asarray(counts, dtype=np.int64)
@@ -46,8 +57,9 @@ class HistoryStore:
                           int(counts.sum()), offsets=offsets, max_tok=int(counts.max()) if counts.size else 0, max_len=max_len)
 
     def append(self, users, k, v, counts=None) -> None:
-        """Events k, v [sum of counts, heads, d] behind the users' histories (one each if counts is not given)."""
-        users = np.asarray(users)
+        """Events k, v [sum of counts, heads, d] behind the users' histories (one each if counts is not given).
+        Each user once."""
+        users = self._known(users, once=True)
         counts = np.ones(len(users), np.int64) if counts is None else np.asarray(counts, dtype=np.int64)
         need = -(-(self.lengths[users] + counts) // st.ST_KV_BLOCK)
         have = -(-self.lengths[users] // st.ST_KV_BLOCK)
@@ -64,8 +76,8 @@ class HistoryStore:
     def attend(self, users, q, counts, n_sel: int = 0, sink: int = 0, recent: int = 0, causal: bool = False, track: bool = False,
                decay: float = 1.0, mask=None) -> torch.Tensor:
         """Outputs like q [sum of counts, q_heads, d] over the users' histories, or over the n_sel blocks that each row
-        selects.  track: the blocks' accumulated weights decay and take on what this call gave them."""
-        users = np.asarray(users)
+        selects.  track: the blocks' accumulated weights decay and take on what this call gave them (each user once)."""
+        users = self._known(users, once=track)
         batch = self.batch(users, counts)
         blocks = None
         if n_sel:
@@ -79,8 +91,8 @@ class HistoryStore:
         return out
 
     def evict(self, users, budget: int, sink: int = 0, recent: int = 1) -> int:
-        """Cuts the users' histories to at most budget blocks; returns how many pages came free."""
-        users = np.asarray(users)
+        """Cuts the users' histories to at most budget blocks; returns how many pages came free.  Each user once."""
+        users = self._known(users, once=True)
         if len(users) == 0:
             return 0
         rows = torch.from_numpy(users).cuda()
