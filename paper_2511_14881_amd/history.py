@@ -46,32 +46,45 @@ class HistoryStore:
             raise ValueError("a user is named twice: join what belongs to one history")
         return users
 
-    def batch(self, users, counts) -> st.KvBatch:
-        """The call's view of these users, counts[i] tokens of users[i] in it."""
-        counts = np.asarray(counts, dtype=np.int64)
+    @staticmethod
+    def _counts(users, counts) -> np.ndarray:
+        counts = np.ones(len(users), np.int64) if counts is None else np.asarray(counts, dtype=np.int64)
+        if counts.shape != (len(users),) or (counts.size and counts.min() < 0):
+            raise ValueError(f"counts must be {len(users)} numbers, none below 0")
+        return counts
+
+    @staticmethod
+    def _view(tables, lengths, counts) -> st.KvBatch:
         offsets = None
         if counts.size and counts.min() != counts.max():
             offsets = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).cuda()
-        max_len = int(self.lengths[users].max()) if len(users) else 0
-        return st.KvBatch(torch.from_numpy(self.tables[users]).cuda(), torch.from_numpy(self.lengths[users]).cuda(),
-                          int(counts.sum()), offsets=offsets, max_tok=int(counts.max()) if counts.size else 0, max_len=max_len)
+        return st.KvBatch(torch.from_numpy(tables).cuda(), torch.from_numpy(lengths).cuda(), int(counts.sum()), offsets=offsets,
+                          max_tok=int(counts.max()) if counts.size else 0, max_len=int(lengths.max()) if lengths.size else 0)
+
+    def batch(self, users, counts) -> st.KvBatch:
+        """The call's view of these users, counts[i] tokens of users[i] in it."""
+        return self._view(self.tables[users], self.lengths[users], self._counts(users, counts))
 
     def append(self, users, k, v, counts=None) -> None:
         """Events k, v [sum of counts, heads, d] behind the users' histories (one each if counts is not given).
-        Each user once."""
+        Each user once.  A call that is refused leaves the store as it was."""
         users = self._known(users, once=True)
-        counts = np.ones(len(users), np.int64) if counts is None else np.asarray(counts, dtype=np.int64)
-        need = -(-(self.lengths[users] + counts) // st.ST_KV_BLOCK)
-        have = -(-self.lengths[users] // st.ST_KV_BLOCK)
+        counts = self._counts(users, counts)
+        tables, lengths = self.tables[users], self.lengths[users]
+        have, need = -(-lengths // st.ST_KV_BLOCK), -(-(lengths + counts) // st.ST_KV_BLOCK)
         if need.size and need.max() > self.max_blocks:
             raise ValueError(f"a history would hold {need.max()} blocks of at most {self.max_blocks}: evict first")
-        if (need - have).sum() > len(self.free):
-            raise ValueError(f"{(need - have).sum()} pages are needed, {len(self.free)} are free: evict first")
-        for u, a, b in zip(users, have, need):
+        taken = int((need - have).sum())
+        if taken > len(self.free):
+            raise ValueError(f"{taken} pages are needed, {len(self.free)} are free: evict first")
+        pages = iter(self.free[len(self.free) - taken:][::-1])
+        for row, a, b in zip(tables, have, need):
             for block in range(a, b):
-                self.tables[u, block] = self.free.pop()
-        self.lengths[users] += counts.astype(np.int32)
-        st.st_kv_append(self.cache, self.batch(users, counts), k, v)
+                row[block] = next(pages)
+        lengths = (lengths + counts).astype(np.int32)
+        st.st_kv_append(self.cache, self._view(tables, lengths, counts), k, v)
+        self.tables[users], self.lengths[users] = tables, lengths
+        del self.free[len(self.free) - taken:]
 
     def attend(self, users, q, counts, n_sel: int = 0, sink: int = 0, recent: int = 0, causal: bool = False, track: bool = False,
                decay: float = 1.0, mask=None) -> torch.Tensor:

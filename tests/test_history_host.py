@@ -104,3 +104,40 @@ def test_users_that_the_store_does_not_have_are_refused(calls, users):
         with pytest.raises((ValueError, IndexError)):
             call()
     assert same(before, state(store)) and not calls.made
+
+
+def test_a_refused_append_leaves_the_store_as_it_was(calls):
+    store = HistoryStore(2, 4, HEADS, D, 3)
+    store.append([0], rows(70), rows(70), [70])
+    before = state(store)
+    calls.refuse.add("append")
+    for users, counts in (([0], [60]), ([1], [65]), ([0, 1], [1, 1])):
+        with pytest.raises(ValueError):
+            store.append(users, rows(3), rows(3), counts)
+        assert same(before, state(store)) and consistent(store)
+    calls.refuse.clear()
+    for users, counts in (([0], [-1]), ([0, 1], [1]), ([0], [1, 2])):
+        with pytest.raises(ValueError, match="counts"):
+            store.append(users, rows(1), rows(1), counts)
+        with pytest.raises(ValueError, match="counts"):
+            store.attend(users, rows(1), counts)
+    for users, counts in (([0], [200]), ([0, 1], [60, 190])):  # more blocks than a history has, more pages than are free
+        with pytest.raises(ValueError, match="evict first"):
+            store.append(users, rows(sum(counts)), rows(sum(counts)), counts)
+    assert same(before, state(store)) and len(calls.made) == 1
+    store.append([0, 1], rows(61), rows(61), [60, 1])
+    assert store.lengths.tolist() == [130, 1] and consistent(store)
+
+
+def test_pages_that_came_free_are_dealt_once(calls):
+    rng = np.random.default_rng(0)
+    store = HistoryStore(5, 40, HEADS, D, 9)
+    for _ in range(60):
+        users = rng.permutation(5)[: rng.integers(1, 6)]
+        counts = rng.integers(0, 130, len(users))
+        try:
+            store.append(users, rows(int(counts.sum())), rows(int(counts.sum())), counts)
+        except ValueError:
+            store.evict(users, int(rng.integers(1, 4)))
+        assert consistent(store)
+    assert {"append", "evict"} <= {name for name, _ in calls.made}
