@@ -44,7 +44,7 @@ class HistoryStore:
             raise ValueError(f"users must be in [0, {len(self.lengths)})")
         if once and len(np.unique(users)) != len(users):
             raise ValueError("a user is named twice: join what belongs to one history")
-        return users
+        return users.astype(np.int64)  # (an empty list comes as floats)
 
     @staticmethod
     def _counts(users, counts) -> np.ndarray:
@@ -70,6 +70,8 @@ class HistoryStore:
         Each user once.  A call that is refused leaves the store as it was."""
         users = self._known(users, once=True)
         counts = self._counts(users, counts)
+        if len(users) == 0:
+            return
         tables, lengths = self.tables[users], self.lengths[users]
         have, need = -(-lengths // st.ST_KV_BLOCK), -(-(lengths + counts) // st.ST_KV_BLOCK)
         if need.size and need.max() > self.max_blocks:
@@ -91,6 +93,9 @@ class HistoryStore:
         """Outputs like q [sum of counts, q_heads, d] over the users' histories, or over the n_sel blocks that each row
         selects.  track: the blocks' accumulated weights decay and take on what this call gave them (each user once)."""
         users = self._known(users, once=track)
+        counts = self._counts(users, counts)
+        if len(users) == 0:
+            return torch.empty_like(q)
         batch = self.batch(users, counts)
         blocks = None
         if n_sel:

@@ -141,3 +141,17 @@ def test_pages_that_came_free_are_dealt_once(calls):
             store.evict(users, int(rng.integers(1, 4)))
         assert consistent(store)
     assert {"append", "evict"} <= {name for name, _ in calls.made}
+
+
+def test_calls_of_no_users_do_nothing(calls):
+    store = HistoryStore(2, 4, HEADS, D, 3)
+    store.append([0], rows(5), rows(5), [5])
+    before, made = state(store), len(calls.made)
+    for none in ([], np.array([], np.int64), np.array([])):
+        store.append(none, rows(0), rows(0))
+        store.append(none, rows(0), rows(0), [])
+        assert store.evict(none, 1) == 0
+        out = store.attend(none, rows(0), [])
+        assert out.shape == (0, HEADS, D) and out.dtype == torch.bfloat16
+        assert store.attend(none, rows(0), [], n_sel=2, track=True).shape == (0, HEADS, D)
+    assert same(before, state(store)) and len(calls.made) == made
