@@ -230,6 +230,8 @@ def st_bloom_layout_bytes(n_items: int, m_bits: int) -> int:
 
 
 def st_bloom_export_signatures(bloom: BloomIndex, stream=None) -> torch.Tensor:
+    if stream is not None:
+        return _on(stream, st_bloom_export_signatures, bloom)
     words = (bloom.m_bits + 63) // 64
     out = torch.empty((bloom.n_items, words), dtype=torch.int64, device="cuda")
     _check(lib().st_bloom_export_signatures(C.c_void_p(bloom.handle), _dptr(out), _stream(stream)))
@@ -237,6 +239,8 @@ def st_bloom_export_signatures(bloom: BloomIndex, stream=None) -> torch.Tensor:
 
 
 def st_bloom_mask(bloom: BloomIndex, filt_ids, filt_offsets, stream=None) -> torch.Tensor:
+    if stream is not None:
+        return _on(stream, st_bloom_mask, bloom, filt_ids, filt_offsets)
     n_f = len(filt_offsets) - 1
     ids, off = _filters(filt_ids, filt_offsets, n_f)
     out = torch.zeros((n_f, (bloom.n_items + 63) // 64), dtype=torch.int64, device="cuda")
@@ -321,6 +325,8 @@ class SearchBuffers:
 
 def st_search(bloom: BloomIndex, items, item_scale, queries, query_scale, filt_ids, filt_offsets,
               K: int, buffers: SearchBuffers | None = None, stream=None):
+    if stream is not None and buffers is None:
+        return _on(stream, st_search, bloom, items, item_scale, queries, query_scale, filt_ids, filt_offsets, K)
     _need(items, torch.int8, "items")
     _need(item_scale, torch.float32, "item_scale")
     _need(queries, torch.int8, "queries")
@@ -345,6 +351,8 @@ def st_search_static(bloom: BloomIndex, items, item_scale, queries, query_scale,
                      K: int, out=None, stream=None):
     """st_search on the library's own fixed workspace (no allocation inside the call).  out: the
     (ids, scores, count) tensors to fill; allocated here, outside the library, if not given."""
+    if stream is not None and out is None:
+        return _on(stream, st_search_static, bloom, items, item_scale, queries, query_scale, filt_ids, filt_offsets, K)
     _need(items, torch.int8, "items")
     _need(item_scale, torch.float32, "item_scale")
     _need(queries, torch.int8, "queries")
@@ -367,6 +375,8 @@ def st_search_static(bloom: BloomIndex, items, item_scale, queries, query_scale,
 def st_search_multitask(bloom: BloomIndex, items, item_scale, queries, query_scale, task_weight,
                         filt_ids, filt_offsets, K: int, buffers: SearchBuffers | None = None,
                         stream=None):
+    if stream is not None and buffers is None:
+        return _on(stream, st_search_multitask, bloom, items, item_scale, queries, query_scale, task_weight, filt_ids, filt_offsets, K)
     _need(items, torch.int8, "items")
     _need(item_scale, torch.float32, "item_scale")
     _need(queries, torch.int8, "queries")
@@ -400,6 +410,8 @@ def _programs(expr_ops, expr_ids, expr_offsets, n: int):
 
 
 def st_bloom_mask_expr(bloom: BloomIndex, expr_ops, expr_ids, expr_offsets, stream=None) -> torch.Tensor:
+    if stream is not None:
+        return _on(stream, st_bloom_mask_expr, bloom, expr_ops, expr_ids, expr_offsets)
     n_e = len(expr_offsets) - 1
     ops, ids, off = _programs(expr_ops, expr_ids, expr_offsets, n_e)
     out = torch.zeros((n_e, (bloom.n_items + 63) // 64), dtype=torch.int64, device="cuda")
@@ -416,6 +428,9 @@ def st_search_expr_workspace_bytes(n_items: int, d: int, batch: int, n_tasks: in
 def st_search_expr(bloom: BloomIndex, items, item_scale, queries, query_scale, expr_ops, expr_ids,
                    expr_offsets, K: int, task_weight=None, buffers: SearchBuffers | None = None, stream=None):
     """queries [B, d] (task_weight None) or [B, T, d] with T weights; query b's filter is program b."""
+    if stream is not None and buffers is None:
+        return _on(stream, st_search_expr, bloom, items, item_scale, queries, query_scale, expr_ops, expr_ids, expr_offsets, K,
+                   task_weight)
     _need(items, torch.int8, "items")
     _need(item_scale, torch.float32, "item_scale")
     _need(queries, torch.int8, "queries")
@@ -463,6 +478,9 @@ def st_search_ivf(bloom: BloomIndex, items, item_scale, centroids, centroid_scal
                   queries, query_scale, expr_ops, expr_ids, expr_offsets, K: int,
                   buffers: IvfBuffers | None = None, stream=None):
     """Returns (ids, scores, count, probes); cluster_offsets int64 [n_clusters + 1] on the device."""
+    if stream is not None and buffers is None:
+        return _on(stream, st_search_ivf, bloom, items, item_scale, centroids, centroid_scale, cluster_offsets, n_probe, queries,
+                   query_scale, expr_ops, expr_ids, expr_offsets, K)
     _need(items, torch.int8, "items")
     _need(item_scale, torch.float32, "item_scale")
     _need(centroids, torch.int8, "centroids")
@@ -495,6 +513,8 @@ def st_stream_read(src: torch.Tensor, sink: torch.Tensor, workgroups: int, strea
 
 def st_quantize_global(x, stream=None):
     """fp32 [N, d] CUDA tensor -> (int8 [N, d], row scales fp32 [N], minmax fp32 [2]) on the device."""
+    if stream is not None:
+        return _on(stream, st_quantize_global, x)
     _need(x, torch.float32, "x")
     if x.dim() != 2:
         raise ValueError("x must be [N, d]")
@@ -509,6 +529,8 @@ def st_quantize_global(x, stream=None):
 
 def st_value_model(task_scores, ops, consts, out=None, stream=None):
     """task_scores fp32 [n, T] CUDA tensor; postfix formula (ops int32, consts fp32) -> fp32 [n]."""
+    if stream is not None and out is None:
+        return _on(stream, st_value_model, task_scores, ops, consts)
     _need(task_scores, torch.float32, "task_scores")
     if task_scores.dim() != 2:
         raise ValueError("task_scores must be [n, T]")
@@ -524,6 +546,8 @@ def st_value_model(task_scores, ops, consts, out=None, stream=None):
 
 
 def st_score_pairs(items, item_scale, queries, query_scale, pair_item, pair_query, stream=None):
+    if stream is not None:
+        return _on(stream, st_score_pairs, items, item_scale, queries, query_scale, pair_item, pair_query)
     _need(items, torch.int8, "items")
     _need(queries, torch.int8, "queries")
     _need(pair_item, torch.int64, "pair_item")
