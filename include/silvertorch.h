@@ -433,6 +433,14 @@ int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void*
                  int32_t sink, int32_t recent, int32_t* dev_out_blocks, void* dev_workspace, int64_t workspace_bytes,
                  void* hip_stream);
 
+/* Diagnostic, host part alone (no device memory is touched): how st_kv_attend (n_sel 0: over all blocks) and st_kv_select would run such a
+ * call.  host_out_plan[10] receives, of the attention, {wavefronts that share a tile of 16 rows (0: the kernel for many rows), tiles of rows
+ * to a sequence and head, blocks to a split, splits, wavefronts that join a row's splits (0: no join), lanes to a block of the kernel that sums
+ * weights (0: none, or no such kernel runs)}, and of the selection {1 if the workgroup that scores also chooses, workgroups
+ * to the blocks of 16 tokens, rounds of 256 blocks of each, keys to a lane of the wavefront that chooses (0: a workgroup does)}. */
+int st_kv_host_plan(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads, int32_t n_sel,
+                    int32_t with_mass, int32_t* host_out_plan);
+
 /* Shrinks each sequence to at most `budget` blocks by the weight they drew: the score of a block is the largest of
  * dev_mass [n_seq, n_heads, max_blocks] (finite, >= 0) over the heads; the first `sink` blocks and the last `recent` stay,
  * then the best by (score desc, block asc).  1 <= recent, sink + recent <= budget.  Of the batch only tables, lengths

@@ -25,7 +25,7 @@ EXPORTS = [
     "st_search_expr", "st_search_ivf_workspace_bytes", "st_search_ivf", "st_quantize_global", "st_value_model",
     "st_search_host_plan", "st_search_host_units", "st_stream_read", "st_search_static",
     "st_kv_append", "st_kv_read", "st_kv_attend_workspace_bytes", "st_kv_attend", "st_kv_select_workspace_bytes",
-    "st_kv_select", "st_kv_evict",
+    "st_kv_select", "st_kv_evict", "st_kv_host_plan",
 ]
 
 ST_OP_LEAF, ST_OP_AND, ST_OP_OR, ST_OP_NOT = 0, 1, 2, 3  # operations of a filter program
@@ -118,6 +118,8 @@ def lib() -> C.CDLL:
         L.st_kv_select_workspace_bytes.argtypes = [p, p, i32, i32]
         L.st_kv_select.restype = C.c_int
         L.st_kv_select.argtypes = [p, p, p, i64, i32, i32, i32, p, i32, i32, i32, i32, p, p, i64, p]
+        L.st_kv_host_plan.restype = C.c_int
+        L.st_kv_host_plan.argtypes = [p, p, i32, i32, i32, p]
         L.st_kv_evict.restype = C.c_int
         L.st_kv_evict.argtypes = [p, p, i32, i32, i32, i32, p, p, p, p, p, p]
         _lib = L
@@ -782,6 +784,14 @@ def st_kv_select(cache: KvCache, batch: KvBatch, q, n_sel: int, causal: bool = T
     _check(lib().st_kv_select(cache._p, batch._p, q.data_ptr(), q_stride, dtype, n_q_heads, int(causal), mask_p, words, n_sel,
                               sink, recent, out.data_ptr(), work.data_ptr(), nbytes, _kv_stream(stream)))
     return out
+
+
+def st_kv_host_plan(cache: KvCache, batch: KvBatch, n_q_heads: int, n_sel: int = 0, mass: bool = False) -> dict:
+    """How an attention and a selection of these sizes would run (no GPU work; see ``include/silvertorch.h``)."""
+    out = np.zeros(10, dtype=np.int32)
+    _check(lib().st_kv_host_plan(cache._p, batch._p, n_q_heads, n_sel, int(mass), _hptr(out)))
+    keys = ("waves", "tiles", "chunk", "splits", "join_waves", "sum_lanes", "score_and_choose", "score_chunks", "score_rounds", "choose_keys")
+    return {k: int(v) for k, v in zip(keys, out)}
 
 
 def st_kv_evict(batch: KvBatch, mass, budget: int, sink: int = 0, recent: int = 1, out=None, stream=None):

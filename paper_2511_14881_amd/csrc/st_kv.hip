@@ -127,8 +127,10 @@ constexpr int kDies = 8;  // of the chip, each with an L2 of its own
 struct AttendPlan {
     bool many;          // the kernel for many rows
     int32_t tile_rows, tiles, chunk, splits, rows_pad, entries, dies, waves;
+    int32_t join_waves;  // to a row whose splits are joined; 0: nothing to join
+    int32_t sum_lanes;   // lanes to a block where a kernel of its own sums the weights; 0: none does
     int64_t units;
-    int64_t grid;
+    int64_t grid, sum_grid;
     int64_t o_bytes, ml_bytes, block_bytes, row_bytes;
     int64_t bytes() const { return o_bytes + ml_bytes + block_bytes + row_bytes; }
 };
@@ -181,6 +183,12 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int64_t keys = sh * p.splits;
     p.dies = per > 1 && (keys % kDies == 0 || keys >= 8 * kDies) ? kDies : 1;
     p.grid = st::round_up(keys, p.dies) * per;
+    p.join_waves = p.splits >= 16 ? 4 : p.splits > 1 ? 1 : 0;
+    // (one workgroup to each sequence and head writes the weights itself, unless there are no tokens)
+    const bool whole_pairs = n_sel == 0 && !p.many && p.tiles == 1 && p.splits == 1 && !b->dev_offsets && b->max_tok > 0;
+    p.sum_lanes = !mass || b->n_seq == 0 || whole_pairs ? 0 : p.rows_pad > 16 ? 64 : 16;
+    const int of = p.sum_lanes ? st::kKvThreads / p.sum_lanes : 1;
+    p.sum_grid = p.sum_lanes == 0 ? 0 : n_sel > 0 ? sh : sh * ((b->max_blocks + of - 1) / of);
     const int64_t uh = p.units * c->n_heads;
     const int64_t parts = p.splits > 1 ? uh * p.splits * p.rows_pad : 0;
     p.o_bytes = st::round_up(parts * c->d * 4, 256);
@@ -201,16 +209,42 @@ int launch_attend(const st::KvAttendArgs& a, const AttendPlan& p, hipStream_t st
         else if (p.waves == 1) hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected, 1>), grid, dim3(64), 0, stream, a);
         else hipLaunchKernelGGL((st::kv_attend_kernel<D, kSelected, 4>), grid, dim3(256), 0, stream, a);
     }
-    if (p.splits > 1) {
+    if (p.join_waves) {
         TimedLaunch t(1, stream);
         const int64_t rows = (int64_t)a.b.n_tok * a.c.n_heads * a.group;
-        if (p.splits >= 16) hipLaunchKernelGGL((st::kv_join_kernel<D, kSelected, 4>), dim3((unsigned)rows), dim3(st::kKvThreads), 0, stream, a);
+        if (p.join_waves == 4) hipLaunchKernelGGL((st::kv_join_kernel<D, kSelected, 4>), dim3((unsigned)rows), dim3(st::kKvThreads), 0, stream, a);
         else hipLaunchKernelGGL((st::kv_join_kernel<D, kSelected, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(st::kKvThreads), 0, stream, a);
     }
     return ST_OK;
 }
 
 int64_t select_stride(const st_kv_batch* b) { return st::round_up(std::max(1, blocks_of(b->max_len)), 16); }
+
+struct SelectPlan {
+    bool one;              // the workgroup that scores also chooses
+    int32_t chunks, rounds;  // workgroups to the blocks of a tile of tokens, and rounds of kKvScoreBlocks of each
+    int32_t keys;          // that a lane holds where a wavefront chooses; 0: a workgroup chooses
+    int64_t groups;
+};
+
+SelectPlan select_plan(const st_kv_cache* c, const st_kv_batch* b)
+{
+    const int32_t blocks = std::max(1, blocks_of(b->max_len)), tiles = (b->max_tok + 15) / 16;
+    const int64_t pairs = (int64_t)b->n_seq * c->n_heads;
+    SelectPlan p = {false, 1, 1, blocks <= 256 ? 4 : blocks <= 512 ? 8 : blocks <= 1024 ? 16 : 0, 0};
+    // One token to a sequence: the workgroup that scores also chooses, as long as its blocks are few enough to be read by one
+    // (or there are as many sequences and heads as compute units anyway).
+    p.one = b->max_tok == 1 && (blocks <= 1024 || pairs >= st::kComputeUnits);
+    if (!p.one) {
+        // rounds of 256 blocks to a workgroup: as many as still leave two workgroups to a compute unit
+        const int all = (blocks + st::kKvScoreBlocks - 1) / st::kKvScoreBlocks;
+        const int64_t want = std::max<int64_t>(1, 2ll * st::kComputeUnits / std::max<int64_t>(1, pairs * tiles));
+        p.chunks = (int32_t)std::min<int64_t>(all, want);
+        p.rounds = (all + p.chunks - 1) / p.chunks;
+    }
+    p.groups = pairs * tiles * p.chunks;
+    return p;
+}
 
 // Kernels whose dynamic LDS may pass the default limit: the limit is raised once.
 template <class K>
@@ -313,25 +347,20 @@ int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void*
                           p.chunk, p.splits, p.tiles, p.tile_rows, p.dies, (uint32_t)(batch->n_seq * cache->n_heads), p.rows_pad, (float*)ws, (float4*)(ws + p.o_bytes),
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes) : nullptr, p.entries,
                           mass ? (float2*)(ws + p.o_bytes + p.ml_bytes + p.block_bytes) : nullptr, dev_mass_in, decay, dev_mass_out};
-    // (one workgroup to each sequence and head writes the weights itself, unless there are no tokens)
-    const bool whole = n_sel == 0 && !p.many && p.tiles == 1 && p.splits == 1 && !batch->dev_offsets;
-    const bool sums = mass && batch->n_seq > 0 && !(whole && batch->max_tok > 0);
-    const int lanes = p.rows_pad > 16 ? 64 : 16, of = st::kKvThreads / lanes;
-    const int64_t sh = (int64_t)batch->n_seq * cache->n_heads;
-    const int64_t groups = n_sel > 0 ? sh : sh * ((batch->max_blocks + of - 1) / of);
     // all that can be refused is, before anything is written
-    if (sums && (rc = check_grid(groups))) return rc;
-    if (sums && n_sel > 0 && (rc = allow_lds(&st::kv_mass_selected_kernel, batch->max_blocks * 4))) return rc;
+    if ((rc = check_grid(p.sum_grid))) return rc;
+    if (p.sum_lanes && n_sel > 0 && (rc = allow_lds(&st::kv_mass_selected_kernel, batch->max_blocks * 4))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
     if (batch->n_tok > 0 && batch->max_tok > 0)
         with_dim(cache->d, [&](auto d) -> int {
             return n_sel > 0 ? launch_attend<decltype(d)::value, true>(a, p, stream) : launch_attend<decltype(d)::value, false>(a, p, stream);
         });
-    if (sums) {
+    if (p.sum_lanes) {
         TimedLaunch t(1, stream);
-        if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, dim3((unsigned)groups), dim3(st::kKvThreads), batch->max_blocks * 4, stream, a);
-        else if (lanes == 64) hipLaunchKernelGGL(st::kv_mass_kernel<64>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
-        else hipLaunchKernelGGL(st::kv_mass_kernel<16>, dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        const dim3 groups((unsigned)p.sum_grid);
+        if (n_sel > 0) hipLaunchKernelGGL(st::kv_mass_selected_kernel, groups, dim3(st::kKvThreads), batch->max_blocks * 4, stream, a);
+        else if (p.sum_lanes == 64) hipLaunchKernelGGL(st::kv_mass_kernel<64>, groups, dim3(st::kKvThreads), 0, stream, a);
+        else hipLaunchKernelGGL(st::kv_mass_kernel<16>, groups, dim3(st::kKvThreads), 0, stream, a);
     }
     ST_HIP(hipGetLastError());
     return ST_OK;
@@ -369,47 +398,51 @@ int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void*
         return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
     if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
     if (batch->n_tok == 0 || batch->max_tok == 0) return ST_OK;
-    const int32_t blocks = std::max(1, blocks_of(batch->max_len));
-    // One token to a sequence: the workgroup that scores also chooses, as long as its blocks are few enough to be read by one
-    // (or there are as many sequences and heads as compute units anyway).
-    const int64_t pairs = (int64_t)batch->n_seq * cache->n_heads;
-    const bool one = batch->max_tok == 1 && (blocks <= 1024 || pairs >= st::kComputeUnits);
+    const SelectPlan p = select_plan(cache, batch);
     st::KvSelectArgs a = {view(cache), view(batch), dev_q, q_stride, dtype == ST_BF16, n_q_heads / cache->n_heads, causal != 0,
-                          dev_mask, mask_words, n_sel, sink, recent, (batch->max_tok + 15) / 16, 1, 1, select_stride(batch),
+                          dev_mask, mask_words, n_sel, sink, recent, (batch->max_tok + 15) / 16, p.chunks, p.rounds, select_stride(batch),
                           (uint32_t*)dev_workspace, dev_out_blocks};
-    if (!one) {
-        // rounds of 256 blocks to a workgroup: as many as still leave two workgroups to a compute unit
-        const int all = (blocks + st::kKvScoreBlocks - 1) / st::kKvScoreBlocks;
-        const int64_t want = std::max<int64_t>(1, 2ll * st::kComputeUnits / std::max<int64_t>(1, pairs * a.tiles));
-        a.chunks = (int32_t)std::min<int64_t>(all, want);
-        a.rounds = (all + a.chunks - 1) / a.chunks;
-    }
-    const int64_t groups = pairs * a.tiles * a.chunks;
     const int64_t rows = (int64_t)batch->n_tok * cache->n_heads;
-    if ((rc = check_grid(groups)) || (rc = check_grid(rows))) return rc;
+    if ((rc = check_grid(p.groups)) || (rc = check_grid(rows))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
     const int lds = (int)select_stride(batch) * 4;
     rc = with_dim(cache->d, [&](auto d) -> int {
         constexpr int D = decltype(d)::value;
         int rc2;
         constexpr int kOneThreads = 512;
-        if (one && (rc2 = allow_lds(&st::kv_score_kernel<D, true, kOneThreads>, lds))) return rc2;
+        if (p.one && (rc2 = allow_lds(&st::kv_score_kernel<D, true, kOneThreads>, lds))) return rc2;
         TimedLaunch t(0, stream);
-        if (one) hipLaunchKernelGGL((st::kv_score_kernel<D, true, kOneThreads>), dim3((unsigned)groups), dim3(kOneThreads), lds, stream, a);
-        else hipLaunchKernelGGL((st::kv_score_kernel<D, false, st::kKvThreads>), dim3((unsigned)groups), dim3(st::kKvThreads), 0, stream, a);
+        if (p.one) hipLaunchKernelGGL((st::kv_score_kernel<D, true, kOneThreads>), dim3((unsigned)p.groups), dim3(kOneThreads), lds, stream, a);
+        else hipLaunchKernelGGL((st::kv_score_kernel<D, false, st::kKvThreads>), dim3((unsigned)p.groups), dim3(st::kKvThreads), 0, stream, a);
         return ST_OK;
     });
     if (rc != ST_OK) return rc;
-    if (!one) {
-        if (blocks > 1024 && (rc = allow_lds(&st::kv_choose_kernel, lds))) return rc;
+    if (!p.one) {
+        if (p.keys == 0 && (rc = allow_lds(&st::kv_choose_kernel, lds))) return rc;
         TimedLaunch t(1, stream);
         const dim3 waves((unsigned)((rows + 3) / 4));
-        if (blocks <= 256) hipLaunchKernelGGL(st::kv_choose_wave_kernel<4>, waves, dim3(st::kKvThreads), 0, stream, a);
-        else if (blocks <= 512) hipLaunchKernelGGL(st::kv_choose_wave_kernel<8>, waves, dim3(st::kKvThreads), 0, stream, a);
-        else if (blocks <= 1024) hipLaunchKernelGGL(st::kv_choose_wave_kernel<16>, waves, dim3(st::kKvThreads), 0, stream, a);
+        if (p.keys == 4) hipLaunchKernelGGL(st::kv_choose_wave_kernel<4>, waves, dim3(st::kKvThreads), 0, stream, a);
+        else if (p.keys == 8) hipLaunchKernelGGL(st::kv_choose_wave_kernel<8>, waves, dim3(st::kKvThreads), 0, stream, a);
+        else if (p.keys == 16) hipLaunchKernelGGL(st::kv_choose_wave_kernel<16>, waves, dim3(st::kKvThreads), 0, stream, a);
         else hipLaunchKernelGGL(st::kv_choose_kernel, dim3((unsigned)rows), dim3(st::kKvThreads), lds, stream, a);
     }
     ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int st_kv_host_plan(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads, int32_t n_sel, int32_t with_mass,
+                    int32_t* host_out_plan)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if (!host_out_plan) return fail(ST_EINVAL, "null argument");
+    if ((rc = check_cache(cache, false, false)) || (rc = check_batch(batch)) || (rc = check_heads(cache, n_q_heads))) return rc;
+    if (n_sel < 0 || n_sel > ST_KV_MAX_BLOCKS) return fail(ST_EINVAL, "n_sel=%d out of range", n_sel);
+    const AttendPlan a = attend_plan(cache, batch, n_q_heads, n_sel, with_mass != 0);
+    const SelectPlan s = select_plan(cache, batch);
+    const int32_t plan[10] = {a.many ? 0 : a.waves, a.tiles, a.chunk, a.splits, a.join_waves, a.sum_lanes, s.one, s.chunks, s.rounds, s.keys};
+    std::copy(plan, plan + 10, host_out_plan);
     return ST_OK;
     });
 }
