@@ -370,7 +370,8 @@ typedef struct st_kv_batch {
     int32_t n_seq;
     int32_t max_blocks;          /* 1 .. ST_KV_MAX_BLOCKS */
     int32_t n_tok;
-    int32_t max_tok;             /* no sequence has more tokens in this call (n_tok / n_seq where dev_offsets is NULL) */
+    int32_t max_tok;             /* no sequence has more tokens in this call (n_tok / n_seq where dev_offsets is NULL); work and workspaces
+                                  * are laid out for n_seq times this many, so that it is best as small as it can be */
     int32_t max_len;             /* no length is larger; at most 64 * max_blocks */
 } st_kv_batch;
 
@@ -407,8 +408,10 @@ int st_kv_read(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_blo
  *              decay * dev_mass_in + the sum of p over its positions and the call's rows of that sequence and head
  *              (dev_mass_in NULL: 0; may be dev_mass_out itself); 0 behind the sequence's last block
  *   workspace  st_kv_attend_workspace_bytes() bytes, 256-byte aligned, scratch
- * Sums, maxima and outputs are accumulated in fp32; the weights are rounded to 11 significant bits before they multiply the values.
- * softmax_scale and decay are finite.  Asynchronous, no allocation; results do not vary from call to call. */
+ * Sums, maxima and outputs are accumulated in fp32.  The weights are rounded before they multiply the values, and outputs are divided by
+ * the sum of the rounded ones: 11 significant bits from a row's largest weight down to 2^-20 of it, lighter ones to within 2^-31 of
+ * the largest.  Logits, queries and value scales may have any size that is finite in fp32 (a value scale below 2^-80 of the largest
+ * that the row sees may count as that).  softmax_scale and decay are finite.  Asynchronous, no allocation; results do not vary from call to call. */
 int64_t st_kv_attend_workspace_bytes(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads,
                                      int32_t n_sel, int32_t with_mass);
 int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_q, int64_t q_stride,
@@ -448,6 +451,7 @@ int st_kv_host_plan(const st_kv_cache* cache, const st_kv_batch* batch, int32_t 
  *   dev_out_tables [n_seq, max_blocks] (-1 behind), dev_out_lengths [n_seq] (64 less for each block that goes),
  *   dev_out_mass [n_seq, n_heads, max_blocks] (0 behind), dev_out_freed [n_seq, max_blocks]: the pages that go, in order (-1
  *   behind), dev_out_n_freed [n_seq]
+ * The positions behind a block that goes move up by 64: masks over positions made before are not valid after.
  * Tables, lengths and mass may be updated in place (out = in).  One kernel, asynchronous, no allocation. */
 int st_kv_evict(const st_kv_batch* batch, const float* dev_mass, int32_t n_heads, int32_t budget, int32_t sink,
                 int32_t recent, int32_t* dev_out_tables, int32_t* dev_out_lengths, float* dev_out_mass,

@@ -623,7 +623,8 @@ class KvCache:
 class KvBatch:
     """The sequences of a call (``st_kv_batch``): tables int32 [n_seq, max_blocks], lengths int32 [n_seq] (the call's
     tokens included), n_tok tokens in all; offsets int32 [n_seq + 1] where sequences have different numbers of them, with
-    max_tok a bound on one sequence's (n_tok if not given).  max_len bounds the lengths (64 * max_blocks if not given)."""
+    max_tok a bound on one sequence's (n_tok if not given: a call of many sequences then takes work and workspace for n_seq * n_tok
+    tokens, so give it where the counts are known).  max_len bounds the lengths (64 * max_blocks if not given)."""
 
     def __init__(self, tables, lengths, n_tok: int, offsets=None, max_tok: int | None = None, max_len: int | None = None):
         _need(tables, torch.int32, "tables")

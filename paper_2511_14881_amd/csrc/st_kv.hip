@@ -76,7 +76,7 @@ int check_mask(const uint64_t* mask, int32_t words, const st_kv_batch* b)
 
 int check_grid(int64_t groups)  // (a launch has fewer than 2^32 threads)
 {
-    return groups <= 0xFFFFFFll ? (int)ST_OK : fail(ST_EINVAL, "too many rows for one call (%lld workgroups)", (long long)groups);
+    return groups <= 0xFFFFFFll ? (int)ST_OK : fail(ST_EINVAL, "too many rows for one call: %lld workgroups of at most 16777215 (they go by n_seq times max_tok)", (long long)groups);
 }
 
 st::KvCacheView view(const st_kv_cache* c)
@@ -111,17 +111,25 @@ int with_dim(int32_t d, F&& body)
 constexpr int64_t kLittle = 512;  // blocks of all sequences and heads
 constexpr int few_rows(int d, int64_t blocks) { return blocks <= kLittle ? 256 : d > 128 ? 96 : d > 96 ? 64 : 128; }
 constexpr int row_waves(int d) { return d > 128 ? 4 : 8; }  // of the kernel for many rows (256: 512 registers to a lane)
-constexpr int kManyRows = 2048;   // tiles that fill the chip with a wavefront each
+// Tiles of 16 rows from which on a wavefront takes a tile by itself.  Calls in us, a wavefront to a tile against four: 8 selected blocks,
+// 1600 tiles 41 against 43, 3200 67 against 72, 6400 102 against 109; 11 blocks, 2048 tiles 55 against 57.  Longer lists do not
+// gain: 2048 tiles of up to 32 blocks 134 against 130, 4096 of them 271 against 245, 1536 of up to 70 blocks 153 against 130.
+constexpr int kManyRows = 2048;
 // Blocks of a split, at least: one for each wavefront that takes blocks by itself, two where the workgroup takes them together.
 // 1500 tokens, 4 heads: 16 rows, d = 128, 13.2 us against 15.8 with splits of 16 blocks; d = 256, 15.2 against 23.6; 256 rows,
 // d = 128, 23.0 against 45.5.  A list of up to whole_list blocks is not split, joining would take longer: 700 tokens, 16 rows,
 // d = 128, 11.2 us against 13.2.
 constexpr int least_chunk(bool many) { return many ? 2 : 4; }
 constexpr int whole_list(int d) { return d > 128 ? 8 : 16; }
-// Many rows: a block takes about this long in microseconds; joining splits this long, and the partial outputs' way out and in.
+// Many rows: a block takes about this long in microseconds; joining splits this long, and the partial outputs' way out and in.  A list is
+// not split where that takes longer (4 heads, 600 rows, calls in us): 8 histories of 300 tokens whole 21.5, split 32.0; 4 of 700 tokens split
+// 30.8, whole 33.8; of 1500 tokens 33.5 and 54.9 (d = 64 27 and 38, d = 256, 400 rows, 46 and 105), of 3000 42 and 96.
 constexpr double rows_block_us(int d) { return d > 128 ? 3.0 : 1.7; }
 constexpr double kRowsJoinUs = 3.0, kRowsJoinBytes = 5e6;  // of a microsecond
-constexpr double kSplitStart = 4.0, kSplitJoin = 6.0;  // start of a workgroup, and joining splits, in blocks
+// Start of a workgroup, and joining splits, in blocks: what decides where the last round of workgroups is to be filled.  Calls in us with
+// these, with (0, 0) and with (12, 18): 64 selected blocks for 24 x 8 sequences and heads 61, 62, 62; 48 for 40 x 8 78, 82, 81; 32 for 175 x 4
+// 100, 112, 93; 1500 tokens over one history of 4000, 8 heads 94, 103, 87; 800 over 8000, 4 heads 87, 85, 86.
+constexpr double kSplitStart = 4.0, kSplitJoin = 6.0;
 constexpr int kDies = 8;  // of the chip, each with an L2 of its own
 
 struct AttendPlan {
@@ -152,7 +160,9 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     p.waves = pairs >= kManyRows ? 1 : 4;
     // Workgroups that the chip holds at a time (registers and LDS), and splits of a row's blocks: one round of workgroups where
     // there are few rows (as long as a split has work for its wavefronts), two where sequences of different lengths
-    // would leave a single round to the longest, and for a lone sequence what wastes least of its last round.
+    // would leave a single round to the longest, and for a lone sequence what wastes least of its last round.  (Calls in us with 4, 3 and
+    // 2 workgroups to a compute unit for d = 64, 96 and more, with 2 for all and with 4: d = 64, 40 x 8192 tokens, 8 heads 51, 55, 51; d = 96 72, 79,
+    // 75; d = 128, 64 x 8192 149, 149, 159; d = 256, 24 x 6000 87, 87, 91.)
     const int64_t slots = (int64_t)st::kComputeUnits * (p.many ? 1 : c->d <= 64 ? 4 : c->d <= 96 ? 3 : 2);
     int64_t splits = 1;
     if (p.waves == 1 && !p.many) splits = 1;
@@ -183,6 +193,7 @@ AttendPlan attend_plan(const st_kv_cache* c, const st_kv_batch* b, int32_t n_q_h
     const int64_t keys = sh * p.splits;
     p.dies = per > 1 && (keys % kDies == 0 || keys >= 8 * kDies) ? kDies : 1;
     p.grid = st::round_up(keys, p.dies) * per;
+    // (calls of one history in us, a wavefront to a row against four: 8 splits 11.9 against 12.2, 16 12.4 and 12.5, 32 13.2 and 12.4, 63 15.6 and 13.5)
     p.join_waves = p.splits >= 16 ? 4 : p.splits > 1 ? 1 : 0;
     // (one workgroup to each sequence and head writes the weights itself, unless there are no tokens)
     const bool whole_pairs = n_sel == 0 && !p.many && p.tiles == 1 && p.splits == 1 && !b->dev_offsets && b->max_tok > 0;
@@ -233,7 +244,9 @@ SelectPlan select_plan(const st_kv_cache* c, const st_kv_batch* b)
     const int64_t pairs = (int64_t)b->n_seq * c->n_heads;
     SelectPlan p = {false, 1, 1, blocks <= 256 ? 4 : blocks <= 512 ? 8 : blocks <= 1024 ? 16 : 0, 0};
     // One token to a sequence: the workgroup that scores also chooses, as long as its blocks are few enough to be read by one
-    // (or there are as many sequences and heads as compute units anyway).
+    // (or there are as many sequences and heads as compute units anyway).  Selection and attention in us, one kernel against two: 8 sequences and
+    // heads of 512 blocks 22.6 against 24.5, of 1024 25.0 and 24.8, of 1500 31.2 and 27.2; 32 of 2500 45 and 35; 256 of 100 blocks 23.6 and
+    // 27.1, of 1500 27.7 and 35.1.
     p.one = b->max_tok == 1 && (blocks <= 1024 || pairs >= st::kComputeUnits);
     if (!p.one) {
         // rounds of 256 blocks to a workgroup: as many as still leave two workgroups to a compute unit
@@ -409,6 +422,7 @@ int st_kv_select(const st_kv_cache* cache, const st_kv_batch* batch, const void*
     rc = with_dim(cache->d, [&](auto d) -> int {
         constexpr int D = decltype(d)::value;
         int rc2;
+        // (256 threads for 8 x 1024 blocks 28.2 us against 25.0, 256 x 1500 34.1 against 27.7; 1024 threads 25.1 and 27.4)
         constexpr int kOneThreads = 512;
         if (p.one && (rc2 = allow_lds(&st::kv_score_kernel<D, true, kOneThreads>, lds))) return rc2;
         TimedLaunch t(0, stream);

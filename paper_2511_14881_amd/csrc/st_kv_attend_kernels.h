@@ -149,9 +149,10 @@ __device__ inline KvTile kv_tile(const KvAttendArgs& a, int seq, int unit, int r
 
 // kWaves wavefronts share the blocks of 16 rows and join what they found in the LDS (one: nothing to join, for calls that
 // fill the chip with rows alone).  Bound by HBM where rows are few: 64 histories of 2144 to 8192 tokens, 8 heads of 128 with 4 query
-// heads each: 143 us, 4.8 TB/s (5.65 with histories of one length; a plain pass over memory reads 6.3), two of 262144 and 163840 tokens 85
+// heads each: 143 us, 4.8 TB/s (5.4 with histories of one length; a plain pass over memory reads 6.3), two of 262144 and 163840 tokens 86
 // us, 5.1 TB/s.  With a tile to every few tokens it is bound by turning integers into floats, once to a tile.  Selected blocks: 16
-// tokens, 8 heads, 64 blocks each, 25 us, 5.4 TB/s; 800 tokens, 4 heads, 8 blocks each, 46 us, 9 TB/s out of the L2.
+// tokens, 8 heads, 64 blocks each, 25 us, 5.4 TB/s; 800 tokens, 4 heads, 8 blocks each, 45 us, 410 MB out of the L2 (9 TB/s),
+// 93 MB behind it.
 template <int D, bool kSelected, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void kv_attend_kernel(KvAttendArgs a)
 {

@@ -10,7 +10,7 @@
 //
 // 500 candidates to each of 16 histories of 1216 to 4096 tokens, 2 query heads to each of 4 heads of 128: 132 us, 660 TFLOP/s;
 // with histories of one length 843 (a large product of matrices in 16 bits reaches 1390), since one round of workgroups lasts
-// as long as the longest history.  2047 tokens over 15001, 5 query heads to each of 3 heads of 96, under a mask: 264 us and 19 to
+// as long as the longest history.  2047 tokens over 15001, 5 query heads to each of 3 heads of 96, under a mask: 274 us and 19 to
 // join.  With one part left out, 138 us (on another card) become 131 (exponentials), 120 (stores to the LDS), 127 (loads), 106 or 104 (either product):
 // the parts hide behind each other about as far as two wavefronts of a SIMD let them.  256 rows to a workgroup of 8 wavefronts
 // rather than 128 to one of 4: 132 against 152; two tiles of 32 rows to a wavefront, 4 wavefronts: 219; products and weights
