@@ -411,7 +411,7 @@ int st_kv_read(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_blo
  * Sums, maxima and outputs are accumulated in fp32.  The weights are rounded before they multiply the values, and outputs are divided by
  * the sum of the rounded ones: 11 significant bits from a row's largest weight down to 2^-20 of it, lighter ones to within 2^-31 of
  * the largest.  Logits, queries and value scales may have any size that is finite in fp32 (a value scale below 2^-80 of the largest
- * that the row sees may count as that).  softmax_scale and decay are finite.  Asynchronous, no allocation; results do not vary from call to call. */
+ * among the blocks that a row and its neighbours see may count as that or as 0).  softmax_scale and decay are finite.  Asynchronous, no allocation; results do not vary from call to call. */
 int64_t st_kv_attend_workspace_bytes(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads,
                                      int32_t n_sel, int32_t with_mass);
 int st_kv_attend(const st_kv_cache* cache, const st_kv_batch* batch, const void* dev_q, int64_t q_stride,

@@ -33,7 +33,7 @@ struct KvAttendArgs {
     uint32_t pairs;      // of sequences and heads
     int32_t rows_pad;    // rows of a unit and head in the workspace
     float* part_o;       // [unit, head, split, rows_pad, d]
-    float4* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of rounded weights, sum of weights
+    float4* part_ml;     // [unit, head, split, rows_pad]: maximum, sum of rounded weights, sum of weights, what part_o is in units of
     float2* block_ml;    // [unit, head, entries, rows_pad]: maximum so far, sum of the block's weights; or null
     int64_t entries;     // blocks, or selected ones
     float2* row_ml;      // [unit, head, rows_pad]: final maximum and sum, written where block_ml is
@@ -49,13 +49,17 @@ __device__ inline float kv_weight(float2 block, float2 row)
 // Whether the workgroup that has all rows and blocks of a sequence and head writes its blocks' weights too.
 __device__ inline bool kv_whole(const KvAttendArgs& a, int n_list) { return a.tiles == 1 && a.tile_rows == 16 && n_list <= a.chunk; }
 
+// Few rows: outputs are sums of up to 2^20 values times 2^15, so that a wavefront that meets value scales above the first of these keeps
+// them in units of the second from there on.
+constexpr float kKvLarge = 0x1p40f, kKvUnit = 0x1p64f;
+
 constexpr float kKvLift = 8.0f;   // weights are 2^8 times themselves,
 constexpr float kKvSlack = 7.0f;  // and the maximum they go by may lie 7 (in powers of two) below the largest logit
 
 // Maxima of this size and more: x * ks - m in one rounding can be above what the rounded products' distance to m allows, by half
 // the spacing of numbers near m, and pass a 16-bit float's range.  Such rows subtract m from the rounded products, which is exact
-// near the largest ones.  (In the branch that moves the maximum; the tests for it: 131.3 us against 130.7 for 500 candidates to each of
-// 16 histories, 294 against 292 for 2047 tokens under a mask.)
+// near the largest ones.  (What looking for them costs: 131.3 us against 130.7 for 500 candidates to each of 16 histories, 294
+// against 292 for 2047 tokens under a mask, nothing for single tokens.)
 __device__ inline bool kv_far(float m) { return fabsf(m) >= 0x1p18f && m != -__builtin_inff(); }
 
 // A query row goes into the product times *up, a power of two that brings its largest magnitude near 2^14, with the sign
@@ -222,7 +226,8 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
     }
 
     float m = -__builtin_inff(), l = 0.0f, l_exact = 0.0f;
-    uint64_t far = 0;  // rows of large logits (kv_far)
+    uint64_t far = 0;    // rows of large logits (kv_far)
+    float o_unit = 1.0f;
     float4v o[kCh];
 #pragma unroll
     for (int c = 0; c < kCh; ++c) o[c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
@@ -245,9 +250,16 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
         if (a.block_ml && j < je && page < 0)
             for (int r = 0; r < 16; ++r) a.block_ml[(uh * a.entries + j) * a.rows_pad + row0 + r] = make_float2(0.0f, 0.0f);
         const int64_t ph_l = (int64_t)max(page, 0) * a.c.n_heads + head;
-        const float ks_l = page >= 0 ? a.c.k_scale[ph_l] : 0.0f, vs_l = page >= 0 ? a.c.v_scale[ph_l] : 0.0f;
+        const float ks_l = page >= 0 ? a.c.k_scale[ph_l] : 0.0f;
+        float vs_l = page >= 0 ? a.c.v_scale[ph_l] : 0.0f;
         uint64_t todo = ballot(page >= 0);
         if (todo == 0) continue;
+        if (o_unit == 1.0f && ballot(vs_l > kKvLarge) != 0) {
+            o_unit = kKvUnit;
+#pragma unroll
+            for (int c = 0; c < kCh; ++c) o[c] *= 1.0f / kKvUnit;
+        }
+        vs_l *= 1.0f / o_unit;
         int it = __builtin_ctzll(todo);
         const uint32_t key_at = n * D + g * 16, val_at = n * kKvBlock + g * 16;
         uint4 kw[4][kWide ? kWide : 1];
@@ -383,16 +395,19 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
     l_exact = sum_over_16_32(l_exact);
 
     // the wavefronts' states into one
-    if (g == 0) s_ml[w][n] = make_float4(m, l, l_exact, 0.0f);
+    if (g == 0) s_ml[w][n] = make_float4(m, l, l_exact, o_unit);
 #pragma unroll
     for (int c = 0; c < kCh; ++c) *(float4v*)&s_o[w][n][c * 16 + g * 4] = o[c];
     __syncthreads();
     const int64_t part = (uh * a.splits + split) * a.rows_pad + row0;
     for (int i = threadIdx.x; i < 16 * (D / 4); i += kWaves * 64) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
-        float top = -__builtin_inff();
+        float top = -__builtin_inff(), y_unit = 1.0f;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[k][r].x);
+        for (int k = 0; k < kWaves; ++k) {
+            top = fmaxf(top, s_ml[k][r].x);
+            y_unit = fmaxf(y_unit, s_ml[k][r].w);
+        }
         float sum = 0.0f, exact = 0.0f;
         float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -400,15 +415,16 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
             const float4 ml = s_ml[k][r];
             const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
             const float4v v = *(const float4v*)&s_o[k][r][c];
+            const float fv = ml.w == y_unit ? f : f * (1.0f / kKvUnit);
             sum += ml.y * f;
             exact += ml.z * f;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) y[u] += v[u] * f;
+            for (int u = 0; u < 4; ++u) y[u] += v[u] * fv;
         }
         if (row0 + r >= t.rows) continue;
         if (t.n_list > a.chunk) {
             *(float4v*)(a.part_o + (part + r) * D + c) = y;
-            if (c == 0) a.part_ml[part + r] = make_float4(top, sum, exact, 0.0f);
+            if (c == 0) a.part_ml[part + r] = make_float4(top, sum, exact, y_unit);
             continue;
         }
         const KvRow to = kv_row(row0 + r, t.tok_unit, head, a.group);
@@ -416,7 +432,7 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 1 && D <= 128 ? 3 : 2) void 
         const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
         uint32_t h[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) h[u] = to_16_bits(y[u] * inv, bf16);
+        for (int u = 0; u < 4; ++u) h[u] = to_16_bits(y[u] * inv * y_unit, bf16);
         *(uint2*)((uint16_t*)a.out + place * D + c) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
         if (c == 0) {
             if (a.lse) a.lse[place] = exact == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(exact)) * 0.69314718056f;
@@ -447,7 +463,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     constexpr int kLanes = D / 4, kTeam = kWaves * 64, kParts = kTeam / kLanes;  // (D = 96: 24 lanes, 16 of 256 idle)
     constexpr int kRows = kKvThreads / kTeam;
     __shared__ float4v s_y[kRows][kParts][kLanes];
-    __shared__ float s_top[kRows][kWaves];
+    __shared__ float2 s_top[kRows][kWaves];
     __shared__ float2 s_sum[kRows][kParts];
     const int team = threadIdx.x / kTeam, me = threadIdx.x % kTeam, lane = me & 63;
     const int64_t heads_all = (int64_t)a.c.n_heads * a.group;
@@ -464,13 +480,23 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     mine = mine && t.n_list > a.chunk;  // (a row in one split has its output already)
     const int splits = mine ? (t.n_list + a.chunk - 1) / a.chunk : 0;
     const int64_t part = uh * a.splits * stride + row;
-    float top = -__builtin_inff();
-    for (int i = me; i < splits; i += kTeam) top = fmaxf(top, a.part_ml[part + i * stride].x);
-    for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-    if (lane == 0) s_top[team][me >> 6] = top;
+    float top = -__builtin_inff(), y_unit = 0.0f;  // the largest maximum, and the largest unit of the parts' outputs
+    for (int i = me; i < splits; i += kTeam) {
+        const float4 ml = a.part_ml[part + i * stride];
+        top = fmaxf(top, ml.x);
+        y_unit = fmaxf(y_unit, ml.w);
+    }
+    for (int k = 32; k > 0; k >>= 1) {
+        top = fmaxf(top, __shfl_xor(top, k));
+        y_unit = fmaxf(y_unit, __shfl_xor(y_unit, k));
+    }
+    if (lane == 0) s_top[team][me >> 6] = make_float2(top, y_unit);
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_top[team][k]);
+    for (int k = 0; k < kWaves; ++k) {
+        top = fmaxf(top, s_top[team][k].x);
+        y_unit = fmaxf(y_unit, s_top[team][k].y);
+    }
     const int c = me % kLanes, from = me / kLanes;
     float sum = 0.0f, exact = 0.0f;
     float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -480,10 +506,11 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
             const float4 ml = a.part_ml[part + i * stride];
             const float4v v = *(const float4v*)(a.part_o + (part + i * stride) * D + c * 4);
             const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
+            const float fv = ml.w == y_unit ? f : f * (ml.w / y_unit);
             sum = __builtin_fmaf(ml.y, f, sum);
             exact = __builtin_fmaf(ml.z, f, exact);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) y[u] = __builtin_fmaf(v[u], f, y[u]);
+            for (int u = 0; u < 4; ++u) y[u] = __builtin_fmaf(v[u], fv, y[u]);
         }
         s_y[team][from][c] = y;
         if (c == 0) s_sum[team][from] = make_float2(sum, exact);
@@ -501,7 +528,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     uint32_t h[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) h[u] = to_16_bits(y[u] * inv, a.bf16 != 0);
+    for (int u = 0; u < 4; ++u) h[u] = to_16_bits(y[u] * inv * y_unit, a.bf16 != 0);
     *(uint2*)((uint16_t*)a.out + place * D + c * 4) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
     if (c == 0) {
         if (a.lse) a.lse[place] = exact == 0.0f ? -__builtin_inff() : (top - kKvLift + log2f(exact)) * 0.69314718056f;

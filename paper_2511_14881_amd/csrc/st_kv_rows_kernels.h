@@ -310,22 +310,22 @@ __global__ __launch_bounds__(kWaves * 64, D > 128 ? 1 : 2) void kv_attend_rows_k
             for (int i = 0; i < 4; ++i) {
                 float4v y;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) y[u] = o[c][4 * i + u] * v_unit;
+                for (int u = 0; u < 4; ++u) y[u] = o[c][4 * i + u];
                 *(float4v*)(a.part_o + part * D + c * 32 + i * 8 + h * 4) = y;
             }
-        if (h == 0) a.part_ml[part] = make_float4(m, sum, exact, 0.0f);
+        if (h == 0) a.part_ml[part] = make_float4(m, sum, exact, v_unit);
         return;
     }
     const KvRow to = kv_row(row, t.tok_unit, head, a.group);  // (kept through the walk it would cost registers: 140 us against 133)
     const int64_t place = to.tok * heads_all + to.q_head;
-    const float inv = sum > 0.0f || sum != sum ? v_unit / sum : 0.0f;
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
     for (int c = 0; c < kCh; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t r[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) r[u] = to_16_bits(o[c][4 * i + u] * inv, bf16);
+            for (int u = 0; u < 4; ++u) r[u] = to_16_bits(o[c][4 * i + u] * inv * v_unit, bf16);
             *(uint2*)((uint16_t*)a.out + place * D + c * 32 + i * 8 + h * 4) = make_uint2(r[0] | r[1] << 16, r[2] | r[3] << 16);
         }
     if (kExact && h == 0) {
