@@ -486,10 +486,12 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
         top = fmaxf(top, ml.x);
         y_unit = fmaxf(y_unit, ml.w);
     }
-    for (int k = 32; k > 0; k >>= 1) {
+    for (int k = 8; k > 0; k >>= 1) {
         top = fmaxf(top, __shfl_xor(top, k));
         y_unit = fmaxf(y_unit, __shfl_xor(y_unit, k));
     }
+    top = max_over_16_32(top);
+    y_unit = max_over_16_32(y_unit);
     if (lane == 0) s_top[team][me >> 6] = make_float2(top, y_unit);
     __syncthreads();
 #pragma unroll
@@ -497,6 +499,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
         top = fmaxf(top, s_top[team][k].x);
         y_unit = fmaxf(y_unit, s_top[team][k].y);
     }
+    const float up = y_unit < 0x1p-64f ? 0x1p64f : 1.0f, per_unit = y_unit > 0.0f ? 1.0f / (y_unit * up) : 0.0f;  // (for denormals)
     const int c = me % kLanes, from = me / kLanes;
     float sum = 0.0f, exact = 0.0f;
     float4v y = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -506,7 +509,7 @@ __global__ __launch_bounds__(kKvThreads) void kv_join_kernel(KvAttendArgs a)
             const float4 ml = a.part_ml[part + i * stride];
             const float4v v = *(const float4v*)(a.part_o + (part + i * stride) * D + c * 4);
             const float f = ml.y > 0.0f || ml.y != ml.y ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
-            const float fv = ml.w == y_unit ? f : f * (ml.w / y_unit);
+            const float fv = f * (ml.w * up * per_unit);
             sum = __builtin_fmaf(ml.y, f, sum);
             exact = __builtin_fmaf(ml.z, f, exact);
 #pragma unroll
