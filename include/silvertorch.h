@@ -344,7 +344,7 @@ int st_value_model(const float* dev_task_scores, int64_t n, int32_t n_tasks,
 #define ST_KV_MAX_BLOCKS 16384  /* blocks of one sequence: 1,048,576 tokens */
 #define ST_KV_MAX_HEADS 1024
 
-typedef enum st_dtype { ST_BF16 = 0, ST_F16 = 1 } st_dtype;
+typedef enum st_dtype { ST_BF16 = 0, ST_F16 = 1, ST_F32 = 2 /* st_norm_rows alone */ } st_dtype;
 
 typedef struct st_kv_cache {
     int8_t* dev_k;
@@ -456,6 +456,88 @@ int st_kv_host_plan(const st_kv_cache* cache, const st_kv_batch* batch, int32_t 
 int st_kv_evict(const st_kv_batch* batch, const float* dev_mass, int32_t n_heads, int32_t budget, int32_t sink,
                 int32_t recent, int32_t* dev_out_tables, int32_t* dev_out_lengths, float* dev_out_mass,
                 int32_t* dev_out_freed, int32_t* dev_out_n_freed, void* hip_stream);
+
+/* Copies pages: page dev_dst[i] of `to` becomes what page dev_src[i] of `from` is (keys, values, scales, bounds), i < n.  Both
+ * caches have the same heads and d and may be one cache.  Page numbers are read on the device and not trusted: a pair
+ * with a number out of its cache is left out.  No page may be written twice by a call, nor be written and read by it: what such a page
+ * holds afterwards is any mix of the rows copied (HistoryStore makes lists without such pages).  One kernel, asynchronous, no allocation. */
+int st_kv_copy(const st_kv_cache* from, const st_kv_cache* to, const int32_t* dev_src, const int32_t* dev_dst, int32_t n,
+               void* hip_stream);
+
+/* ------------------------------------------------------------------ a layer around the cached histories
+ * What stands between an event's embedding and the calls on cached histories, and between those and the search: the norm
+ * that turns rows into int8 with a scale each (the layout of the search's queries), the projection of such rows by
+ * shared int8 weights with a low-rank adapter for each row's tenant, and rotary positions.  Serving only. */
+
+/* Norm of rows, with the residual's addition before it and int8 rows behind it.  For each row, w = 1 without dev_weight:
+ *   h     = x + residual, rounded to dtype (x itself without a residual)
+ *   t     = h * w                                    one fp32 rounding
+ *   u     = max |t| / 127                            one fp32 rounding
+ *   q     = rint(t / u) kept in [-127, 127]          ties to even, the quotient rounded to fp32; 0 where u is 0
+ *   rms   = 1 / sqrt(mean of h * h + eps)            1 where normalise is 0
+ *   scale = u * rms,  y = t * rms rounded to dtype
+ * The integers do not contain the mean, so that they are bit-exact whatever order its sum has.  Rows with squares beyond fp32's
+ * range are formed with h / 2^70 throughout.  A row in which an h or a t is infinite or no number gives q = 0, scale = NaN, y = NaN.
+ *   dev_x, dev_residual  rows of d values of dtype (ST_BF16, ST_F16, ST_F32), strides in elements: multiples of 8, at least d
+ *   dev_weight           [d] of dtype, or NULL
+ *   dev_out_sum          h, rows sum_stride apart, or NULL; may be dev_x or dev_residual with the same stride
+ *   dev_out_q, dev_out_scale  [n_rows, d] int8 and [n_rows] fp32, both or neither
+ *   dev_out_y            [n_rows, d] of dtype, or NULL;  of dev_out_sum, dev_out_q and dev_out_y one at least is given
+ * d is a multiple of 16, at most ST_MAX_ROW; 0 <= n_rows < 2^31; 1e-12 <= eps <= 1 where normalise is not 0.  Rows 16-byte aligned.
+ * Outputs lie apart from each other and, but for dev_out_sum, from the inputs.  One kernel, asynchronous, no allocation. */
+#define ST_MAX_ROW 16384
+int st_norm_rows(const void* dev_x, int64_t x_stride, const void* dev_residual, int64_t residual_stride,
+                 const void* dev_weight, int32_t dtype, int64_t n_rows, int32_t d, int32_t normalise, float eps,
+                 void* dev_out_sum, int64_t sum_stride, int8_t* dev_out_q, float* dev_out_scale, void* dev_out_y,
+                 void* hip_stream);
+
+/* Low-rank adapters beside a projection from k to n values: for adapter i rows dev_a[i] [rank, k], dev_b[i] [n, rank] of the
+ * output's dtype, finite, and a factor.  rank is a multiple of 8, 8 .. ST_MAX_RANK (a smaller one is filled up with zeros). */
+#define ST_MAX_RANK 128
+#define ST_MAX_ADAPTERS 65536
+typedef struct st_adapters {
+    const void* dev_a;       /* [n_adapters, rank, k] */
+    const void* dev_b;       /* [n_adapters, n, rank] */
+    const float* dev_alpha;  /* [n_adapters], finite */
+    int32_t n_adapters;      /* 1 .. ST_MAX_ADAPTERS */
+    int32_t rank;
+} st_adapters;
+
+/* Projection of int8 rows by shared int8 weights, with each row's adapter:
+ *   out[t][c] = dot(x[t], w[c]) * x_scale[t] * w_scale[c]  +  alpha[i] x_scale[t] sum_r b[i][c][r] dot(a[i][r], x[t]),  i = adapter_of[t]
+ *   dev_x [n_rows, k] int8, dev_x_scale [n_rows] fp32: what st_norm_rows writes;  dev_w [n, k] int8, dev_w_scale [n] fp32
+ *   adapters        NULL (no second term; dev_adapter_of is NULL too)
+ *   dev_adapter_of  int32 [n_rows]; a number that no adapter has means none.  Rows may be in any order; equal neighbours share loads
+ *   dev_out         rows of n values of dtype (ST_BF16, ST_F16), out_stride elements apart (a multiple of 8, at least n)
+ *   workspace       st_project_workspace_bytes() bytes, 256-byte aligned, scratch
+ * The first sum is exact (int32).  The inner values of an adapter, dot(a, x), are summed in fp32, divided by the power of two
+ * that leaves the largest of a row's in [1, 2), and rounded to dtype before b multiplies them; all else is fp32, and outputs are rounded once.
+ * k and n are multiples of 16, k at most ST_MAX_ROW, n at most ST_MAX_OUT, n_rows >= 0.  Arrays 16-byte aligned (dev_x_scale, dev_adapter_of 4).
+ * A row's result does not depend on the other rows.  A row whose x_scale is no number gives none.  Asynchronous, no allocation. */
+#define ST_MAX_OUT 65536
+int64_t st_project_workspace_bytes(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters);
+int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, int32_t k, const int8_t* dev_w,
+               const float* dev_w_scale, int32_t n, const st_adapters* adapters, const int32_t* dev_adapter_of,
+               int32_t dtype, void* dev_out, int64_t out_stride, void* dev_workspace, int64_t workspace_bytes,
+               void* hip_stream);
+
+/* Rotary positions on several axes, of the queries and keys of n_tok tokens in one call.  A row of d values begins with
+ * `pairs` rotated pairs, pairs = the sum of host_sections: (i, i + pairs), or (2 i, 2 i + 1) where interleaved is not 0; the
+ * values behind them stay as they are.  Pair i belongs to axis 0 for i < host_sections[0], then to axis 1, and so on:
+ *   angle = position[axis][t] * freq[i] in fp64;   (a, b) -> (a cos - b sin, a sin + b cos), by -angle where inverse is not 0
+ *   dev_q, dev_k    rows [n_tok, n_q_heads, d] and [n_tok, n_k_heads, d] of dtype (ST_BF16, ST_F16), strides in elements
+ *                   (multiples of 8, at least heads * d), 16-byte aligned; either may be NULL with 0 heads
+ *   dev_positions   int32 [n_axes, n_tok]: any, a time in seconds among them
+ *   dev_freqs       fp64 [pairs], radians to a position, |freq| <= 2 pi
+ *   dev_out_q, dev_out_k  rows like dev_q and dev_k; either may be its input with the same stride
+ * d is a multiple of 8, at most 512; pairs a multiple of 8, 8 <= pairs <= d / 2; 1 <= n_axes <= ST_MAX_AXES; sections >= 0.
+ * Angles are reduced in fp64, cos and sin are the hardware's (absolute error 2^-20 at most, well below the outputs' roundings), products
+ * are fp32 and rounded once.  The inverse is also the gradient's way back.  One kernel, asynchronous, no allocation. */
+#define ST_MAX_AXES 8
+int st_rotate(const void* dev_q, int64_t q_stride, int32_t n_q_heads, const void* dev_k, int64_t k_stride, int32_t n_k_heads,
+              int32_t d, int32_t dtype, int32_t n_tok, const int32_t* dev_positions, const double* dev_freqs,
+              const int32_t* host_sections, int32_t n_axes, int32_t interleaved, int32_t inverse, void* dev_out_q,
+              int64_t out_q_stride, void* dev_out_k, int64_t out_k_stride, void* hip_stream);
 
 /* Bandwidth probe for benchmarks: one kernel that reads bytes / 16 16-byte pieces of dev_src
  * (16-byte aligned) with `workgroups` workgroups of 256 threads and writes one uint32 per workgroup

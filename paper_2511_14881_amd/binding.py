@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -25,7 +26,8 @@ EXPORTS = [
     "st_search_expr", "st_search_ivf_workspace_bytes", "st_search_ivf", "st_quantize_global", "st_value_model",
     "st_search_host_plan", "st_search_host_units", "st_stream_read", "st_search_static",
     "st_kv_append", "st_kv_read", "st_kv_attend_workspace_bytes", "st_kv_attend", "st_kv_select_workspace_bytes",
-    "st_kv_select", "st_kv_evict", "st_kv_host_plan",
+    "st_kv_select", "st_kv_evict", "st_kv_host_plan", "st_kv_copy",
+    "st_norm_rows", "st_project_workspace_bytes", "st_project", "st_rotate",
 ]
 
 ST_OP_LEAF, ST_OP_AND, ST_OP_OR, ST_OP_NOT = 0, 1, 2, 3  # operations of a filter program
@@ -122,6 +124,16 @@ def lib() -> C.CDLL:
         L.st_kv_host_plan.argtypes = [p, p, i32, i32, i32, p]
         L.st_kv_evict.restype = C.c_int
         L.st_kv_evict.argtypes = [p, p, i32, i32, i32, i32, p, p, p, p, p, p]
+        L.st_kv_copy.restype = C.c_int
+        L.st_kv_copy.argtypes = [p, p, p, p, i32, p]
+        L.st_norm_rows.restype = C.c_int
+        L.st_norm_rows.argtypes = [p, i64, p, i64, p, i32, i64, i32, i32, C.c_float, p, i64, p, p, p, p]
+        L.st_project_workspace_bytes.restype = i64
+        L.st_project_workspace_bytes.argtypes = [i32, i32, i32, p]
+        L.st_project.restype = C.c_int
+        L.st_project.argtypes = [p, p, i32, i32, p, p, i32, p, p, i32, p, i64, p, i64, p]
+        L.st_rotate.restype = C.c_int
+        L.st_rotate.argtypes = [p, i64, i32, p, i64, i32, i32, i32, i32, p, p, p, i32, i32, i32, p, i64, p, i64, p]
         _lib = L
     return _lib
 
@@ -156,7 +168,8 @@ def _on(stream, call, *args):
     with torch.cuda.stream(stream):
         got = call(*args)
     for t in got if isinstance(got, tuple) else (got,):
-        t.record_stream(here)
+        if t is not None:
+            t.record_stream(here)
     return got
 
 
@@ -816,3 +829,214 @@ def st_kv_evict(batch: KvBatch, mass, budget: int, sink: int = 0, recent: int = 
     _check(lib().st_kv_evict(batch._p, mass.data_ptr(), mass.shape[1], budget, sink, recent, t.data_ptr(), n.data_ptr(),
                              m.data_ptr(), f.data_ptr(), nf.data_ptr(), _kv_stream(stream)))
     return out
+
+
+def st_kv_copy(from_cache: KvCache, to_cache: KvCache, src, dst, stream=None) -> None:
+    """Page dst[i] of to_cache becomes what page src[i] of from_cache is (int32 tensors of one length; a pair with a number out
+    of its cache is left out).  No page may be written twice, or be written and read by one call."""
+    _need(src, torch.int32, "src")
+    _need(dst, torch.int32, "dst")
+    if src.dim() != 1 or src.shape != dst.shape:
+        raise ValueError("src and dst must be lists of one length")
+    _here(src, dst, from_cache.k, to_cache.k)
+    _check(lib().st_kv_copy(from_cache._p, to_cache._p, src.data_ptr(), dst.data_ptr(), src.numel(), _kv_stream(stream)))
+
+
+# ------------------------------------------------------------------ a layer around the cached histories
+
+ST_F32, ST_MAX_ROW, ST_MAX_RANK, ST_MAX_ADAPTERS, ST_MAX_OUT, ST_MAX_AXES = 2, 16384, 128, 65536, 65536, 8
+_ROW_TYPES = {torch.bfloat16: ST_BF16, torch.float16: ST_F16, torch.float32: ST_F32}
+
+
+def _here(*tensors):
+    """Work runs on the current device's streams: what lies on another device is refused."""
+    device = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{device}")
+
+
+def _layer_rows(t, name: str, dtype=None, shape=None):
+    """Rows [n, d], values of a row side by side; rows may be further apart.  Returns the stride."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _ROW_TYPES and (dtype is None or t.dtype == dtype)):
+        raise TypeError(f"{name} must be a CUDA tensor of {dtype or 'torch.bfloat16, torch.float16 or torch.float32'}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be {'[n, d]' if shape is None else list(shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"the values of a row of {name} must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class NormRows(NamedTuple):
+    """What st_norm_rows returns; None where it was not asked for."""
+    q: torch.Tensor | None
+    scale: torch.Tensor | None
+    total: torch.Tensor | None
+    y: torch.Tensor | None
+
+
+class RowBuffers:
+    """Outputs of repeated st_norm_rows calls of one shape.  total, y: room for the sum with the residual, for the norm's output."""
+
+    def __init__(self, n: int, d: int, dtype, total: bool = False, q: bool = True, y: bool = False, device="cuda"):
+        self.q = torch.empty((n, d), dtype=torch.int8, device=device) if q else None
+        self.scale = torch.empty(n, dtype=torch.float32, device=device) if q else None
+        self.total = torch.empty((n, d), dtype=dtype, device=device) if total else None
+        self.y = torch.empty((n, d), dtype=dtype, device=device) if y else None
+
+
+def st_norm_rows(x, weight=None, residual=None, eps: float = 1e-6, normalise: bool = True, total=None, q: bool = True, y: bool = False,
+                 buffers: RowBuffers | None = None, stream=None) -> NormRows:
+    """RMS norm of the rows x [n, d] (bf16, fp16 or fp32), or of their sum with the residual, as int8 rows with a scale each:
+    the layout of the search's queries and of st_project's rows.  normalise False: the rows are quantised as they are.
+    total: where the sum goes (x or the residual itself is allowed; a new tensor if none is given); y: the norm's output in x's type
+    too; q False: that alone.  What buffers has room for is written there, and no more."""
+    if stream is not None:
+        return _on(stream, st_norm_rows, x, weight, residual, eps, normalise, total, q, y, buffers)
+    x_stride = _layer_rows(x, "x")
+    n, d = x.shape
+    r_stride = t_stride = 0
+    if residual is not None:
+        r_stride = _layer_rows(residual, "residual", x.dtype, (n, d))
+    if weight is not None:
+        _need(weight, x.dtype, "weight")
+        if weight.shape != (d,):
+            raise ValueError(f"weight must be [{d}]")
+    if buffers is None:
+        total = torch.empty((n, d), dtype=x.dtype, device=x.device) if total is None and residual is not None else total
+        out_q, scale, out_y = None, None, torch.empty((n, d), dtype=x.dtype, device=x.device) if y else None
+        if q:
+            out_q, scale = torch.empty((n, d), dtype=torch.int8, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device)
+    else:
+        out_q, scale, out_y = buffers.q, buffers.scale, buffers.y
+        total = buffers.total if total is None else total
+        for t, shape, dtype, name in ((out_q, (n, d), torch.int8, "q"), (scale, (n,), torch.float32, "scale"), (out_y, (n, d), x.dtype, "y")):
+            if t is not None:
+                _kv_out(t, shape, dtype, name)
+    if total is not None:
+        t_stride = _layer_rows(total, "total", x.dtype, (n, d))
+    if out_q is None and out_y is None and total is None:
+        raise ValueError("nothing to write: ask for q, y or total")
+    _here(x, residual, weight, total, out_q, scale, out_y)
+    _check(lib().st_norm_rows(x.data_ptr(), x_stride, _dptr(residual), r_stride, _dptr(weight), _ROW_TYPES[x.dtype], n, d, int(normalise),
+                              eps, _dptr(total), t_stride, _dptr(out_q), _dptr(scale), _dptr(out_y), _kv_stream(None)))
+    return NormRows(out_q, scale, total, out_y)
+
+
+class _AdaptersC(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("alpha", C.c_void_p), ("n_adapters", C.c_int32), ("rank", C.c_int32)]
+
+
+class Adapters:
+    """Low-rank adapters of a projection (``st_adapters``): a [n_adapters, rank, k] and b [n_adapters, n, rank], bf16 or fp16,
+    alpha fp32 [n_adapters]."""
+
+    def __init__(self, a, b, alpha):
+        if not (isinstance(a, torch.Tensor) and a.dtype in _KV_TYPES):
+            raise TypeError("a must be a CUDA tensor of torch.bfloat16 or torch.float16")
+        _need(a, a.dtype, "a")
+        _need(b, a.dtype, "b")
+        _need(alpha, torch.float32, "alpha")
+        if a.dim() != 3 or b.dim() != 3 or alpha.shape != (a.shape[0],) or b.shape[0] != a.shape[0] or b.shape[2] != a.shape[1]:
+            raise ValueError("a must be [n_adapters, rank, k], b [n_adapters, n, rank], alpha [n_adapters]")
+        self.a, self.b, self.alpha = a, b, alpha
+        self.n_adapters, self.rank, self.k = a.shape
+        self.n, self.dtype = b.shape[1], a.dtype
+        self._c = _AdaptersC(a.data_ptr(), b.data_ptr(), alpha.data_ptr(), self.n_adapters, self.rank)
+        self._p = C.cast(C.pointer(self._c), C.c_void_p)
+
+
+class ProjectBuffers:
+    """Output and workspace of repeated st_project calls of one shape."""
+
+    def __init__(self, n_rows: int, k: int, n: int, dtype=torch.bfloat16, adapters: Adapters | None = None, device="cuda"):
+        self.nbytes = st_project_workspace_bytes(n_rows, k, n, adapters)
+        self.out = torch.empty((n_rows, n), dtype=dtype, device=device)
+        self.workspace = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+
+
+def st_project_workspace_bytes(n_rows: int, k: int, n: int, adapters: Adapters | None = None) -> int:
+    return _check(lib().st_project_workspace_bytes(n_rows, k, n, None if adapters is None else adapters._p))
+
+
+def st_project(x, x_scale, w, w_scale, adapters: Adapters | None = None, adapter_of=None, dtype=None, out=None,
+               buffers: ProjectBuffers | None = None, stream=None) -> torch.Tensor:
+    """Rows x int8 [n_rows, k] with scales fp32 [n_rows] through the weights w int8 [n, k] with scales fp32 [n], and through each row's
+    adapter (adapter_of int32 [n_rows]; a number that none has: without).  Returns [n_rows, n] of dtype: the adapters' type,
+    that of out or buffers, or bf16."""
+    if stream is not None:
+        return _on(stream, st_project, x, x_scale, w, w_scale, adapters, adapter_of, dtype, out, buffers)
+    for t, kind, name in ((x, torch.int8, "x"), (x_scale, torch.float32, "x_scale"), (w, torch.int8, "w"), (w_scale, torch.float32, "w_scale")):
+        _need(t, kind, name)
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x_scale.shape != x.shape[:1] or w_scale.shape != w.shape[:1]:
+        raise ValueError("x must be [n_rows, k], w [n, k], with a scale to each row")
+    rows, k = x.shape
+    n = w.shape[0]
+    if (adapters is None) != (adapter_of is None):
+        raise ValueError("adapters and adapter_of go together")
+    if adapters is not None:
+        _need(adapter_of, torch.int32, "adapter_of")
+        if adapter_of.shape != (rows,):
+            raise ValueError(f"adapter_of must be [{rows}]")
+        if adapters.k != k or adapters.n != n:
+            raise ValueError(f"the adapters go from {adapters.k} to {adapters.n} values, the weights from {k} to {n}")
+        _here(adapters.a, adapters.b, adapters.alpha, adapter_of)
+    if buffers is not None:
+        out = buffers.out if out is None else out
+        work, nbytes = buffers.workspace, buffers.nbytes
+    else:
+        nbytes = st_project_workspace_bytes(rows, k, n, adapters)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    if dtype is None:
+        dtype = adapters.dtype if adapters is not None else out.dtype if out is not None else torch.bfloat16
+    if dtype not in _KV_TYPES or (adapters is not None and adapters.dtype != dtype):
+        raise TypeError("the output is torch.bfloat16 or torch.float16, and of the adapters' type")
+    if out is None:
+        out = torch.empty((rows, n), dtype=dtype, device=x.device)
+    stride = _layer_rows(out, "out", dtype, (rows, n))
+    _here(x, x_scale, w, w_scale, out, work)
+    _check(lib().st_project(x.data_ptr(), x_scale.data_ptr(), rows, k, w.data_ptr(), w_scale.data_ptr(), n,
+                            None if adapters is None else adapters._p, _dptr(adapter_of), _KV_TYPES[dtype], out.data_ptr(), stride,
+                            work.data_ptr(), nbytes, _kv_stream(None)))
+    return out
+
+
+def st_rotate(q, k, positions, freqs, sections, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
+    """Rotary positions of queries and keys, rows [n_tok, heads, d] of bf16 or fp16 (one of them may be None): positions int32
+    [n_axes, n_tok], freqs fp64 [pairs], sections: pairs of each axis.  Returns (q, k) rotated, new tensors unless out = (q, k) names
+    what to fill (q and k themselves are allowed)."""
+    if stream is not None:
+        return _on(stream, st_rotate, q, k, positions, freqs, sections, interleaved, inverse, out)
+    some = q if q is not None else k
+    if not isinstance(some, torch.Tensor) or some.dim() != 3:
+        raise ValueError("queries or keys must be given as [n_tok, heads, d]")
+    n_tok, _, d = some.shape
+    _need(positions, torch.int32, "positions")
+    _need(freqs, torch.float64, "freqs")
+    sections = np.ascontiguousarray(np.asarray(sections, dtype=np.int32))
+    if positions.dim() != 2 or positions.shape[1] != n_tok or sections.shape != positions.shape[:1] or freqs.numel() != int(sections.sum()):
+        raise ValueError(f"positions must be [n_axes, {n_tok}], with a section to each axis and a frequency to each pair")
+    out = (None, None) if out is None else out
+    args, outs, dtype = [], [], None
+    for t, o, name in ((q, out[0], "q"), (k, out[1], "k")):
+        if t is None:
+            if o is not None:
+                raise ValueError(f"an output for {name}, which is not given")
+            args.append((None, 0, 0, None, 0))
+            outs.append(None)
+            continue
+        stride, kind = _kv_rows(t, n_tok, d, name)
+        if dtype is not None and kind != dtype:
+            raise TypeError("queries and keys must be of one type")
+        dtype = kind
+        if o is None:
+            o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        if o.dtype != t.dtype or o.shape != t.shape:
+            raise ValueError(f"the output of {name} must be like it")
+        args.append((t.data_ptr(), stride, t.shape[1], o.data_ptr(), _kv_rows(o, n_tok, d, f"output of {name}")[0]))
+        outs.append(o)
+    _here(q, k, positions, freqs, *outs)
+    (qp, qs, qh, oqp, oqs), (kp, ks, kh, okp, oks) = args
+    _check(lib().st_rotate(qp, qs, qh, kp, ks, kh, d, dtype, n_tok, positions.data_ptr(), freqs.data_ptr(), _hptr(sections), len(sections),
+                           int(interleaved), int(inverse), oqp, oqs, okp, oks, _kv_stream(None)))
+    return tuple(outs)

@@ -320,6 +320,31 @@ int st_kv_read(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_blo
     });
 }
 
+int st_kv_copy(const st_kv_cache* from, const st_kv_cache* to, const int32_t* dev_src, const int32_t* dev_dst, int32_t n,
+               void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if ((rc = check_cache(from, true, true)) || (rc = check_cache(to, true, true))) return rc;
+    if (from->n_heads != to->n_heads || from->d != to->d)
+        return fail(ST_EINVAL, "pages of %d heads of %d do not fit a cache of %d heads of %d", from->n_heads, from->d, to->n_heads, to->d);
+    if (n < 0) return fail(ST_EINVAL, "negative size");
+    if (n == 0) return ST_OK;
+    if (!dev_src || !dev_dst) return fail(ST_EINVAL, "null argument");
+    if (((uintptr_t)dev_src & 3) || ((uintptr_t)dev_dst & 3)) return fail(ST_EINVAL, "misaligned list of pages (4 B)");
+    st::KvCopyArgs a = {view(from), view(to), dev_src, dev_dst, 0, from->n_heads * from->d * (ST_KV_BLOCK / 16), from->n_heads * from->d / 8};
+    a.parts = (2 * a.rows16 + a.bounds16 + st::kKvThreads * st::kCopyLoads - 1) / (st::kKvThreads * st::kCopyLoads);
+    const int64_t groups = (int64_t)n * a.parts;
+    if (groups > 0xFFFFFFll) return fail(ST_EINVAL, "too many pages for one call: %lld workgroups of at most 16777215", (long long)groups);
+    {
+        TimedLaunch t(0, (hipStream_t)hip_stream);
+        hipLaunchKernelGGL(st::kv_copy_kernel, dim3((unsigned)groups), dim3(st::kKvThreads), 0, (hipStream_t)hip_stream, a);
+    }
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
 int64_t st_kv_attend_workspace_bytes(const st_kv_cache* cache, const st_kv_batch* batch, int32_t n_q_heads,
                                      int32_t n_sel, int32_t with_mass)
 {

@@ -277,6 +277,44 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvReadArgs a)
     }
 }
 
+// ---------------------------------------------------------------- pages copied
+struct KvCopyArgs {
+    KvCacheView from, to;
+    const int32_t* src;
+    const int32_t* dst;
+    int32_t parts;           // workgroups to a page
+    int32_t rows16, bounds16;  // pieces of 16 bytes of a page's keys (values as many), and of its bounds
+};
+
+constexpr int kCopyLoads = 4;  // 16-byte pieces of a thread
+
+// A page is one run of pieces, keys, values and bounds behind each other; each workgroup takes kKvThreads * kCopyLoads of them.
+__global__ __launch_bounds__(kKvThreads) void kv_copy_kernel(KvCopyArgs a)
+{
+    const int i = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    const int from = kv_page_of(a.from, a.src[i]), to = kv_page_of(a.to, a.dst[i]);
+    if (from < 0 || to < 0) return;
+    const int all = 2 * a.rows16 + a.bounds16;
+    uint4 w[kCopyLoads];
+    const int first = part * (kKvThreads * kCopyLoads) + threadIdx.x;
+    auto place = [&](const KvCacheView& c, int page, int p) -> uint4* {
+        if (p < a.rows16) return (uint4*)c.k + (int64_t)page * a.rows16 + p;
+        if (p < 2 * a.rows16) return (uint4*)c.v + (int64_t)page * a.rows16 + (p - a.rows16);
+        return (uint4*)c.bounds + (int64_t)page * a.bounds16 + (p - 2 * a.rows16);
+    };
+#pragma unroll
+    for (int u = 0; u < kCopyLoads; ++u)
+        if (first + u * kKvThreads < all) w[u] = *place(a.from, from, first + u * kKvThreads);
+#pragma unroll
+    for (int u = 0; u < kCopyLoads; ++u)
+        if (first + u * kKvThreads < all) *place(a.to, to, first + u * kKvThreads) = w[u];
+    if (part == a.parts - 1)
+        for (int h = threadIdx.x; h < a.from.n_heads; h += kKvThreads) {
+            a.to.k_scale[(int64_t)to * a.to.n_heads + h] = a.from.k_scale[(int64_t)from * a.from.n_heads + h];
+            a.to.v_scale[(int64_t)to * a.to.n_heads + h] = a.from.v_scale[(int64_t)from * a.from.n_heads + h];
+        }
+}
+
 // ---------------------------------------------------------------- the best n of an array of keys
 // Marks the `want` largest keys (0: not to be had; equal keys: the lower index first) of keys[0 .. n) by a walk over
 // their four bytes from the top, and hands each marked index to emit(index, rank), rank counting the marked ones in index order.

@@ -1,0 +1,233 @@
+// Entry points of a layer around the cached histories (silvertorch.h): argument checks, launch shapes and launches.
+#include "st_host.h"
+#include "st_layer_kernels.h"
+#include "st_plan.h"
+#include "st_project_kernels.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+using st::fail;
+using st::guarded;
+using st::TimedLaunch;
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+// Rows that a call reads or writes; NULL passes.
+int check_rows(const char* name, const void* p, int64_t stride, int64_t least)
+{
+    if (!p) return ST_OK;
+    if (stride < least || stride % 8 != 0 || misaligned(p))
+        return fail(ST_EINVAL, "%s: rows of %lld elements, %lld apart, have to begin at multiples of 16 bytes", name, (long long)least, (long long)stride);
+    return ST_OK;
+}
+
+int check_grid(int64_t groups)  // (a launch has fewer than 2^32 threads)
+{
+    return groups <= 0x7FFFFFll ? (int)ST_OK : fail(ST_EINVAL, "too many rows for one call: %lld workgroups of at most 8388607", (long long)groups);
+}
+
+template <int kType, int kLanes, int kVectors>
+int launch_norm(const st::NormArgs& a, hipStream_t stream)
+{
+    const int64_t groups = (a.n_rows + st::kLayerThreads / kLanes - 1) / (st::kLayerThreads / kLanes);
+    int rc;
+    if ((rc = check_grid(groups))) return rc;
+    TimedLaunch t(0, stream);
+    hipLaunchKernelGGL((st::norm_rows_kernel<kType, kLanes, kVectors>), dim3((unsigned)groups), dim3(st::kLayerThreads), 0, stream, a);
+    return ST_OK;
+}
+
+// Threads to a row: enough that each holds few vectors, few enough that rows of a few hundred bytes share a wavefront.
+template <int kType>
+int norm_of_type(const st::NormArgs& a, hipStream_t stream)
+{
+    if (a.d <= 128) return launch_norm<kType, 16, 1>(a, stream);
+    if (a.d <= 512) return launch_norm<kType, 64, 1>(a, stream);
+    if (a.d <= 1024) return launch_norm<kType, 64, 2>(a, stream);
+    if (a.d <= 2048) return launch_norm<kType, 64, 4>(a, stream);
+    if (a.d <= 4096) return launch_norm<kType, 256, 2>(a, stream);
+    if (a.d <= 8192) return launch_norm<kType, 256, 4>(a, stream);
+    return launch_norm<kType, 256, 8>(a, stream);
+}
+
+int check_project(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters)
+{
+    if (n_rows < 0) return fail(ST_EINVAL, "negative size");
+    if (k < 16 || k > ST_MAX_ROW || k % 16 != 0) return fail(ST_EINVAL, "k=%d must be a multiple of 16 up to %d", k, ST_MAX_ROW);
+    if (n < 16 || n > ST_MAX_OUT || n % 16 != 0) return fail(ST_EINVAL, "n=%d must be a multiple of 16 up to %d", n, ST_MAX_OUT);
+    if (!adapters) return ST_OK;
+    if (adapters->n_adapters < 1 || adapters->n_adapters > ST_MAX_ADAPTERS) return fail(ST_EINVAL, "n_adapters=%d out of range", adapters->n_adapters);
+    if (adapters->rank < 8 || adapters->rank > ST_MAX_RANK || adapters->rank % 8 != 0)
+        return fail(ST_EINVAL, "rank=%d must be a multiple of 8 up to %d", adapters->rank, ST_MAX_RANK);
+    return ST_OK;
+}
+
+struct ProjectSpace {
+    int64_t inner, power;
+    int64_t bytes() const { return inner + power; }
+};
+
+ProjectSpace project_space(int32_t n_rows, const st_adapters* adapters)
+{
+    if (!adapters) return {0, 0};
+    return {st::round_up((int64_t)n_rows * adapters->rank * 2, 256), st::round_up((int64_t)n_rows * 4, 256)};
+}
+
+}  // namespace
+
+extern "C" {
+
+int st_norm_rows(const void* dev_x, int64_t x_stride, const void* dev_residual, int64_t residual_stride,
+                 const void* dev_weight, int32_t dtype, int64_t n_rows, int32_t d, int32_t normalise, float eps,
+                 void* dev_out_sum, int64_t sum_stride, int8_t* dev_out_q, float* dev_out_scale, void* dev_out_y,
+                 void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if (dtype != ST_BF16 && dtype != ST_F16 && dtype != ST_F32) return fail(ST_EINVAL, "unknown dtype %d", dtype);
+    if (n_rows < 0 || n_rows > 0x7FFFFFFFll) return fail(ST_EINVAL, "n_rows=%lld out of range", (long long)n_rows);
+    if (d < 16 || d > ST_MAX_ROW || d % 16 != 0) return fail(ST_EINVAL, "d=%d must be a multiple of 16 up to %d", d, ST_MAX_ROW);
+    if (normalise && !(eps >= 1e-12f && eps <= 1.0f)) return fail(ST_EINVAL, "eps=%g must be in [1e-12, 1]", (double)eps);
+    if (n_rows == 0) return ST_OK;
+    if (!dev_x || (!dev_out_sum && !dev_out_q && !dev_out_y) || !dev_out_q != !dev_out_scale) return fail(ST_EINVAL, "null argument");
+    if ((rc = check_rows("x", dev_x, x_stride, d)) || (rc = check_rows("residual", dev_residual, residual_stride, d)) ||
+        (rc = check_rows("sum", dev_out_sum, sum_stride, d)))
+        return rc;
+    if (misaligned(dev_weight) || misaligned(dev_out_q) || misaligned(dev_out_y) || ((uintptr_t)dev_out_scale & 3))
+        return fail(ST_EINVAL, "misaligned buffer (16 B)");
+    const st::NormArgs a = {dev_x, dev_residual, dev_weight, dev_out_sum, dev_out_q, dev_out_scale, dev_out_y, x_stride, residual_stride,
+                            sum_stride, n_rows, d, normalise != 0, eps};
+    hipStream_t stream = (hipStream_t)hip_stream;
+    rc = dtype == ST_BF16 ? norm_of_type<ST_BF16>(a, stream) : dtype == ST_F16 ? norm_of_type<ST_F16>(a, stream) : norm_of_type<ST_F32>(a, stream);
+    if (rc != ST_OK) return rc;
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int64_t st_project_workspace_bytes(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters)
+{
+    int rc;
+    if ((rc = check_project(n_rows, k, n, adapters))) return rc;
+    return std::max<int64_t>(256, project_space(n_rows, adapters).bytes());
+}
+
+int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, int32_t k, const int8_t* dev_w,
+               const float* dev_w_scale, int32_t n, const st_adapters* adapters, const int32_t* dev_adapter_of,
+               int32_t dtype, void* dev_out, int64_t out_stride, void* dev_workspace, int64_t workspace_bytes,
+               void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if (dtype != ST_BF16 && dtype != ST_F16) return fail(ST_EINVAL, "unknown dtype %d", dtype);
+    if ((rc = check_project(n_rows, k, n, adapters))) return rc;
+    if (n_rows == 0) return ST_OK;
+    if (!dev_x || !dev_x_scale || !dev_w || !dev_w_scale || !dev_out || !adapters != !dev_adapter_of ||
+        (adapters && (!adapters->dev_a || !adapters->dev_b || !adapters->dev_alpha)))
+        return fail(ST_EINVAL, "null argument");
+    if (misaligned(dev_x) || misaligned(dev_w) || misaligned(dev_w_scale) || ((uintptr_t)dev_x_scale & 3) || ((uintptr_t)dev_adapter_of & 3) ||
+        (adapters && (misaligned(adapters->dev_a) || misaligned(adapters->dev_b) || ((uintptr_t)adapters->dev_alpha & 3))))
+        return fail(ST_EINVAL, "misaligned buffer (16 B)");
+    if ((rc = check_rows("out", dev_out, out_stride, n))) return rc;
+    const ProjectSpace space = project_space(n_rows, adapters);
+    if (space.bytes() > 0 && (!dev_workspace || workspace_bytes < space.bytes()))
+        return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)space.bytes());
+    if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
+    char* ws = (char*)dev_workspace;
+    st::ProjectArgs p = {dev_x, dev_x_scale, dev_w, dev_w_scale, nullptr, nullptr, nullptr, dev_adapter_of, (uint16_t*)ws,
+                         (float*)(ws + space.inner), dev_out, out_stride, n_rows, k, n, 0, 0, dtype == ST_BF16};
+    if (adapters) {
+        p.a = (const uint16_t*)adapters->dev_a;
+        p.b = (const uint16_t*)adapters->dev_b;
+        p.alpha = adapters->dev_alpha;
+        p.n_adapters = adapters->n_adapters;
+        p.rank = adapters->rank;
+    }
+    const int64_t tiles = ((int64_t)n_rows + 127) / 128 * ((n + 127) / 128);
+    if ((rc = check_grid(tiles)) || (rc = check_grid(((int64_t)n_rows + 15) / 16))) return rc;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    if (adapters) {
+        TimedLaunch t(1, stream);
+        const dim3 groups((unsigned)((n_rows + 15) / 16)), threads(st::kInnerWaves * 64);
+        if (p.rank <= 16) hipLaunchKernelGGL(st::project_inner_kernel<1>, groups, threads, 0, stream, p);
+        else if (p.rank <= 32) hipLaunchKernelGGL(st::project_inner_kernel<2>, groups, threads, 0, stream, p);
+        else if (p.rank <= 64) hipLaunchKernelGGL(st::project_inner_kernel<4>, groups, threads, 0, stream, p);
+        else hipLaunchKernelGGL(st::project_inner_kernel<8>, groups, threads, 0, stream, p);
+    }
+    {
+        TimedLaunch t(0, stream);
+        hipLaunchKernelGGL(st::project_tile_kernel, dim3((unsigned)tiles), dim3(256), 0, stream, p);
+    }
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int st_rotate(const void* dev_q, int64_t q_stride, int32_t n_q_heads, const void* dev_k, int64_t k_stride, int32_t n_k_heads,
+              int32_t d, int32_t dtype, int32_t n_tok, const int32_t* dev_positions, const double* dev_freqs,
+              const int32_t* host_sections, int32_t n_axes, int32_t interleaved, int32_t inverse, void* dev_out_q,
+              int64_t out_q_stride, void* dev_out_k, int64_t out_k_stride, void* hip_stream)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if (dtype != ST_BF16 && dtype != ST_F16) return fail(ST_EINVAL, "unknown dtype %d", dtype);
+    if (n_tok < 0) return fail(ST_EINVAL, "negative size");
+    if (d < 16 || d > 512 || d % 8 != 0) return fail(ST_EINVAL, "d=%d must be a multiple of 8 from 16 to 512", d);
+    if (n_q_heads < 0 || n_k_heads < 0 || n_q_heads > 64 * ST_KV_MAX_HEADS || n_k_heads > ST_KV_MAX_HEADS)
+        return fail(ST_EINVAL, "heads out of range");
+    if (n_axes < 1 || n_axes > ST_MAX_AXES) return fail(ST_EINVAL, "n_axes=%d out of range", n_axes);
+    if (!host_sections) return fail(ST_EINVAL, "null argument");
+    st::RotateArgs a = {};
+    for (int i = 0; i < n_axes; ++i) {
+        if (host_sections[i] < 0 || host_sections[i] > d / 2) return fail(ST_EINVAL, "section of %d pairs out of range", host_sections[i]);
+        a.pairs += host_sections[i];
+        a.ends[i] = a.pairs;
+    }
+    if (a.pairs < 8 || a.pairs % 8 != 0 || a.pairs > d / 2) return fail(ST_EINVAL, "%d pairs must be a multiple of 8 up to d / 2 = %d", a.pairs, d / 2);
+    if (n_tok == 0 || n_q_heads + n_k_heads == 0) return ST_OK;
+    if (!dev_positions || !dev_freqs || (n_q_heads > 0 && (!dev_q || !dev_out_q)) || (n_k_heads > 0 && (!dev_k || !dev_out_k)))
+        return fail(ST_EINVAL, "null argument");
+    if (((uintptr_t)dev_positions & 3) || ((uintptr_t)dev_freqs & 7)) return fail(ST_EINVAL, "misaligned positions or frequencies");
+    const int64_t q_width = (int64_t)n_q_heads * d, k_width = (int64_t)n_k_heads * d;
+    if ((n_q_heads > 0 && ((rc = check_rows("queries", dev_q, q_stride, q_width)) || (rc = check_rows("queries out", dev_out_q, out_q_stride, q_width)))) ||
+        (n_k_heads > 0 && ((rc = check_rows("keys", dev_k, k_stride, k_width)) || (rc = check_rows("keys out", dev_out_k, out_k_stride, k_width)))))
+        return rc;
+    if ((n_q_heads > 0 && dev_q == dev_out_q && q_stride != out_q_stride) || (n_k_heads > 0 && dev_k == dev_out_k && k_stride != out_k_stride))
+        return fail(ST_EINVAL, "rows rotated in place keep their stride");
+    a.in[0] = (const uint16_t*)dev_q;
+    a.in[1] = (const uint16_t*)dev_k;
+    a.out[0] = (uint16_t*)dev_out_q;
+    a.out[1] = (uint16_t*)dev_out_k;
+    a.in_stride[0] = q_stride;
+    a.in_stride[1] = k_stride;
+    a.out_stride[0] = out_q_stride;
+    a.out_stride[1] = out_k_stride;
+    a.heads[0] = n_q_heads;
+    a.heads[1] = n_k_heads;
+    a.d = d;
+    a.n_tok = n_tok;
+    a.n_axes = n_axes;
+    a.positions = dev_positions;
+    a.freqs = dev_freqs;
+    a.bf16 = dtype == ST_BF16;
+    a.interleaved = interleaved != 0;
+    a.inverse = inverse != 0;
+    a.columns = a.pairs / 8 + (d - 2 * a.pairs) / 8;
+    const int heads = n_q_heads + n_k_heads;
+    a.head_parts = std::max(1, heads / 4);
+    const int64_t groups = ((int64_t)n_tok * a.columns * a.head_parts + st::kLayerThreads - 1) / st::kLayerThreads;
+    if ((rc = check_grid(groups))) return rc;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    {
+        TimedLaunch t(0, stream);
+        hipLaunchKernelGGL(st::rotate_kernel, dim3((unsigned)groups), dim3(st::kLayerThreads), 0, stream, a);
+    }
+    ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+}  // extern "C"

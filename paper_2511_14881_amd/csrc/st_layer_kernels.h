@@ -1,0 +1,283 @@
+// Rows on their way into and out of the calls on cached histories (definitions: silvertorch.h): the norm that turns
+// them into int8, and rotary positions.
+#pragma once
+#include "st_kv_device.h"
+
+namespace st {
+
+constexpr int kLayerThreads = 256;
+
+// Sums and maxima over 16, 64 or 256 threads, in every one of them: rotations inside rows of 16 lanes, then swaps of rows and halves,
+// then four words of the LDS.  Partners add the same two numbers, so all lanes hold the same bits.
+template <int N>
+__device__ inline float row_ror(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xF, 0xF, false));
+}
+template <int N>
+__device__ inline uint32_t row_ror(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xF, 0xF, false);
+}
+template <int kLanes>
+__device__ inline float sum_of_lanes(float v, float* part)
+{
+    v += row_ror<8>(v);
+    v += row_ror<4>(v);
+    v += row_ror<2>(v);
+    v += row_ror<1>(v);
+    if (kLanes >= 64) v = sum_over_16_32(v);
+    if (kLanes == 256) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = (part[0] + part[1]) + (part[2] + part[3]);
+    }
+    return v;
+}
+template <int kLanes>
+__device__ inline uint32_t max_of_lanes(uint32_t v, uint32_t* part)
+{
+    v = max(v, row_ror<8>(v));
+    v = max(v, row_ror<4>(v));
+    v = max(v, row_ror<2>(v));
+    v = max(v, row_ror<1>(v));
+    if (kLanes >= 64) {
+        auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max((uint32_t)r[0], (uint32_t)r[1]);
+        r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max((uint32_t)r[0], (uint32_t)r[1]);
+    }
+    if (kLanes == 256) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = max(max(part[0], part[1]), max(part[2], part[3]));
+    }
+    return v;
+}
+
+// Eight neighbouring values of a type as they lie in memory, and as floats.
+template <int kType>
+struct Eight {
+    uint4 w;
+    __device__ void load(const void* p, int64_t at) { w = *(const uint4*)((const uint16_t*)p + at); }
+    __device__ void floats(float* f) const { eight_floats(w, kType == ST_BF16, f); }
+    __device__ static void store(void* p, int64_t at, const float* f)
+    {
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = to_16_bits(f[2 * i], kType == ST_BF16) | to_16_bits(f[2 * i + 1], kType == ST_BF16) << 16;
+        *(uint4*)((uint16_t*)p + at) = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+    __device__ static float rounded(float f)
+    {
+        const uint32_t b = to_16_bits(f, kType == ST_BF16);
+        return kType == ST_BF16 ? bf16_float(b) : f16_float(b);
+    }
+};
+template <>
+struct Eight<ST_F32> {
+    float4 a, b;
+    __device__ void load(const void* p, int64_t at)
+    {
+        a = *(const float4*)((const float*)p + at);
+        b = *(const float4*)((const float*)p + at + 4);
+    }
+    __device__ void floats(float* f) const
+    {
+        f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    }
+    __device__ static void store(void* p, int64_t at, const float* f)
+    {
+        *(float4*)((float*)p + at) = make_float4(f[0], f[1], f[2], f[3]);
+        *(float4*)((float*)p + at + 4) = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    __device__ static float rounded(float f) { return f; }
+};
+
+// ---------------------------------------------------------------- norm
+struct NormArgs {
+    const void* x;
+    const void* residual;
+    const void* weight;
+    void* sum;
+    int8_t* q;
+    float* scale;
+    void* y;
+    int64_t x_stride, residual_stride, sum_stride, n_rows;
+    int32_t d, normalise;
+    float eps;
+};
+
+// A row's threads hold it in registers, eight neighbouring values to a vector and kVectors vectors to a thread, so that it is read once.
+template <int kType, int kLanes, int kVectors>
+__global__ __launch_bounds__(kLayerThreads) void norm_rows_kernel(NormArgs a)
+{
+    __shared__ float s_sum[kLayerThreads / 64];
+    __shared__ uint32_t s_max[2 * (kLayerThreads / 64)];
+    const int lane = threadIdx.x % kLanes;
+    const int64_t row = (int64_t)blockIdx.x * (kLayerThreads / kLanes) + threadIdx.x / kLanes;
+    const bool live = row < a.n_rows;
+    const int64_t at = live ? row : a.n_rows - 1;  // (a wavefront's lanes all take part in its steps)
+    const int n8 = a.d >> 3;
+    Eight<kType> x[kVectors], r[kVectors];
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i)
+        if (i * kLanes + lane < n8) x[i].load(a.x, at * a.x_stride + (i * kLanes + lane) * 8);
+    if (a.residual)
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i)
+            if (i * kLanes + lane < n8) r[i].load(a.residual, at * a.residual_stride + (i * kLanes + lane) * 8);
+    float h[kVectors][8];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) h[i][u] = 0.0f;
+        if (i * kLanes + lane >= n8) continue;
+        x[i].floats(h[i]);
+        if (a.residual) {
+            float f[8];
+            r[i].floats(f);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) h[i][u] = Eight<kType>::rounded(h[i][u] + f[u]);
+        }
+        if (a.sum && live) Eight<kType>::store(a.sum, row * a.sum_stride + (i * kLanes + lane) * 8, h[i]);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum += h[i][u] * h[i][u];
+    }
+    float rms = 1.0f;
+    if (a.normalise) {
+        sum = sum_of_lanes<kLanes>(sum, s_sum);
+        float eps = a.eps;
+        if (!(sum < 0x1p120f)) {  // (not for NaN either, which stays one)
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    h[i][u] *= 0x1p-70f;
+                    sum += h[i][u] * h[i][u];
+                }
+            if (kLanes == 256) __syncthreads();  // the words of the sum before are read
+            sum = sum_of_lanes<kLanes>(sum, s_sum);
+            eps = 0.0f;  // (eps / 2^140 beside at least 2^-34)
+        }
+        rms = 1.0f / __fsqrt_rn(sum / (float)a.d + eps);
+    }
+    uint32_t top = 0;  // largest magnitude as its bits, of which NaN's are the largest
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        if (i * kLanes + lane >= n8) continue;
+        if (a.weight) {
+            Eight<kType> w;
+            float f[8];
+            w.load(a.weight, (i * kLanes + lane) * 8);
+            w.floats(f);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) h[i][u] *= f[u];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) top = max(top, __float_as_uint(h[i][u]) & 0x7FFFFFFFu);
+    }
+    top = max_of_lanes<kLanes>(top, s_max);
+    const bool bad = top >= 0x7F800000u || !(rms < __builtin_inff());
+    const float unit = __fdiv_rn(__uint_as_float(top), 127.0f);
+    const float nan = __uint_as_float(0x7FC00000u);
+    if (!live) return;
+    if (a.scale && lane == 0) a.scale[row] = bad ? nan : unit * rms;
+    const bool zero = bad || !(unit > 0.0f);
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        const int v = i * kLanes + lane;
+        if (v >= n8) continue;
+        if (a.q) {
+            uint32_t w[2] = {0, 0};
+            if (!zero)
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    w[u / 4] |= (uint32_t)((int)fminf(fmaxf(rintf(__fdiv_rn(h[i][u], unit)), -127.0f), 127.0f) & 255) << (8 * (u & 3));
+            *(uint2*)(a.q + row * a.d + v * 8) = make_uint2(w[0], w[1]);
+        }
+        if (a.y) {
+            float f[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) f[u] = bad ? nan : h[i][u] * rms;
+            Eight<kType>::store(a.y, row * a.d + v * 8, f);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- rotary positions
+constexpr int kAxes = 8;
+
+struct RotateArgs {
+    const uint16_t* in[2];  // queries, keys
+    uint16_t* out[2];
+    int64_t in_stride[2], out_stride[2];
+    int32_t heads[2];
+    int32_t d, pairs, n_tok, n_axes;
+    int32_t ends[kAxes];  // pairs of the axes so far
+    const int32_t* positions;
+    const double* freqs;
+    int32_t bf16, interleaved, inverse, head_parts, columns;  // columns: threads to a token and part of the heads
+};
+
+// A thread takes eight pairs of a token (or eight values that are not rotated) through all heads of its part: their cos and sin
+// are formed once.
+__global__ __launch_bounds__(kLayerThreads) void rotate_kernel(RotateArgs a)
+{
+    const int64_t at = (int64_t)blockIdx.x * kLayerThreads + threadIdx.x;
+    const int column = (int)(at % a.columns);
+    const int64_t rest = at / a.columns;
+    const int part = (int)(rest % a.head_parts);
+    const int64_t tok = rest / a.head_parts;
+    if (tok >= a.n_tok) return;
+    const int heads = a.heads[0] + a.heads[1];
+    const int first = (int)((int64_t)heads * part / a.head_parts), last = (int)((int64_t)heads * (part + 1) / a.head_parts);
+    const bool bf16 = a.bf16 != 0;
+    if (column >= a.pairs / 8) {  // values behind the pairs
+        const int c = 2 * a.pairs + (column - a.pairs / 8) * 8;
+        for (int i = first; i < last; ++i) {
+            const int k = i >= a.heads[0], h = k ? i - a.heads[0] : i;
+            if (a.out[k] == a.in[k]) continue;
+            *(uint4*)(a.out[k] + tok * a.out_stride[k] + (int64_t)h * a.d + c) = *(const uint4*)(a.in[k] + tok * a.in_stride[k] + (int64_t)h * a.d + c);
+        }
+        return;
+    }
+    float cs[8], sn[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int pair = column * 8 + u;
+        int axis = 0;
+        for (int e = 0; e < a.n_axes - 1; ++e) axis += pair >= a.ends[e];
+        const double turns = (double)a.positions[(int64_t)axis * a.n_tok + tok] * (a.freqs[pair] * 0.15915494309189533577);
+        const float turn = (float)(turns - rint(turns));
+        cs[u] = __builtin_amdgcn_cosf(turn);
+        sn[u] = __builtin_amdgcn_sinf(a.inverse ? -turn : turn);
+    }
+    const int c0 = a.interleaved ? column * 16 : column * 8, c1 = a.interleaved ? c0 + 8 : c0 + a.pairs;
+    for (int i = first; i < last; ++i) {
+        const int k = i >= a.heads[0], h = k ? i - a.heads[0] : i;
+        const uint16_t* in = a.in[k] + tok * a.in_stride[k] + (int64_t)h * a.d;
+        uint16_t* out = a.out[k] + tok * a.out_stride[k] + (int64_t)h * a.d;
+        float f[16], g[16];
+        eight_floats(*(const uint4*)(in + c0), bf16, f);
+        eight_floats(*(const uint4*)(in + c1), bf16, f + 8);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float x = a.interleaved ? f[2 * u] : f[u], y = a.interleaved ? f[2 * u + 1] : f[8 + u];
+            const float p = x * cs[u] - y * sn[u], q = x * sn[u] + y * cs[u];
+            g[a.interleaved ? 2 * u : u] = p;
+            g[a.interleaved ? 2 * u + 1 : 8 + u] = q;
+        }
+        if (bf16) {
+            Eight<ST_BF16>::store(out, c0, g);
+            Eight<ST_BF16>::store(out, c1, g + 8);
+        } else {
+            Eight<ST_F16>::store(out, c0, g);
+            Eight<ST_F16>::store(out, c1, g + 8);
+        }
+    }
+}
+
+}  // namespace st
