@@ -327,24 +327,6 @@ struct KvPick {
     uint32_t state;     // 1: all keys of these bytes are
 };
 
-template <int kThreads>
-__device__ inline uint32_t wg_scan_add(uint32_t v, uint32_t* part, uint32_t* total)  // exclusive
-{
-    const int tid = threadIdx.x, w = tid >> 6;
-    const uint32_t inc = wave_scan_add(v);
-    if ((tid & 63) == 63) part[w] = inc;
-    __syncthreads();
-    uint32_t before = 0, all = 0;
-#pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) {
-        const uint32_t p = part[i];
-        before += i < w ? p : 0u;
-        all += p;
-    }
-    *total = all;
-    return before + inc - v;
-}
-
 template <int kThreads, class Emit>
 __device__ inline int kv_pick(const uint32_t* keys, int n, int want, KvPick<kThreads>* s, Emit emit)
 {

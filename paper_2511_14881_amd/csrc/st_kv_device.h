@@ -168,6 +168,25 @@ __device__ inline float add_halves(const half8& p, float sum)
     return __builtin_amdgcn_fdot2(__builtin_shufflevector(p, p, 6, 7), one, sum, false);
 }
 
+// Exclusive prefix sum over a workgroup; part: a word for each wavefront.
+template <int kThreads>
+__device__ inline uint32_t wg_scan_add(uint32_t v, uint32_t* part, uint32_t* total)
+{
+    const int tid = threadIdx.x, w = tid >> 6;
+    const uint32_t inc = wave_scan_add(v);
+    if ((tid & 63) == 63) part[w] = inc;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < kThreads / 64; ++i) {
+        const uint32_t p = part[i];
+        before += i < w ? p : 0u;
+        all += p;
+    }
+    *total = all;
+    return before + inc - v;
+}
+
 // x where the bit is 1, -inf where it is 0.
 __device__ inline float kv_seen(float x, uint32_t bits, int bit)
 {

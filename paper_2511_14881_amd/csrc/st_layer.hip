@@ -65,15 +65,75 @@ int check_project(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapt
     return ST_OK;
 }
 
-struct ProjectSpace {
-    int64_t inner, power;
-    int64_t bytes() const { return inner + power; }
+// Rows up to which a workgroup takes all of them.
+constexpr int kFewRows = 64;
+// Adapters from which on rows are brought into their order first.
+constexpr int kOrderFrom = 5;
+
+struct ProjectPlan {
+    int64_t inner, power, order;  // bytes
+    int64_t bytes() const { return inner + power + order; }
 };
 
-ProjectSpace project_space(int32_t n_rows, const st_adapters* adapters)
+ProjectPlan project_plan(int32_t n_rows, const st_adapters* adapters)
 {
-    if (!adapters) return {0, 0};
-    return {st::round_up((int64_t)n_rows * adapters->rank * 2, 256), st::round_up((int64_t)n_rows * 4, 256)};
+    if (!adapters) return {0, 0, 0};
+    const int64_t values = (int64_t)n_rows * adapters->rank, words = st::round_up((int64_t)n_rows * 4, 256);
+    if (n_rows <= kFewRows) return {st::round_up(values * 4 * st::kInnerParts, 256), 0, 0};
+    return {st::round_up(values * 2, 256), words, adapters->n_adapters >= kOrderFrom ? words : 0};
+}
+
+// Edge of the tiles of many rows by an estimate of the call's microseconds: what one workgroup takes alone, or what all take
+// together; 64: tiles x a share of the chip; 128: two workgroups to a compute unit, a last round of them costs about a quarter; 256: whole
+// rounds of one to a compute unit.  Measured with 64 / 128 / 256 (k x n, rows): 4096 x 5120, 512 22.9 / 24.5 / 47, 1024 44 / 35 / 48, 2048
+// 75 / 61 / 56, 4096 144 / 103 / 112, 8192 295 / 208 / 192; 2048 x 2560, 1024 13.3 / 15.7 / 29, 4096 42 / 37 / 33, 8192 79 / 60 / 65; 1024 x
+// 1024, 2048 7.6 / 10.4 / 19, 8192 21.8 / 20.1 / 22.5; 512 x 8192, 512 8.9 / 9.1 / 14.9, 2048 29 / 24 / 24, 8192 109 / 92 / 112.
+int project_edge(int32_t n_rows, int32_t k, int32_t n)
+{
+    const double steps = (k + 127) / 128;
+    auto tiles = [&](int64_t edge) { return (double)((n_rows + edge - 1) / edge * ((n + edge - 1) / edge)); };
+    const double c64 = std::max(3 + 0.45 * steps, tiles(64) * (0.0035 + 0.00078 * steps));
+    const double c128 = std::max(6 + 0.55 * steps, (tiles(128) / (2 * st::kComputeUnits) + 0.25) * (6 + 1.05 * steps));
+    const double c256 = std::ceil(tiles(256) / st::kComputeUnits) * std::max(23.0, 12 + 1.35 * steps);
+    return c64 <= c128 && c64 <= c256 ? 64 : c128 <= c256 ? 128 : 256;
+}
+
+template <bool kBf16, int kM>
+void launch_inner(const st::ProjectArgs& p, hipStream_t stream)
+{
+    const int64_t tiles = (p.n_rows + 16ll * kM - 1) / (16 * kM);
+    const int64_t split = std::max<int64_t>(1, std::min<int64_t>({1024 / tiles, p.n_adapters, 16 * kM}));
+    const dim3 groups((unsigned)tiles, (unsigned)split), threads(st::kInnerParts * 64);
+    if (p.rank <= 16) hipLaunchKernelGGL((st::project_inner_kernel<kBf16, 1, kM>), groups, threads, 0, stream, p);
+    else if (p.rank <= 32) hipLaunchKernelGGL((st::project_inner_kernel<kBf16, 2, kM>), groups, threads, 0, stream, p);
+    else if (p.rank <= 64) hipLaunchKernelGGL((st::project_inner_kernel<kBf16, 4, kM>), groups, threads, 0, stream, p);
+    else hipLaunchKernelGGL((st::project_inner_kernel<kBf16, 8, kM>), groups, threads, 0, stream, p);
+}
+
+template <bool kBf16>
+void launch_project(const st::ProjectArgs& p, int edge, unsigned tiles, hipStream_t stream)
+{
+    if (p.a) {
+        TimedLaunch t(1, stream);
+        if (p.order)
+            hipLaunchKernelGGL(st::project_order_kernel, dim3((unsigned)((p.n_rows + (int64_t)st::kOrderRows - 1) / st::kOrderRows)), dim3(st::kOrderThreads), 0, stream, p);
+        if (p.n_rows <= kFewRows)
+            hipLaunchKernelGGL((st::project_parts_kernel<kBf16>), dim3((unsigned)((p.n_rows + 15) / 16), (unsigned)std::min({p.n_adapters, p.n_rows, 16}),
+                                                                       (unsigned)((p.rank + 15) / 16 * st::kInnerParts)), dim3(64), 0, stream, p);
+        else if (p.n_rows <= 2048) launch_inner<kBf16, 1>(p, stream);
+        else launch_inner<kBf16, 4>(p, stream);
+    }
+    TimedLaunch t(0, stream);
+    if (p.n_rows <= kFewRows) {
+        const dim3 groups((unsigned)((p.n + 31) / 32)), threads(st::kFewWaves * 64);
+        if (p.n_rows <= 32) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 1>), groups, threads, 0, stream, p);
+        else hipLaunchKernelGGL((st::project_few_kernel<kBf16, 2>), groups, threads, 0, stream, p);
+        return;
+    }
+    const dim3 groups(tiles);
+    if (edge == 64) hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 2, 1, 1>), groups, dim3(256), 0, stream, p);
+    else if (edge == 128) hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 2, 2, 2>), groups, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 4, 4, 2>), groups, dim3(512), 0, stream, p);
 }
 
 }  // namespace
@@ -112,7 +172,7 @@ int64_t st_project_workspace_bytes(int32_t n_rows, int32_t k, int32_t n, const s
 {
     int rc;
     if ((rc = check_project(n_rows, k, n, adapters))) return rc;
-    return std::max<int64_t>(256, project_space(n_rows, adapters).bytes());
+    return std::max<int64_t>(256, project_plan(n_rows, adapters).bytes());
 }
 
 int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, int32_t k, const int8_t* dev_w,
@@ -132,13 +192,13 @@ int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, in
         (adapters && (misaligned(adapters->dev_a) || misaligned(adapters->dev_b) || ((uintptr_t)adapters->dev_alpha & 3))))
         return fail(ST_EINVAL, "misaligned buffer (16 B)");
     if ((rc = check_rows("out", dev_out, out_stride, n))) return rc;
-    const ProjectSpace space = project_space(n_rows, adapters);
-    if (space.bytes() > 0 && (!dev_workspace || workspace_bytes < space.bytes()))
-        return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)space.bytes());
+    const ProjectPlan plan = project_plan(n_rows, adapters);
+    if (plan.bytes() > 0 && (!dev_workspace || workspace_bytes < plan.bytes()))
+        return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)plan.bytes());
     if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");
     char* ws = (char*)dev_workspace;
-    st::ProjectArgs p = {dev_x, dev_x_scale, dev_w, dev_w_scale, nullptr, nullptr, nullptr, dev_adapter_of, (uint16_t*)ws,
-                         (float*)(ws + space.inner), dev_out, out_stride, n_rows, k, n, 0, 0, dtype == ST_BF16};
+    st::ProjectArgs p = {dev_x, dev_x_scale, dev_w, dev_w_scale, nullptr, nullptr, nullptr, dev_adapter_of, (uint16_t*)ws, (float*)(ws + plan.inner), (float*)ws,
+                         plan.order ? (int32_t*)(ws + plan.inner + plan.power) : nullptr, dev_out, out_stride, n_rows, k, n, 0, 0};
     if (adapters) {
         p.a = (const uint16_t*)adapters->dev_a;
         p.b = (const uint16_t*)adapters->dev_b;
@@ -146,21 +206,12 @@ int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, in
         p.n_adapters = adapters->n_adapters;
         p.rank = adapters->rank;
     }
-    const int64_t tiles = ((int64_t)n_rows + 127) / 128 * ((n + 127) / 128);
+    const int edge = project_edge(n_rows, k, n);
+    const int64_t tiles = ((int64_t)n_rows + edge - 1) / edge * ((n + edge - 1) / edge);
     if ((rc = check_grid(tiles)) || (rc = check_grid(((int64_t)n_rows + 15) / 16))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
-    if (adapters) {
-        TimedLaunch t(1, stream);
-        const dim3 groups((unsigned)((n_rows + 15) / 16)), threads(st::kInnerWaves * 64);
-        if (p.rank <= 16) hipLaunchKernelGGL(st::project_inner_kernel<1>, groups, threads, 0, stream, p);
-        else if (p.rank <= 32) hipLaunchKernelGGL(st::project_inner_kernel<2>, groups, threads, 0, stream, p);
-        else if (p.rank <= 64) hipLaunchKernelGGL(st::project_inner_kernel<4>, groups, threads, 0, stream, p);
-        else hipLaunchKernelGGL(st::project_inner_kernel<8>, groups, threads, 0, stream, p);
-    }
-    {
-        TimedLaunch t(0, stream);
-        hipLaunchKernelGGL(st::project_tile_kernel, dim3((unsigned)tiles), dim3(256), 0, stream, p);
-    }
+    if (dtype == ST_BF16) launch_project<true>(p, edge, (unsigned)tiles, stream);
+    else launch_project<false>(p, edge, (unsigned)tiles, stream);
     ST_HIP(hipGetLastError());
     return ST_OK;
     });

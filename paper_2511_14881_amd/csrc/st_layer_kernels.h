@@ -55,23 +55,33 @@ __device__ inline uint32_t max_of_lanes(uint32_t v, uint32_t* part)
     return v;
 }
 
+// To the nearest 16-bit numbers, ties to even (the hardware's conversions; NaN stays one).
+template <bool kBf16>
+__device__ inline uint16_t one_16(float f)
+{
+    return kBf16 ? __builtin_bit_cast(uint16_t, (__bf16)f) : __builtin_bit_cast(uint16_t, (_Float16)f);
+}
+template <bool kBf16>
+__device__ inline uint32_t two_16(float a, float b)
+{
+    return (uint32_t)one_16<kBf16>(a) | (uint32_t)one_16<kBf16>(b) << 16;
+}
+
 // Eight neighbouring values of a type as they lie in memory, and as floats.
 template <int kType>
 struct Eight {
+    static constexpr bool kBf16 = kType == ST_BF16;
     uint4 w;
     __device__ void load(const void* p, int64_t at) { w = *(const uint4*)((const uint16_t*)p + at); }
-    __device__ void floats(float* f) const { eight_floats(w, kType == ST_BF16, f); }
+    __device__ void floats(float* f) const { eight_floats(w, kBf16, f); }
     __device__ static void store(void* p, int64_t at, const float* f)
     {
-        uint32_t r[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = to_16_bits(f[2 * i], kType == ST_BF16) | to_16_bits(f[2 * i + 1], kType == ST_BF16) << 16;
-        *(uint4*)((uint16_t*)p + at) = make_uint4(r[0], r[1], r[2], r[3]);
+        *(uint4*)((uint16_t*)p + at) = make_uint4(two_16<kBf16>(f[0], f[1]), two_16<kBf16>(f[2], f[3]), two_16<kBf16>(f[4], f[5]), two_16<kBf16>(f[6], f[7]));
     }
     __device__ static float rounded(float f)
     {
-        const uint32_t b = to_16_bits(f, kType == ST_BF16);
-        return kType == ST_BF16 ? bf16_float(b) : f16_float(b);
+        const uint32_t b = one_16<kBf16>(f);
+        return kBf16 ? bf16_float(b) : f16_float(b);
     }
 };
 template <>

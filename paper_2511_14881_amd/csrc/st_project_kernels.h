@@ -1,9 +1,11 @@
 // Projection of int8 rows by shared int8 weights, with a low-rank adapter for each row (definition: silvertorch.h).
 #pragma once
-#include "st_kv_device.h"
+#include "st_layer_kernels.h"
 
 namespace st {
 
+typedef int int16v __attribute__((ext_vector_type(16)));
+typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 
 struct ProjectArgs {
@@ -17,9 +19,11 @@ struct ProjectArgs {
     const int32_t* adapter_of;
     uint16_t* inner;    // [n_rows, rank]: alpha x_scale a x / 2^e, rounded
     float* power;       // [n_rows]: 2^e
+    float* parts;       // few rows, in place of inner and power: [kInnerParts, n_rows, rank], a x over a part of k each
+    int32_t* order;     // [n_rows]: rows of one adapter side by side; NULL: as they come
     void* out;
     int64_t out_stride;
-    int32_t n_rows, k, n, n_adapters, rank, bf16;
+    int32_t n_rows, k, n, n_adapters, rank;
 };
 
 // The adapter of a row, -1: none.
@@ -30,29 +34,54 @@ __device__ inline int project_adapter(const ProjectArgs& a, int64_t row)
     return i >= 0 && i < a.n_adapters ? i : -1;
 }
 
-// The smallest number above `last` that a lane of the wavefront holds, INT32_MAX if there is none.
-template <int N>
+// The row at place m of the order, n_rows behind the last.
+__device__ inline int64_t project_place(const ProjectArgs& p, int64_t m)
+{
+    if (m >= p.n_rows) return p.n_rows;
+    return p.order ? p.order[m] : m;
+}
+
+// The smallest number above `last` that a lane holds, INT32_MAX if there is none.  Lanes that lie kLanes apart hold the same.
+template <int kLanes, int N>
 __device__ inline int next_of(const int (&v)[N], int last)
 {
-    int m = 0x7FFFFFFF;
+    uint32_t m = 0x7FFFFFFF;
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = v[i] > last && v[i] < m ? v[i] : m;
-    for (int o = 32; o > 0; o >>= 1) m = min(m, __shfl_xor(m, o));
-    return m;
+    for (int i = 0; i < N; ++i) m = v[i] > last ? min(m, (uint32_t)v[i]) : m;
+    m = min(m, row_ror<8>(m));
+    m = min(m, row_ror<4>(m));
+    m = min(m, row_ror<2>(m));
+    m = min(m, row_ror<1>(m));
+    if (kLanes == 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+        m = min((uint32_t)r[0], (uint32_t)r[1]);
+    }
+    return __builtin_amdgcn_readfirstlane((int)m);
 }
 
 // D += A B of 16-bit floats, 16 x 16 x 32: lane l holds row l % 16 of A and column l % 16 of B, elements (l / 16) * 8 ..; of D
 // column l % 16, rows (l / 16) * 4 ..
-__device__ inline float4v mfma_16(const uint4& a, const uint4& b, const float4v& d, bool bf16)
+template <bool kBf16>
+__device__ inline float4v mfma_16(const uint4& a, const uint4& b, const float4v& d)
 {
-    if (bf16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, a), __builtin_bit_cast(bhalf8, b), d, 0, 0, 0);
+    if (kBf16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, a), __builtin_bit_cast(bhalf8, b), d, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), d, 0, 0, 0);
 }
 
-// Eight int8 as 16-bit floats, exactly.
-__device__ inline uint4 eight_16(uint32_t lo, uint32_t hi, bool bf16)
+// The same, 32 x 32 x 16: lane l holds row l % 32 of A and column l % 32 of B, elements (l / 32) * 8 ..; of D column l % 32, rows
+// 8 * (i / 4) + 4 * (l / 32) + i % 4.
+template <bool kBf16>
+__device__ inline float16v mfma_32(const uint4& a, const uint4& b, const float16v& d)
 {
-    if (!bf16) return __builtin_bit_cast(uint4, eight_halves(lo, hi));
+    if (kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bhalf8, a), __builtin_bit_cast(bhalf8, b), d, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), d, 0, 0, 0);
+}
+
+// Eight int8 as 16-bit floats, exactly.
+template <bool kBf16>
+__device__ inline uint4 eight_16(uint32_t lo, uint32_t hi)
+{
+    if (!kBf16) return __builtin_bit_cast(uint4, eight_halves(lo, hi));
     uint32_t r[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -63,194 +92,620 @@ __device__ inline uint4 eight_16(uint32_t lo, uint32_t hi, bool bf16)
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// ---------------------------------------------------------------- inner values of the adapters
-constexpr int kInnerWaves = 8;
+// ---------------------------------------------------------------- rows in the order of their adapters
+// Rows of a segment are dealt into buckets by adapter (those without one behind the others), so that a tile of the kernels below
+// meets few adapters: each costs it a load of operands and products with all its rows.  A segment to a workgroup, counts and places in the
+// LDS; which of a bucket's rows comes first may vary from call to call, and no row's result goes by it.
+constexpr int kOrderThreads = 512, kOrderRows = 2048, kBuckets = 2048;
 
-// One workgroup to 16 rows; its wavefronts share k between them and join their sums in the LDS.  Each adapter among the rows in turn:
-// the other rows' results of it are not used.
-template <int kTiles>  // of 16 ranks
-__global__ __launch_bounds__(kInnerWaves * 64) void project_inner_kernel(ProjectArgs p)
+__global__ __launch_bounds__(kOrderThreads) void project_order_kernel(ProjectArgs p)
 {
-    constexpr int kRanks = 16 * kTiles;
-    __shared__ float s_sum[kInnerWaves][16][kRanks + 4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row0 = (int64_t)blockIdx.x * 16, row = row0 + (lane & 15);
-    const int8_t* x = p.x + min(row, (int64_t)p.n_rows - 1) * p.k;
-    const bool bf16 = p.bf16 != 0;
-    int mine[1] = {project_adapter(p, row)};
-    for (int a = next_of(mine, -1); a != 0x7FFFFFFF; a = next_of(mine, a)) {
-        const uint16_t* wa = p.a + (int64_t)a * p.rank * p.k;
-        float4v acc[kTiles] = {};
-        for (int k0 = wave * 64; k0 < p.k; k0 += kInnerWaves * 64) {
-            const int k = k0 + (lane >> 4) * 16;
-            const bool in = k < p.k;
-            uint4 xi = make_uint4(0, 0, 0, 0);
-            if (in) xi = *(const uint4*)(x + k);
-            const uint4 x0 = eight_16(xi.x, xi.y, bf16), x1 = eight_16(xi.z, xi.w, bf16);
+    __shared__ uint32_t count[kBuckets];
+    __shared__ uint32_t part[kOrderThreads / 64];
+    constexpr int kEach = kOrderRows / kOrderThreads, kOwn = kBuckets / kOrderThreads;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int64_t first = (int64_t)blockIdx.x * kOrderRows;
+    int bucket[kEach];
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                const int r = t * 16 + (lane & 15);
-                uint4 a0 = make_uint4(0, 0, 0, 0), a1 = a0;
-                if (in && r < p.rank) {
-                    a0 = *(const uint4*)(wa + (int64_t)r * p.k + k);
-                    a1 = *(const uint4*)(wa + (int64_t)r * p.k + k + 8);
-                }
-                acc[t] = mfma_16(a0, x0, acc[t], bf16);
-                acc[t] = mfma_16(a1, x1, acc[t], bf16);
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t row = first + i * kOrderThreads + tid;
+        const int a = project_adapter(p, row);
+        bucket[i] = row >= p.n_rows ? -1 : a < 0 ? kBuckets - 1 : a % (kBuckets - 1);
+    }
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) count[i * kOrderThreads + tid] = 0;
+    __syncthreads();
+    // Places among the counts of `count`; a wavefront whose rows share a bucket asks once.
+    auto take = [&](int b) -> uint32_t {
+        const int b0 = __builtin_amdgcn_readfirstlane(b);
+        if (ballot(b != b0) == 0) {
+            uint32_t at = 0;
+            if (lane == 0 && b0 >= 0) at = atomicAdd(&count[b0], 64u);
+            return (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + lane;
+        }
+        return b >= 0 ? atomicAdd(&count[b], 1u) : 0u;
+    };
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) (void)take(bucket[i]);
+    __syncthreads();
+    uint32_t own[kOwn], sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        own[i] = sum;
+        sum += count[tid * kOwn + i];
+    }
+    const uint32_t before = wg_scan_add<kOrderThreads>(sum, part, &total);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) count[tid * kOwn + i] = before + own[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t at = take(bucket[i]);
+        if (bucket[i] >= 0) p.order[first + at] = (int32_t)(first + i * kOrderThreads + tid);
+    }
+}
+
+// ---------------------------------------------------------------- inner values of the adapters
+constexpr int kInnerParts = 8;
+
+// What one wavefront does for 16 kM rows, an adapter, kTiles x 16 of its ranks and a part of k: the 64 values from 64 (part + 8 i) on,
+// i = 0, 1, ..  `wa`: the lane's row and place in a, `ranks`: how many of the ranks there are.  Loads of kChunks of those run ahead.
+template <bool kBf16, int kTiles, int kM>
+struct InnerPart {
+    static constexpr int kFit = 96 / (kTiles * 8 + kM * 4), kChunks = kFit < 1 ? 1 : kFit > 8 ? 8 : kFit;
+    uint4 xv[kChunks][kM];
+    float4v acc[kM][kTiles];
+
+    __device__ void load_x(const int8_t* const (&x)[kM], int k0, int k_end)
+    {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const int k = k0 + c * (kInnerParts * 64);
+            const bool in = k + (int)((threadIdx.x & 63) >> 4) * 16 < k_end;
+#pragma unroll
+            for (int i = 0; i < kM; ++i) {
+                xv[c][i] = make_uint4(0, 0, 0, 0);
+                if (in) xv[c][i] = *(const uint4*)(x[i] + k);
             }
         }
-        __syncthreads();  // the sums of the adapter before are read
+    }
+    // The first chunks of x are there.
+    __device__ void run(const int8_t* const (&x)[kM], const uint16_t* wa, int ranks, int part, int k_end)
+    {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-            *(float4v*)&s_sum[wave][lane & 15][t * 16 + (lane >> 4) * 4] = acc[t];
-        __syncthreads();
-        // 32 threads to a row
-        const int m = tid >> 5, l = tid & 31;
-        if (project_adapter(p, row0 + m) == a) {
-            const float factor = p.alpha[a] * p.x_scale[row0 + m];
-            float v[(kRanks + 31) / 32];
+        for (int i = 0; i < kM; ++i)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) acc[i][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k0 = part * 64; k0 < k_end; k0 += kChunks * kInnerParts * 64) {
+            uint4 av[kChunks][kTiles][2];
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                const int k = k0 + c * (kInnerParts * 64);
+                const bool in = k + (lane >> 4) * 16 < k_end;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    av[c][t][0] = av[c][t][1] = make_uint4(0, 0, 0, 0);
+                    if (in && t * 16 + (lane & 15) < ranks) {
+                        av[c][t][0] = *(const uint4*)(wa + (int64_t)t * 16 * k_end + k);
+                        av[c][t][1] = *(const uint4*)(wa + (int64_t)t * 16 * k_end + k + 8);
+                    }
+                }
+            }
+            if (k0 != part * 64) load_x(x, k0, k_end);
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                for (int i = 0; i < kM; ++i) {
+                    const uint4 x0 = eight_16<kBf16>(xv[c][i].x, xv[c][i].y), x1 = eight_16<kBf16>(xv[c][i].z, xv[c][i].w);
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+                        acc[i][t] = mfma_16<kBf16>(av[c][t][0], x0, acc[i][t]);
+                        acc[i][t] = mfma_16<kBf16>(av[c][t][1], x1, acc[i][t]);
+                    }
+                }
+        }
+    }
+};
+
+// The power of two of a row's largest inner value (its bits), kept within what can be inverted; 1 where there is none or it is no number.
+__device__ inline uint32_t project_exponent(uint32_t top)
+{
+    const uint32_t e = top >> 23;
+    return e < 27 || e == 255 ? 127u : min(e, 227u);
+}
+
+// 16 kM rows and every gridDim.y-th adapter among them; the other rows' results of an adapter are not kept.  A wavefront to each part of
+// k; the parts are summed in their order, so that a row's sums have one order whatever kM, the grid and the kernel.
+template <bool kBf16, int kTiles, int kM>
+__global__ __launch_bounds__(kInnerParts * 64) void project_inner_kernel(ProjectArgs p)
+{
+    constexpr int kRanks = 16 * kTiles;
+    __shared__ float s_sum[kInnerParts][16][kRanks + 4];
+    const int tid = threadIdx.x, lane = tid & 63, part = tid >> 6;
+    const int64_t m0 = (int64_t)blockIdx.x * (16 * kM);
+    const int8_t* x[kM];
+    int mine[kM];
+#pragma unroll
+    for (int i = 0; i < kM; ++i) {
+        const int64_t row = project_place(p, m0 + 16 * i + (lane & 15));
+        mine[i] = project_adapter(p, row);
+        x[i] = p.x + min(row, (int64_t)p.n_rows - 1) * p.k + (lane >> 4) * 16;
+    }
+    // 32 threads to a row when the parts are summed
+    const int m = tid >> 5, l = tid & 31;
+    int64_t row[kM];
+    int of[kM];
+    float scale[kM];
+#pragma unroll
+    for (int i = 0; i < kM; ++i) {
+        row[i] = project_place(p, m0 + 16 * i + m);
+        of[i] = project_adapter(p, row[i]);
+        scale[i] = row[i] < p.n_rows ? p.x_scale[row[i]] : 0.0f;
+    }
+    InnerPart<kBf16, kTiles, kM> inner;
+    int index = 0;
+    for (int a = next_of<16>(mine, -1); a != 0x7FFFFFFF; a = next_of<16>(mine, a), ++index) {
+        if (index % gridDim.y != blockIdx.y) continue;
+        inner.load_x(x, part * 64, p.k);
+        const float alpha = p.alpha[a];
+        inner.run(x, p.a + ((int64_t)a * p.rank + (lane & 15)) * p.k + (lane >> 4) * 16, p.rank, part, p.k);
+        constexpr int kEach = (kRanks + 31) / 32;
+#pragma unroll
+        for (int i = 0; i < kM; ++i) {
+            __syncthreads();  // the sums before are read
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) *(float4v*)&s_sum[part][lane & 15][t * 16 + (lane >> 4) * 4] = inner.acc[i][t];
+            __syncthreads();
+            if (of[i] != a) continue;
+            const float factor = alpha * scale[i];
+            float v[kEach];
             uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < (kRanks + 31) / 32; ++i) {
-                const int r = i * 32 + l;
-                v[i] = 0.0f;
+            for (int c = 0; c < kEach; ++c) {
+                const int r = c * 32 + l;
+                v[c] = 0.0f;
                 if (r < p.rank) {
-                    for (int u = 0; u < kInnerWaves; ++u) v[i] += s_sum[u][m][r];
-                    v[i] *= factor;
+                    v[c] = s_sum[0][m][r];
+#pragma unroll
+                    for (int u = 1; u < kInnerParts; ++u) v[c] += s_sum[u][m][r];
+                    v[c] *= factor;
                 }
-                top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+                top = max(top, __float_as_uint(v[c]) & 0x7FFFFFFFu);
             }
-            for (int o = 16; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-            // 2^e of the largest, kept within what can be inverted; 1 where there is none or it is no number
-            uint32_t e = top >> 23;
-            e = e < 27 ? 127u : e == 255 ? 127u : min(e, 227u);
+            top = max(top, row_ror<8>(top));
+            top = max(top, row_ror<4>(top));
+            top = max(top, row_ror<2>(top));
+            top = max(top, row_ror<1>(top));
+            const auto both = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+            const uint32_t e = project_exponent(max((uint32_t)both[0], (uint32_t)both[1]));
             const float down = __uint_as_float((254u - e) << 23);
 #pragma unroll
-            for (int i = 0; i < (kRanks + 31) / 32; ++i) {
-                const int r = i * 32 + l;
-                if (r < p.rank) p.inner[(row0 + m) * p.rank + r] = (uint16_t)to_16_bits(v[i] * down, bf16);
+            for (int c = 0; c < kEach; ++c) {
+                const int r = c * 32 + l;
+                if (r < p.rank) p.inner[row[i] * p.rank + r] = one_16<kBf16>(v[c] * down);
             }
-            if (l == 0) p.power[row0 + m] = __uint_as_float(e << 23);
+            if (l == 0) p.power[row[i]] = __uint_as_float(e << 23);
         }
     }
 }
 
-// ---------------------------------------------------------------- what follows the int8 products
-// A wavefront holds kM x kN tiles of 16 rows x 16 columns: in tile (i, j) lane l has row m0 + 16 i + l % 16, columns
-// n0 + 16 j + (l / 16) * 4 .. + 3.  Scales, the adapters' products on top of the scaled sums (both over 2^e), rounding, stores.
-template <int kM, int kN>
-__device__ inline void project_finish(const ProjectArgs& p, int4v (&dot)[kM][kN], int64_t m0, int n0)
+// For few rows: a workgroup of one wavefront to each 16 rows, adapter among them, 16 ranks and part of k, so that the adapters' rows
+// come in over the whole chip (16 rows, 8 adapters, rank 64, k = 4096: 4.7 us against 20 us by eight workgroups of the kernel
+// above).  The sums of a part stay as they are.
+template <bool kBf16>
+__global__ __launch_bounds__(64) void project_parts_kernel(ProjectArgs p)
 {
-    const int lane = threadIdx.x & 63;
-    const bool bf16 = p.bf16 != 0;
-    float xs[kM], power[kM];
-    int mine[kM];
-#pragma unroll
-    for (int i = 0; i < kM; ++i) {
-        const int64_t row = m0 + 16 * i + (lane & 15);
-        xs[i] = row < p.n_rows ? p.x_scale[row] : 0.0f;
-        mine[i] = -1;
-        power[i] = 1.0f;
-        if (p.a) {
-            mine[i] = project_adapter(p, row);
-            if (mine[i] >= 0) {
-                power[i] = p.power[row];
-                xs[i] *= __uint_as_float(0x7F000000u - __float_as_uint(power[i]));  // 1 / 2^e
-            }
-        }
+    const int lane = threadIdx.x, part = blockIdx.z % kInnerParts, rank0 = blockIdx.z / kInnerParts * 16;
+    const int row = blockIdx.x * 16 + (lane & 15);
+    const int8_t* x[1] = {p.x + (int64_t)min(row, p.n_rows - 1) * p.k + (lane >> 4) * 16};
+    const int mine[1] = {project_adapter(p, row)};
+    InnerPart<kBf16, 1, 1> inner;
+    inner.load_x(x, part * 64, p.k);
+    int a = next_of<16>(mine, -1);
+    for (int i = 0; i < (int)blockIdx.y && a != 0x7FFFFFFF; ++i) a = next_of<16>(mine, a);
+    if (a == 0x7FFFFFFF) return;
+    inner.run(x, p.a + ((int64_t)a * p.rank + rank0 + (lane & 15)) * p.k + (lane >> 4) * 16, p.rank - rank0, part, p.k);
+    const int r = rank0 + (lane >> 4) * 4;
+    if (mine[0] == a && r < p.rank) *(float4v*)(p.parts + ((int64_t)part * p.n_rows + row) * p.rank + r) = inner.acc[0][0];
+}
+
+// ---------------------------------------------------------------- what follows the int8 products
+// Tiles are 32 rows x 32 columns, as the columns and rows of a matrix product w x^T: lane l has row m0 + l % 32, and columns
+// n0 + 8 * (u / 4) + 4 * (l / 32) + u % 4 for u < 16.  The sums of products take on scales and the adapters' part in the same registers.
+struct ProjectRow {
+    int adapter;
+    float scale;  // x_scale / 2^e
+    float power;  // 2^e
+};
+
+__device__ inline ProjectRow project_row(const ProjectArgs& p, int64_t row)
+{
+    ProjectRow r = {-1, row < p.n_rows ? p.x_scale[row] : 0.0f, 1.0f};
+    if (p.a && (r.adapter = project_adapter(p, row)) >= 0) {
+        r.power = p.power[row];
+        r.scale *= __uint_as_float(0x7F000000u - __float_as_uint(r.power));
     }
-    float4v sum[kM][kN];
+    return r;
+}
+
+// Eight of a row's inner values, from rank r on; zeros for a row of another adapter and behind the last rank.
+__device__ inline uint4 project_inner_values(const ProjectArgs& p, int64_t row, int r, bool mine)
+{
+    if (mine && r < p.rank) return *(const uint4*)(p.inner + row * p.rank + r);
+    return make_uint4(0, 0, 0, 0);
+}
+
+// The weights' scales of a lane's columns.
+template <int kN>
+__device__ inline void project_scales(const ProjectArgs& p, float4v (&ws)[kN][4], int n0)
+{
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int n = n0 + 32 * j + 8 * g + (threadIdx.x >> 5 & 1) * 4;
+            ws[j][g] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            if (n < p.n) ws[j][g] = *(const float4v*)(p.w_scale + n);
+        }
+}
+
+// Rounding; eight neighbouring columns to a lane: lanes l and l + 32 hold four of each eight and swap half of them.
+// out[j][g]: columns 32 j + 16 g + 8 * (l / 32) ..
+template <bool kBf16, int kN>
+__device__ inline void project_round(const float16v (&sum)[kN], float power, uint4 (&out)[kN][2])
+{
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-        const int n = n0 + 16 * j + (lane >> 4) * 4;
-        float4v ws = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (n < p.n) ws = *(const float4v*)(p.w_scale + n);
+        uint32_t h[8];
 #pragma unroll
-        for (int i = 0; i < kM; ++i)
+        for (int i = 0; i < 8; ++i) h[i] = two_16<kBf16>(sum[j][2 * i] * power, sum[j][2 * i + 1] * power);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) sum[i][j][u] = (float)dot[i][j][u] * xs[i] * ws[u];
+        for (int g = 0; g < 2; ++g) {
+            // words 4 g, 4 g + 1: columns 16 g + 4 half ..; words 4 g + 2, 4 g + 3: columns 16 g + 8 + 4 half ..
+            const auto a = __builtin_amdgcn_permlane32_swap(h[4 * g], h[4 * g + 2], false, false);
+            const auto b = __builtin_amdgcn_permlane32_swap(h[4 * g + 1], h[4 * g + 3], false, false);
+            out[j][g] = make_uint4(a[0], b[0], a[1], b[1]);
+        }
     }
-    if (p.a)
-        for (int a = next_of(mine, -1); a != 0x7FFFFFFF; a = next_of(mine, a)) {
+}
+
+// A row of tiles of a wavefront: scales, the adapters' products on top, rounding.
+template <bool kBf16, int kN>
+__device__ inline void project_finish(const ProjectArgs& p, const int16v (&dot)[kN], const ProjectRow& mine, const float4v (&ws)[kN][4],
+                                      int64_t row, int n0, uint4 (&out)[kN][2])
+{
+    const int lane = threadIdx.x & 63;
+    float16v sum[kN];
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (int u = 0; u < 16; ++u) sum[j][u] = (float)dot[j][u] * mine.scale * ws[j][u / 4][u % 4];
+    if (p.a) {
+        const int all[1] = {mine.adapter};
+        for (int a = next_of<32>(all, -1); a != 0x7FFFFFFF; a = next_of<32>(all, a)) {
             const uint16_t* wb = p.b + (int64_t)a * p.n * p.rank;
-            for (int r0 = 0; r0 < p.rank; r0 += 32) {
-                const int r = r0 + (lane >> 4) * 8;
+            for (int r0 = 0; r0 < p.rank; r0 += 16) {
+                const int r = r0 + (lane >> 5) * 8;
+                const uint4 v = project_inner_values(p, row, r, mine.adapter == a);
                 uint4 b[kN];
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
-                    const int n = n0 + 16 * j + (lane & 15);
+                    const int n = n0 + 32 * j + (lane & 31);
                     b[j] = make_uint4(0, 0, 0, 0);
                     if (n < p.n && r < p.rank) b[j] = *(const uint4*)(wb + (int64_t)n * p.rank + r);
                 }
 #pragma unroll
-                for (int i = 0; i < kM; ++i) {
-                    if (ballot(mine[i] == a) == 0) continue;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (mine[i] == a && r < p.rank) v = *(const uint4*)(p.inner + (m0 + 16 * i + (lane & 15)) * p.rank + r);
-#pragma unroll
-                    for (int j = 0; j < kN; ++j) sum[i][j] = mfma_16(b[j], v, sum[i][j], bf16);
-                }
+                for (int j = 0; j < kN; ++j) sum[j] = mfma_32<kBf16>(b[j], v, sum[j]);
             }
         }
-#pragma unroll
-    for (int i = 0; i < kM; ++i) {
-        const int64_t row = m0 + 16 * i + (lane & 15);
-        if (row >= p.n_rows) continue;
-#pragma unroll
-        for (int j = 0; j < kN; ++j) {
-            const int n = n0 + 16 * j + (lane >> 4) * 4;
-            if (n >= p.n) continue;
-            uint32_t h[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) h[u] = to_16_bits(sum[i][j][u] * power[i], bf16);
-            *(uint2*)((uint16_t*)p.out + row * p.out_stride + n) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-        }
     }
+    project_round<kBf16, kN>(sum, mine.power, out);
 }
 
-// ---------------------------------------------------------------- tiles of 128 x 128
-// Rows and weights pass through the LDS, 64 values of k at a time; four wavefronts have 64 x 64 each.
-__global__ __launch_bounds__(256) void project_tile_kernel(ProjectArgs p)
+template <int kN>
+__device__ inline void project_store(const ProjectArgs& p, const uint4 (&out)[kN][2], int64_t row, int n0)
 {
-    constexpr int kRow = 80;  // bytes of a row in the LDS
-    __shared__ __align__(16) int8_t s_x[128 * kRow], s_w[128 * kRow];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int tiles_n = (p.n + 127) / 128;
-    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * 128;
-    const int n0 = (int)(blockIdx.x % tiles_n) * 128;
-    const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-    int4v dot[4][4] = {};
-    for (int k0 = 0; k0 < p.k; k0 += 64) {
-        uint4 xv[2], wv[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = (i * 256 + tid) >> 2, k = k0 + (tid & 3) * 16;
-            xv[i] = wv[i] = make_uint4(0, 0, 0, 0);
-            if (k < p.k) {
-                xv[i] = *(const uint4*)(p.x + min(m0 + row, (int64_t)p.n_rows - 1) * p.k + k);
-                wv[i] = *(const uint4*)(p.w + (int64_t)min(n0 + row, p.n - 1) * p.k + k);
-            }
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int n = n0 + 32 * j + 16 * g + (threadIdx.x >> 5 & 1) * 8;
+            if (row < p.n_rows && n < p.n) *(uint4*)((uint16_t*)p.out + row * p.out_stride + n) = out[j][g];
         }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = ((i * 256 + tid) >> 2) * kRow + (tid & 3) * 16;
-            *(uint4*)(s_x + at) = xv[i];
-            *(uint4*)(s_w + at) = wv[i];
-        }
-        __syncthreads();
-        int4v xf[4], wf[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            xf[i] = *(const int4v*)(s_x + (wm + i * 16 + (lane & 15)) * kRow + (lane >> 4) * 16);
-            wf[i] = *(const int4v*)(s_w + (wn + i * 16 + (lane & 15)) * kRow + (lane >> 4) * 16);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) dot[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[j], xf[i], dot[i][j], 0, 0, 0);
+}
+
+// ---------------------------------------------------------------- tiles that share rows and weights
+// Rows and weights go from memory to the LDS past the registers, 128 values of k (a step, a memory line of each row) at a time, a
+// step and a half ahead of the products.  Operands of half a step are in registers before its products begin: while one half
+// multiplies, those of the next are read from the LDS.  A row's eight pieces of 16 bytes lie in an order that the row's number
+// gives, so that 16 lanes that read one piece of 16 rows meet all banks.  The last k % 128 values come first, through
+// registers, with zeros behind them.
+// 16 bytes for each lane, from where it points to `to` + 16 * lane (`to` the same in all lanes).
+__device__ inline void load_to_lds(const int8_t* from, int8_t* to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// kWM x kWN wavefronts of kTM x kTN tiles of 32 x 32
+template <bool kBf16, int kWM, int kWN, int kTM, int kTN>
+__global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs p)
+{
+    constexpr int kWaves = kWM * kWN, kBM = kWM * kTM * 32, kBN = kWN * kTN * 32;
+    constexpr int kLoads = (kBM + kBN) / 8 / kWaves;  // of 1024 bytes, a wavefront's of a step
+    static_assert((kBM + kBN) / 8 % kWaves == 0, "a step's loads are shared evenly");
+    __shared__ __align__(1024) int8_t lds[2][(kBM + kBN) * 128];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tiles_n = (p.n + kBN - 1) / kBN, tiles_m = (int)(((int64_t)p.n_rows + kBM - 1) / kBM);
+    // A die's workgroups take neighbouring tiles, eight rows of tiles at a time.
+    int id = blockIdx.x;
+    {
+        const int all = tiles_m * tiles_n, die = id & 7, q = all >> 3, r = all & 7;
+        id = die * q + min(die, r) + (id >> 3);
     }
-    project_finish<4, 4>(p, dot, m0 + wm, n0 + wn);
+    const int group = id / (8 * tiles_n), in = id % (8 * tiles_n), high = min(8, tiles_m - group * 8);
+    const int64_t m0 = (int64_t)(group * 8 + in % high) * kBM;
+    const int n0 = in / high * kBN;
+
+    // what this lane loads: of each eight rows row lane / 8, the piece that lies at place lane % 8
+    const int8_t* from[kLoads];
+    const int steps = (p.k + 127) >> 7, tail = p.k & 127;
+    auto piece_of = [&](int i) { return ((lane & 7) ^ ((((wave * kLoads + i) & 1) * 4 + (lane >> 4)) & 7)) * 16; };
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int first = (wave * kLoads + i) * 8;
+        const bool rows = first < kBM;
+        const int8_t* base = rows ? p.x : p.w;
+        int64_t row = (int64_t)n0 + first - kBM + (lane >> 3);
+        if (rows) row = project_place(p, m0 + first + (lane >> 3));
+        from[i] = base + min(row, (int64_t)(rows ? p.n_rows : p.n) - 1) * p.k + piece_of(i);
+    }
+    if (tail) {
+        uint4 v[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (piece_of(i) < tail) v[i] = *(const uint4*)(from[i] + (p.k - tail));
+            if (piece_of(i) >= p.k) from[i] -= piece_of(i);  // (loads of steps that there are not stay inside the row)
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) *(uint4*)(&lds[0][(wave * kLoads + i) * 1024 + lane * 16]) = v[i];
+    }
+    int ahead = tail ? 1 : 0;  // the step that is loaded next; behind the last one it is loaded again, to where it is not read
+    int on = 0;
+    auto load_one = [&](int i) {
+        load_to_lds(from[i], &lds[ahead & 1][(wave * kLoads + i) * 1024]);
+        from[i] += on;
+    };
+    auto load = [&]() {
+        on = ahead + 1 < steps ? 128 : 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_one(i);
+        ++ahead;
+    };
+    if (!tail) load();
+    load();
+
+    const int wm = wave / kWN * kTM * 32, wn = wave % kWN * kTN * 32;
+    // of row lane % 32 piece lane / 32, of which pieces + 2, + 4, + 6 are those with another bit
+    const int at = (lane & 31) * 128 + (((lane >> 5) ^ ((lane >> 1) & 7)) * 16);
+    struct Operands {
+        int4v x[2][kTM], w[2][kTN];
+    };
+    constexpr int kReads = 2 * (kTM + kTN), kProducts = 2 * kTM * kTN;
+    auto fetch_one = [&](Operands& o, int stage, int half, int r) {
+        const int h = r / (kTM + kTN), i = r % (kTM + kTN);
+        const int8_t* s = &lds[stage][at ^ (half * 64 + h * 32)];
+        if (i < kTM) o.x[h][i] = *(const int4v*)(s + (wm + i * 32) * 128);
+        else o.w[h][i - kTM] = *(const int4v*)(s + (kBM + wn + (i - kTM) * 32) * 128);
+    };
+    int16v dot[kTM][kTN] = {};
+    // The products of half a step, and between them the reads of the next half's operands and, in the second half, the loads of the
+    // step after the next: a wavefront is alone on its SIMD and issues in order, so that loads in a row would leave the
+    // matrix unit without work while they queue.
+    auto half_step = [&](const Operands& now, Operands& next, int stage, int half, bool loads) {
+#pragma unroll
+        for (int m = 0; m < kProducts; ++m) {
+            const int h = m / (kTM * kTN), i = m / kTN % kTM, j = m % kTN;
+            dot[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(now.w[h][j], now.x[h][i], dot[i][j], 0, 0, 0);
+#pragma unroll
+            for (int r = min(kReads, 2 * m * kReads / kProducts); r < min(kReads, 2 * (m + 1) * kReads / kProducts); ++r) fetch_one(next, stage, half, r);
+            if (loads)
+#pragma unroll
+                for (int l = min(kLoads, 2 * m * kLoads / kProducts); l < min(kLoads, 2 * (m + 1) * kLoads / kProducts); ++l) load_one(l);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    Operands a, b;
+    // the first step lies in the LDS
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+#pragma unroll
+    for (int r = 0; r < kReads; ++r) fetch_one(a, 0, 0, r);
+    for (int s = 0; s < steps; ++s) {
+        half_step(a, b, s & 1, 1, false);
+        // the next step lies in the LDS for all wavefronts, and none reads this one any more
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        on = ahead + 1 < steps ? 128 : 0;
+        half_step(b, a, (s + 1) & 1, 0, true);
+        ++ahead;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // All loads come before the first store: a wait for a load would be one for the stores before it too.
+    int64_t at_row[kTM];
+    ProjectRow rows[kTM];
+    float4v ws[kTN][4];
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) {
+        at_row[i] = project_place(p, m0 + wm + 32 * i + (lane & 31));
+        rows[i] = project_row(p, at_row[i]);
+    }
+    project_scales<kTN>(p, ws, n0 + wn);
+    uint4 out[kTM][kTN][2];
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) {
+        project_finish<kBf16, kTN>(p, dot[i], rows[i], ws, at_row[i], n0 + wn, out[i]);
+        __builtin_amdgcn_sched_barrier(0);  // (rows of tiles one after the other: all at once do not fit the registers)
+    }
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) project_store<kTN>(p, out[i], at_row[i], n0 + wn);
+}
+
+// ---------------------------------------------------------------- few rows
+// Up to 32 kTM rows: bound by the weights' way from memory, each read once.  A workgroup has 32 columns; its wavefronts take 64 values of
+// k each in turn, straight into the operands of the matrix instructions, and join their sums in the LDS.  Then each wavefront has a
+// tile and every kShare-th adapter among the rows: it multiplies those, and stores the rows (its lanes) that have one of them.
+constexpr int kFewWaves = 8;
+
+template <bool kBf16, int kTM>
+__global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs p)
+{
+    constexpr int kChunks = 8 / kTM;          // loaded ahead of their products
+    constexpr int kShare = kFewWaves / kTM;   // wavefronts to a tile
+    constexpr int kHeld = 4;                  // operands of adapters (16 ranks x 32 columns) that are loaded ahead
+    __shared__ __align__(16) int32_t s_dot[kFewWaves][kTM][1024];
+    __shared__ __align__(16) uint16_t s_inner[32 * kTM][ST_MAX_RANK + 8];
+    __shared__ float s_power[32 * kTM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = blockIdx.x * 32, n = n0 + (lane & 31);
+    const int8_t* x[kTM];
+    const int8_t* w = p.w + (int64_t)min(n, p.n - 1) * p.k + (lane >> 5) * 32;
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) x[i] = p.x + (int64_t)min(32 * i + (lane & 31), p.n_rows - 1) * p.k + (lane >> 5) * 32;
+    int4v wv[kChunks][2], xv[kChunks][kTM][2];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = k0 + c * (kFewWaves * 64) + h * 16;
+                const bool in = k + (lane >> 5) * 32 < p.k;
+                wv[c][h] = int4v{0, 0, 0, 0};
+                if (in) wv[c][h] = *(const int4v*)(w + k);
+#pragma unroll
+                for (int i = 0; i < kTM; ++i) {
+                    xv[c][i][h] = int4v{0, 0, 0, 0};
+                    if (in) xv[c][i][h] = *(const int4v*)(x[i] + k);
+                }
+            }
+    };
+    load(wave * 64);
+    const int tile = wave / kShare, share = wave % kShare;
+    const int64_t row = 32 * tile + (lane & 31);
+    const float scale = row < p.n_rows ? p.x_scale[row] : 0.0f;
+    const int adapter = p.a ? project_adapter(p, row) : -1;
+    float4v ws[1][4];
+    project_scales<1>(p, ws, n0);
+    // the adapters of the tile's rows: lanes that are the first with theirs, and of those the wavefront's
+    uint32_t left = 0;
+    bool stores = true;
+    const int ranks16 = (p.rank + 15) >> 4;
+    int next = 0, c = 0;  // the adapter and chunk of ranks whose operand comes next; c == ranks16: go on to another
+    uint4 held[kHeld];
+    int held_of[kHeld];
+    auto operand = [&](int a, int at) -> uint4 {
+        const int r = at * 16 + (lane >> 5) * 8;
+        if (n < p.n && r < p.rank) return *(const uint4*)(p.b + ((int64_t)a * p.n + n) * p.rank + r);
+        return make_uint4(0, 0, 0, 0);
+    };
+    auto advance = [&]() -> bool {
+        if (++c < ranks16) return true;
+        if (!left) return false;
+        next = __builtin_amdgcn_readlane(adapter, __builtin_ctz(left));
+        left &= left - 1;
+        c = 0;
+        return true;
+    };
+    if (p.a) {
+        bool again = adapter < 0;
+        int first = lane & 31;  // the first row with this one's adapter
+        for (int i = min(p.n_rows - 32 * tile, 32) - 1; i >= 0; --i)
+            if (__builtin_amdgcn_readlane(adapter, i) == adapter) first = i;
+        again = again || first != (lane & 31);
+        const uint32_t firsts = (uint32_t)ballot(!again);
+        const int index = __builtin_popcount(firsts & ((1u << first) - 1));  // of this row's adapter among them
+        stores = adapter < 0 ? share == 0 : index % kShare == share;
+        left = (uint32_t)ballot(!again && index % kShare == share);
+        c = ranks16 - 1;
+    }
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        held_of[i] = -1;
+        if (p.a && advance()) {
+            held_of[i] = next * 8 + c;
+            held[i] = operand(next, c);
+        }
+    }
+    if (p.a) {
+        // the inner values: their parts summed in order, the power of two of the largest, rounding; kWide threads to a row, two ranks each
+        constexpr int kWide = kFewWaves * 2 / kTM;
+        const int m = tid / kWide, l = tid % kWide;
+        const int i = m < p.n_rows ? project_adapter(p, m) : -1;
+        const float factor = i >= 0 ? p.alpha[i] * p.x_scale[m] : 0.0f;
+        float2 v[ST_MAX_RANK / 2 / kWide];
+        uint32_t top = 0;
+#pragma unroll
+        for (int t = 0; t < ST_MAX_RANK / 2 / kWide; ++t) {
+            const int r = 2 * (t * kWide + l);
+            v[t] = make_float2(0.0f, 0.0f);
+            if (i < 0 || r >= p.rank) continue;
+            float2 u[kInnerParts];
+#pragma unroll
+            for (int q = 0; q < kInnerParts; ++q) u[q] = *(const float2*)(p.parts + ((int64_t)q * p.n_rows + m) * p.rank + r);
+            v[t] = u[0];
+#pragma unroll
+            for (int q = 1; q < kInnerParts; ++q) {
+                v[t].x += u[q].x;
+                v[t].y += u[q].y;
+            }
+            v[t].x *= factor;
+            v[t].y *= factor;
+            top = max(top, max(__float_as_uint(v[t].x) & 0x7FFFFFFFu, __float_as_uint(v[t].y) & 0x7FFFFFFFu));
+        }
+        for (int o = kWide / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        const uint32_t e = project_exponent(top);
+        const float down = __uint_as_float((254u - e) << 23);
+#pragma unroll
+        for (int t = 0; t < ST_MAX_RANK / 2 / kWide; ++t)
+            if (2 * t * kWide < 16 * ranks16) *(uint32_t*)&s_inner[m][2 * (t * kWide + l)] = two_16<kBf16>(v[t].x * down, v[t].y * down);
+        if (l == 0) s_power[m] = i >= 0 ? __uint_as_float(e << 23) : 1.0f;
+    }
+    int16v dot[kTM] = {};
+    for (int k0 = wave * 64; k0 < p.k;) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < kTM; ++i) dot[i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[c][h], xv[c][i][h], dot[i], 0, 0, 0);
+        if ((k0 += kChunks * kFewWaves * 64) < p.k) load(k0);
+    }
+#pragma unroll
+    for (int i = 0; i < kTM; ++i)
+#pragma unroll
+        for (int u = 0; u < 16; ++u) s_dot[wave][i][u * 64 + lane] = dot[i][u];
+    __syncthreads();
+    const float power = p.a ? s_power[row] : 1.0f, down = scale * __uint_as_float(0x7F000000u - __float_as_uint(power));
+    float16v sum[1];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+        int d = 0;
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v) d += s_dot[v][tile][u * 64 + lane];
+        sum[0][u] = (float)d * down * ws[0][u / 4][u % 4];
+    }
+    auto add = [&](int a, int at, const uint4& b) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (adapter == a) v = *(const uint4*)&s_inner[row][at * 16 + (lane >> 5) * 8];
+        sum[0] = mfma_32<kBf16>(b, v, sum[0]);
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if (held_of[i] >= 0) add(held_of[i] >> 3, held_of[i] & 7, held[i]);
+    if (p.a)
+        while (advance()) add(next, c, operand(next, c));
+    uint4 out[1][2];
+    project_round<kBf16, 1>(sum, power, out);
+    project_store<1>(p, out, stores ? row : (int64_t)p.n_rows, n0);
 }
 
 }  // namespace st
