@@ -521,6 +521,11 @@ int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, in
                int32_t dtype, void* dev_out, int64_t out_stride, void* dev_workspace, int64_t workspace_bytes,
                void* hip_stream);
 
+/* Diagnostic, host part alone (no device memory is touched): how st_project would run such a call.  host_out_plan[3] receives {edge of the tiles that
+ * share rows and weights (0: a workgroup takes all rows), rows to a workgroup that sums an adapter's inner values (1: a wavefront to
+ * each part of k; 0: none does, or the kernel of the products does itself), 1 if rows are brought into their adapters' order first}. */
+int st_project_host_plan(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters, int32_t* host_out_plan);
+
 /* Rotary positions on several axes, of the queries and keys of n_tok tokens in one call.  A row of d values begins with
  * `pairs` rotated pairs, pairs = the sum of host_sections: (i, i + pairs), or (2 i, 2 i + 1) where interleaved is not 0; the
  * values behind them stay as they are.  Pair i belongs to axis 0 for i < host_sections[0], then to axis 1, and so on:

@@ -27,7 +27,7 @@ EXPORTS = [
     "st_search_host_plan", "st_search_host_units", "st_stream_read", "st_search_static",
     "st_kv_append", "st_kv_read", "st_kv_attend_workspace_bytes", "st_kv_attend", "st_kv_select_workspace_bytes",
     "st_kv_select", "st_kv_evict", "st_kv_host_plan", "st_kv_copy",
-    "st_norm_rows", "st_project_workspace_bytes", "st_project", "st_rotate",
+    "st_norm_rows", "st_project_workspace_bytes", "st_project", "st_project_host_plan", "st_rotate",
 ]
 
 ST_OP_LEAF, ST_OP_AND, ST_OP_OR, ST_OP_NOT = 0, 1, 2, 3  # operations of a filter program
@@ -132,6 +132,8 @@ def lib() -> C.CDLL:
         L.st_project_workspace_bytes.argtypes = [i32, i32, i32, p]
         L.st_project.restype = C.c_int
         L.st_project.argtypes = [p, p, i32, i32, p, p, i32, p, p, i32, p, i64, p, i64, p]
+        L.st_project_host_plan.restype = C.c_int
+        L.st_project_host_plan.argtypes = [i32, i32, i32, p, p]
         L.st_rotate.restype = C.c_int
         L.st_rotate.argtypes = [p, i64, i32, p, i64, i32, i32, i32, i32, p, p, p, i32, i32, i32, p, i64, p, i64, p]
         _lib = L
@@ -852,19 +854,39 @@ def _here(*tensors):
     """Work runs on the current device's streams: what lies on another device is refused."""
     device = torch.cuda.current_device() if _raw_device is None else _raw_device()
     for t in tensors:
-        if t is not None and t.device.index != device:
+        if t is not None and t.get_device() != device:
             raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{device}")
 
 
-def _layer_rows(t, name: str, dtype=None, shape=None):
-    """Rows [n, d], values of a row side by side; rows may be further apart.  Returns the stride."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _ROW_TYPES and (dtype is None or t.dtype == dtype)):
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _layer_rows(t, name: str, n=None, d=None, dtype=None):
+    """Rows [n, d], values of a row side by side; rows may be further apart.  Returns (n, d, stride, type)."""
+    kind = _ROW_TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if kind is None or (dtype is not None and t.dtype != dtype):
         raise TypeError(f"{name} must be a CUDA tensor of {dtype or 'torch.bfloat16, torch.float16 or torch.float32'}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{name} must be {'[n, d]' if shape is None else list(shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (n is not None and (shape[0] != n or shape[1] != d)):
+        raise ValueError(f"{name} must be {'[n, d]' if n is None else [n, d]}")
+    if stride[1] != 1 and shape[1] > 1:
         raise ValueError(f"the values of a row of {name} must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1], kind
+
+
+def _layer_heads(t, name: str):
+    """Rows [n_tok, heads, d], whole heads side by side; rows may be further apart.  Returns (n_tok, heads, d, stride, type)."""
+    kind = _KV_TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if kind is None:
+        raise TypeError(f"{name} must be a CUDA tensor of torch.bfloat16 or torch.float16")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3:
+        raise ValueError(f"{name} must be [n_tok, heads, d]")
+    n, heads, d = shape
+    if stride[2] != 1 or (heads > 1 and stride[1] != d):
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
+    return n, heads, d, stride[0] if n > 1 else heads * d, kind
 
 
 class NormRows(NamedTuple):
@@ -893,33 +915,35 @@ def st_norm_rows(x, weight=None, residual=None, eps: float = 1e-6, normalise: bo
     too; q False: that alone.  What buffers has room for is written there, and no more."""
     if stream is not None:
         return _on(stream, st_norm_rows, x, weight, residual, eps, normalise, total, q, y, buffers)
-    x_stride = _layer_rows(x, "x")
-    n, d = x.shape
+    n, d, x_stride, kind = _layer_rows(x, "x")
+    dtype = x.dtype
     r_stride = t_stride = 0
     if residual is not None:
-        r_stride = _layer_rows(residual, "residual", x.dtype, (n, d))
+        r_stride = _layer_rows(residual, "residual", n, d, dtype)[2]
     if weight is not None:
-        _need(weight, x.dtype, "weight")
-        if weight.shape != (d,):
+        _need(weight, dtype, "weight")
+        if weight.numel() != d:
             raise ValueError(f"weight must be [{d}]")
     if buffers is None:
-        total = torch.empty((n, d), dtype=x.dtype, device=x.device) if total is None and residual is not None else total
-        out_q, scale, out_y = None, None, torch.empty((n, d), dtype=x.dtype, device=x.device) if y else None
+        total = torch.empty((n, d), dtype=dtype, device=x.device) if total is None and residual is not None else total
+        out_q, scale, out_y = None, None, torch.empty((n, d), dtype=dtype, device=x.device) if y else None
         if q:
             out_q, scale = torch.empty((n, d), dtype=torch.int8, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device)
     else:
         out_q, scale, out_y = buffers.q, buffers.scale, buffers.y
         total = buffers.total if total is None else total
-        for t, shape, dtype, name in ((out_q, (n, d), torch.int8, "q"), (scale, (n,), torch.float32, "scale"), (out_y, (n, d), x.dtype, "y")):
-            if t is not None:
-                _kv_out(t, shape, dtype, name)
+        if out_q is not None:
+            _kv_out(out_q, (n, d), torch.int8, "q")
+            _kv_out(scale, (n,), torch.float32, "scale")
+        if out_y is not None:
+            _kv_out(out_y, (n, d), dtype, "y")
     if total is not None:
-        t_stride = _layer_rows(total, "total", x.dtype, (n, d))
+        t_stride = _layer_rows(total, "total", n, d, dtype)[2]
     if out_q is None and out_y is None and total is None:
         raise ValueError("nothing to write: ask for q, y or total")
     _here(x, residual, weight, total, out_q, scale, out_y)
-    _check(lib().st_norm_rows(x.data_ptr(), x_stride, _dptr(residual), r_stride, _dptr(weight), _ROW_TYPES[x.dtype], n, d, int(normalise),
-                              eps, _dptr(total), t_stride, _dptr(out_q), _dptr(scale), _dptr(out_y), _kv_stream(None)))
+    _check(lib().st_norm_rows(x.data_ptr(), x_stride, _ptr(residual), r_stride, _ptr(weight), kind, n, d, normalise,
+                              eps, _ptr(total), t_stride, _ptr(out_q), _ptr(scale), _ptr(out_y), _kv_stream(None)))
     return NormRows(out_q, scale, total, out_y)
 
 
@@ -966,12 +990,15 @@ def st_project(x, x_scale, w, w_scale, adapters: Adapters | None = None, adapter
     that of out or buffers, or bf16."""
     if stream is not None:
         return _on(stream, st_project, x, x_scale, w, w_scale, adapters, adapter_of, dtype, out, buffers)
-    for t, kind, name in ((x, torch.int8, "x"), (x_scale, torch.float32, "x_scale"), (w, torch.int8, "w"), (w_scale, torch.float32, "w_scale")):
-        _need(t, kind, name)
-    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x_scale.shape != x.shape[:1] or w_scale.shape != w.shape[:1]:
+    _need(x, torch.int8, "x")
+    _need(x_scale, torch.float32, "x_scale")
+    _need(w, torch.int8, "w")
+    _need(w_scale, torch.float32, "w_scale")
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x must be [n_rows, k] and w [n, k]")
+    (rows, k), (n, w_k) = x.shape, w.shape
+    if w_k != k or x_scale.shape != (rows,) or w_scale.shape != (n,):
         raise ValueError("x must be [n_rows, k], w [n, k], with a scale to each row")
-    rows, k = x.shape
-    n = w.shape[0]
     if (adapters is None) != (adapter_of is None):
         raise ValueError("adapters and adapter_of go together")
     if adapters is not None:
@@ -993,12 +1020,20 @@ def st_project(x, x_scale, w, w_scale, adapters: Adapters | None = None, adapter
         raise TypeError("the output is torch.bfloat16 or torch.float16, and of the adapters' type")
     if out is None:
         out = torch.empty((rows, n), dtype=dtype, device=x.device)
-    stride = _layer_rows(out, "out", dtype, (rows, n))
+    stride = _layer_rows(out, "out", rows, n, dtype)[2]
     _here(x, x_scale, w, w_scale, out, work)
     _check(lib().st_project(x.data_ptr(), x_scale.data_ptr(), rows, k, w.data_ptr(), w_scale.data_ptr(), n,
-                            None if adapters is None else adapters._p, _dptr(adapter_of), _KV_TYPES[dtype], out.data_ptr(), stride,
+                            None if adapters is None else adapters._p, _ptr(adapter_of), _KV_TYPES[dtype], out.data_ptr(), stride,
                             work.data_ptr(), nbytes, _kv_stream(None)))
     return out
+
+
+def st_project_host_plan(n_rows: int, k: int, n: int, n_adapters: int = 0, rank: int = 16) -> dict:
+    """How a projection of these sizes would run (no GPU work; see ``include/silvertorch.h``)."""
+    out = np.zeros(3, dtype=np.int32)
+    adapters = C.cast(C.pointer(_AdaptersC(None, None, None, n_adapters, rank)), C.c_void_p) if n_adapters else None
+    _check(lib().st_project_host_plan(n_rows, k, n, adapters, _hptr(out)))
+    return {name: int(v) for name, v in zip(("edge", "inner_rows", "order"), out)}
 
 
 def st_rotate(q, k, positions, freqs, sections, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
@@ -1007,36 +1042,39 @@ def st_rotate(q, k, positions, freqs, sections, interleaved: bool = False, inver
     what to fill (q and k themselves are allowed)."""
     if stream is not None:
         return _on(stream, st_rotate, q, k, positions, freqs, sections, interleaved, inverse, out)
-    some = q if q is not None else k
-    if not isinstance(some, torch.Tensor) or some.dim() != 3:
-        raise ValueError("queries or keys must be given as [n_tok, heads, d]")
-    n_tok, _, d = some.shape
     _need(positions, torch.int32, "positions")
     _need(freqs, torch.float64, "freqs")
-    sections = np.ascontiguousarray(np.asarray(sections, dtype=np.int32))
-    if positions.dim() != 2 or positions.shape[1] != n_tok or sections.shape != positions.shape[:1] or freqs.numel() != int(sections.sum()):
-        raise ValueError(f"positions must be [n_axes, {n_tok}], with a section to each axis and a frequency to each pair")
-    out = (None, None) if out is None else out
-    args, outs, dtype = [], [], None
-    for t, o, name in ((q, out[0], "q"), (k, out[1], "k")):
+    n_tok = d = kind = None
+    args, outs = [], []
+    for t, o, name in ((q, out[0] if out else None, "q"), (k, out[1] if out else None, "k")):
         if t is None:
             if o is not None:
                 raise ValueError(f"an output for {name}, which is not given")
             args.append((None, 0, 0, None, 0))
             outs.append(None)
             continue
-        stride, kind = _kv_rows(t, n_tok, d, name)
-        if dtype is not None and kind != dtype:
-            raise TypeError("queries and keys must be of one type")
-        dtype = kind
+        n, heads, width, stride, dtype = _layer_heads(t, name)
+        if kind is None:
+            n_tok, d, kind = n, width, dtype
+        elif (n, width, dtype) != (n_tok, d, kind):
+            raise ValueError("queries and keys must be of one type, with as many tokens and one width of a head")
         if o is None:
-            o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        if o.dtype != t.dtype or o.shape != t.shape:
-            raise ValueError(f"the output of {name} must be like it")
-        args.append((t.data_ptr(), stride, t.shape[1], o.data_ptr(), _kv_rows(o, n_tok, d, f"output of {name}")[0]))
+            o, o_stride = torch.empty((n, heads, width), dtype=t.dtype, device=t.device), heads * width
+        elif o is t:
+            o_stride = stride
+        else:
+            m, o_heads, o_width, o_stride, o_type = _layer_heads(o, f"output of {name}")
+            if (m, o_heads, o_width, o_type) != (n, heads, width, dtype):
+                raise ValueError(f"the output of {name} must be like it")
+        args.append((t.data_ptr(), stride, heads, o.data_ptr(), o_stride))
         outs.append(o)
+    if kind is None:
+        raise ValueError("queries or keys must be given")
+    n_axes = len(sections)
+    if positions.shape != (n_axes, n_tok) or freqs.numel() != sum(sections):
+        raise ValueError(f"positions must be [n_axes, {n_tok}], with a section to each axis and a frequency to each pair")
     _here(q, k, positions, freqs, *outs)
     (qp, qs, qh, oqp, oqs), (kp, ks, kh, okp, oks) = args
-    _check(lib().st_rotate(qp, qs, qh, kp, ks, kh, d, dtype, n_tok, positions.data_ptr(), freqs.data_ptr(), _hptr(sections), len(sections),
-                           int(interleaved), int(inverse), oqp, oqs, okp, oks, _kv_stream(None)))
+    _check(lib().st_rotate(qp, qs, qh, kp, ks, kh, d, kind, n_tok, positions.data_ptr(), freqs.data_ptr(), (C.c_int32 * n_axes)(*sections), n_axes,
+                           interleaved, inverse, oqp, oqs, okp, oks, _kv_stream(None)))
     return tuple(outs)

@@ -67,7 +67,12 @@ int check_project(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapt
 
 // Rows up to which a workgroup takes all of them.
 constexpr int kFewRows = 64;
-// Adapters from which on rows are brought into their order first.
+// Rows up to which a workgroup that sums inner values takes 16, beyond 32.  Kernel in us, 16 / 32 / 64: 2048 rows, k = 4096, rank 16 9.9 / 11.7 /
+// 17.4; 4096, 1024, 64 14.5 / 13.9 / 18.7; 16384, 4096, 32 57 / 36 / 39.
+constexpr int kOneTileRows = 2048;
+// Adapters from which on rows are brought into their order first.  Calls in us, ordered against as they come: mixed rows 2048, 8 adapters
+// 69 / 95, 4096, 16 adapters of rank 64 34 / 103, 16384, 16 of rank 32 409 / 791, 256, 32 30 / 32; 1001, 5 16.9 / 18.7.  Rows that come in
+// runs pay for it: 1000, 16 adapters 26.7 / 21.9, 16384 385 / 373.
 constexpr int kOrderFrom = 5;
 
 struct ProjectPlan {
@@ -83,18 +88,20 @@ ProjectPlan project_plan(int32_t n_rows, const st_adapters* adapters)
     return {st::round_up(values * 2, 256), words, adapters->n_adapters >= kOrderFrom ? words : 0};
 }
 
-// Edge of the tiles of many rows by an estimate of the call's microseconds: what one workgroup takes alone, or what all take
-// together; 64: tiles x a share of the chip; 128: two workgroups to a compute unit, a last round of them costs about a quarter; 256: whole
-// rounds of one to a compute unit.  Measured with 64 / 128 / 256 (k x n, rows): 4096 x 5120, 512 22.9 / 24.5 / 47, 1024 44 / 35 / 48, 2048
-// 75 / 61 / 56, 4096 144 / 103 / 112, 8192 295 / 208 / 192; 2048 x 2560, 1024 13.3 / 15.7 / 29, 4096 42 / 37 / 33, 8192 79 / 60 / 65; 1024 x
-// 1024, 2048 7.6 / 10.4 / 19, 8192 21.8 / 20.1 / 22.5; 512 x 8192, 512 8.9 / 9.1 / 14.9, 2048 29 / 24 / 24, 8192 109 / 92 / 112.
+// Edge of the tiles of many rows by an estimate of the call's microseconds.  64 (three workgroups to a compute unit): the longer of one
+// workgroup's way alone and its share of all; 128 (two): rounds, and a quarter for the last; 256 (one): whole rounds and the last by how
+// full it is.  Measured with 64 / 128 / 256 (k x n, rows): 4096 x 5120, 256 15.3 / 23.9 / 46, 512 22.6 / 24.4 / 47, 1024 40 / 35 / 48, 2048
+// 71 / 60 / 52, 4096 135 / 101 / 107, 8192 287 / 205 / 182, 16384 561 / 403 / 329; 2048 x 2560, 1024 14.3 / 15.9 / 29, 4096 40 / 36 / 32,
+// 8192 77 / 58 / 64; 1024 x 1024, 2048 7.4 / 10.4 / 19, 8192 22.5 / 18.1 / 22.2; 512 x 8192, 512 9.9 / 8.9 / 15, 2048 29 / 23 / 22, 8192
+// 113 / 91 / 109.
 int project_edge(int32_t n_rows, int32_t k, int32_t n)
 {
     const double steps = (k + 127) / 128;
     auto tiles = [&](int64_t edge) { return (double)((n_rows + edge - 1) / edge * ((n + edge - 1) / edge)); };
-    const double c64 = std::max(3 + 0.45 * steps, tiles(64) * (0.0035 + 0.00078 * steps));
+    const double c64 = std::max(3.5 + 0.24 * steps, 4 + tiles(64) * (0.0035 + 0.00078 * steps));
     const double c128 = std::max(6 + 0.55 * steps, (tiles(128) / (2 * st::kComputeUnits) + 0.25) * (6 + 1.05 * steps));
-    const double c256 = std::ceil(tiles(256) / st::kComputeUnits) * std::max(23.0, 12 + 1.35 * steps);
+    const double all = tiles(256) / st::kComputeUnits, full = std::floor(all), last = all - full;
+    const double c256 = full * std::max(23.0, 12 + 1.55 * steps) + (last > 0 ? std::max(18.0, 8 + (1.25 + 0.3 * last) * steps) : 0);
     return c64 <= c128 && c64 <= c256 ? 64 : c128 <= c256 ? 128 : 256;
 }
 
@@ -110,30 +117,47 @@ void launch_inner(const st::ProjectArgs& p, hipStream_t stream)
     else hipLaunchKernelGGL((st::project_inner_kernel<kBf16, 8, kM>), groups, threads, 0, stream, p);
 }
 
-template <bool kBf16>
-void launch_project(const st::ProjectArgs& p, int edge, unsigned tiles, hipStream_t stream)
+// What a call runs: a function of its sizes alone.
+struct ProjectRoute {
+    bool few, fused;  // few: a workgroup takes all rows; fused: it sums the inner values too
+    int edge;         // of the tiles where there are many
+    bool order;
+    int64_t tiles;
+};
+
+ProjectRoute project_route(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters)
 {
-    if (p.a) {
+    ProjectRoute r;
+    r.few = n_rows <= kFewRows;
+    const int64_t ranks = adapters ? (int64_t)n_rows * ((adapters->rank + 15) / 16 * 16) : 0;
+    r.fused = adapters && ranks <= st::kFusedRanks && ranks * k <= st::kFusedValues;
+    r.edge = project_edge(n_rows, k, n);
+    r.order = adapters && !r.few && adapters->n_adapters >= kOrderFrom;
+    r.tiles = r.few ? (n + 31) / 32 : ((int64_t)n_rows + r.edge - 1) / r.edge * ((n + r.edge - 1) / r.edge);
+    return r;
+}
+
+template <bool kBf16>
+void launch_project(const st::ProjectArgs& p, const ProjectRoute& r, hipStream_t stream)
+{
+    if (p.a && !r.fused) {
         TimedLaunch t(1, stream);
         if (p.order)
             hipLaunchKernelGGL(st::project_order_kernel, dim3((unsigned)((p.n_rows + (int64_t)st::kOrderRows - 1) / st::kOrderRows)), dim3(st::kOrderThreads), 0, stream, p);
-        if (p.n_rows <= kFewRows)
+        if (r.few)
             hipLaunchKernelGGL((st::project_parts_kernel<kBf16>), dim3((unsigned)((p.n_rows + 15) / 16), (unsigned)std::min({p.n_adapters, p.n_rows, 16}),
                                                                        (unsigned)((p.rank + 15) / 16 * st::kInnerParts)), dim3(64), 0, stream, p);
-        else if (p.n_rows <= 2048) launch_inner<kBf16, 1>(p, stream);
-        else launch_inner<kBf16, 4>(p, stream);
+        else if (p.n_rows <= kOneTileRows) launch_inner<kBf16, 1>(p, stream);
+        else launch_inner<kBf16, 2>(p, stream);
     }
     TimedLaunch t(0, stream);
-    if (p.n_rows <= kFewRows) {
-        const dim3 groups((unsigned)((p.n + 31) / 32)), threads(st::kFewWaves * 64);
-        if (p.n_rows <= 32) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 1>), groups, threads, 0, stream, p);
-        else hipLaunchKernelGGL((st::project_few_kernel<kBf16, 2>), groups, threads, 0, stream, p);
-        return;
-    }
-    const dim3 groups(tiles);
-    if (edge == 64) hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 2, 1, 1>), groups, dim3(256), 0, stream, p);
-    else if (edge == 128) hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 2, 2, 2>), groups, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 4, 4, 2>), groups, dim3(512), 0, stream, p);
+    const dim3 groups((unsigned)r.tiles), few(st::kFewWaves * 64);
+    if (r.fused) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 1, true>), groups, few, 0, stream, p);
+    else if (r.few && p.n_rows <= 32) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 1, false>), groups, few, 0, stream, p);
+    else if (r.few) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 2, false>), groups, few, 0, stream, p);
+    else if (r.edge == 64) hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 2, 1, 1, 3>), groups, dim3(256), 0, stream, p);
+    else if (r.edge == 128) hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 2, 2, 2, 2>), groups, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((st::project_tile_kernel<kBf16, 2, 4, 4, 2, 2>), groups, dim3(512), 0, stream, p);
 }
 
 }  // namespace
@@ -206,13 +230,26 @@ int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, in
         p.n_adapters = adapters->n_adapters;
         p.rank = adapters->rank;
     }
-    const int edge = project_edge(n_rows, k, n);
-    const int64_t tiles = ((int64_t)n_rows + edge - 1) / edge * ((n + edge - 1) / edge);
-    if ((rc = check_grid(tiles)) || (rc = check_grid(((int64_t)n_rows + 15) / 16))) return rc;
+    const ProjectRoute route = project_route(n_rows, k, n, adapters);
+    if ((rc = check_grid(route.tiles)) || (rc = check_grid(((int64_t)n_rows + 15) / 16))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
-    if (dtype == ST_BF16) launch_project<true>(p, edge, (unsigned)tiles, stream);
-    else launch_project<false>(p, edge, (unsigned)tiles, stream);
+    if (dtype == ST_BF16) launch_project<true>(p, route, stream);
+    else launch_project<false>(p, route, stream);
     ST_HIP(hipGetLastError());
+    return ST_OK;
+    });
+}
+
+int st_project_host_plan(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters, int32_t* host_out_plan)
+{
+    return guarded([&]() -> int {
+    int rc;
+    if (!host_out_plan) return fail(ST_EINVAL, "null argument");
+    if ((rc = check_project(n_rows, k, n, adapters))) return rc;
+    const ProjectRoute r = project_route(n_rows, k, n, adapters);
+    host_out_plan[0] = r.few ? 0 : r.edge;
+    host_out_plan[1] = !adapters || r.fused ? 0 : r.few ? 1 : n_rows <= kOneTileRows ? 16 : 32;
+    host_out_plan[2] = r.order;
     return ST_OK;
     });
 }
@@ -263,19 +300,27 @@ int st_rotate(const void* dev_q, int64_t q_stride, int32_t n_q_heads, const void
     a.n_axes = n_axes;
     a.positions = dev_positions;
     a.freqs = dev_freqs;
-    a.bf16 = dtype == ST_BF16;
-    a.interleaved = interleaved != 0;
     a.inverse = inverse != 0;
-    a.columns = a.pairs / 8 + (d - 2 * a.pairs) / 8;
-    const int heads = n_q_heads + n_k_heads;
-    a.head_parts = std::max(1, heads / 4);
-    const int64_t groups = ((int64_t)n_tok * a.columns * a.head_parts + st::kLayerThreads - 1) / st::kLayerThreads;
-    if ((rc = check_grid(groups))) return rc;
+    a.columns = a.pairs / 8 + (d - 2 * a.pairs + 15) / 16;
+    const int64_t groups = ((int64_t)n_tok * a.columns + st::kLayerThreads - 1) / st::kLayerThreads;
+    // Heads to a thread: fewer where all would leave the chip idle.
+    const bool many = groups * ((n_q_heads + 7) / 8 + (n_k_heads + 7) / 8) >= 4 * st::kComputeUnits;
+    const int each = many ? 8 : 2;
+    a.parts[0] = (n_q_heads + each - 1) / each;
+    a.parts[1] = (n_k_heads + each - 1) / each;
+    if (a.parts[0] + a.parts[1] > 65535) return fail(ST_EINVAL, "too many heads for one call");
+    if ((rc = check_grid(groups * (a.parts[0] + a.parts[1])))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
-    {
+    const auto launch = [&](auto bf16, auto pairs) {
+        const dim3 grid((unsigned)groups, (unsigned)(a.parts[0] + a.parts[1])), threads(st::kLayerThreads);
         TimedLaunch t(0, stream);
-        hipLaunchKernelGGL(st::rotate_kernel, dim3((unsigned)groups), dim3(st::kLayerThreads), 0, stream, a);
-    }
+        if (many) hipLaunchKernelGGL((st::rotate_kernel<decltype(bf16)::value, decltype(pairs)::value, 8>), grid, threads, 0, stream, a);
+        else hipLaunchKernelGGL((st::rotate_kernel<decltype(bf16)::value, decltype(pairs)::value, 2>), grid, threads, 0, stream, a);
+    };
+    const auto yes = std::true_type();
+    const auto no = std::false_type();
+    if (dtype == ST_BF16) interleaved ? launch(yes, yes) : launch(yes, no);
+    else interleaved ? launch(no, yes) : launch(no, no);
     ST_HIP(hipGetLastError());
     return ST_OK;
     });

@@ -229,29 +229,41 @@ struct RotateArgs {
     int32_t ends[kAxes];  // pairs of the axes so far
     const int32_t* positions;
     const double* freqs;
-    int32_t bf16, interleaved, inverse, head_parts, columns;  // columns: threads to a token and part of the heads
+    int32_t inverse, parts[2], columns;  // parts: of the heads of queries and keys; columns: threads to a token and part
 };
 
-// A thread takes eight pairs of a token (or eight values that are not rotated) through all heads of its part: their cos and sin
-// are formed once.
+// A thread takes eight pairs of a token (or 16 values that are not rotated) through kHeads heads: all loads first, then cos and sin, formed once,
+// then the products.  Turns are counted in fp64, of which the fraction goes to the hardware's cos and sin of turns.
+template <bool kBf16, bool kInterleaved, int kHeads>
 __global__ __launch_bounds__(kLayerThreads) void rotate_kernel(RotateArgs a)
 {
     const int64_t at = (int64_t)blockIdx.x * kLayerThreads + threadIdx.x;
     const int column = (int)(at % a.columns);
-    const int64_t rest = at / a.columns;
-    const int part = (int)(rest % a.head_parts);
-    const int64_t tok = rest / a.head_parts;
+    const int64_t tok = at / a.columns;
     if (tok >= a.n_tok) return;
-    const int heads = a.heads[0] + a.heads[1];
-    const int first = (int)((int64_t)heads * part / a.head_parts), last = (int)((int64_t)heads * (part + 1) / a.head_parts);
-    const bool bf16 = a.bf16 != 0;
-    if (column >= a.pairs / 8) {  // values behind the pairs
-        const int c = 2 * a.pairs + (column - a.pairs / 8) * 8;
-        for (int i = first; i < last; ++i) {
-            const int k = i >= a.heads[0], h = k ? i - a.heads[0] : i;
-            if (a.out[k] == a.in[k]) continue;
-            *(uint4*)(a.out[k] + tok * a.out_stride[k] + (int64_t)h * a.d + c) = *(const uint4*)(a.in[k] + tok * a.in_stride[k] + (int64_t)h * a.d + c);
+    const int k = (int)blockIdx.y >= a.parts[0], first = ((int)blockIdx.y - (k ? a.parts[0] : 0)) * kHeads;
+    const int n = min(kHeads, a.heads[k] - first);
+    const uint16_t* in = a.in[k] + tok * a.in_stride[k] + (int64_t)first * a.d;
+    uint16_t* out = a.out[k] + tok * a.out_stride[k] + (int64_t)first * a.d;
+    const bool turns = column < a.pairs / 8;
+    const int plain = 2 * a.pairs + (column - a.pairs / 8) * 16;  // (the second eight values may lie behind the row)
+    const int c0 = !turns ? plain : kInterleaved ? column * 16 : column * 8;
+    const int c1 = !turns ? min(plain + 8, a.d - 8) : kInterleaved ? c0 + 8 : c0 + a.pairs;
+    if (!turns && in == out) return;
+    uint4 v[kHeads][2];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+        if (h < n) {
+            v[h][0] = *(const uint4*)(in + (int64_t)h * a.d + c0);
+            v[h][1] = *(const uint4*)(in + (int64_t)h * a.d + c1);
         }
+    if (!turns) {
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h)
+            if (h < n) {
+                *(uint4*)(out + (int64_t)h * a.d + c0) = v[h][0];
+                *(uint4*)(out + (int64_t)h * a.d + c1) = v[h][1];
+            }
         return;
     }
     float cs[8], sn[8];
@@ -260,34 +272,26 @@ __global__ __launch_bounds__(kLayerThreads) void rotate_kernel(RotateArgs a)
         const int pair = column * 8 + u;
         int axis = 0;
         for (int e = 0; e < a.n_axes - 1; ++e) axis += pair >= a.ends[e];
-        const double turns = (double)a.positions[(int64_t)axis * a.n_tok + tok] * (a.freqs[pair] * 0.15915494309189533577);
-        const float turn = (float)(turns - rint(turns));
+        const double t = (double)a.positions[(int64_t)axis * a.n_tok + tok] * (a.freqs[pair] * 0.15915494309189533577);
+        const float turn = (float)(t - rint(t));
         cs[u] = __builtin_amdgcn_cosf(turn);
         sn[u] = __builtin_amdgcn_sinf(a.inverse ? -turn : turn);
     }
-    const int c0 = a.interleaved ? column * 16 : column * 8, c1 = a.interleaved ? c0 + 8 : c0 + a.pairs;
-    for (int i = first; i < last; ++i) {
-        const int k = i >= a.heads[0], h = k ? i - a.heads[0] : i;
-        const uint16_t* in = a.in[k] + tok * a.in_stride[k] + (int64_t)h * a.d;
-        uint16_t* out = a.out[k] + tok * a.out_stride[k] + (int64_t)h * a.d;
-        float f[16], g[16];
-        eight_floats(*(const uint4*)(in + c0), bf16, f);
-        eight_floats(*(const uint4*)(in + c1), bf16, f + 8);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float x = a.interleaved ? f[2 * u] : f[u], y = a.interleaved ? f[2 * u + 1] : f[8 + u];
-            const float p = x * cs[u] - y * sn[u], q = x * sn[u] + y * cs[u];
-            g[a.interleaved ? 2 * u : u] = p;
-            g[a.interleaved ? 2 * u + 1 : 8 + u] = q;
+    for (int h = 0; h < kHeads; ++h)
+        if (h < n) {
+            float f[16], g[16];
+            eight_floats(v[h][0], kBf16, f);
+            eight_floats(v[h][1], kBf16, f + 8);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int x = kInterleaved ? 2 * u : u, y = kInterleaved ? 2 * u + 1 : 8 + u;
+                g[x] = f[x] * cs[u] - f[y] * sn[u];
+                g[y] = f[x] * sn[u] + f[y] * cs[u];
+            }
+            Eight<kBf16 ? ST_BF16 : ST_F16>::store(out, (int64_t)h * a.d + c0, g);
+            Eight<kBf16 ? ST_BF16 : ST_F16>::store(out, (int64_t)h * a.d + c1, g + 8);
         }
-        if (bf16) {
-            Eight<ST_BF16>::store(out, c0, g);
-            Eight<ST_BF16>::store(out, c1, g + 8);
-        } else {
-            Eight<ST_F16>::store(out, c0, g);
-            Eight<ST_F16>::store(out, c1, g + 8);
-        }
-    }
 }
 
 }  // namespace st

@@ -150,51 +150,52 @@ constexpr int kInnerParts = 8;
 
 // What one wavefront does for 16 kM rows, an adapter, kTiles x 16 of its ranks and a part of k: the 64 values from 64 (part + 8 i) on,
 // i = 0, 1, ..  `wa`: the lane's row and place in a, `ranks`: how many of the ranks there are.  Loads of kChunks of those run ahead.
-template <bool kBf16, int kTiles, int kM>
+template <bool kBf16, int kTiles, int kM, int kRegisters = 96>
 struct InnerPart {
-    static constexpr int kFit = 96 / (kTiles * 8 + kM * 4), kChunks = kFit < 1 ? 1 : kFit > 8 ? 8 : kFit;
-    uint4 xv[kChunks][kM];
+    static constexpr int kFit = kRegisters / (kTiles * 8 + kM * 4), kChunks = kFit < 1 ? 1 : kFit > 8 ? 8 : kFit;
+    uint4 xv[kChunks][kM], av[kChunks][kTiles][2];
     float4v acc[kM][kTiles];
 
-    __device__ void load_x(const int8_t* const (&x)[kM], int k0, int k_end)
+    __device__ void load_x(const int8_t* const (&x)[kM], int c, int k, int k_end)
     {
+        const bool in = k + (int)((threadIdx.x & 63) >> 4) * 16 < k_end;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int k = k0 + c * (kInnerParts * 64);
-            const bool in = k + (int)((threadIdx.x & 63) >> 4) * 16 < k_end;
+        for (int i = 0; i < kM; ++i) {
+            xv[c][i] = make_uint4(0, 0, 0, 0);
+            if (in) xv[c][i] = *(const uint4*)(x[i] + k);
+        }
+    }
+    __device__ void load_a(const uint16_t* wa, int ranks, int c, int k, int k_end)
+    {
+        const int lane = threadIdx.x & 63;
+        const bool in = k + (lane >> 4) * 16 < k_end;
 #pragma unroll
-            for (int i = 0; i < kM; ++i) {
-                xv[c][i] = make_uint4(0, 0, 0, 0);
-                if (in) xv[c][i] = *(const uint4*)(x[i] + k);
+        for (int t = 0; t < kTiles; ++t) {
+            av[c][t][0] = av[c][t][1] = make_uint4(0, 0, 0, 0);
+            if (in && t * 16 + (lane & 15) < ranks) {
+                av[c][t][0] = *(const uint4*)(wa + (int64_t)t * 16 * k_end + k);
+                av[c][t][1] = *(const uint4*)(wa + (int64_t)t * 16 * k_end + k + 8);
             }
         }
     }
-    // The first chunks of x are there.
+    __device__ void first_x(const int8_t* const (&x)[kM], int part, int k_end)
+    {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) load_x(x, c, (part + c * kInnerParts) * 64, k_end);
+    }
+    // The first chunks of x are there.  A chunk's registers take on a later one as soon as its products are under way.
     __device__ void run(const int8_t* const (&x)[kM], const uint16_t* wa, int ranks, int part, int k_end)
     {
-        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < kM; ++i)
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) acc[i][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k0 = part * 64; k0 < k_end; k0 += kChunks * kInnerParts * 64) {
-            uint4 av[kChunks][kTiles][2];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) load_a(wa, ranks, c, (part + c * kInnerParts) * 64, k_end);
+        for (int k0 = part * 64; k0 < k_end; k0 += kChunks * kInnerParts * 64)
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
-                const int k = k0 + c * (kInnerParts * 64);
-                const bool in = k + (lane >> 4) * 16 < k_end;
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    av[c][t][0] = av[c][t][1] = make_uint4(0, 0, 0, 0);
-                    if (in && t * 16 + (lane & 15) < ranks) {
-                        av[c][t][0] = *(const uint4*)(wa + (int64_t)t * 16 * k_end + k);
-                        av[c][t][1] = *(const uint4*)(wa + (int64_t)t * 16 * k_end + k + 8);
-                    }
-                }
-            }
-            if (k0 != part * 64) load_x(x, k0, k_end);
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
+                if (k0 + c * kInnerParts * 64 >= k_end) break;  // (its registers were not loaded again)
 #pragma unroll
                 for (int i = 0; i < kM; ++i) {
                     const uint4 x0 = eight_16<kBf16>(xv[c][i].x, xv[c][i].y), x1 = eight_16<kBf16>(xv[c][i].z, xv[c][i].w);
@@ -204,7 +205,12 @@ struct InnerPart {
                         acc[i][t] = mfma_16<kBf16>(av[c][t][1], x1, acc[i][t]);
                     }
                 }
-        }
+                const int k = k0 + (kChunks + c) * kInnerParts * 64;
+                if (k < k_end) {
+                    load_x(x, c, k, k_end);
+                    load_a(wa, ranks, c, k, k_end);
+                }
+            }
     }
 };
 
@@ -243,11 +249,11 @@ __global__ __launch_bounds__(kInnerParts * 64) void project_inner_kernel(Project
         of[i] = project_adapter(p, row[i]);
         scale[i] = row[i] < p.n_rows ? p.x_scale[row[i]] : 0.0f;
     }
-    InnerPart<kBf16, kTiles, kM> inner;
+    InnerPart<kBf16, kTiles, kM, kM == 1 ? 96 : 48> inner;
     int index = 0;
     for (int a = next_of<16>(mine, -1); a != 0x7FFFFFFF; a = next_of<16>(mine, a), ++index) {
         if (index % gridDim.y != blockIdx.y) continue;
-        inner.load_x(x, part * 64, p.k);
+        inner.first_x(x, part, p.k);
         const float alpha = p.alpha[a];
         inner.run(x, p.a + ((int64_t)a * p.rank + (lane & 15)) * p.k + (lane >> 4) * 16, p.rank, part, p.k);
         constexpr int kEach = (kRanks + 31) / 32;
@@ -301,7 +307,7 @@ __global__ __launch_bounds__(64) void project_parts_kernel(ProjectArgs p)
     const int8_t* x[1] = {p.x + (int64_t)min(row, p.n_rows - 1) * p.k + (lane >> 4) * 16};
     const int mine[1] = {project_adapter(p, row)};
     InnerPart<kBf16, 1, 1> inner;
-    inner.load_x(x, part * 64, p.k);
+    inner.first_x(x, part, p.k);
     int a = next_of<16>(mine, -1);
     for (int i = 0; i < (int)blockIdx.y && a != 0x7FFFFFFF; ++i) a = next_of<16>(mine, a);
     if (a == 0x7FFFFFFF) return;
@@ -416,25 +422,32 @@ __device__ inline void project_store(const ProjectArgs& p, const uint4 (&out)[kN
 }
 
 // ---------------------------------------------------------------- tiles that share rows and weights
-// Rows and weights go from memory to the LDS past the registers, 128 values of k (a step, a memory line of each row) at a time, a
-// step and a half ahead of the products.  Operands of half a step are in registers before its products begin: while one half
-// multiplies, those of the next are read from the LDS.  A row's eight pieces of 16 bytes lie in an order that the row's number
-// gives, so that 16 lanes that read one piece of 16 rows meet all banks.  The last k % 128 values come first, through
-// registers, with zeros behind them.
+// Rows and weights go from memory to the LDS past the registers, 128 values of k (a step, a memory line of each row) at a time,
+// kStages - 1 steps ahead of the products at most.  Operands of half a step are in registers before its products begin: while one
+// half multiplies, those of the next are read from the LDS.  A row's eight pieces of 16 bytes lie in an order that the row's
+// number gives, so that 16 lanes that read one piece of 16 rows meet all banks (no conflicts counted).  The last k % 128 values
+// come first, through registers, with zeros behind them.
+//
+// Bound by the matrix units and, with the whole chip at work, by its power: 8192 x 8192 x 8192 takes 511 us (2150 TOP/s), the products
+// alone 334, without loads 423, without reads of the LDS 457 (the clock is at 1.8 GHz then, 2.4 with a tenth of the chip, where a
+// step of 256 x 256 takes 1.02 us and its products 0.85).  16384 x 4096 x 5120: 323 us, 2130 TOP/s.  Tried: four wavefronts with 128 x 128 each
+// (345 us; fewer reads, but a SIMD waits with its only wavefront), steps of 64 values with four and five stages (356), tiles of
+// 256 x 128 (498), loads and reads in the first half of the products between which they stand (327).
 // 16 bytes for each lane, from where it points to `to` + 16 * lane (`to` the same in all lanes).
 __device__ inline void load_to_lds(const int8_t* from, int8_t* to)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// kWM x kWN wavefronts of kTM x kTN tiles of 32 x 32
-template <bool kBf16, int kWM, int kWN, int kTM, int kTN>
+// kWM x kWN wavefronts of kTM x kTN tiles of 32 x 32, kStages steps in the LDS
+template <bool kBf16, int kWM, int kWN, int kTM, int kTN, int kStages>
 __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs p)
 {
-    constexpr int kWaves = kWM * kWN, kBM = kWM * kTM * 32, kBN = kWN * kTN * 32;
+    constexpr int kWaves = kWM * kWN, kBM = kWM * kTM * 32, kBN = kWN * kTN * 32, kStage = (kBM + kBN) * 128;
     constexpr int kLoads = (kBM + kBN) / 8 / kWaves;  // of 1024 bytes, a wavefront's of a step
     static_assert((kBM + kBN) / 8 % kWaves == 0, "a step's loads are shared evenly");
-    __shared__ __align__(1024) int8_t lds[2][(kBM + kBN) * 128];
+    static_assert((kStages - 1) * kLoads <= 63, "loads in flight are counted in six bits");
+    __shared__ __align__(1024) int8_t lds[kStages * kStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles_n = (p.n + kBN - 1) / kBN, tiles_m = (int)(((int64_t)p.n_rows + kBM - 1) / kBM);
     // A die's workgroups take neighbouring tiles, eight rows of tiles at a time.
@@ -447,10 +460,12 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
     const int64_t m0 = (int64_t)(group * 8 + in % high) * kBM;
     const int n0 = in / high * kBN;
 
+    // The place of a row's piece in the row's 128 bytes: 16 neighbouring rows have a piece at 16 places of the banks.
+    auto place = [](int row, int piece) { return piece ^ ((row >> 1) & 7); };
     // what this lane loads: of each eight rows row lane / 8, the piece that lies at place lane % 8
     const int8_t* from[kLoads];
     const int steps = (p.k + 127) >> 7, tail = p.k & 127;
-    auto piece_of = [&](int i) { return ((lane & 7) ^ ((((wave * kLoads + i) & 1) * 4 + (lane >> 4)) & 7)) * 16; };
+    auto piece_of = [&](int i) { return place((wave * kLoads + i) * 8 + (lane >> 3), lane & 7) * 16; };
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
         const int first = (wave * kLoads + i) * 8;
@@ -469,65 +484,69 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
             if (piece_of(i) >= p.k) from[i] -= piece_of(i);  // (loads of steps that there are not stay inside the row)
         }
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) *(uint4*)(&lds[0][(wave * kLoads + i) * 1024 + lane * 16]) = v[i];
+        for (int i = 0; i < kLoads; ++i) *(uint4*)(lds + (wave * kLoads + i) * 1024 + lane * 16) = v[i];
     }
     int ahead = tail ? 1 : 0;  // the step that is loaded next; behind the last one it is loaded again, to where it is not read
-    int on = 0;
+    int to = ahead, on = 0;    // its stage
     auto load_one = [&](int i) {
-        load_to_lds(from[i], &lds[ahead & 1][(wave * kLoads + i) * 1024]);
+        load_to_lds(from[i], lds + to * kStage + (wave * kLoads + i) * 1024);
         from[i] += on;
     };
-    auto load = [&]() {
+    auto loaded = [&]() {
+        ++ahead;
+        to = to + 1 == kStages ? 0 : to + 1;
         on = ahead + 1 < steps ? 128 : 0;
+    };
+    on = ahead + 1 < steps ? 128 : 0;
+    for (int s = ahead; s < kStages; ++s) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) load_one(i);
-        ++ahead;
-    };
-    if (!tail) load();
-    load();
+        loaded();
+    }
 
     const int wm = wave / kWN * kTM * 32, wn = wave % kWN * kTN * 32;
     // of row lane % 32 piece lane / 32, of which pieces + 2, + 4, + 6 are those with another bit
-    const int at = (lane & 31) * 128 + (((lane >> 5) ^ ((lane >> 1) & 7)) * 16);
+    const int at = (lane & 31) * 128 + place(lane & 31, lane >> 5) * 16;
     struct Operands {
         int4v x[2][kTM], w[2][kTN];
     };
     constexpr int kReads = 2 * (kTM + kTN), kProducts = 2 * kTM * kTN;
     auto fetch_one = [&](Operands& o, int stage, int half, int r) {
         const int h = r / (kTM + kTN), i = r % (kTM + kTN);
-        const int8_t* s = &lds[stage][at ^ (half * 64 + h * 32)];
+        const int8_t* s = lds + stage * kStage + (at ^ (half * 64 + h * 32));
         if (i < kTM) o.x[h][i] = *(const int4v*)(s + (wm + i * 32) * 128);
         else o.w[h][i - kTM] = *(const int4v*)(s + (kBM + wn + (i - kTM) * 32) * 128);
     };
     int16v dot[kTM][kTN] = {};
-    // The products of half a step, and between them the reads of the next half's operands and, in the second half, the loads of the
-    // step after the next: a wavefront is alone on its SIMD and issues in order, so that loads in a row would leave the
-    // matrix unit without work while they queue.
+    // The products of 64 values of k, and between them the reads of the next 64's operands and loads of a later step: a wavefront has its
+    // SIMD with one other at most and issues in order, so that loads in a row would leave the matrix unit without work
+    // while they queue.
     auto half_step = [&](const Operands& now, Operands& next, int stage, int half, bool loads) {
 #pragma unroll
         for (int m = 0; m < kProducts; ++m) {
             const int h = m / (kTM * kTN), i = m / kTN % kTM, j = m % kTN;
             dot[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(now.w[h][j], now.x[h][i], dot[i][j], 0, 0, 0);
 #pragma unroll
-            for (int r = min(kReads, 2 * m * kReads / kProducts); r < min(kReads, 2 * (m + 1) * kReads / kProducts); ++r) fetch_one(next, stage, half, r);
+            for (int r = m * kReads / kProducts; r < (m + 1) * kReads / kProducts; ++r) fetch_one(next, stage, half, r);
             if (loads)
 #pragma unroll
-                for (int l = min(kLoads, 2 * m * kLoads / kProducts); l < min(kLoads, 2 * (m + 1) * kLoads / kProducts); ++l) load_one(l);
+                for (int l = m * kLoads / kProducts; l < (m + 1) * kLoads / kProducts; ++l) load_one(l);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     Operands a, b;
     // the first step lies in the LDS
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 1) * kLoads) : "memory");
 #pragma unroll
     for (int r = 0; r < kReads; ++r) fetch_one(a, 0, 0, r);
+    int stage = 0;
     for (int s = 0; s < steps; ++s) {
-        half_step(a, b, s & 1, 1, false);
+        half_step(a, b, stage, 1, false);
         // the next step lies in the LDS for all wavefronts, and none reads this one any more
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        on = ahead + 1 < steps ? 128 : 0;
-        half_step(b, a, (s + 1) & 1, 0, true);
-        ++ahead;
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        half_step(b, a, stage, 0, true);
+        loaded();
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // All loads come before the first store: a wait for a load would be one for the stores before it too.
@@ -556,39 +575,65 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
 // tile and every kShare-th adapter among the rows: it multiplies those, and stores the rows (its lanes) that have one of them.
 constexpr int kFewWaves = 8;
 
-template <bool kBf16, int kTM>
+// kWithInner: the adapters' inner values are summed here too, by each workgroup for itself, a part of k by each wavefront: one launch
+// where the rows' adapters have up to kFusedRanks ranks in all and few values (rank 16, one row, from 512 values: a call 7.0 us against 9.9 with a
+// kernel of their own, from 4096 14.6 against 12.7; rank 32, from 4096: 18.5 and 13.5).
+constexpr int kFusedRanks = 32, kFusedValues = 32768;  // ranks times k
+
+template <bool kBf16, int kTM, bool kWithInner>
 __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs p)
 {
-    constexpr int kChunks = 8 / kTM;          // loaded ahead of their products
+    static_assert(kFewWaves == kInnerParts, "a wavefront to each part of k");
+    static_assert(!kWithInner || kTM == 1, "few rows");
+    constexpr int kRows = 32 * kTM + 32, kLoads = kRows / 4 / kFewWaves;  // of a step, and loads of 1024 bytes of a wavefront
+    constexpr int kStages = kTM == 1 ? 4 : 5;
     constexpr int kShare = kFewWaves / kTM;   // wavefronts to a tile
     constexpr int kHeld = 4;                  // operands of adapters (16 ranks x 32 columns) that are loaded ahead
-    __shared__ __align__(16) int32_t s_dot[kFewWaves][kTM][1024];
-    __shared__ __align__(16) uint16_t s_inner[32 * kTM][ST_MAX_RANK + 8];
-    __shared__ float s_power[32 * kTM];
+    constexpr int kInner = kStages * kRows * 256, kInnerRow = ST_MAX_RANK + 8, kPower = kInner + 32 * kTM * kInnerRow * 2;
+    constexpr int kParts = kPower + 32 * kTM * 4;
+    // (one array for all: beside another the compiler has the reads of a step wait for the loads of later ones)
+    __shared__ __align__(1024) int8_t lds[kParts + (kWithInner ? kInnerParts * kFusedRanks * 4 : 0)];
+    static_assert(kInner >= kFewWaves * kTM * 4096, "the sums take the place of the steps");
+    int32_t(*s_dot)[kTM][1024] = (int32_t(*)[kTM][1024])lds;
+    uint16_t(*s_inner)[kInnerRow] = (uint16_t(*)[kInnerRow])(lds + kInner);
+    float* s_power = (float*)(lds + kPower);
+    float* s_parts = (float*)(lds + kParts);  // [part][row][rank]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = blockIdx.x * 32, n = n0 + (lane & 31);
-    const int8_t* x[kTM];
-    const int8_t* w = p.w + (int64_t)min(n, p.n - 1) * p.k + (lane >> 5) * 32;
+    // what this lane loads: of each four rows row lane / 16, the piece that lies at place lane % 16
+    const int8_t* from[kLoads];
+    const int steps = (p.k + 255) >> 8, tail = p.k & 255;
+    auto piece_of = [&](int i) { return ((lane & 15) ^ (((wave * kLoads + i) * 4 + (lane >> 4)) & 15)) * 16; };
 #pragma unroll
-    for (int i = 0; i < kTM; ++i) x[i] = p.x + (int64_t)min(32 * i + (lane & 31), p.n_rows - 1) * p.k + (lane >> 5) * 32;
-    int4v wv[kChunks][2], xv[kChunks][kTM][2];
-    auto load = [&](int k0) {
+    for (int i = 0; i < kLoads; ++i) {
+        const int at = (wave * kLoads + i) * 4 + (lane >> 4);
+        const bool rows = at < 32 * kTM;
+        from[i] = (rows ? p.x : p.w) + (int64_t)(rows ? min(at, p.n_rows - 1) : min(n0 + at - 32 * kTM, p.n - 1)) * p.k + piece_of(i);
+    }
+    int ahead = 0, to = 0;  // the step that is loaded next and its stage; behind the last one it is loaded again, to where it is not read
+    if (tail) {
+        uint4 v[kLoads];
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c)
+        for (int i = 0; i < kLoads; ++i) {
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (piece_of(i) < tail) v[i] = *(const uint4*)(from[i] + (p.k - tail));
+            if (piece_of(i) >= p.k) from[i] -= piece_of(i);  // (loads of steps that there are not stay inside the row)
+        }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = k0 + c * (kFewWaves * 64) + h * 16;
-                const bool in = k + (lane >> 5) * 32 < p.k;
-                wv[c][h] = int4v{0, 0, 0, 0};
-                if (in) wv[c][h] = *(const int4v*)(w + k);
+        for (int i = 0; i < kLoads; ++i) *(uint4*)(lds + (wave * kLoads + i) * 1024 + lane * 16) = v[i];
+        ahead = to = 1;
+    }
+    auto load = [&]() {
+        const int on = ahead + 1 < steps ? 256 : 0;
 #pragma unroll
-                for (int i = 0; i < kTM; ++i) {
-                    xv[c][i][h] = int4v{0, 0, 0, 0};
-                    if (in) xv[c][i][h] = *(const int4v*)(x[i] + k);
-                }
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            load_to_lds(from[i], lds + to * (kRows * 256) + (wave * kLoads + i) * 1024);
+            from[i] += on;
+        }
+        ++ahead;
+        to = to + 1 == kStages ? 0 : to + 1;
     };
-    load(wave * 64);
+    while (ahead < kStages - 1) load();
     const int tile = wave / kShare, share = wave % kShare;
     const int64_t row = 32 * tile + (lane & 31);
     const float scale = row < p.n_rows ? p.x_scale[row] : 0.0f;
@@ -635,27 +680,65 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
             held[i] = operand(next, c);
         }
     }
+    if (kWithInner) {
+        InnerPart<kBf16, 1, 1, 36> inner;
+        const int8_t* xs[1] = {p.x + (int64_t)min(lane & 15, p.n_rows - 1) * p.k + (lane >> 4) * 16};
+        const int of[1] = {project_adapter(p, lane & 15)};
+        for (int a = next_of<16>(of, -1); a != 0x7FFFFFFF; a = next_of<16>(of, a))
+            for (int rank0 = 0; rank0 < p.rank; rank0 += 16) {
+                inner.first_x(xs, wave, p.k);
+                inner.run(xs, p.a + ((int64_t)a * p.rank + rank0 + (lane & 15)) * p.k + (lane >> 4) * 16, p.rank - rank0, wave, p.k);
+                const int r = rank0 + (lane >> 4) * 4;
+                if (of[0] == a && r < p.rank) *(float4v*)&s_parts[(wave * p.n_rows + (lane & 15)) * p.rank + r] = inner.acc[0][0];
+            }
+        __syncthreads();
+    }
+    // the parts of the inner values: kWide threads to a row, two ranks at a time
+    constexpr int kWide = kFewWaves * 2 / kTM, kTurns = ST_MAX_RANK / 2 / kWide;
+    const int m = tid / kWide, l = tid % kWide;
+    float factor = 0.0f;
+    bool has = false;
+    float2 parts[kTurns][kInnerParts];
     if (p.a) {
-        // the inner values: their parts summed in order, the power of two of the largest, rounding; kWide threads to a row, two ranks each
-        constexpr int kWide = kFewWaves * 2 / kTM;
-        const int m = tid / kWide, l = tid % kWide;
         const int i = m < p.n_rows ? project_adapter(p, m) : -1;
-        const float factor = i >= 0 ? p.alpha[i] * p.x_scale[m] : 0.0f;
-        float2 v[ST_MAX_RANK / 2 / kWide];
+        has = i >= 0;
+        if (has) {
+            factor = p.alpha[i] * p.x_scale[m];
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t)
+                if (2 * (t * kWide + l) < p.rank)
+#pragma unroll
+                    for (int q = 0; q < kInnerParts; ++q)
+                        parts[t][q] = *(const float2*)((kWithInner ? s_parts : p.parts) + ((int64_t)q * p.n_rows + m) * p.rank + 2 * (t * kWide + l));
+        }
+    }
+    int16v dot[kTM] = {};
+    // a wavefront has 32 of a step's 256 values of k: pieces 2 wave and 2 wave + 1
+    const int at = (lane & 31) * 256 + (((2 * wave + (lane >> 5)) ^ (lane & 15)) * 16);
+    for (int s = 0, stage = 0; s < steps; ++s) {
+        // this step lies in the LDS for all wavefronts, and none reads the one before any more
+        if (kWithInner || s > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        load();
+        const int8_t* held = lds + stage * (kRows * 256) + at;
+        const int4v wv = *(const int4v*)(held + 32 * kTM * 256);
+#pragma unroll
+        for (int i = 0; i < kTM; ++i) dot[i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv, *(const int4v*)(held + i * 32 * 256), dot[i], 0, 0, 0);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    if (p.a) {
+        // the inner values: their parts summed in order, the power of two of the largest, rounding
         uint32_t top = 0;
+        float2 v[kTurns];
 #pragma unroll
-        for (int t = 0; t < ST_MAX_RANK / 2 / kWide; ++t) {
-            const int r = 2 * (t * kWide + l);
+        for (int t = 0; t < kTurns; ++t) {
             v[t] = make_float2(0.0f, 0.0f);
-            if (i < 0 || r >= p.rank) continue;
-            float2 u[kInnerParts];
-#pragma unroll
-            for (int q = 0; q < kInnerParts; ++q) u[q] = *(const float2*)(p.parts + ((int64_t)q * p.n_rows + m) * p.rank + r);
-            v[t] = u[0];
+            if (!has || 2 * (t * kWide + l) >= p.rank) continue;
+            v[t] = parts[t][0];
 #pragma unroll
             for (int q = 1; q < kInnerParts; ++q) {
-                v[t].x += u[q].x;
-                v[t].y += u[q].y;
+                v[t].x += parts[t][q].x;
+                v[t].y += parts[t][q].y;
             }
             v[t].x *= factor;
             v[t].y *= factor;
@@ -665,34 +748,31 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
         const uint32_t e = project_exponent(top);
         const float down = __uint_as_float((254u - e) << 23);
 #pragma unroll
-        for (int t = 0; t < ST_MAX_RANK / 2 / kWide; ++t)
+        for (int t = 0; t < kTurns; ++t)
             if (2 * t * kWide < 16 * ranks16) *(uint32_t*)&s_inner[m][2 * (t * kWide + l)] = two_16<kBf16>(v[t].x * down, v[t].y * down);
-        if (l == 0) s_power[m] = i >= 0 ? __uint_as_float(e << 23) : 1.0f;
+        if (l == 0) s_power[m] = has ? __uint_as_float(e << 23) : 1.0f;
     }
-    int16v dot[kTM] = {};
-    for (int k0 = wave * 64; k0 < p.k;) {
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < kTM; ++i) dot[i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[c][h], xv[c][i][h], dot[i], 0, 0, 0);
-        if ((k0 += kChunks * kFewWaves * 64) < p.k) load(k0);
-    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the steps are read, and nothing is on its way to them
 #pragma unroll
     for (int i = 0; i < kTM; ++i)
 #pragma unroll
-        for (int u = 0; u < 16; ++u) s_dot[wave][i][u * 64 + lane] = dot[i][u];
+        for (int g = 0; g < 4; ++g) *(int4*)&s_dot[wave][i][g * 256 + lane * 4] = make_int4(dot[i][4 * g], dot[i][4 * g + 1], dot[i][4 * g + 2], dot[i][4 * g + 3]);
+    __syncthreads();
+    if (tid < 256 * kTM) {  // four sums to a thread
+        int4* at = (int4*)&s_dot[0][0][0] + tid;
+        int4 d = *at;
+#pragma unroll
+        for (int v = 1; v < kFewWaves; ++v) {
+            const int4 o = at[v * 256 * kTM];
+            d = make_int4(d.x + o.x, d.y + o.y, d.z + o.z, d.w + o.w);
+        }
+        *at = d;
+    }
     __syncthreads();
     const float power = p.a ? s_power[row] : 1.0f, down = scale * __uint_as_float(0x7F000000u - __float_as_uint(power));
     float16v sum[1];
 #pragma unroll
-    for (int u = 0; u < 16; ++u) {
-        int d = 0;
-#pragma unroll
-        for (int v = 0; v < kFewWaves; ++v) d += s_dot[v][tile][u * 64 + lane];
-        sum[0][u] = (float)d * down * ws[0][u / 4][u % 4];
-    }
+    for (int u = 0; u < 16; ++u) sum[0][u] = (float)s_dot[0][tile][u / 4 * 256 + lane * 4 + u % 4] * down * ws[0][u / 4][u % 4];
     auto add = [&](int a, int at, const uint4& b) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (adapter == a) v = *(const uint4*)&s_inner[row][at * 16 + (lane >> 5) * 8];

@@ -155,11 +155,19 @@ PROJECTIONS = [
     ("bf16", 515, 320, 784, 100, 16, "runs"),
     ("f16", 1025, 144, 272, 11, 104, "mixed"),
     ("bf16", 2049, 128, 512, 4, 120, "runs"),
+    ("bf16", 600, 64, 64, 5000, 8, "mixed"),  # more adapters than the order has buckets
+    ("f16", 2, 1008, 80, 2, 16, "mixed"),
+    # k that ends in each of the chunks a part's loads run ahead by
+    ("bf16", 40, 4624, 32, 3, 16, "mixed"),
+    ("f16", 70, 5152, 32, 3, 64, "mixed"),
+    ("bf16", 2100, 4720, 32, 2, 32, "runs"),
+    ("f16", 2100, 2592, 32, 6, 128, "mixed"),
+    ("bf16", 1, 992, 48, 4, 32, "mixed"),
 ]
 
 
-def project_case(case):
-    dtype, rows, k, n, count, rank, order = PROJECTIONS[case]
+def project_case(cases, case):
+    dtype, rows, k, n, count, rank, order = cases[case]
     rng = np.random.default_rng(1000 + case)
     x, w = integers(rng, rows, k), integers(rng, n, k)
     xs = torch.from_numpy(np.exp(rng.normal(-4, 1, rows)).astype(np.float32))
@@ -179,7 +187,7 @@ def call(args, **kw):
 @pytest.mark.parametrize("case", range(len(PROJECTIONS)))
 def test_projection_matches_plain(case):
     say(f"[layer] projection case {case}: {PROJECTIONS[case]}")
-    dtype, args = project_case(case)
+    dtype, args = project_case(PROJECTIONS, case)
     n_rows, n = args[0].shape[0], args[2].shape[0]
     out = torch.full((n_rows + 1, n + 8 * (case % 3)), 7.0, dtype=R.TYPES[dtype], device="cuda")
     got = call(args, out=out[:n_rows, :n])
@@ -193,9 +201,44 @@ def test_projection_matches_plain(case):
     assert torch.equal(call(args, dtype=R.TYPES[dtype]), got)  # the same bits again
 
 
+LARGE = [
+    # dtype, rows, k, n, adapters, rank, order: tiles of each edge, with rows and columns behind the last whole tile
+    ("f16", 1030, 144, 8208, 6, 16, "mixed"),
+    ("bf16", 2100, 528, 5136, 3, 48, "mixed"),
+    ("bf16", 3000, 208, 4112, 16, 128, "runs"),
+    ("f16", 2060, 4112, 5136, 9, 8, "mixed"),
+    ("bf16", 4100, 1040, 5152, 300, 24, "mixed"),
+    ("f16", 16400, 256, 1040, 0, 0, None),
+    ("bf16", 2500, 64, 1040, 4, 16, "runs"),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LARGE)))
+def test_large_projection_matches_plain(case):
+    """Some rows of calls that take the larger tiles."""
+    say(f"[layer] large projection case {case}: {LARGE[case]}, {st.st_project_host_plan(*LARGE[case][1:6])}")
+    dtype, args = project_case(LARGE, case)
+    n_rows, n = args[0].shape[0], args[2].shape[0]
+    out = torch.full((n_rows + 1, n + 8), 7.0, dtype=R.TYPES[dtype], device="cuda")
+    got = call(args, out=out[:n_rows, :n])
+    torch.cuda.synchronize()
+    rng = np.random.default_rng(case)
+    some = np.unique(np.concatenate([rng.integers(0, n_rows, 60), [0, 31, 32, n_rows - 1, n_rows - 2]]))
+    want, bound = R.project(*(t[some] if i in (0, 1, 7) else t for i, t in enumerate(args)), dtype=dtype)
+    off = np.abs(got[torch.from_numpy(some).cuda()].double().cpu().numpy() - want)
+    over = off - bound
+    assert over.max() <= 0, f"off by {off.max()} at {np.unravel_index(over.argmax(), over.shape)}"
+    assert (out[n_rows] == 7.0).all() and (out[:, n:] == 7.0).all() and torch.isfinite(got.float()).all()
+    # the rest by calls of fewer rows, which run otherwise: the same bits
+    for first in range(0, n_rows, 1000):
+        last = min(first + 60, n_rows)
+        part = call(tuple(t[first:last] if i in (0, 1, 7) else t for i, t in enumerate(args)), dtype=R.TYPES[dtype])
+        assert torch.equal(part, got[first:last])
+
+
 @pytest.mark.parametrize("case", [2, 5, 9, 11, 14])
 def test_projection_of_a_row_does_not_depend_on_others(case):
-    dtype, args = project_case(case)
+    dtype, args = project_case(PROJECTIONS, case)
     want = call(args, dtype=R.TYPES[dtype])
     order = torch.from_numpy(np.random.default_rng(7).permutation(args[0].shape[0]))
     got = call((args[0][order], args[1][order], *args[2:7], args[7][order]), dtype=R.TYPES[dtype])

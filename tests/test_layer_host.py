@@ -101,3 +101,23 @@ def test_bad_copies_are_refused():
 def test_calls_of_nothing_do_nothing():
     assert norm(n=0) == st.ST_OK and project(rows=0) == st.ST_OK and rotate(n=0) == st.ST_OK
     assert rotate(qh=0, kh=0, q=None, k=None, oq=None, ok=None) == st.ST_OK
+
+
+def test_routes_of_projections():
+    """Each of the ways a projection can run is taken by some call, and the sizes of the GPU tests take them all."""
+    plan = st.st_project_host_plan
+    assert plan(1, 512, 1024, 8, 16) == {"edge": 0, "inner_rows": 0, "order": 0}
+    assert plan(1, 512, 1024) == {"edge": 0, "inner_rows": 0, "order": 0}
+    assert plan(1, 4096, 1024, 8, 16) == {"edge": 0, "inner_rows": 1, "order": 0}
+    assert plan(64, 512, 1024, 8, 16) == {"edge": 0, "inner_rows": 1, "order": 0}
+    assert plan(65, 512, 1024, 4, 16) == {"edge": 64, "inner_rows": 16, "order": 0}
+    assert plan(1001, 1040, 1296, 5, 8) == {"edge": 64, "inner_rows": 16, "order": 1}
+    assert plan(16384, 4096, 5120, 16, 32) == {"edge": 256, "inner_rows": 32, "order": 1}
+    assert plan(16384, 4096, 5120) == {"edge": 256, "inner_rows": 0, "order": 0}
+    from tests.test_gpu_layer import LARGE, PROJECTIONS
+    taken = [plan(rows, k, n, count, rank) for _, rows, k, n, count, rank, _ in LARGE + PROJECTIONS]
+    assert {p["edge"] for p in taken} == {0, 64, 128, 256} and {p["inner_rows"] for p in taken} == {0, 1, 16, 32}
+    assert {(p["edge"], p["order"]) for p in taken} >= {(64, 0), (64, 1), (128, 0), (128, 1), (256, 0), (256, 1)}
+    for args in ((-1, 64, 64), (1, 60, 64), (1, 64, 60), (1, 64, 64, 1, 7)):
+        with pytest.raises(st.StError):
+            plan(*args)
