@@ -25,7 +25,8 @@ from paper_2511_14881_amd import binding as st
 
 class HistoryStore:
     """Pages of one ``KvCache`` dealt out to users.  Tables and lengths are kept on the host, where pages are
-    handed out and taken back, and copied to the device for a call; the blocks' accumulated weights stay there."""
+    handed out and taken back, and copied to the device for a call; the blocks' accumulated weights stay there.
+    Histories may share pages (``fork``): a page is written by an append only where one history has it, and comes free with the last."""
 
     def __init__(self, n_users: int, n_pages: int, n_heads: int, d: int, max_blocks: int):
         self.cache = st.KvCache.empty(n_pages, n_heads, d)
@@ -34,6 +35,7 @@ class HistoryStore:
         self.lengths = np.zeros(n_users, np.int32)
         self.mass = torch.zeros((n_users, n_heads, max_blocks), dtype=torch.float32, device="cuda")
         self.free = list(range(n_pages - 1, -1, -1))
+        self.shares = np.zeros(n_pages, np.int32)  # histories that hold a page
 
     def _known(self, users, once: bool = False) -> np.ndarray:
         """The users as an array of indices.  once: none may be named twice, since the call writes to their histories."""
@@ -76,16 +78,29 @@ class HistoryStore:
         have, need = -(-lengths // st.ST_KV_BLOCK), -(-(lengths + counts) // st.ST_KV_BLOCK)
         if need.size and need.max() > self.max_blocks:
             raise ValueError(f"a history would hold {need.max()} blocks of at most {self.max_blocks}: evict first")
-        taken = int((need - have).sum())
+        # where the block that the first event goes to is shared, the history gets a copy of its own; the last holder keeps the page
+        shares, copied = self.shares.copy(), []
+        for i in np.flatnonzero((lengths % st.ST_KV_BLOCK > 0) & (counts > 0)):
+            page = tables[i, have[i] - 1]
+            if shares[page] > 1:
+                shares[page] -= 1
+                copied.append((i, page))
+        taken = int((need - have).sum()) + len(copied)
         if taken > len(self.free):
             raise ValueError(f"{taken} pages are needed, {len(self.free)} are free: evict first")
         pages = iter(self.free[len(self.free) - taken:][::-1])
         for row, a, b in zip(tables, have, need):
             for block in range(a, b):
                 row[block] = next(pages)
+                shares[row[block]] = 1
+        if copied:
+            for i, _ in copied:
+                tables[i, have[i] - 1] = next(pages)
+                shares[tables[i, have[i] - 1]] = 1
+            self._copy(self.cache, self.cache, [page for _, page in copied], [tables[i, have[i] - 1] for i, _ in copied])
         lengths = (lengths + counts).astype(np.int32)
         st.st_kv_append(self.cache, self._view(tables, lengths, counts), k, v)
-        self.tables[users], self.lengths[users] = tables, lengths
+        self.tables[users], self.lengths[users], self.shares = tables, lengths, shares
         del self.free[len(self.free) - taken:]
 
     def attend(self, users, q, counts, n_sel: int = 0, sink: int = 0, recent: int = 0, causal: bool = False, track: bool = False,
@@ -119,9 +134,83 @@ class HistoryStore:
         self.tables[users], self.lengths[users] = tables.cpu().numpy(), lengths.cpu().numpy()
         self.mass[rows] = mass
         pages, count = freed.cpu().numpy(), n_freed.cpu().numpy()
-        for i, n in enumerate(count):
-            self.free.extend(pages[i, :n].tolist())
-        return int(count.sum())
+        return sum(self._give_back(pages[i, :n]) for i, n in enumerate(count))
+
+    def _give_back(self, pages) -> int:
+        """One history less holds the pages; returns how many came free."""
+        before = len(self.free)
+        for page in pages.tolist():
+            self.shares[page] -= 1
+            if self.shares[page] == 0:
+                self.free.append(page)
+        return len(self.free) - before
+
+    @staticmethod
+    def _copy(from_cache, to_cache, src, dst) -> None:
+        lists = torch.from_numpy(np.array([src, dst], np.int32)).cuda()
+        st.st_kv_copy(from_cache, to_cache, lists[0], lists[1])
+
+    def fork(self, users, to) -> None:
+        """Each of the users `to`, whose histories are empty, gets the history of the user beside it, with its blocks' weights.  The
+        pages are shared until one of the histories appends to a page that is not full."""
+        users, to = self._known(users), self._known(to, once=True)
+        if users.shape != to.shape:
+            raise ValueError("as many users to fork as histories to fill")
+        if self.lengths[to].any():
+            raise ValueError("a history that is not empty would be lost: release it first")
+        if len(users) == 0:
+            return
+        self.tables[to], self.lengths[to] = self.tables[users], self.lengths[users]
+        held = self.tables[to]
+        np.add.at(self.shares, held[held >= 0], 1)
+        self.mass[torch.from_numpy(to).cuda()] = self.mass[torch.from_numpy(users).cuda()]
+
+    def release(self, users) -> int:
+        """The users' histories end; returns how many pages came free.  Each user once."""
+        users = self._known(users, once=True)
+        if len(users) == 0:
+            return 0
+        freed = sum(self._give_back(row[row >= 0]) for row in self.tables[users])
+        self.tables[users], self.lengths[users] = -1, 0
+        self.mass[torch.from_numpy(users).cuda()] = 0.0
+        return freed
+
+    def compact(self) -> int:
+        """Moves what lies behind the first pages of the cache, as many as are in use, into the free ones among them; returns how
+        many pages moved."""
+        used = np.flatnonzero(self.shares)
+        src = used[used >= len(used)]
+        dst = np.flatnonzero(self.shares[: len(used)] == 0)
+        if len(src):
+            self._copy(self.cache, self.cache, src, dst)
+            place = np.arange(len(self.shares), dtype=np.int32)
+            place[src] = dst
+            self._moved(place, len(self.shares))
+        return len(src)
+
+    def resize(self, n_pages: int) -> None:
+        """A cache of n_pages pages, at least those in use, in place of the one so far; the pages in use are its first ones.  Batches and
+        buffers that a program holds of the cache so far are not of the new one."""
+        used = np.flatnonzero(self.shares)
+        if n_pages < max(1, len(used)):
+            raise ValueError(f"{len(used)} pages are in use, {n_pages} are too few")
+        cache = st.KvCache.empty(n_pages, self.cache.n_heads, self.cache.d)
+        if len(used):
+            self._copy(self.cache, cache, used, np.arange(len(used)))
+        place = np.full(len(self.shares), -1, np.int32)
+        place[used] = np.arange(len(used))
+        self._moved(place, n_pages)
+        self.cache = cache
+
+    def _moved(self, place, n_pages: int) -> None:
+        """Page p is now page place[p], of n_pages."""
+        used = np.flatnonzero(self.shares)
+        shares = np.zeros(n_pages, np.int32)
+        shares[place[used]] = self.shares[used]
+        held = self.tables >= 0
+        self.tables[held] = place[self.tables[held]]
+        self.shares = shares
+        self.free = [int(p) for p in np.flatnonzero(shares == 0)[::-1]]
 
 
 def main():
