@@ -2,13 +2,15 @@
 """Users' event histories beside the index: a store of cached keys and values (``HistoryStore``), and a serving loop that
 runs it with the search as they would be used together.
 
-    python -m paper_2511_14881_amd.history [--items 200000] [--users 64] [--events 3000] [--steps 8]
+    python -m paper_2511_14881_amd.history [--items 200000] [--users 64] [--events 3000] [--steps 8] [--layer]
 
 Each step of the loop searches the index for every user (``st_search``), lets the retrieved candidates attend to the
 user's history, whole or in the blocks each candidate selects, ranks them by the attended interest, appends the
 winner to the history as a new event, lets the newest event attend and so accumulate what weight the blocks draw, and
 cuts histories that outgrow their budget.  The events' keys are item embeddings, their values the embeddings again: a
-stand-in for the trained projections of a ranking model.  Prints one JSON line.
+stand-in for the trained projections of a ranking model.  With --layer they go through a layer with such projections
+(``HistoryLayer``, its weights random, an adapter for each of three markets, positions by index and time), which also
+makes the next search's queries and each user's alternative: a fork of the history that takes the second best event.  Prints one JSON line.
 """
 from __future__ import annotations
 
@@ -213,6 +215,64 @@ class HistoryStore:
         self.free = [int(p) for p in np.flatnonzero(shares == 0)[::-1]]
 
 
+def _loop_with_layer(args, cfg, w, bloom):
+    from paper_2511_14881_amd.layer import HistoryLayer
+
+    gen = torch.Generator(device="cuda").manual_seed(cfg.seed)
+    heads, kv_heads, d, markets, rank, width, n_users, K = 4, 2, 64, 3, 16, cfg.d, args.users, cfg.top_k
+
+    def normal(*shape, size=1.0):
+        return (torch.randn(shape, generator=gen, device="cuda") * size).to(torch.bfloat16)
+
+    def adapters(n, k):
+        return normal(markets, rank, k, size=k ** -0.5), normal(markets, n, rank, size=0.1), torch.full((markets,), 0.5, device="cuda")
+
+    n_qkv = (heads + 2 * kv_heads) * d
+    # an index, and a time in seconds with periods from a minute to a year
+    freqs = torch.cat([10000.0 ** (-torch.arange(16) / 16), 2 * np.pi / 60 * (60 / 3.2e7) ** (torch.arange(16) / 16)]).double().cuda()
+    layer = HistoryLayer(heads, kv_heads, d, torch.ones(width, dtype=torch.bfloat16, device="cuda"), normal(n_qkv, width, size=width ** -0.5),
+                         normal(width, heads * d, size=(heads * d) ** -0.5), (16, 16), freqs, adapters(n_qkv, width),
+                         adapters(width, heads * d))
+    embedding = (w.items.float() * w.item_scale[:, None]).to(torch.bfloat16)
+    users, blocks = np.arange(n_users), args.events // st.ST_KV_BLOCK + 4
+    store = HistoryStore(2 * n_users, 2 * n_users * blocks, kv_heads, d, max_blocks=blocks)  # and a place for each user's alternative
+    market = torch.arange(n_users, dtype=torch.int32, device="cuda") % markets
+    counts = np.maximum(1, args.events - np.arange(n_users) * args.events // (2 * n_users))
+    repeat = torch.from_numpy(counts).cuda()
+    index = torch.cat([torch.arange(n) for n in counts]).int().cuda()
+    seen = torch.randint(0, cfg.n_items, (int(counts.sum()),), generator=gen, device="cuda")
+    layer.take_in(store, users, embedding[seen], torch.stack([index, 1_700_000_000 + 60 * index]), counts, market.repeat_interleave(repeat))
+    state = embedding[seen[repeat.cumsum(0) - 1]]
+    at, freed, begun = repeat.int(), 0, time.perf_counter()
+    for step in range(args.steps):
+        now = torch.stack([at, 1_700_000_000 + 60 * at])
+        out, total = layer(store, users, state, now, tenants=market, track=True, decay=0.9)
+        query = st.st_norm_rows(out, layer.norm, total)
+        ids, _, _ = st.st_search(bloom, w.items, w.item_scale, query.q, query.scale, w.filt_ids, w.filt_offsets, K)[:3]
+        rows = embedding[ids.clamp_min(0)].view(-1, width)
+        interest, _ = layer(store, users, rows, now.repeat_interleave(K, 1), [K] * n_users, market.repeat_interleave(K), append=False,
+                            n_sel=args.select if step % 2 else 0)
+        rank_by = (interest.float() * rows.float()).sum(1).view(n_users, K).masked_fill(ids < 0, -float("inf"))
+        best = ids.gather(1, rank_by.topk(min(2, K)).indices).clamp_min(0)
+        # what each history would be with the second best event instead
+        others = users + n_users
+        freed += store.release(others)
+        store.fork(users, others)
+        other, _ = layer(store, others, embedding[best[:, -1]], now + 1, tenants=market)
+        state, at = embedding[best[:, 0]], at + 1
+        over = users[-(-store.lengths[:n_users] // st.ST_KV_BLOCK) > args.budget]
+        freed += store.evict(over, args.budget, sink=1, recent=2)
+    freed += store.release(users + n_users)
+    moved = store.compact()
+    store.resize(max(1, int((store.shares > 0).sum())))
+    torch.cuda.synchronize()
+    spent = time.perf_counter() - begun
+    print(json.dumps({"users": n_users, "items": cfg.n_items, "candidates": K, "steps": args.steps, "ms_per_step": spent * 1e3 / args.steps,
+                      "pages_freed": freed, "pages_moved": moved, "pages": store.cache.n_pages, "longest": int(store.lengths.max()),
+                      "finite": bool(torch.isfinite(rank_by[ids >= 0]).all() and torch.isfinite(other.float()).all())}))
+    bloom.free()
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--items", type=int, default=200_000)
@@ -222,6 +282,7 @@ def main():
     ap.add_argument("--select", type=int, default=8, help="blocks each candidate reads in every other step (0: always all)")
     ap.add_argument("--budget", type=int, default=40, help="blocks a history may hold")
     ap.add_argument("--steps", type=int, default=8)
+    ap.add_argument("--layer", action="store_true", help="a layer with projections, adapters and positions in place of bare embeddings")
     args = ap.parse_args()
     from paper_2511_14881_amd import synth
 
@@ -231,6 +292,8 @@ def main():
     cfg = synth.scaled(synth.CONFIGS["mid"], args.items, batch=args.users, top_k=args.candidates)
     w = synth.make_workload(cfg, device="cuda")
     bloom = st.st_bloom_build(w.feat_offsets, w.feat_ids, cfg.n_items, cfg.m_bits, cfg.k_hashes)
+    if args.layer:
+        return _loop_with_layer(args, cfg, w, bloom)
     heads, d = 2, cfg.d // 2
     embedding = (w.items.float() * w.item_scale[:, None]).to(torch.bfloat16).view(cfg.n_items, heads, d)
     users = np.arange(args.users)
