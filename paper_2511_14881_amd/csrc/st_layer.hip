@@ -70,10 +70,14 @@ constexpr int kFewRows = 64;
 // Rows up to which a workgroup that sums inner values takes 16, beyond 32.  Kernel in us, 16 / 32 / 64: 2048 rows, k = 4096, rank 16 9.9 / 11.7 /
 // 17.4; 4096, 1024, 64 14.5 / 13.9 / 18.7; 16384, 4096, 32 57 / 36 / 39.
 constexpr int kOneTileRows = 2048;
-// Adapters from which on rows are brought into their order first.  Calls in us, ordered against as they come: mixed rows 2048, 8 adapters
-// 69 / 95, 4096, 16 adapters of rank 64 34 / 103, 16384, 16 of rank 32 409 / 791, 256, 32 30 / 32; 1001, 5 16.9 / 18.7.  Rows that come in
-// runs pay for it: 1000, 16 adapters 26.7 / 21.9, 16384 385 / 373.
-constexpr int kOrderFrom = 5;
+// Whether rows are brought into the order of their adapters first: each adapter more in a tile costs loads and products by its rank.
+// Calls in us, as they come / ordered, mixed rows: 256 rows, 32 adapters of rank 16 32 / 30; 1001, 5 of 8 17.5 / 16.7, 2 of 32 14.6 / 18.1; 300, 3
+// of 64 14.5 / 16.6; 2048, 8 of 16 95 / 69; 4096, 2 of 16 47 / 52, 2 of 64 61.3 / 60.8, 3 of 32 58 / 52, 16 of 64 103 / 34; 16384, 3 of 32
+// 180 / 157, 16 of 32 791 / 409.  Rows that come in runs pay for it: 1000, 16 adapters 21.9 / 26.7, 16384 373 / 385.
+bool project_ordered(int32_t n_rows, const st_adapters* a)
+{
+    return n_rows > kFewRows && (a->n_adapters >= 5 || (n_rows > kOneTileRows && (a->n_adapters - 1) * a->rank >= 64));
+}
 
 struct ProjectPlan {
     int64_t inner, power, order;  // bytes
@@ -85,7 +89,7 @@ ProjectPlan project_plan(int32_t n_rows, const st_adapters* adapters)
     if (!adapters) return {0, 0, 0};
     const int64_t values = (int64_t)n_rows * adapters->rank, words = st::round_up((int64_t)n_rows * 4, 256);
     if (n_rows <= kFewRows) return {st::round_up(values * 4 * st::kInnerParts, 256), 0, 0};
-    return {st::round_up(values * 2, 256), words, adapters->n_adapters >= kOrderFrom ? words : 0};
+    return {st::round_up(values * 2, 256), words, project_ordered(n_rows, adapters) ? words : 0};
 }
 
 // Edge of the tiles of many rows by an estimate of the call's microseconds.  64 (three workgroups to a compute unit): the longer of one
@@ -132,7 +136,7 @@ ProjectRoute project_route(int32_t n_rows, int32_t k, int32_t n, const st_adapte
     const int64_t ranks = adapters ? (int64_t)n_rows * ((adapters->rank + 15) / 16 * 16) : 0;
     r.fused = adapters && ranks <= st::kFusedRanks && ranks * k <= st::kFusedValues;
     r.edge = project_edge(n_rows, k, n);
-    r.order = adapters && !r.few && adapters->n_adapters >= kOrderFrom;
+    r.order = adapters && project_ordered(n_rows, adapters);
     r.tiles = r.few ? (n + 31) / 32 : ((int64_t)n_rows + r.edge - 1) / r.edge * ((n + r.edge - 1) / r.edge);
     return r;
 }

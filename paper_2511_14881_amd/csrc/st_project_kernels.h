@@ -34,11 +34,29 @@ __device__ inline int project_adapter(const ProjectArgs& a, int64_t row)
     return i >= 0 && i < a.n_adapters ? i : -1;
 }
 
-// The row at place m of the order, n_rows behind the last.
-__device__ inline int64_t project_place(const ProjectArgs& p, int64_t m)
+// The rows at some places of the order, the last row's for a place behind it.  All loads begin together: a wait for each would be a trip
+// to memory for each.
+template <int N>
+__device__ inline void project_places(const ProjectArgs& p, const int64_t (&m)[N], int64_t (&row)[N])
 {
-    if (m >= p.n_rows) return p.n_rows;
-    return p.order ? p.order[m] : m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) row[i] = min(m[i], (int64_t)p.n_rows - 1);
+    if (p.order) {
+        int32_t at[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] = p.order[row[i]];
+#pragma unroll
+        for (int i = 0; i < N; ++i) row[i] = at[i];
+    }
+}
+// The adapters of those rows, -1 for a place behind the last row too.
+template <int N>
+__device__ inline void project_adapters(const ProjectArgs& p, const int64_t (&m)[N], const int64_t (&row)[N], int (&of)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) of[i] = p.adapter_of[row[i]];
+#pragma unroll
+    for (int i = 0; i < N; ++i) of[i] = m[i] < p.n_rows && of[i] >= 0 && of[i] < p.n_adapters ? of[i] : -1;
 }
 
 // The smallest number above `last` that a lane holds, INT32_MAX if there is none.  Lanes that lie kLanes apart hold the same.
@@ -90,6 +108,12 @@ __device__ inline uint4 eight_16(uint32_t lo, uint32_t hi)
         r[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// 16 bytes for each lane, from where it points to `to` + 16 * lane (`to` the same in all lanes).
+__device__ inline void load_to_lds(const int8_t* from, int8_t* to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
 // ---------------------------------------------------------------- rows in the order of their adapters
@@ -221,49 +245,175 @@ __device__ inline uint32_t project_exponent(uint32_t top)
     return e < 27 || e == 255 ? 127u : min(e, 227u);
 }
 
+// The same for many rows: operands come through the LDS, in space of the wavefront's own, kSlots - 1 steps ahead.  A load straight into a
+// lane's operand touches 64 places with 64 lanes, which an address unit takes one by one; rows in the LDS come in by lines.  A step is
+// 64 values of k and two tiles of ranks; the rows come with a chunk's first.
+template <bool kBf16, int kTiles, int kM>
+struct InnerStream {
+    static constexpr int kGroup = kTiles < 2 ? 1 : 2, kGroups = kTiles / kGroup;  // tiles of ranks to a step, steps to 64 values
+    static constexpr int kSlot = kM * 1024 + kGroup * 2048, kSlots = kGroup < 2 ? 4 : 3, kBytes = kSlots * kSlot;
+    static constexpr int kRowLoads = kM, kRankLoads = 2 * kGroup;
+    float4v acc[kM][kTiles];
+    const int8_t* x[kM];  // of each 16 rows row lane / 4, its first piece
+    const uint16_t* a;    // of the adapter's first rank
+    int k, rank, part, slot, to;
+
+    // The place of a row's piece of 16 bytes: 16 neighbouring rows have a piece at 16 places of the banks.
+    __device__ static int row_place(int row, int piece) { return piece ^ ((row >> 2) & 3); }
+    __device__ static int rank_place(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+
+    template <int kG>
+    __device__ void load(int8_t* own, int chunk)
+    {
+        const int lane = threadIdx.x & 63, k0 = chunk * 64;
+        int8_t* at = own + to * kSlot;
+        if (kG == 0) {
+            const int piece = row_place(lane >> 2, lane & 3) * 16;
+#pragma unroll
+            for (int i = 0; i < kM; ++i) load_to_lds(x[i] + k0 + (k0 + piece < k ? piece : 0), at + i * 1024);
+        }
+#pragma unroll
+        for (int t = 0; t < kRankLoads; ++t) {
+            const int row = t * 8 + (lane >> 3), piece = rank_place(row, lane & 7) * 8;
+            load_to_lds((const int8_t*)(a + (int64_t)min(kG * kGroup * 16 + row, rank - 1) * k + k0 + (k0 + piece < k ? piece : 0)), at + kM * 1024 + t * 1024);
+        }
+        to = to + 1 == kSlots ? 0 : to + 1;
+    }
+    // One step, of group kG of its chunk: `ahead_chunk` is that of the step kSlots - 1 further on.
+    template <int kG>
+    __device__ void one(int8_t* own, int chunk, int ahead_chunk, uint4 (&x0)[kM], uint4 (&x1)[kM])
+    {
+        constexpr int kNext = (kG + 1) % kGroups == 0 ? kRowLoads + kRankLoads : kRankLoads;
+        // this step lies in the LDS, and the one before it is read
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kSlots == 3 ? kNext : 2 * kNext) : "memory");
+        load<(kG + kSlots - 1) % kGroups>(own, ahead_chunk);
+        const int lane = threadIdx.x & 63, piece = lane >> 4;
+        const int8_t* at = own + slot * kSlot;
+        slot = slot + 1 == kSlots ? 0 : slot + 1;
+        if (kG == 0) {
+            const uint32_t in = chunk * 64 + piece * 16 < k ? 0xFFFFFFFFu : 0u;  // (behind a row's end lies something else)
+#pragma unroll
+            for (int i = 0; i < kM; ++i) {
+                const int4v v = *(const int4v*)(at + i * 1024 + (lane & 15) * 64 + row_place(lane & 15, piece) * 16);
+                x0[i] = eight_16<kBf16>(v[0] & in, v[1] & in);
+                x1[i] = eight_16<kBf16>(v[2] & in, v[3] & in);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < kGroup; ++t) {
+            const int8_t* row = at + kM * 1024 + (t * 16 + (lane & 15)) * 128;
+            const int4v v0 = *(const int4v*)(row + rank_place(lane & 15, 2 * piece) * 16), v1 = *(const int4v*)(row + rank_place(lane & 15, 2 * piece + 1) * 16);
+            const uint4 a0 = make_uint4(v0[0], v0[1], v0[2], v0[3]), a1 = make_uint4(v1[0], v1[1], v1[2], v1[3]);
+#pragma unroll
+            for (int i = 0; i < kM; ++i) {
+                float4v& d = acc[i][kG * kGroup + t];
+                d = mfma_16<kBf16>(a0, x0[i], d);
+                d = mfma_16<kBf16>(a1, x1[i], d);
+            }
+        }
+    }
+    template <int kG>
+    __device__ void first(int8_t* own, int last)
+    {
+        if constexpr (kG < kSlots - 1) {
+            load<kG % kGroups>(own, min(part + kG / kGroups * kInnerParts, last));
+            first<kG + 1>(own, last);
+        }
+    }
+    template <int kG>
+    __device__ void all(int8_t* own, int chunk, int last, uint4 (&x0)[kM], uint4 (&x1)[kM])
+    {
+        if constexpr (kG < kGroups) {
+            one<kG>(own, chunk, min(chunk + (kG + kSlots - 1) / kGroups * kInnerParts, last), x0, x1);
+            all<kG + 1>(own, chunk, last, x0, x1);
+        }
+    }
+    __device__ void run(int8_t* own)
+    {
+#pragma unroll
+        for (int i = 0; i < kM; ++i)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) acc[i][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        const int chunks = (k + 63) >> 6;
+        if (part >= chunks) return;
+        const int last = part + (chunks - 1 - part) / kInnerParts * kInnerParts;  // (loaded again where a step further on is not)
+        slot = to = 0;
+        first<0>(own, last);
+        uint4 x0[kM], x1[kM];
+        for (int chunk = part; chunk <= last; chunk += kInnerParts) all<0>(own, chunk, last, x0, x1);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    }
+};
+
 // 16 kM rows and every gridDim.y-th adapter among them; the other rows' results of an adapter are not kept.  A wavefront to each part of
-// k; the parts are summed in their order, so that a row's sums have one order whatever kM, the grid and the kernel.
+// k; the parts are summed in their order, so that a row's sums have one order whatever kM, the grid and the kernel.  kM 1: operands
+// straight from memory (shorter where there are few workgroups); 2: through the LDS.
 template <bool kBf16, int kTiles, int kM>
 __global__ __launch_bounds__(kInnerParts * 64) void project_inner_kernel(ProjectArgs p)
 {
-    constexpr int kRanks = 16 * kTiles;
-    __shared__ float s_sum[kInnerParts][16][kRanks + 4];
-    const int tid = threadIdx.x, lane = tid & 63, part = tid >> 6;
+    constexpr int kRanks = 16 * kTiles, kRow = kRanks + 4;
+    constexpr int kSums = kInnerParts * 16 * kRow * 4, kSteps = kM == 1 ? 0 : kInnerParts * InnerStream<kBf16, kTiles, kM>::kBytes;
+    __shared__ __align__(1024) int8_t lds[kSums > kSteps ? kSums : kSteps];  // steps, and then sums [part][16][kRow]
+    float* s_sum = (float*)lds;
+    const int tid = threadIdx.x, lane = tid & 63, part = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t m0 = (int64_t)blockIdx.x * (16 * kM);
-    const int8_t* x[kM];
-    int mine[kM];
-#pragma unroll
-    for (int i = 0; i < kM; ++i) {
-        const int64_t row = project_place(p, m0 + 16 * i + (lane & 15));
-        mine[i] = project_adapter(p, row);
-        x[i] = p.x + min(row, (int64_t)p.n_rows - 1) * p.k + (lane >> 4) * 16;
-    }
-    // 32 threads to a row when the parts are summed
+    // rows of each 16: that whose adapter counts as a lane's, that which the lane loads, and that which it sums with 31 others
     const int m = tid >> 5, l = tid & 31;
-    int64_t row[kM];
-    int of[kM];
+    int64_t at[3 * kM], rows[3 * kM];
+    int of[3 * kM], mine[kM];
     float scale[kM];
+    const int8_t* x[kM];
 #pragma unroll
     for (int i = 0; i < kM; ++i) {
-        row[i] = project_place(p, m0 + 16 * i + m);
-        of[i] = project_adapter(p, row[i]);
-        scale[i] = row[i] < p.n_rows ? p.x_scale[row[i]] : 0.0f;
+        at[i] = m0 + 16 * i + (lane & 15);
+        at[kM + i] = m0 + 16 * i + (kM == 1 ? lane & 15 : lane >> 2);
+        at[2 * kM + i] = m0 + 16 * i + m;
     }
-    InnerPart<kBf16, kTiles, kM, kM == 1 ? 96 : 48> inner;
+    project_places<3 * kM>(p, at, rows);
+#pragma unroll
+    for (int i = 0; i < kM; ++i) scale[i] = p.x_scale[rows[2 * kM + i]];
+    project_adapters<3 * kM>(p, at, rows, of);
+#pragma unroll
+    for (int i = 0; i < kM; ++i) {
+        mine[i] = of[i];
+        x[i] = p.x + rows[kM + i] * p.k + (kM == 1 ? (lane >> 4) * 16 : 0);
+    }
     int index = 0;
     for (int a = next_of<16>(mine, -1); a != 0x7FFFFFFF; a = next_of<16>(mine, a), ++index) {
         if (index % gridDim.y != blockIdx.y) continue;
-        inner.first_x(x, part, p.k);
         const float alpha = p.alpha[a];
-        inner.run(x, p.a + ((int64_t)a * p.rank + (lane & 15)) * p.k + (lane >> 4) * 16, p.rank, part, p.k);
+        const uint16_t* wa = p.a + (int64_t)a * p.rank * p.k;
+        float4v acc[kM][kTiles];
+        if constexpr (kM == 1) {
+            InnerPart<kBf16, kTiles, kM> inner;
+            inner.first_x(x, part, p.k);
+            inner.run(x, wa + (int64_t)(lane & 15) * p.k + (lane >> 4) * 16, p.rank, part, p.k);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) acc[0][t] = inner.acc[0][t];
+        } else {
+            InnerStream<kBf16, kTiles, kM> inner;
+#pragma unroll
+            for (int i = 0; i < kM; ++i) inner.x[i] = x[i];
+            inner.a = wa;
+            inner.k = p.k;
+            inner.rank = p.rank;
+            inner.part = part;
+            __syncthreads();  // the sums before are read
+            inner.run(lds + part * InnerStream<kBf16, kTiles, kM>::kBytes);
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) acc[i][t] = inner.acc[i][t];
+        }
         constexpr int kEach = (kRanks + 31) / 32;
 #pragma unroll
         for (int i = 0; i < kM; ++i) {
-            __syncthreads();  // the sums before are read
+            __syncthreads();  // the sums before, or the steps, are read
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) *(float4v*)&s_sum[part][lane & 15][t * 16 + (lane >> 4) * 4] = inner.acc[i][t];
+            for (int t = 0; t < kTiles; ++t) *(float4v*)&s_sum[(part * 16 + (lane & 15)) * kRow + t * 16 + (lane >> 4) * 4] = acc[i][t];
             __syncthreads();
-            if (of[i] != a) continue;
+            if (of[2 * kM + i] != a) continue;
+            const int64_t row = rows[2 * kM + i];
             const float factor = alpha * scale[i];
             float v[kEach];
             uint32_t top = 0;
@@ -272,9 +422,9 @@ __global__ __launch_bounds__(kInnerParts * 64) void project_inner_kernel(Project
                 const int r = c * 32 + l;
                 v[c] = 0.0f;
                 if (r < p.rank) {
-                    v[c] = s_sum[0][m][r];
+                    v[c] = s_sum[m * kRow + r];
 #pragma unroll
-                    for (int u = 1; u < kInnerParts; ++u) v[c] += s_sum[u][m][r];
+                    for (int u = 1; u < kInnerParts; ++u) v[c] += s_sum[(u * 16 + m) * kRow + r];
                     v[c] *= factor;
                 }
                 top = max(top, __float_as_uint(v[c]) & 0x7FFFFFFFu);
@@ -289,9 +439,9 @@ __global__ __launch_bounds__(kInnerParts * 64) void project_inner_kernel(Project
 #pragma unroll
             for (int c = 0; c < kEach; ++c) {
                 const int r = c * 32 + l;
-                if (r < p.rank) p.inner[row[i] * p.rank + r] = one_16<kBf16>(v[c] * down);
+                if (r < p.rank) p.inner[row * p.rank + r] = one_16<kBf16>(v[c] * down);
             }
-            if (l == 0) p.power[row[i]] = __uint_as_float(e << 23);
+            if (l == 0) p.power[row] = __uint_as_float(e << 23);
         }
     }
 }
@@ -325,14 +475,23 @@ struct ProjectRow {
     float power;  // 2^e
 };
 
-__device__ inline ProjectRow project_row(const ProjectArgs& p, int64_t row)
+template <int N>
+__device__ inline void project_rows(const ProjectArgs& p, const int64_t (&m)[N], const int64_t (&row)[N], ProjectRow (&r)[N])
 {
-    ProjectRow r = {-1, row < p.n_rows ? p.x_scale[row] : 0.0f, 1.0f};
-    if (p.a && (r.adapter = project_adapter(p, row)) >= 0) {
-        r.power = p.power[row];
-        r.scale *= __uint_as_float(0x7F000000u - __float_as_uint(r.power));
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = {-1, p.x_scale[row[i]], 1.0f};
+    if (!p.a) return;
+    int of[N];
+    float power[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) power[i] = p.power[row[i]];  // (what a row without an adapter has is not used)
+    project_adapters<N>(p, m, row, of);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        r[i].adapter = of[i];
+        r[i].power = of[i] >= 0 ? power[i] : 1.0f;
+        r[i].scale *= __uint_as_float(0x7F000000u - __float_as_uint(r[i].power));
     }
-    return r;
 }
 
 // Eight of a row's inner values, from rank r on; zeros for a row of another adapter and behind the last rank.
@@ -433,12 +592,6 @@ __device__ inline void project_store(const ProjectArgs& p, const uint4 (&out)[kN
 // step of 256 x 256 takes 1.02 us and its products 0.85).  16384 x 4096 x 5120: 323 us, 2130 TOP/s.  Tried: four wavefronts with 128 x 128 each
 // (345 us; fewer reads, but a SIMD waits with its only wavefront), steps of 64 values with four and five stages (356), tiles of
 // 256 x 128 (498), loads and reads in the first half of the products between which they stand (327).
-// 16 bytes for each lane, from where it points to `to` + 16 * lane (`to` the same in all lanes).
-__device__ inline void load_to_lds(const int8_t* from, int8_t* to)
-{
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
-
 // kWM x kWN wavefronts of kTM x kTN tiles of 32 x 32, kStages steps in the LDS
 template <bool kBf16, int kWM, int kWN, int kTM, int kTN, int kStages>
 __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs p)
@@ -466,14 +619,17 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
     const int8_t* from[kLoads];
     const int steps = (p.k + 127) >> 7, tail = p.k & 127;
     auto piece_of = [&](int i) { return place((wave * kLoads + i) * 8 + (lane >> 3), lane & 7) * 16; };
+    {
+        int64_t at[kLoads], rows[kLoads];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int first = (wave * kLoads + i) * 8;
-        const bool rows = first < kBM;
-        const int8_t* base = rows ? p.x : p.w;
-        int64_t row = (int64_t)n0 + first - kBM + (lane >> 3);
-        if (rows) row = project_place(p, m0 + first + (lane >> 3));
-        from[i] = base + min(row, (int64_t)(rows ? p.n_rows : p.n) - 1) * p.k + piece_of(i);
+        for (int i = 0; i < kLoads; ++i) at[i] = m0 + (wave * kLoads + i) * 8 + (lane >> 3);
+        project_places<kLoads>(p, at, rows);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int first = (wave * kLoads + i) * 8;
+            const int64_t row = first < kBM ? rows[i] : min(n0 + first - kBM + (lane >> 3), p.n - 1);
+            from[i] = (first < kBM ? p.x : p.w) + row * p.k + piece_of(i);
+        }
     }
     if (tail) {
         uint4 v[kLoads];
@@ -553,10 +709,14 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
     int64_t at_row[kTM];
     ProjectRow rows[kTM];
     float4v ws[kTN][4];
+    {
+        int64_t m[kTM];
 #pragma unroll
-    for (int i = 0; i < kTM; ++i) {
-        at_row[i] = project_place(p, m0 + wm + 32 * i + (lane & 31));
-        rows[i] = project_row(p, at_row[i]);
+        for (int i = 0; i < kTM; ++i) m[i] = m0 + wm + 32 * i + (lane & 31);
+        project_places<kTM>(p, m, at_row);
+        project_rows<kTM>(p, m, at_row, rows);
+#pragma unroll
+        for (int i = 0; i < kTM; ++i) at_row[i] = m[i] < p.n_rows ? at_row[i] : (int64_t)p.n_rows;
     }
     project_scales<kTN>(p, ws, n0 + wn);
     uint4 out[kTM][kTN][2];
@@ -591,7 +751,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     constexpr int kHeld = 4;                  // operands of adapters (16 ranks x 32 columns) that are loaded ahead
     constexpr int kInner = kStages * kRows * 256, kInnerRow = ST_MAX_RANK + 8, kPower = kInner + 32 * kTM * kInnerRow * 2;
     constexpr int kParts = kPower + 32 * kTM * 4;
-    // (one array for all: beside another the compiler has the reads of a step wait for the loads of later ones)
+    // (one array for all, read as int4v: beside another, or read as a struct, the compiler has the reads of a step wait for the loads of later ones)
     __shared__ __align__(1024) int8_t lds[kParts + (kWithInner ? kInnerParts * kFusedRanks * 4 : 0)];
     static_assert(kInner >= kFewWaves * kTM * 4096, "the sums take the place of the steps");
     int32_t(*s_dot)[kTM][1024] = (int32_t(*)[kTM][1024])lds;
@@ -600,6 +760,18 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     float* s_parts = (float*)(lds + kParts);  // [part][row][rank]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = blockIdx.x * 32, n = n0 + (lane & 31);
+    // (what others' addresses come from is asked for before the steps: loads end in the order in which they begin)
+    const int tile = wave / kShare, share = wave % kShare;
+    const int64_t row = 32 * tile + (lane & 31);
+    const float scale = row < p.n_rows ? p.x_scale[row] : 0.0f;
+    const int asked = p.a && row < p.n_rows ? p.adapter_of[row] : -1;
+    float4v ws[1][4];
+    project_scales<1>(p, ws, n0);
+    // the parts of the inner values: kWide threads to a row, two ranks at a time
+    constexpr int kWide = kFewWaves * 2 / kTM, kTurns = ST_MAX_RANK / 2 / kWide;
+    const int m = tid / kWide, l = tid % kWide;
+    const int part_asked = p.a && m < p.n_rows ? p.adapter_of[m] : -1;
+    const float part_scale = p.a && m < p.n_rows ? p.x_scale[m] : 0.0f;
     // what this lane loads: of each four rows row lane / 16, the piece that lies at place lane % 16
     const int8_t* from[kLoads];
     const int steps = (p.k + 255) >> 8, tail = p.k & 255;
@@ -634,12 +806,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
         to = to + 1 == kStages ? 0 : to + 1;
     };
     while (ahead < kStages - 1) load();
-    const int tile = wave / kShare, share = wave % kShare;
-    const int64_t row = 32 * tile + (lane & 31);
-    const float scale = row < p.n_rows ? p.x_scale[row] : 0.0f;
-    const int adapter = p.a ? project_adapter(p, row) : -1;
-    float4v ws[1][4];
-    project_scales<1>(p, ws, n0);
+    const int adapter = asked >= 0 && asked < p.n_adapters ? asked : -1, part_of = part_asked >= 0 && part_asked < p.n_adapters ? part_asked : -1;
     // the adapters of the tile's rows: lanes that are the first with theirs, and of those the wavefront's
     uint32_t left = 0;
     bool stores = true;
@@ -693,32 +860,24 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
             }
         __syncthreads();
     }
-    // the parts of the inner values: kWide threads to a row, two ranks at a time
-    constexpr int kWide = kFewWaves * 2 / kTM, kTurns = ST_MAX_RANK / 2 / kWide;
-    const int m = tid / kWide, l = tid % kWide;
-    float factor = 0.0f;
-    bool has = false;
+    float alpha = 0.0f;
+    const bool has = part_of >= 0;
     float2 parts[kTurns][kInnerParts];
-    if (p.a) {
-        const int i = m < p.n_rows ? project_adapter(p, m) : -1;
-        has = i >= 0;
-        if (has) {
-            factor = p.alpha[i] * p.x_scale[m];
+    if (has) {
+        alpha = p.alpha[part_of];
 #pragma unroll
-            for (int t = 0; t < kTurns; ++t)
-                if (2 * (t * kWide + l) < p.rank)
+        for (int t = 0; t < kTurns; ++t)
+            if (2 * (t * kWide + l) < p.rank)
 #pragma unroll
-                    for (int q = 0; q < kInnerParts; ++q)
-                        parts[t][q] = *(const float2*)((kWithInner ? s_parts : p.parts) + ((int64_t)q * p.n_rows + m) * p.rank + 2 * (t * kWide + l));
-        }
+                for (int q = 0; q < kInnerParts; ++q)
+                    parts[t][q] = *(const float2*)((kWithInner ? s_parts : p.parts) + ((int64_t)q * p.n_rows + m) * p.rank + 2 * (t * kWide + l));
     }
     int16v dot[kTM] = {};
     // a wavefront has 32 of a step's 256 values of k: pieces 2 wave and 2 wave + 1
     const int at = (lane & 31) * 256 + (((2 * wave + (lane >> 5)) ^ (lane & 15)) * 16);
     for (int s = 0, stage = 0; s < steps; ++s) {
         // this step lies in the LDS for all wavefronts, and none reads the one before any more
-        if (kWithInner || s > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
         load();
         const int8_t* held = lds + stage * (kRows * 256) + at;
         const int4v wv = *(const int4v*)(held + 32 * kTM * 256);
@@ -728,6 +887,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     }
     if (p.a) {
         // the inner values: their parts summed in order, the power of two of the largest, rounding
+        const float factor = alpha * part_scale;
         uint32_t top = 0;
         float2 v[kTurns];
 #pragma unroll

@@ -204,12 +204,14 @@ def test_projection_matches_plain(case):
 LARGE = [
     # dtype, rows, k, n, adapters, rank, order: tiles of each edge, with rows and columns behind the last whole tile
     ("f16", 1030, 144, 8208, 6, 16, "mixed"),
-    ("bf16", 2100, 528, 5136, 3, 48, "mixed"),
+    ("bf16", 2100, 528, 5136, 3, 24, "mixed"),
     ("bf16", 3000, 208, 4112, 16, 128, "runs"),
     ("f16", 2060, 4112, 5136, 9, 8, "mixed"),
     ("bf16", 4100, 1040, 5152, 300, 24, "mixed"),
     ("f16", 16400, 256, 1040, 0, 0, None),
     ("bf16", 2500, 64, 1040, 4, 16, "runs"),
+    ("bf16", 2300, 2064, 288, 2, 72, "mixed"),
+    ("f16", 2050, 128, 16, 3, 16, "none"),
 ]
 
 
