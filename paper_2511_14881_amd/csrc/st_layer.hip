@@ -306,20 +306,14 @@ int st_rotate(const void* dev_q, int64_t q_stride, int32_t n_q_heads, const void
     a.freqs = dev_freqs;
     a.inverse = inverse != 0;
     a.columns = a.pairs / 8 + (d - 2 * a.pairs + 15) / 16;
-    const int64_t groups = ((int64_t)n_tok * a.columns + st::kLayerThreads - 1) / st::kLayerThreads;
-    // Heads to a thread: fewer where all would leave the chip idle.
-    const bool many = groups * ((n_q_heads + 7) / 8 + (n_k_heads + 7) / 8) >= 4 * st::kComputeUnits;
-    const int each = many ? 8 : 2;
-    a.parts[0] = (n_q_heads + each - 1) / each;
-    a.parts[1] = (n_k_heads + each - 1) / each;
-    if (a.parts[0] + a.parts[1] > 65535) return fail(ST_EINVAL, "too many heads for one call");
-    if ((rc = check_grid(groups * (a.parts[0] + a.parts[1])))) return rc;
+    a.parts[0] = (n_q_heads + st::kRotateHeads - 1) / st::kRotateHeads;
+    a.parts[1] = (n_k_heads + st::kRotateHeads - 1) / st::kRotateHeads;
+    const int64_t groups = ((int64_t)n_tok * a.columns * (a.parts[0] + a.parts[1]) + st::kLayerThreads - 1) / st::kLayerThreads;
+    if ((rc = check_grid(groups))) return rc;
     hipStream_t stream = (hipStream_t)hip_stream;
     const auto launch = [&](auto bf16, auto pairs) {
-        const dim3 grid((unsigned)groups, (unsigned)(a.parts[0] + a.parts[1])), threads(st::kLayerThreads);
         TimedLaunch t(0, stream);
-        if (many) hipLaunchKernelGGL((st::rotate_kernel<decltype(bf16)::value, decltype(pairs)::value, 8>), grid, threads, 0, stream, a);
-        else hipLaunchKernelGGL((st::rotate_kernel<decltype(bf16)::value, decltype(pairs)::value, 2>), grid, threads, 0, stream, a);
+        hipLaunchKernelGGL((st::rotate_kernel<decltype(bf16)::value, decltype(pairs)::value>), dim3((unsigned)groups), dim3(st::kLayerThreads), 0, stream, a);
     };
     const auto yes = std::true_type();
     const auto no = std::false_type();

@@ -229,20 +229,25 @@ struct RotateArgs {
     int32_t ends[kAxes];  // pairs of the axes so far
     const int32_t* positions;
     const double* freqs;
-    int32_t inverse, parts[2], columns;  // parts: of the heads of queries and keys; columns: threads to a token and part
+    int32_t inverse, parts[2], columns;  // parts: threads to a token and column for the heads of queries and keys; columns: threads to a token and part
 };
 
-// A thread takes eight pairs of a token (or 16 values that are not rotated) through kHeads heads: all loads first, then cos and sin, formed once,
-// then the products.  Turns are counted in fp64, of which the fraction goes to the hardware's cos and sin of turns.
-template <bool kBf16, bool kInterleaved, int kHeads>
+// (a, b) -> (a cos - b sin, a sin + b cos).  Bound by the rows read and written once.  A thread takes eight pairs of a token (or 16
+// values that are not rotated) through up to kRotateHeads heads: all loads first, then cos and sin, formed once, then the products.  Its
+// heads lie parts[] apart, so that at each step neighbouring threads take a token's neighbouring heads, and a wavefront's accesses are
+// one stretch of the row: 32768 tokens, 32 heads of 128, in place, 123.5 us (5.4 TB/s); with a thread's heads side by side 160 us.
+// One, two and eight heads to a thread: 215, 142 and 125 us (8000 tokens of 8 heads 13.3, 11.6 and 12.1, four 11.4; calls of few tokens
+// take the same with any).  Turns are counted in fp64, of which the fraction goes to the hardware's cos and sin of turns.
+constexpr int kRotateHeads = 4;
+template <bool kBf16, bool kInterleaved>
 __global__ __launch_bounds__(kLayerThreads) void rotate_kernel(RotateArgs a)
 {
     const int64_t at = (int64_t)blockIdx.x * kLayerThreads + threadIdx.x;
-    const int column = (int)(at % a.columns);
-    const int64_t tok = at / a.columns;
+    const int column = (int)(at % a.columns), all = a.parts[0] + a.parts[1];
+    const int64_t rest = at / a.columns, tok = rest / all;
     if (tok >= a.n_tok) return;
-    const int k = (int)blockIdx.y >= a.parts[0], first = ((int)blockIdx.y - (k ? a.parts[0] : 0)) * kHeads;
-    const int n = min(kHeads, a.heads[k] - first);
+    const int part = (int)(rest % all), k = part >= a.parts[0], first = k ? part - a.parts[0] : part;
+    const int n = (a.heads[k] - first + a.parts[k] - 1) / a.parts[k], step = a.parts[k] * a.d;
     const uint16_t* in = a.in[k] + tok * a.in_stride[k] + (int64_t)first * a.d;
     uint16_t* out = a.out[k] + tok * a.out_stride[k] + (int64_t)first * a.d;
     const bool turns = column < a.pairs / 8;
@@ -250,19 +255,19 @@ __global__ __launch_bounds__(kLayerThreads) void rotate_kernel(RotateArgs a)
     const int c0 = !turns ? plain : kInterleaved ? column * 16 : column * 8;
     const int c1 = !turns ? min(plain + 8, a.d - 8) : kInterleaved ? c0 + 8 : c0 + a.pairs;
     if (!turns && in == out) return;
-    uint4 v[kHeads][2];
+    uint4 v[kRotateHeads][2];
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h)
+    for (int h = 0; h < kRotateHeads; ++h)
         if (h < n) {
-            v[h][0] = *(const uint4*)(in + (int64_t)h * a.d + c0);
-            v[h][1] = *(const uint4*)(in + (int64_t)h * a.d + c1);
+            v[h][0] = *(const uint4*)(in + (int64_t)h * step + c0);
+            v[h][1] = *(const uint4*)(in + (int64_t)h * step + c1);
         }
     if (!turns) {
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h)
+        for (int h = 0; h < kRotateHeads; ++h)
             if (h < n) {
-                *(uint4*)(out + (int64_t)h * a.d + c0) = v[h][0];
-                *(uint4*)(out + (int64_t)h * a.d + c1) = v[h][1];
+                *(uint4*)(out + (int64_t)h * step + c0) = v[h][0];
+                *(uint4*)(out + (int64_t)h * step + c1) = v[h][1];
             }
         return;
     }
@@ -278,7 +283,7 @@ __global__ __launch_bounds__(kLayerThreads) void rotate_kernel(RotateArgs a)
         sn[u] = __builtin_amdgcn_sinf(a.inverse ? -turn : turn);
     }
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h)
+    for (int h = 0; h < kRotateHeads; ++h)
         if (h < n) {
             float f[16], g[16];
             eight_floats(v[h][0], kBf16, f);
@@ -289,8 +294,8 @@ __global__ __launch_bounds__(kLayerThreads) void rotate_kernel(RotateArgs a)
                 g[x] = f[x] * cs[u] - f[y] * sn[u];
                 g[y] = f[x] * sn[u] + f[y] * cs[u];
             }
-            Eight<kBf16 ? ST_BF16 : ST_F16>::store(out, (int64_t)h * a.d + c0, g);
-            Eight<kBf16 ? ST_BF16 : ST_F16>::store(out, (int64_t)h * a.d + c1, g + 8);
+            Eight<kBf16 ? ST_BF16 : ST_F16>::store(out, (int64_t)h * step + c0, g);
+            Eight<kBf16 ? ST_BF16 : ST_F16>::store(out, (int64_t)h * step + c1, g + 8);
         }
 }
 
