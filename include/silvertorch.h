@@ -492,13 +492,13 @@ int st_norm_rows(const void* dev_x, int64_t x_stride, const void* dev_residual, 
                  void* hip_stream);
 
 /* Low-rank adapters beside a projection from k to n values: for adapter i rows dev_a[i] [rank, k], dev_b[i] [n, rank] of the
- * output's dtype, finite, and a factor.  rank is a multiple of 8, 8 .. ST_MAX_RANK (a smaller one is filled up with zeros). */
+ * output's dtype and a factor.  rank is a multiple of 8, 8 .. ST_MAX_RANK (a smaller one is filled up with zeros). */
 #define ST_MAX_RANK 128
 #define ST_MAX_ADAPTERS 65536
 typedef struct st_adapters {
     const void* dev_a;       /* [n_adapters, rank, k] */
     const void* dev_b;       /* [n_adapters, n, rank] */
-    const float* dev_alpha;  /* [n_adapters], finite */
+    const float* dev_alpha;  /* [n_adapters] */
     int32_t n_adapters;      /* 1 .. ST_MAX_ADAPTERS */
     int32_t rank;
 } st_adapters;
@@ -511,9 +511,10 @@ typedef struct st_adapters {
  *   dev_out         rows of n values of dtype (ST_BF16, ST_F16), out_stride elements apart (a multiple of 8, at least n)
  *   workspace       st_project_workspace_bytes() bytes, 256-byte aligned, scratch
  * The first sum is exact (int32).  The inner values of an adapter, dot(a, x), are summed in fp32, divided by the power of two
- * that leaves the largest of a row's in [1, 2), and rounded to dtype before b multiplies them; all else is fp32, and outputs are rounded once.
+ * that leaves the largest of a row's in [1, 2) (2^-100 to 2^100; 1 where the largest is below), and rounded to dtype before b multiplies them; all else is fp32, and outputs are rounded once.
  * k and n are multiples of 16, k at most ST_MAX_ROW, n at most ST_MAX_OUT, n_rows >= 0.  Arrays 16-byte aligned (dev_x_scale, dev_adapter_of 4).
- * A row's result does not depend on the other rows.  A row whose x_scale is no number gives none.  Asynchronous, no allocation. */
+ * A row's result does not depend on the other rows, nor on adapters that are not its own, whatever these hold.  A row whose x_scale is no
+ * number gives none.  Asynchronous, no allocation. */
 #define ST_MAX_OUT 65536
 int64_t st_project_workspace_bytes(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters);
 int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, int32_t k, const int8_t* dev_w,

@@ -184,6 +184,8 @@ int st_norm_rows(const void* dev_x, int64_t x_stride, const void* dev_residual, 
     if ((rc = check_rows("x", dev_x, x_stride, d)) || (rc = check_rows("residual", dev_residual, residual_stride, d)) ||
         (rc = check_rows("sum", dev_out_sum, sum_stride, d)))
         return rc;
+    if ((dev_out_sum == dev_x && sum_stride != x_stride) || (dev_out_sum && dev_out_sum == dev_residual && sum_stride != residual_stride))
+        return fail(ST_EINVAL, "a sum in the place of x or of the residual keeps its stride");
     if (misaligned(dev_weight) || misaligned(dev_out_q) || misaligned(dev_out_y) || ((uintptr_t)dev_out_scale & 3))
         return fail(ST_EINVAL, "misaligned buffer (16 B)");
     const st::NormArgs a = {dev_x, dev_residual, dev_weight, dev_out_sum, dev_out_q, dev_out_scale, dev_out_y, x_stride, residual_stride,

@@ -535,6 +535,16 @@ __device__ inline void project_round(const float16v (&sum)[kN], float power, uin
     }
 }
 
+// Sums of the rows of one adapter with its part, of other rows as they were: what they would take on is 0 times an adapter's values, which
+// is no number for an infinite one.
+__device__ inline float16v project_with(const float16v& sum, const float16v& with, bool mine)
+{
+    float16v r;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) r[u] = mine ? with[u] : sum[u];
+    return r;
+}
+
 // A row of tiles of a wavefront: scales, the adapters' products on top, rounding.
 template <bool kBf16, int kN>
 __device__ inline void project_finish(const ProjectArgs& p, const int16v (&dot)[kN], const ProjectRow& mine, const float4v (&ws)[kN][4],
@@ -550,6 +560,7 @@ __device__ inline void project_finish(const ProjectArgs& p, const int16v (&dot)[
         const int all[1] = {mine.adapter};
         for (int a = next_of<32>(all, -1); a != 0x7FFFFFFF; a = next_of<32>(all, a)) {
             const uint16_t* wb = p.b + (int64_t)a * p.n * p.rank;
+            const bool alone = ballot(mine.adapter != a) == 0;
             for (int r0 = 0; r0 < p.rank; r0 += 16) {
                 const int r = r0 + (lane >> 5) * 8;
                 const uint4 v = project_inner_values(p, row, r, mine.adapter == a);
@@ -560,8 +571,13 @@ __device__ inline void project_finish(const ProjectArgs& p, const int16v (&dot)[
                     b[j] = make_uint4(0, 0, 0, 0);
                     if (n < p.n && r < p.rank) b[j] = *(const uint4*)(wb + (int64_t)n * p.rank + r);
                 }
+                if (alone) {
 #pragma unroll
-                for (int j = 0; j < kN; ++j) sum[j] = mfma_32<kBf16>(b[j], v, sum[j]);
+                    for (int j = 0; j < kN; ++j) sum[j] = mfma_32<kBf16>(b[j], v, sum[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kN; ++j) sum[j] = project_with(sum[j], mfma_32<kBf16>(b[j], v, sum[j]), mine.adapter == a);
+                }
             }
         }
     }
@@ -936,7 +952,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     auto add = [&](int a, int at, const uint4& b) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (adapter == a) v = *(const uint4*)&s_inner[row][at * 16 + (lane >> 5) * 8];
-        sum[0] = mfma_32<kBf16>(b, v, sum[0]);
+        sum[0] = project_with(sum[0], mfma_32<kBf16>(b, v, sum[0]), adapter == a);
     };
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)

@@ -82,11 +82,11 @@ class HistoryStore:
             raise ValueError(f"a history would hold {need.max()} blocks of at most {self.max_blocks}: evict first")
         # where the block that the first event goes to is shared, the history gets a copy of its own; the last holder keeps the page
         shares, copied = self.shares.copy(), []
-        for i in np.flatnonzero((lengths % st.ST_KV_BLOCK > 0) & (counts > 0)):
-            page = tables[i, have[i] - 1]
-            if shares[page] > 1:
-                shares[page] -= 1
-                copied.append((i, page))
+        tails = tables[np.arange(len(users)), np.maximum(have - 1, 0)]
+        for i in np.flatnonzero((lengths % st.ST_KV_BLOCK > 0) & (counts > 0) & (self.shares[tails] > 1)):
+            if shares[tails[i]] > 1:
+                shares[tails[i]] -= 1
+                copied.append((i, tails[i]))
         taken = int((need - have).sum()) + len(copied)
         if taken > len(self.free):
             raise ValueError(f"{taken} pages are needed, {len(self.free)} are free: evict first")

@@ -381,3 +381,75 @@ def test_copied_pages(heads, d):
     st.st_kv_copy(one, other, *lists)
     assert all(torch.equal(a, b) for a, b in zip(parts(other), want))
     st.st_kv_copy(one, one, lists[0][:0], lists[1][:0])
+
+
+@pytest.mark.parametrize("case", [("bf16", 17, 128, 128, 5, 24), ("f16", 64, 512, 80, 20, 16), ("bf16", 2, 512, 64, 2, 16), ("f16", 130, 208, 144, 4, 40),
+                                  ("bf16", 600, 96, 272, 9, 16), ("f16", 2100, 128, 5136, 3, 24), ("bf16", 4100, 64, 5152, 30, 8)])
+def test_projection_beside_adapters_that_are_no_numbers(case):
+    """Infinities and NaN in one tenant's adapter, another's factor that is none: the other tenants' rows keep their bits."""
+    say(f"[layer] projection beside bad adapters {case}")
+    dtype, rows, k, n, count, rank = case
+    args = project_case([(*case, "mixed")], 0)[1]
+    args[7][:count] = torch.arange(count, dtype=torch.int32)[: rows]
+    want = call(args, dtype=R.TYPES[dtype])
+    a, b, alpha = (t.clone() for t in args[4:7])
+    b[0, 0::3], b[0, 1::3] = float("inf"), float("nan")
+    a[0, 0], a[0, -1] = float("-inf"), float("nan")
+    alpha[count - 1] = float("nan")
+    got = call((*args[:4], a, b, alpha, args[7]), dtype=R.TYPES[dtype])
+    kept = ((args[7] != 0) & (args[7] != count - 1)).cuda()
+    assert torch.equal(got[kept], want[kept]) and not torch.isfinite(got[~kept][:, 0]).any()
+
+
+def test_offsets_beyond_32_bits():
+    """Rows, heads, adapters, outputs and pages that lie more than 2^31 elements behind the first: as in a call of their own."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n, d, last = 131072 + 40, 16384, 70
+    say("[layer] norm beyond 2^31 values")
+    x = torch.empty((n, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    rows, own = st.st_norm_rows(x), st.st_norm_rows(x[-last:].clone())
+    assert torch.equal(rows.q[-last:], own.q) and torch.equal(rows.scale[-last:], own.scale)
+    del x
+    say("[layer] projection of more than 2^31 values")
+    w, ws = torch.randint(-128, 128, (32, d), dtype=torch.int8, device="cuda"), torch.full((32,), 2.0 ** -12, device="cuda")
+    ad = st.Adapters(torch.randn((6, 8, d), device="cuda").bfloat16(), torch.randn((6, 32, 8), device="cuda").bfloat16(), torch.ones(6, device="cuda"))
+    of = torch.arange(n, dtype=torch.int32, device="cuda") % 7
+    got = st.st_project(rows.q, rows.scale, w, ws, ad, of)
+    assert torch.equal(got[-last:], st.st_project(own.q, own.scale, w, ws, ad, of[-last:].clone()))
+    del rows, got
+    say("[layer] adapters beyond 2^31 values")
+    count, k = st.ST_MAX_ADAPTERS, 4112
+    a, b = (torch.empty(shape, dtype=torch.float16, device="cuda").normal_(generator=gen) for shape in ((count, 8, k), (count, k, 8)))
+    alpha = torch.rand(count, device="cuda", generator=gen)
+    w, ws = torch.randint(-128, 128, (k, k), dtype=torch.int8, device="cuda"), torch.full((k,), 2.0 ** -16, device="cuda")
+    many = st.Adapters(a, b, alpha)
+    few = st.Adapters(a[-16:].clone(), b[-16:].clone(), alpha[-16:].clone())
+    for m in (1, 20, 70):
+        of = torch.randint(count - 16, count, (m,), dtype=torch.int32, device="cuda")
+        q, scale = torch.randint(-128, 128, (m, k), dtype=torch.int8, device="cuda"), torch.full((m,), 2.0 ** -6, device="cuda")
+        assert torch.equal(st.st_project(q, scale, w, ws, many, of), st.st_project(q, scale, w, ws, few, of - (count - 16)))
+    del a, b, many
+    say("[layer] outputs beyond 2^31 values")
+    m, stride = 16500, 131072
+    base = torch.zeros((m * stride,), dtype=torch.bfloat16, device="cuda")
+    q, scale = torch.randint(-128, 128, (m, 64), dtype=torch.int8, device="cuda"), torch.full((m,), 2.0 ** -6, device="cuda")
+    w, ws = w[:64, :64].contiguous(), ws[:64].contiguous()
+    got = st.st_project(q, scale, w, ws, out=base.as_strided((m, 64), (stride, 1)))
+    assert torch.equal(got, st.st_project(q, scale, w, ws))
+    del base, got
+    say("[layer] rotation beyond 2^31 values")
+    n, heads, d = 262144 + 40, 64, 128
+    q = torch.empty((n, heads, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    pos = torch.randint(0, 1 << 30, (1, n), dtype=torch.int32, device="cuda")
+    freqs = torch.rand(32, dtype=torch.float64, device="cuda")
+    want = st.st_rotate(q[-last:].clone(), None, pos[:, -last:].contiguous(), freqs, (32,))[0]
+    st.st_rotate(q, None, pos, freqs, (32,), out=(q, None))
+    assert torch.equal(q[-last:], want)
+    del q
+    say("[layer] pages beyond 2^31 bytes")
+    cache = st.KvCache.empty(33000, 8, 128)
+    for t in (cache.k, cache.v, cache.bounds):
+        t[32990:] = torch.randint(-128, 128, t[32990:].shape, dtype=torch.int8, device="cuda")
+    st.st_kv_copy(cache, cache, *(torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([32999, 32991], [1, 32980])))
+    for t in (cache.k, cache.v, cache.bounds):
+        assert torch.equal(t[1], t[32999]) and torch.equal(t[32980], t[32991]) and t[1].any()

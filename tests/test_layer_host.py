@@ -52,7 +52,7 @@ def test_bad_norms_are_refused():
     for kw in (dict(dtype=3), dict(dtype=-1), dict(n=-1), dict(n=1 << 31), dict(d=0), dict(d=24), dict(d=16400), dict(eps=0.0), dict(eps=NAN),
                dict(eps=2.0), dict(eps=1e-13), dict(x=None), dict(q=None), dict(scale=None), dict(q=None, scale=None, total=None),
                dict(x=P + 8), dict(xs=255), dict(xs=250), dict(xs=252), dict(rs=248), dict(ts=260), dict(r=P + 2), dict(w=P + 4),
-               dict(total=P + 8), dict(y=P + 2), dict(scale=P + 2)):
+               dict(total=P + 8), dict(y=P + 2), dict(scale=P + 2), dict(ts=264, r=None), dict(x=P + 4096, ts=264)):
         assert norm(**kw) == st.ST_EINVAL, kw
         assert st.last_error()
     assert norm(n=(1 << 31) - 1, d=16384, xs=16384, rs=16384, ts=16384) == st.ST_EINVAL  # more workgroups than a launch has
