@@ -333,8 +333,8 @@ int st_kv_copy(const st_kv_cache* from, const st_kv_cache* to, const int32_t* de
     if (!dev_src || !dev_dst) return fail(ST_EINVAL, "null argument");
     if (((uintptr_t)dev_src & 3) || ((uintptr_t)dev_dst & 3)) return fail(ST_EINVAL, "misaligned list of pages (4 B)");
     st::KvCopyArgs a = {view(from), view(to), dev_src, dev_dst, 0, from->n_heads * from->d * (ST_KV_BLOCK / 16), from->n_heads * from->d / 8};
-    a.parts = (2 * a.rows16 + a.bounds16 + st::kKvThreads * st::kCopyLoads - 1) / (st::kKvThreads * st::kCopyLoads);
-    const int64_t groups = (int64_t)n * a.parts;
+    a.parts = (a.rows16 + st::kKvThreads * st::kCopyLoads - 1) / (st::kKvThreads * st::kCopyLoads);
+    const int64_t groups = (int64_t)n * (2 * a.parts + 1);
     if (groups > 0xFFFFFFll) return fail(ST_EINVAL, "too many pages for one call: %lld workgroups of at most 16777215", (long long)groups);
     {
         TimedLaunch t(0, (hipStream_t)hip_stream);

@@ -282,37 +282,40 @@ struct KvCopyArgs {
     KvCacheView from, to;
     const int32_t* src;
     const int32_t* dst;
-    int32_t parts;           // workgroups to a page
+    int32_t parts;             // workgroups to a page's keys, and as many to its values
     int32_t rows16, bounds16;  // pieces of 16 bytes of a page's keys (values as many), and of its bounds
 };
 
 constexpr int kCopyLoads = 4;  // 16-byte pieces of a thread
 
-// A page is one run of pieces, keys, values and bounds behind each other; each workgroup takes kKvThreads * kCopyLoads of them.
+// A workgroup takes kKvThreads * kCopyLoads pieces of a page's keys or values, or all of its bounds and scales.
 __global__ __launch_bounds__(kKvThreads) void kv_copy_kernel(KvCopyArgs a)
 {
-    const int i = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-    const int from = kv_page_of(a.from, a.src[i]), to = kv_page_of(a.to, a.dst[i]);
+    const int each = 2 * a.parts + 1, i = blockIdx.x / each, part = blockIdx.x % each, tid = threadIdx.x;
+    const int32_t src = a.src[i], dst = a.dst[i];
+    const int from = kv_page_of(a.from, src), to = kv_page_of(a.to, dst);
     if (from < 0 || to < 0) return;
-    const int all = 2 * a.rows16 + a.bounds16;
-    uint4 w[kCopyLoads];
-    const int first = part * (kKvThreads * kCopyLoads) + threadIdx.x;
-    auto place = [&](const KvCacheView& c, int page, int p) -> uint4* {
-        if (p < a.rows16) return (uint4*)c.k + (int64_t)page * a.rows16 + p;
-        if (p < 2 * a.rows16) return (uint4*)c.v + (int64_t)page * a.rows16 + (p - a.rows16);
-        return (uint4*)c.bounds + (int64_t)page * a.bounds16 + (p - 2 * a.rows16);
-    };
-#pragma unroll
-    for (int u = 0; u < kCopyLoads; ++u)
-        if (first + u * kKvThreads < all) w[u] = *place(a.from, from, first + u * kKvThreads);
-#pragma unroll
-    for (int u = 0; u < kCopyLoads; ++u)
-        if (first + u * kKvThreads < all) *place(a.to, to, first + u * kKvThreads) = w[u];
-    if (part == a.parts - 1)
-        for (int h = threadIdx.x; h < a.from.n_heads; h += kKvThreads) {
-            a.to.k_scale[(int64_t)to * a.to.n_heads + h] = a.from.k_scale[(int64_t)from * a.from.n_heads + h];
-            a.to.v_scale[(int64_t)to * a.to.n_heads + h] = a.from.v_scale[(int64_t)from * a.from.n_heads + h];
+    const int heads = a.from.n_heads;
+    if (part == 2 * a.parts) {
+        for (int h = tid; h < heads; h += kKvThreads) {
+            const float k = a.from.k_scale[(int64_t)from * heads + h], v = a.from.v_scale[(int64_t)from * heads + h];
+            a.to.k_scale[(int64_t)to * heads + h] = k;
+            a.to.v_scale[(int64_t)to * heads + h] = v;
         }
+        for (int p = tid; p < a.bounds16; p += kKvThreads)
+            ((int4v*)a.to.bounds)[(int64_t)to * a.bounds16 + p] = ((const int4v*)a.from.bounds)[(int64_t)from * a.bounds16 + p];
+        return;
+    }
+    const bool keys = part < a.parts;
+    const int4v* in = (const int4v*)(keys ? a.from.k : a.from.v) + (int64_t)from * a.rows16;
+    int4v* out = (int4v*)(keys ? a.to.k : a.to.v) + (int64_t)to * a.rows16;
+    const int first = (keys ? part : part - a.parts) * (kKvThreads * kCopyLoads) + tid;
+    int4v w[kCopyLoads];
+#pragma unroll
+    for (int u = 0; u < kCopyLoads; ++u) w[u] = in[min(first + u * kKvThreads, a.rows16 - 1)];
+#pragma unroll
+    for (int u = 0; u < kCopyLoads; ++u)
+        if (first + u * kKvThreads < a.rows16) __builtin_nontemporal_store(w[u], out + first + u * kKvThreads);
 }
 
 // ---------------------------------------------------------------- the best n of an array of keys

@@ -74,6 +74,7 @@ struct Eight {
     uint4 w;
     __device__ void load(const void* p, int64_t at) { w = *(const uint4*)((const uint16_t*)p + at); }
     __device__ void floats(float* f) const { eight_floats(w, kBf16, f); }
+    __device__ void wait() { asm volatile("" : "+v"(w.x)); }  // its load has ended behind this
     __device__ static void store(void* p, int64_t at, const float* f)
     {
         *(uint4*)((uint16_t*)p + at) = make_uint4(two_16<kBf16>(f[0], f[1]), two_16<kBf16>(f[2], f[3]), two_16<kBf16>(f[4], f[5]), two_16<kBf16>(f[6], f[7]));
@@ -96,6 +97,7 @@ struct Eight<ST_F32> {
     {
         f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
     }
+    __device__ void wait() { asm volatile("" : "+v"(a.x), "+v"(b.x)); }
     __device__ static void store(void* p, int64_t at, const float* f)
     {
         *(float4*)((float*)p + at) = make_float4(f[0], f[1], f[2], f[3]);
@@ -129,21 +131,27 @@ __global__ __launch_bounds__(kLayerThreads) void norm_rows_kernel(NormArgs a)
     const bool live = row < a.n_rows;
     const int64_t at = live ? row : a.n_rows - 1;  // (a wavefront's lanes all take part in its steps)
     const int n8 = a.d >> 3;
-    Eight<kType> x[kVectors], r[kVectors];
+    // All loads come first and without conditions (behind a row's end its last vector is read again): one under a condition is waited for
+    // before the next, and one behind a store waits for that too.
+    Eight<kType> x[kVectors], r[kVectors], w[kVectors];
+    int64_t v8[kVectors];
 #pragma unroll
-    for (int i = 0; i < kVectors; ++i)
-        if (i * kLanes + lane < n8) x[i].load(a.x, at * a.x_stride + (i * kLanes + lane) * 8);
+    for (int i = 0; i < kVectors; ++i) {
+        v8[i] = min(i * kLanes + lane, n8 - 1) * 8;
+        x[i].load(a.x, at * a.x_stride + v8[i]);
+    }
     if (a.residual)
 #pragma unroll
-        for (int i = 0; i < kVectors; ++i)
-            if (i * kLanes + lane < n8) r[i].load(a.residual, at * a.residual_stride + (i * kLanes + lane) * 8);
+        for (int i = 0; i < kVectors; ++i) r[i].load(a.residual, at * a.residual_stride + v8[i]);
+    if (a.weight)
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) w[i].load(a.weight, v8[i]);
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) w[i].wait();
     float h[kVectors][8];
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) h[i][u] = 0.0f;
-        if (i * kLanes + lane >= n8) continue;
         x[i].floats(h[i]);
         if (a.residual) {
             float f[8];
@@ -151,7 +159,12 @@ __global__ __launch_bounds__(kLayerThreads) void norm_rows_kernel(NormArgs a)
 #pragma unroll
             for (int u = 0; u < 8; ++u) h[i][u] = Eight<kType>::rounded(h[i][u] + f[u]);
         }
-        if (a.sum && live) Eight<kType>::store(a.sum, row * a.sum_stride + (i * kLanes + lane) * 8, h[i]);
+        if (i * kLanes + lane < n8) {
+            if (a.sum && live) Eight<kType>::store(a.sum, row * a.sum_stride + v8[i], h[i]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) h[i][u] = 0.0f;
+        }
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum += h[i][u] * h[i][u];
     }
@@ -177,14 +190,11 @@ __global__ __launch_bounds__(kLayerThreads) void norm_rows_kernel(NormArgs a)
     uint32_t top = 0;  // largest magnitude as its bits, of which NaN's are the largest
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
-        if (i * kLanes + lane >= n8) continue;
         if (a.weight) {
-            Eight<kType> w;
             float f[8];
-            w.load(a.weight, (i * kLanes + lane) * 8);
-            w.floats(f);
+            w[i].floats(f);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) h[i][u] *= f[u];
+            for (int u = 0; u < 8; ++u) h[i][u] = i * kLanes + lane < n8 ? h[i][u] * f[u] : 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) top = max(top, __float_as_uint(h[i][u]) & 0x7FFFFFFFu);
