@@ -116,6 +116,12 @@ __device__ inline void load_to_lds(const int8_t* from, int8_t* to)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
+// The same, 4 bytes.
+__device__ inline void word_to_lds(const void* from, int8_t* to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+}
+
 // ---------------------------------------------------------------- rows in the order of their adapters
 // Rows of a segment are dealt into buckets by adapter (those without one behind the others), so that a tile of the kernels below
 // meets few adapters: each costs it a load of operands and products with all its rows.  A segment to a workgroup, counts and places in the
@@ -470,34 +476,15 @@ __global__ __launch_bounds__(64) void project_parts_kernel(ProjectArgs p)
 // Tiles are 32 rows x 32 columns, as the columns and rows of a matrix product w x^T: lane l has row m0 + l % 32, and columns
 // n0 + 8 * (u / 4) + 4 * (l / 32) + u % 4 for u < 16.  The sums of products take on scales and the adapters' part in the same registers.
 struct ProjectRow {
-    int adapter;
+    int row, adapter;
     float scale;  // x_scale / 2^e
     float power;  // 2^e
 };
 
-template <int N>
-__device__ inline void project_rows(const ProjectArgs& p, const int64_t (&m)[N], const int64_t (&row)[N], ProjectRow (&r)[N])
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i) r[i] = {-1, p.x_scale[row[i]], 1.0f};
-    if (!p.a) return;
-    int of[N];
-    float power[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) power[i] = p.power[row[i]];  // (what a row without an adapter has is not used)
-    project_adapters<N>(p, m, row, of);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        r[i].adapter = of[i];
-        r[i].power = of[i] >= 0 ? power[i] : 1.0f;
-        r[i].scale *= __uint_as_float(0x7F000000u - __float_as_uint(r[i].power));
-    }
-}
-
 // Eight of a row's inner values, from rank r on; zeros for a row of another adapter and behind the last rank.
-__device__ inline uint4 project_inner_values(const ProjectArgs& p, int64_t row, int r, bool mine)
+__device__ inline uint4 project_inner_values(const ProjectArgs& p, int row, int r, bool mine)
 {
-    if (mine && r < p.rank) return *(const uint4*)(p.inner + row * p.rank + r);
+    if (mine && r < p.rank) return *(const uint4*)(p.inner + (int64_t)row * p.rank + r);
     return make_uint4(0, 0, 0, 0);
 }
 
@@ -545,43 +532,47 @@ __device__ inline float16v project_with(const float16v& sum, const float16v& wit
     return r;
 }
 
-// A row of tiles of a wavefront: scales, the adapters' products on top, rounding.
-template <bool kBf16, int kN>
-__device__ inline void project_finish(const ProjectArgs& p, const int16v (&dot)[kN], const ProjectRow& mine, const float4v (&ws)[kN][4],
-                                      int64_t row, int n0, uint4 (&out)[kN][2])
+// The adapters' products on top of the scaled sums of kTM x kTN tiles, 16 ranks of an adapter at a time, all rows' operands with one trip to
+// memory.
+template <bool kBf16, int kTM, int kTN>
+__device__ inline void project_add_adapters(const ProjectArgs& p, float16v (&sum)[kTM][kTN], const ProjectRow (&rows)[kTM], int n0)
 {
     const int lane = threadIdx.x & 63;
-    float16v sum[kN];
+    int of[kTM];
 #pragma unroll
-    for (int j = 0; j < kN; ++j)
+    for (int i = 0; i < kTM; ++i) of[i] = rows[i].adapter;
+    for (int a = next_of<32>(of, -1); a != 0x7FFFFFFF; a = next_of<32>(of, a)) {
+        const uint16_t* wb = p.b + (int64_t)a * p.n * p.rank;
+        bool alone = true;
 #pragma unroll
-        for (int u = 0; u < 16; ++u) sum[j][u] = (float)dot[j][u] * mine.scale * ws[j][u / 4][u % 4];
-    if (p.a) {
-        const int all[1] = {mine.adapter};
-        for (int a = next_of<32>(all, -1); a != 0x7FFFFFFF; a = next_of<32>(all, a)) {
-            const uint16_t* wb = p.b + (int64_t)a * p.n * p.rank;
-            const bool alone = ballot(mine.adapter != a) == 0;
-            for (int r0 = 0; r0 < p.rank; r0 += 16) {
-                const int r = r0 + (lane >> 5) * 8;
-                const uint4 v = project_inner_values(p, row, r, mine.adapter == a);
-                uint4 b[kN];
+        for (int i = 0; i < kTM; ++i) alone = alone && ballot(of[i] != a) == 0;
+        for (int r0 = 0; r0 < p.rank; r0 += 16) {
+            const int r = r0 + (lane >> 5) * 8;
+            uint4 v[kTM], b[kTN];
 #pragma unroll
-                for (int j = 0; j < kN; ++j) {
-                    const int n = n0 + 32 * j + (lane & 31);
-                    b[j] = make_uint4(0, 0, 0, 0);
-                    if (n < p.n && r < p.rank) b[j] = *(const uint4*)(wb + (int64_t)n * p.rank + r);
-                }
-                if (alone) {
+            for (int i = 0; i < kTM; ++i) v[i] = project_inner_values(p, rows[i].row, r, of[i] == a);
 #pragma unroll
-                    for (int j = 0; j < kN; ++j) sum[j] = mfma_32<kBf16>(b[j], v, sum[j]);
-                } else {
+            for (int j = 0; j < kTN; ++j) {
+                const int n = n0 + 32 * j + (lane & 31);
+                b[j] = make_uint4(0, 0, 0, 0);
+                if (n < p.n && r < p.rank) b[j] = *(const uint4*)(wb + (int64_t)n * p.rank + r);
+            }
+            if (alone) {
 #pragma unroll
-                    for (int j = 0; j < kN; ++j) sum[j] = project_with(sum[j], mfma_32<kBf16>(b[j], v, sum[j]), mine.adapter == a);
-                }
+                for (int i = 0; i < kTM; ++i)
+#pragma unroll
+                    for (int j = 0; j < kTN; ++j) sum[i][j] = mfma_32<kBf16>(b[j], v[i], sum[i][j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kTM; ++i)
+#pragma unroll
+                    for (int j = 0; j < kTN; ++j) {
+                        sum[i][j] = project_with(sum[i][j], mfma_32<kBf16>(b[j], v[i], sum[i][j]), of[i] == a);
+                        __builtin_amdgcn_sched_barrier(0);  // (one tile's sums twice, not all)
+                    }
             }
         }
     }
-    project_round<kBf16, kN>(sum, mine.power, out);
 }
 
 template <int kN>
@@ -594,6 +585,26 @@ __device__ inline void project_store(const ProjectArgs& p, const uint4 (&out)[kN
             const int n = n0 + 32 * j + 16 * g + (threadIdx.x >> 5 & 1) * 8;
             if (row < p.n_rows && n < p.n) *(uint4*)((uint16_t*)p.out + row * p.out_stride + n) = out[j][g];
         }
+}
+
+// The same by whole lines, through 4096 bytes of the LDS that are the wavefront's own: neighbouring lanes store a row's neighbouring
+// columns, 128 bytes of it (as they lie in the registers, 32; 1024 values of k, 16384 x 4096: 121 us against 107; half lines
+// with tiles of 64 gain nothing).  row: -1 behind the last one.
+__device__ inline void project_store_lines(const ProjectArgs& p, const uint4 (&out)[2][2], int row, int n0, int8_t* own)
+{
+    const int lane = threadIdx.x & 63, m = lane & 31;
+    auto place = [](int m, int piece) { return m * 128 + (piece ^ (m & 7)) * 16; };
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) *(int4v*)(own + place(m, j * 4 + g * 2 + (lane >> 5))) = __builtin_bit_cast(int4v, out[j][g]);
+    const int n = n0 + (lane & 7) * 8;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int at = q * 8 + (lane >> 3), to = __shfl(row, at);
+        const int4v v = *(const int4v*)(own + place(at, lane & 7));
+        if (to >= 0 && n < p.n) *(int4v*)((uint16_t*)p.out + to * p.out_stride + n) = v;
+    }
 }
 
 // ---------------------------------------------------------------- tiles that share rows and weights
@@ -616,7 +627,10 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
     constexpr int kLoads = (kBM + kBN) / 8 / kWaves;  // of 1024 bytes, a wavefront's of a step
     static_assert((kBM + kBN) / 8 % kWaves == 0, "a step's loads are shared evenly");
     static_assert((kStages - 1) * kLoads <= 63, "loads in flight are counted in six bits");
-    __shared__ __align__(1024) int8_t lds[kStages * kStage];
+    static_assert(kWaves * 64 >= kBM && kWaves * 64 >= kBN, "a thread to each row and column");
+    // behind the steps: of the rows their number, adapter, scale and power of two, of the columns the scale
+    constexpr int kRowOf = kStages * kStage, kAdapter = kRowOf + kBM * 4, kScale = kAdapter + kBM * 4, kPower = kScale + kBM * 4, kColumn = kPower + kBM * 4;
+    __shared__ __align__(1024) int8_t lds[kColumn + kBN * 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles_n = (p.n + kBN - 1) / kBN, tiles_m = (int)(((int64_t)p.n_rows + kBM - 1) / kBM);
     // A die's workgroups take neighbouring tiles, eight rows of tiles at a time.
@@ -636,10 +650,22 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
     const int steps = (p.k + 127) >> 7, tail = p.k & 127;
     auto piece_of = [&](int i) { return place((wave * kLoads + i) * 8 + (lane >> 3), lane & 7) * 16; };
     {
-        int64_t at[kLoads], rows[kLoads];
+        // (64 rows' or columns' words are a wavefront's where wave * 64 lies among them)
+        int64_t at[kLoads + 1], rows[kLoads + 1];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) at[i] = m0 + (wave * kLoads + i) * 8 + (lane >> 3);
-        project_places<kLoads>(p, at, rows);
+        at[kLoads] = m0 + wave * 64 + lane;
+        project_places<kLoads + 1>(p, at, rows);
+        if (wave * 64 < kBM) {
+            const int64_t row = rows[kLoads];
+            word_to_lds(p.x_scale + row, lds + kScale + wave * 256);
+            if (p.a) {
+                word_to_lds(p.adapter_of + row, lds + kAdapter + wave * 256);
+                word_to_lds(p.power + row, lds + kPower + wave * 256);
+            }
+            if (p.order) word_to_lds(p.order + min(at[kLoads], (int64_t)p.n_rows - 1), lds + kRowOf + wave * 256);
+        }
+        if (wave * 64 < kBN) word_to_lds(p.w_scale + min(n0 + wave * 64 + lane, p.n - 1), lds + kColumn + wave * 256);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int first = (wave * kLoads + i) * 8;
@@ -720,29 +746,49 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
         half_step(b, a, stage, 0, true);
         loaded();
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the steps are read, and nothing is on its way to them
     // All loads come before the first store: a wait for a load would be one for the stores before it too.
-    int64_t at_row[kTM];
-    ProjectRow rows[kTM];
-    float4v ws[kTN][4];
-    {
-        int64_t m[kTM];
-#pragma unroll
-        for (int i = 0; i < kTM; ++i) m[i] = m0 + wm + 32 * i + (lane & 31);
-        project_places<kTM>(p, m, at_row);
-        project_rows<kTM>(p, m, at_row, rows);
-#pragma unroll
-        for (int i = 0; i < kTM; ++i) at_row[i] = m[i] < p.n_rows ? at_row[i] : (int64_t)p.n_rows;
-    }
-    project_scales<kTN>(p, ws, n0 + wn);
+    const int half = lane >> 5;
+    auto word = [&](int at, int i) { return *(const int*)(lds + at + i * 4); };
+    // Two rows of tiles at a time: all at once do not fit the registers, and one by one they take as many trips to memory.
+    constexpr int kAtOnce = kTM < 4 ? 1 : 2;
     uint4 out[kTM][kTN][2];
 #pragma unroll
-    for (int i = 0; i < kTM; ++i) {
-        project_finish<kBf16, kTN>(p, dot[i], rows[i], ws, at_row[i], n0 + wn, out[i]);
-        __builtin_amdgcn_sched_barrier(0);  // (rows of tiles one after the other: all at once do not fit the registers)
+    for (int i0 = 0; i0 < kTM; i0 += kAtOnce) {
+        float16v sum[kAtOnce][kTN];
+        ProjectRow mine[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int m = wm + 32 * (i0 + i) + (lane & 31);
+            mine[i] = {p.order ? word(kRowOf, m) : (int)min(m0 + m, (int64_t)p.n_rows - 1), -1, __int_as_float(word(kScale, m)), 1.0f};
+            if (p.a) {
+                const int of = word(kAdapter, m);
+                if (m0 + m < p.n_rows && of >= 0 && of < p.n_adapters) {
+                    mine[i].adapter = of;
+                    mine[i].power = __int_as_float(word(kPower, m));
+                }
+                mine[i].scale *= __uint_as_float(0x7F000000u - __float_as_uint(mine[i].power));
+            }
+#pragma unroll
+            for (int j = 0; j < kTN; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int4v ws = *(const int4v*)(lds + kColumn + (wn + 32 * j + 8 * g + 4 * half) * 4);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) sum[i][j][4 * g + u] = (float)dot[i0 + i][j][4 * g + u] * mine[i].scale * __int_as_float(ws[u]);
+                }
+        }
+        if (p.a) project_add_adapters<kBf16, kAtOnce, kTN>(p, sum, mine, n0 + wn);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) project_round<kBf16, kTN>(sum[i], mine[i].power, out[i0 + i]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int i = 0; i < kTM; ++i) project_store<kTN>(p, out[i], at_row[i], n0 + wn);
+    for (int i = 0; i < kTM; ++i) {
+        const int m = wm + 32 * i + (lane & 31), row = p.order ? word(kRowOf, m) : (int)min(m0 + m, (int64_t)p.n_rows - 1);
+        if constexpr (kTN == 2) project_store_lines(p, out[i], m0 + m < p.n_rows ? row : -1, n0 + wn, lds + wave * 4096);
+        else project_store<kTN>(p, out[i], m0 + m < p.n_rows ? (int64_t)row : (int64_t)p.n_rows, n0 + wn);
+    }
 }
 
 // ---------------------------------------------------------------- few rows
