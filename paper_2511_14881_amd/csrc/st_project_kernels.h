@@ -614,11 +614,15 @@ __device__ inline void project_store_lines(const ProjectArgs& p, const uint4 (&o
 // number gives, so that 16 lanes that read one piece of 16 rows meet all banks (no conflicts counted).  The last k % 128 values
 // come first, through registers, with zeros behind them.
 //
-// Bound by the matrix units and, with the whole chip at work, by its power: 8192 x 8192 x 8192 takes 511 us (2150 TOP/s), the products
+// Bound by the matrix units and, with the whole chip at work, by its power: 8192 x 8192 x 8192 takes 512 us (2150 TOP/s), the products
 // alone 334, without loads 423, without reads of the LDS 457 (the clock is at 1.8 GHz then, 2.4 with a tenth of the chip, where a
-// step of 256 x 256 takes 1.02 us and its products 0.85).  16384 x 4096 x 5120: 323 us, 2130 TOP/s.  Tried: four wavefronts with 128 x 128 each
-// (345 us; fewer reads, but a SIMD waits with its only wavefront), steps of 64 values with four and five stages (356), tiles of
-// 256 x 128 (498), loads and reads in the first half of the products between which they stand (327).
+// step of 256 x 256 takes 1.02 us and its products 0.85).  16384 x 4096 x 5120: 315 us, 2180 TOP/s, with 16 adapters of rank 32 in runs of rows 365
+// in all.  What follows the products takes some 8 us of a tile of 256 x 256, half of it the stores, which all workgroups begin at once.
+// Its rows' and columns' words therefore come with the first steps, and the adapters' operands with one trip for two rows of tiles (16384 x
+// 4096 x 4096 266 us -> 255; with the adapters above 377 -> 365).  Tried: four wavefronts with 128 x 128 each
+// (345 us for 323; fewer reads, but a SIMD waits with its only wavefront), steps of 64 values with four and five stages (356), tiles of
+// 256 x 128 (498), loads and reads in the first half of the products between which they stand (327); all rows of tiles at once behind
+// the products (registers spill); stores past the caches (417 for 348).
 // kWM x kWN wavefronts of kTM x kTN tiles of 32 x 32, kStages steps in the LDS
 template <bool kBf16, int kWM, int kWN, int kTM, int kTN, int kStages>
 __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs p)
@@ -792,7 +796,7 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
 }
 
 // ---------------------------------------------------------------- few rows
-// Up to 32 kTM rows: bound by the weights' way from memory, each read once.  A workgroup has 32 columns; its wavefronts take 64 values of
+// Up to 32 kTM rows: bound by the weights' way from memory, each read once (4096 x 5120: one row 7.2 us a call, 64 9.4, of which a launch is 5).  A workgroup has 32 columns; its wavefronts take 64 values of
 // k each in turn, straight into the operands of the matrix instructions, and join their sums in the LDS.  Then each wavefront has a
 // tile and every kShare-th adapter among the rows: it multiplies those, and stores the rows (its lanes) that have one of them.
 constexpr int kFewWaves = 8;
