@@ -796,9 +796,12 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
 }
 
 // ---------------------------------------------------------------- few rows
-// Up to 32 kTM rows: bound by the weights' way from memory, each read once (4096 x 5120: one row 7.2 us a call, 64 9.4, of which a launch is 5).  A workgroup has 32 columns; its wavefronts take 64 values of
-// k each in turn, straight into the operands of the matrix instructions, and join their sums in the LDS.  Then each wavefront has a
-// tile and every kShare-th adapter among the rows: it multiplies those, and stores the rows (its lanes) that have one of them.
+// Up to 32 kTM rows: bound by the weights' way from memory, each read once (4096 x 5120: one row 7.2 us a call, 64 9.3, of which a launch is 5;
+// 64 of 32 adapters of rank 16 18).  A workgroup has 32 columns; rows and weights come to the LDS kStages - 1 steps of 256 values of k ahead, of
+// which each wavefront multiplies 32; they join their sums in the LDS.  Then each wavefront has a tile and every kShare-th adapter among the
+// rows: it multiplies those, and stores the rows (its lanes) that have one of them.  Tried: further adapters' operands four at a time too
+// (the same); the parts of the inner values summed before this kernel, by workgroups of all parts (18.9 for 18.2 with rank 16, 19.7 for
+// 22.6 with three adapters of rank 128).
 constexpr int kFewWaves = 8;
 
 // kWithInner: the adapters' inner values are summed here too, by each workgroup for itself, a part of k by each wavefront: one launch
