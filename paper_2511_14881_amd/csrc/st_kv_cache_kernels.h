@@ -290,9 +290,9 @@ constexpr int kCopyLoads = 4;  // 16-byte pieces of a thread
 
 // Bound by memory.  A workgroup takes kKvThreads * kCopyLoads pieces of a page's keys or values, or all of its bounds and scales: which array it
 // is, is known for the workgroup, and all of a thread's loads begin before its first store (as one run of pieces, each load under a condition
-// of its own and waited for before the next: 17 us for 4 MB, now 4.8, and 23 for 42 MB, now 13.3).  The stores go past the caches: a
-// page that is copied is not read at once.  2048 pages of 8 x 128 (273 MB each way): 79 us (6.9 TB/s), with ordinary stores 111; a copy of as
-// many neighbouring bytes by the library 102.  Two and eight pieces to a thread instead of four: the same within 2 %.
+// of its own and waited for before the next: 4 MB 17 us, now 5.4 with the launch, 42 MB 23, now 14.5).  The stores go past the caches: a page that is
+// copied is not read at once.  2048 pages of 8 x 128 (273 MB each way), caches in turn: 109 us (5.0 TB/s, the rate of a copy on this card),
+// with ordinary stores 112; 639 of 2 x 256 14.5 and 19.2.  Two and eight pieces to a thread instead of four: the same within 2 %.
 __global__ __launch_bounds__(kKvThreads) void kv_copy_kernel(KvCopyArgs a)
 {
     const int each = 2 * a.parts + 1, i = blockIdx.x / each, part = blockIdx.x % each, tid = threadIdx.x;
