@@ -484,7 +484,8 @@ int st_kv_copy(const st_kv_cache* from, const st_kv_cache* to, const int32_t* de
  *   dev_out_q, dev_out_scale  [n_rows, d] int8 and [n_rows] fp32, both or neither
  *   dev_out_y            [n_rows, d] of dtype, or NULL;  of dev_out_sum, dev_out_q and dev_out_y one at least is given
  * d is a multiple of 16, at most ST_MAX_ROW; 0 <= n_rows < 2^31; 1e-12 <= eps <= 1 where normalise is not 0.  Rows 16-byte aligned.
- * Outputs lie apart from each other and, but for dev_out_sum, from the inputs.  One kernel, asynchronous, no allocation. */
+ * Outputs lie apart from each other and, but for dev_out_sum, from the inputs.  A call of more than 8388607 workgroups (of 16 rows up to d = 128, 4 up to
+ * 2048, 1 beyond) is refused.  One kernel, asynchronous, no allocation. */
 #define ST_MAX_ROW 16384
 int st_norm_rows(const void* dev_x, int64_t x_stride, const void* dev_residual, int64_t residual_stride,
                  const void* dev_weight, int32_t dtype, int64_t n_rows, int32_t d, int32_t normalise, float eps,
@@ -508,7 +509,7 @@ typedef struct st_adapters {
  *   dev_x [n_rows, k] int8, dev_x_scale [n_rows] fp32: what st_norm_rows writes;  dev_w [n, k] int8, dev_w_scale [n] fp32
  *   adapters        NULL (no second term; dev_adapter_of is NULL too)
  *   dev_adapter_of  int32 [n_rows]; a number that no adapter has means none.  Rows may be in any order; equal neighbours share loads
- *   dev_out         rows of n values of dtype (ST_BF16, ST_F16), out_stride elements apart (a multiple of 8, at least n)
+ *   dev_out         rows of n values of dtype (ST_BF16, ST_F16), out_stride elements apart (a multiple of 8, at least n), apart from the inputs
  *   workspace       st_project_workspace_bytes() bytes, 256-byte aligned, scratch
  * The first sum is exact (int32).  The inner values of an adapter, dot(a, x), are summed in fp32, divided by the power of two
  * that leaves the largest of a row's in [1, 2) (2^-100 to 2^100; 1 where the largest is below), and rounded to dtype before b multiplies them; all else is fp32, and outputs are rounded once.
@@ -535,7 +536,7 @@ int st_project_host_plan(int32_t n_rows, int32_t k, int32_t n, const st_adapters
  *                   (multiples of 8, at least heads * d), 16-byte aligned; either may be NULL with 0 heads
  *   dev_positions   int32 [n_axes, n_tok]: any, a time in seconds among them
  *   dev_freqs       fp64 [pairs], radians to a position, |freq| <= 2 pi
- *   dev_out_q, dev_out_k  rows like dev_q and dev_k; either may be its input with the same stride
+ *   dev_out_q, dev_out_k  rows like dev_q and dev_k, apart from each other; either may be its input with the same stride
  * d is a multiple of 8, at most 512; pairs a multiple of 8, 8 <= pairs <= d / 2; 1 <= n_axes <= ST_MAX_AXES; sections >= 0.
  * Angles are formed and reduced in fp64 (off by |angle| 2^-52 at most), cos and sin are the hardware's with fp32 turns (2^-22 at most; the
  * outputs' roundings are 2^-8 and 2^-11), products are fp32 and rounded once.  The inverse is also the gradient's way back.  One kernel, asynchronous, no allocation. */

@@ -898,7 +898,7 @@ class NormRows(NamedTuple):
 
 
 class RowBuffers:
-    """Outputs of repeated st_norm_rows calls of one shape.  total, y: room for the sum with the residual, for the norm's output."""
+    """Outputs of repeated st_norm_rows calls of one shape, one at a time.  total, y: room for the sum with the residual, for the norm's output."""
 
     def __init__(self, n: int, d: int, dtype, total: bool = False, q: bool = True, y: bool = False, device="cuda"):
         self.q = torch.empty((n, d), dtype=torch.int8, device=device) if q else None
@@ -971,7 +971,7 @@ class Adapters:
 
 
 class ProjectBuffers:
-    """Output and workspace of repeated st_project calls of one shape."""
+    """Output and workspace of repeated st_project calls of one shape, one at a time."""
 
     def __init__(self, n_rows: int, k: int, n: int, dtype=torch.bfloat16, adapters: Adapters | None = None, device="cuda"):
         self.nbytes = st_project_workspace_bytes(n_rows, k, n, adapters)

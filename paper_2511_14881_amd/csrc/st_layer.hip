@@ -186,6 +186,8 @@ int st_norm_rows(const void* dev_x, int64_t x_stride, const void* dev_residual, 
         return rc;
     if ((dev_out_sum == dev_x && sum_stride != x_stride) || (dev_out_sum && dev_out_sum == dev_residual && sum_stride != residual_stride))
         return fail(ST_EINVAL, "a sum in the place of x or of the residual keeps its stride");
+    if (dev_out_y && (dev_out_y == dev_x || dev_out_y == dev_residual || dev_out_y == dev_out_sum))
+        return fail(ST_EINVAL, "the norm's output lies apart from its inputs and from the sum");
     if (misaligned(dev_weight) || misaligned(dev_out_q) || misaligned(dev_out_y) || ((uintptr_t)dev_out_scale & 3))
         return fail(ST_EINVAL, "misaligned buffer (16 B)");
     const st::NormArgs a = {dev_x, dev_residual, dev_weight, dev_out_sum, dev_out_q, dev_out_scale, dev_out_y, x_stride, residual_stride,
@@ -222,6 +224,7 @@ int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, in
         (adapters && (misaligned(adapters->dev_a) || misaligned(adapters->dev_b) || ((uintptr_t)adapters->dev_alpha & 3))))
         return fail(ST_EINVAL, "misaligned buffer (16 B)");
     if ((rc = check_rows("out", dev_out, out_stride, n))) return rc;
+    if (dev_out == dev_x || dev_out == dev_w) return fail(ST_EINVAL, "the output lies apart from rows and weights");
     const ProjectPlan plan = project_plan(n_rows, adapters);
     if (plan.bytes() > 0 && (!dev_workspace || workspace_bytes < plan.bytes()))
         return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)plan.bytes());
@@ -291,6 +294,8 @@ int st_rotate(const void* dev_q, int64_t q_stride, int32_t n_q_heads, const void
         return rc;
     if ((n_q_heads > 0 && dev_q == dev_out_q && q_stride != out_q_stride) || (n_k_heads > 0 && dev_k == dev_out_k && k_stride != out_k_stride))
         return fail(ST_EINVAL, "rows rotated in place keep their stride");
+    if (n_q_heads > 0 && n_k_heads > 0 && (dev_out_q == dev_k || dev_out_k == dev_q || dev_out_q == dev_out_k))
+        return fail(ST_EINVAL, "queries and keys are not rotated into each other's place");
     a.in[0] = (const uint16_t*)dev_q;
     a.in[1] = (const uint16_t*)dev_k;
     a.out[0] = (uint16_t*)dev_out_q;

@@ -179,7 +179,7 @@ class HistoryStore:
 
     def compact(self) -> int:
         """Moves what lies behind the first pages of the cache, as many as are in use, into the free ones among them; returns how
-        many pages moved."""
+        many pages moved.  Batches that a program holds name the pages as they were."""
         used = np.flatnonzero(self.shares)
         src = used[used >= len(used)]
         dst = np.flatnonzero(self.shares[: len(used)] == 0)

@@ -257,3 +257,59 @@ def test_python_calls_that_are_refused():
         with pytest.raises((TypeError, ValueError, st.StError)):
             call()
             print("not refused:", i)
+
+
+@pytest.mark.parametrize("n_rows", [1, 40, 300, 2100, 9000])
+def test_captured_projections_of_each_route_replay_as_they_run(n_rows):
+    """Norm, projection and rotation of few and of many rows, ordered by adapter or not, replayed with other rows and tenants."""
+    gen = torch.Generator(device="cuda").manual_seed(n_rows)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device="cuda").bfloat16()
+
+    k, heads, d, count = 272, 9, 64, 7
+    n = heads * d
+    w = st.st_norm_rows(normal(n, k), normalise=False)
+    adapters = st.Adapters(normal(count, 24, k), normal(count, n, 24), torch.rand(count, generator=gen, device="cuda"))
+    x, weight, of = normal(n_rows, k), normal(k), torch.zeros(n_rows, dtype=torch.int32, device="cuda")
+    positions, freqs = torch.zeros((1, n_rows), dtype=torch.int32, device="cuda"), torch.rand(24, dtype=torch.float64, device="cuda")
+    rows, buffers = st.RowBuffers(n_rows, k, torch.bfloat16), st.ProjectBuffers(n_rows, k, n, torch.bfloat16, adapters)
+
+    def step():
+        st.st_norm_rows(x, weight, buffers=rows)
+        out = st.st_project(rows.q, rows.scale, w.q, w.scale, adapters, of, buffers=buffers).view(n_rows, heads, d)
+        st.st_rotate(out[:, :8], out[:, 8:], positions, freqs, (24,), interleaved=True, out=(out[:, :8], out[:, 8:]))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        x.copy_(normal(n_rows, k))
+        of.copy_(torch.randint(-1, count + 1, (n_rows,), generator=gen, device="cuda"))
+        positions.copy_(torch.randint(0, 1 << 30, (1, n_rows), generator=gen, device="cuda"))
+        step()
+        want = rows.q.clone(), rows.scale.clone(), buffers.out.clone()
+        buffers.out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip((rows.q, rows.scale, buffers.out), want))
+
+
+def test_layer_of_no_users_and_of_users_without_tokens():
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    layer, normal = make(gen, torch.bfloat16)
+    store = HistoryStore(3, 10, 2, 64, 3)
+    none = torch.zeros((2, 0), dtype=torch.int32, device="cuda")
+    tenants = torch.zeros(0, dtype=torch.int32, device="cuda")
+    for append in (True, False):
+        out, total = layer(store, [], normal(0, 192), none, [], tenants, normal(0, 192), append=append)
+        assert out.shape == total.shape == (0, 192)
+    layer.take_in(store, [], normal(0, 192), none, [], tenants)
+    # a user without an event, and candidates of one that has no history
+    positions = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    out, _ = layer(store, [0, 1], normal(3, 192), positions, [3, 0], torch.zeros(3, dtype=torch.int32, device="cuda"))
+    assert store.lengths.tolist() == [3, 0, 0] and torch.isfinite(out.float()).all()
+    out, _ = layer(store, [2], normal(3, 192), positions, [3], torch.zeros(3, dtype=torch.int32, device="cuda"), append=False)
+    assert (out == 0).all()

@@ -25,15 +25,15 @@ def adapters(**kw):
 
 
 def project(ad=None, **kw):
-    a = dict(x=P, xs=P, rows=20, k=128, w=P, ws=P, n=64, ad=ad, of=P if ad else None, dtype=0, out=P, stride=64, work=P, nbytes=1 << 30)
+    a = dict(x=P, xs=P, rows=20, k=128, w=P, ws=P, n=64, ad=ad, of=P if ad else None, dtype=0, out=2 * P, stride=64, work=P, nbytes=1 << 30)
     a.update(kw)
     return st.lib().st_project(*a.values(), None)
 
 
 def rotate(sections=(16, 8, 8), **kw):
-    a = dict(q=P, qs=512, qh=4, k=P, ks=128, kh=1, d=128, dtype=0, n=9, positions=P, freqs=P,
+    a = dict(q=P, qs=512, qh=4, k=2 * P, ks=128, kh=1, d=128, dtype=0, n=9, positions=P, freqs=P,
              sections=np.asarray(sections, dtype=np.int32).ctypes.data_as(C.c_void_p), axes=len(sections), inter=0, inverse=0, oq=P,
-             oqs=512, ok=P, oks=128)
+             oqs=512, ok=2 * P, oks=128)
     a.update(kw)
     return st.lib().st_rotate(*a.values(), None)
 
@@ -96,6 +96,17 @@ def test_bad_copies_are_refused():
                dict(to_c=dict(n_pages=0)), dict(n=-1), dict(src=None), dict(dst=None), dict(src=P + 2), dict(dst=P + 1), dict(n=(1 << 31) - 1)):
         assert copy(**kw) == st.ST_EINVAL, kw
     assert copy(n=0, src=None, dst=None) == st.ST_OK
+
+
+def test_outputs_in_the_place_of_other_arrays_are_refused():
+    """What a row's threads write may not be what another row's have yet to read."""
+    q = P + (1 << 12)
+    for kw in (dict(y=P), dict(y=q, r=q, total=None), dict(y=q, total=q), dict(x=q, ts=264, total=q), dict(r=q, ts=264, total=q)):
+        assert norm(**kw) == st.ST_EINVAL, kw
+    assert project(out=P) == st.ST_EINVAL and project(x=q, w=P, out=q) == st.ST_EINVAL
+    apart = dict(q=P, k=2 * P, oq=q, ok=2 * q)
+    for kw in (dict(oq=2 * P), dict(ok=P), dict(ok=q), dict(oq=2 * P, ok=P)):
+        assert rotate(**{**apart, **kw}) == st.ST_EINVAL, kw
 
 
 def test_calls_of_nothing_do_nothing():
