@@ -524,7 +524,7 @@ int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, in
                void* hip_stream);
 
 /* Diagnostic, host part alone (no device memory is touched): how st_project would run such a call.  host_out_plan[3] receives {edge of the tiles that
- * share rows and weights (0: a workgroup takes all rows), rows to a workgroup that sums an adapter's inner values (1: a wavefront to
+ * share rows and weights (0: a workgroup takes up to 64 rows and 32 columns), rows to a workgroup that sums an adapter's inner values (1: a wavefront to
  * each part of k; 0: none does, or the kernel of the products does itself), 1 if rows are brought into their adapters' order first}. */
 int st_project_host_plan(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters, int32_t* host_out_plan);
 

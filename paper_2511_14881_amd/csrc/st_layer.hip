@@ -65,8 +65,19 @@ int check_project(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapt
     return ST_OK;
 }
 
-// Rows up to which a workgroup takes all of them.
-constexpr int kFewRows = 64;
+// Rows that a workgroup takes where there are few, and rows up to which there may be several such workgroups to 32 columns: as long as the
+// compute units take all of them at once, they need no more time than one, and the adapters' inner values come in over the whole chip, unless
+// those are many.  Calls in us, tiles / this, mixed rows: k = 4096, n = 896, 96 rows without adapters 9.9 / 8.1, 36 adapters of rank 16
+// 29.9 / 16.9, 8 of 128 58 / 30, 384 rows 10.5 / 8.7, 25.2 / 23.3, 53.2 / 53.9; k = n = 512 7.0 / 6.6, 13.6 / 13.1, 21.0 / 24.5; 229 rows, 752, 1568, 20
+// of 128 33.0 / 35.5; 128 rows, 512, 4096 6.7 / 7.0, 16.8 / 13.0.  In more than one round: 96 rows, k = 4096, n = 5120 10.6 / 14.8; of more rows:
+// 1024, 4096, 256, 36 adapters of rank 16 24.6 / 36.3.
+constexpr int kFewRows = 64, kFewMost = 384, kFewRanks = 24576;  // of all rows
+bool project_few(int32_t n_rows, int32_t n, const st_adapters* a)
+{
+    if (n_rows <= kFewRows) return true;
+    return n_rows <= kFewMost && (n_rows + kFewRows - 1) / kFewRows * ((n + 31) / 32) <= st::kComputeUnits && (!a || n_rows * a->rank <= kFewRanks);
+}
+
 // Rows up to which a workgroup that sums inner values takes 16, beyond 32.  Kernel in us, 16 / 32 / 64: 2048 rows, k = 4096, rank 16 9.9 / 11.7 /
 // 17.4; 4096, 1024, 64 14.5 / 13.9 / 18.7; 16384, 4096, 32 57 / 36 / 39.
 constexpr int kOneTileRows = 2048;
@@ -76,7 +87,7 @@ constexpr int kOneTileRows = 2048;
 // 180 / 157, 16 of 32 791 / 409.  Rows that come in runs pay for it: 1000, 16 adapters 21.9 / 26.7, 16384 373 / 385.
 bool project_ordered(int32_t n_rows, const st_adapters* a)
 {
-    return n_rows > kFewRows && (a->n_adapters >= 5 || (n_rows > kOneTileRows && (a->n_adapters - 1) * a->rank >= 64));
+    return a->n_adapters >= 5 || (n_rows > kOneTileRows && (a->n_adapters - 1) * a->rank >= 64);
 }
 
 struct ProjectPlan {
@@ -84,11 +95,11 @@ struct ProjectPlan {
     int64_t bytes() const { return inner + power + order; }
 };
 
-ProjectPlan project_plan(int32_t n_rows, const st_adapters* adapters)
+ProjectPlan project_plan(int32_t n_rows, int32_t n, const st_adapters* adapters)
 {
     if (!adapters) return {0, 0, 0};
     const int64_t values = (int64_t)n_rows * adapters->rank, words = st::round_up((int64_t)n_rows * 4, 256);
-    if (n_rows <= kFewRows) return {st::round_up(values * 4 * st::kInnerParts, 256), 0, 0};
+    if (project_few(n_rows, n, adapters)) return {st::round_up(values * 4 * st::kInnerParts, 256), 0, 0};
     return {st::round_up(values * 2, 256), words, project_ordered(n_rows, adapters) ? words : 0};
 }
 
@@ -123,7 +134,7 @@ void launch_inner(const st::ProjectArgs& p, hipStream_t stream)
 
 // What a call runs: a function of its sizes alone.
 struct ProjectRoute {
-    bool few, fused;  // few: a workgroup takes all rows; fused: it sums the inner values too
+    bool few, fused;  // few: a workgroup takes 64 rows; fused: it sums the inner values too
     int edge;         // of the tiles where there are many
     bool order;
     int64_t tiles;
@@ -132,11 +143,11 @@ struct ProjectRoute {
 ProjectRoute project_route(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapters)
 {
     ProjectRoute r;
-    r.few = n_rows <= kFewRows;
+    r.few = project_few(n_rows, n, adapters);
     const int64_t ranks = adapters ? (int64_t)n_rows * ((adapters->rank + 15) / 16 * 16) : 0;
     r.fused = adapters && ranks <= st::kFusedRanks && ranks * k <= st::kFusedValues;
     r.edge = project_edge(n_rows, k, n);
-    r.order = adapters && project_ordered(n_rows, adapters);
+    r.order = adapters && !r.few && project_ordered(n_rows, adapters);
     r.tiles = r.few ? (n + 31) / 32 : ((int64_t)n_rows + r.edge - 1) / r.edge * ((n + r.edge - 1) / r.edge);
     return r;
 }
@@ -155,7 +166,7 @@ void launch_project(const st::ProjectArgs& p, const ProjectRoute& r, hipStream_t
         else launch_inner<kBf16, 2>(p, stream);
     }
     TimedLaunch t(0, stream);
-    const dim3 groups((unsigned)r.tiles), few(st::kFewWaves * 64);
+    const dim3 groups((unsigned)r.tiles, r.few ? (unsigned)((p.n_rows + kFewRows - 1) / kFewRows) : 1u), few(st::kFewWaves * 64);
     if (r.fused) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 1, true>), groups, few, 0, stream, p);
     else if (r.few && p.n_rows <= 32) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 1, false>), groups, few, 0, stream, p);
     else if (r.few) hipLaunchKernelGGL((st::project_few_kernel<kBf16, 2, false>), groups, few, 0, stream, p);
@@ -204,7 +215,7 @@ int64_t st_project_workspace_bytes(int32_t n_rows, int32_t k, int32_t n, const s
 {
     int rc;
     if ((rc = check_project(n_rows, k, n, adapters))) return rc;
-    return std::max<int64_t>(256, project_plan(n_rows, adapters).bytes());
+    return std::max<int64_t>(256, project_plan(n_rows, n, adapters).bytes());
 }
 
 int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, int32_t k, const int8_t* dev_w,
@@ -225,7 +236,7 @@ int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, in
         return fail(ST_EINVAL, "misaligned buffer (16 B)");
     if ((rc = check_rows("out", dev_out, out_stride, n))) return rc;
     if (dev_out == dev_x || dev_out == dev_w) return fail(ST_EINVAL, "the output lies apart from rows and weights");
-    const ProjectPlan plan = project_plan(n_rows, adapters);
+    const ProjectPlan plan = project_plan(n_rows, n, adapters);
     if (plan.bytes() > 0 && (!dev_workspace || workspace_bytes < plan.bytes()))
         return fail(ST_EWORKSPACE, "workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)plan.bytes());
     if ((uintptr_t)dev_workspace & 255) return fail(ST_EINVAL, "misaligned workspace (256 B)");

@@ -796,7 +796,7 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
 }
 
 // ---------------------------------------------------------------- few rows
-// Up to 32 kTM rows: bound by the weights' way from memory, each read once (4096 x 5120: one row 7.2 us a call, 64 9.3, of which a launch is 5;
+// Up to 32 kTM rows to a workgroup: bound by the weights' way from memory, read once for as many (4096 x 5120: one row 7.2 us a call, 64 9.3, of which a launch is 5;
 // 64 of 32 adapters of rank 16 18).  A workgroup has 32 columns; rows and weights come to the LDS kStages - 1 steps of 256 values of k ahead, of
 // which each wavefront multiplies 32; they join their sums in the LDS.  Then each wavefront has a tile and every kShare-th adapter among the
 // rows: it multiplies those, and stores the rows (its lanes) that have one of them.  Tried: further adapters' operands four at a time too
@@ -829,18 +829,19 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     float* s_parts = (float*)(lds + kParts);  // [part][row][rank]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = blockIdx.x * 32, n = n0 + (lane & 31);
+    const int row0 = blockIdx.y * (32 * kTM), n_rows = min(p.n_rows - row0, 32 * kTM);  // rows are counted from row0 on
     // (what others' addresses come from is asked for before the steps: loads end in the order in which they begin)
     const int tile = wave / kShare, share = wave % kShare;
-    const int64_t row = 32 * tile + (lane & 31);
-    const float scale = row < p.n_rows ? p.x_scale[row] : 0.0f;
-    const int asked = p.a && row < p.n_rows ? p.adapter_of[row] : -1;
+    const int row = 32 * tile + (lane & 31);
+    const float scale = row < n_rows ? p.x_scale[row0 + row] : 0.0f;
+    const int asked = p.a && row < n_rows ? p.adapter_of[row0 + row] : -1;
     float4v ws[1][4];
     project_scales<1>(p, ws, n0);
     // the parts of the inner values: kWide threads to a row, two ranks at a time
     constexpr int kWide = kFewWaves * 2 / kTM, kTurns = ST_MAX_RANK / 2 / kWide;
     const int m = tid / kWide, l = tid % kWide;
-    const int part_asked = p.a && m < p.n_rows ? p.adapter_of[m] : -1;
-    const float part_scale = p.a && m < p.n_rows ? p.x_scale[m] : 0.0f;
+    const int part_asked = p.a && m < n_rows ? p.adapter_of[row0 + m] : -1;
+    const float part_scale = p.a && m < n_rows ? p.x_scale[row0 + m] : 0.0f;
     // what this lane loads: of each four rows row lane / 16, the piece that lies at place lane % 16
     const int8_t* from[kLoads];
     const int steps = (p.k + 255) >> 8, tail = p.k & 255;
@@ -849,7 +850,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     for (int i = 0; i < kLoads; ++i) {
         const int at = (wave * kLoads + i) * 4 + (lane >> 4);
         const bool rows = at < 32 * kTM;
-        from[i] = (rows ? p.x : p.w) + (int64_t)(rows ? min(at, p.n_rows - 1) : min(n0 + at - 32 * kTM, p.n - 1)) * p.k + piece_of(i);
+        from[i] = (rows ? p.x : p.w) + (int64_t)(rows ? row0 + min(at, n_rows - 1) : min(n0 + at - 32 * kTM, p.n - 1)) * p.k + piece_of(i);
     }
     int ahead = 0, to = 0;  // the step that is loaded next and its stage; behind the last one it is loaded again, to where it is not read
     if (tail) {
@@ -899,7 +900,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     if (p.a) {
         bool again = adapter < 0;
         int first = lane & 31;  // the first row with this one's adapter
-        for (int i = min(p.n_rows - 32 * tile, 32) - 1; i >= 0; --i)
+        for (int i = min(n_rows - 32 * tile, 32) - 1; i >= 0; --i)
             if (__builtin_amdgcn_readlane(adapter, i) == adapter) first = i;
         again = again || first != (lane & 31);
         const uint32_t firsts = (uint32_t)ballot(!again);
@@ -939,7 +940,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
             if (2 * (t * kWide + l) < p.rank)
 #pragma unroll
                 for (int q = 0; q < kInnerParts; ++q)
-                    parts[t][q] = *(const float2*)((kWithInner ? s_parts : p.parts) + ((int64_t)q * p.n_rows + m) * p.rank + 2 * (t * kWide + l));
+                    parts[t][q] = *(const float2*)((kWithInner ? s_parts : p.parts) + ((int64_t)q * p.n_rows + row0 + m) * p.rank + 2 * (t * kWide + l));
     }
     int16v dot[kTM] = {};
     // a wavefront has 32 of a step's 256 values of k: pieces 2 wave and 2 wave + 1
@@ -1014,7 +1015,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
         while (advance()) add(next, c, operand(next, c));
     uint4 out[1][2];
     project_round<kBf16, 1>(sum, power, out);
-    project_store<1>(p, out, stores ? row : (int64_t)p.n_rows, n0);
+    project_store<1>(p, out, stores && row < n_rows ? (int64_t)row0 + row : (int64_t)p.n_rows, n0);
 }
 
 }  // namespace st

@@ -163,6 +163,20 @@ PROJECTIONS = [
     ("bf16", 2100, 4720, 32, 2, 32, "runs"),
     ("f16", 2100, 2592, 32, 6, 128, "mixed"),
     ("bf16", 1, 992, 48, 4, 32, "mixed"),
+    # several workgroups of 64 rows, and rows or columns beyond what those take
+    ("bf16", 100, 512, 4096, 9, 24, "mixed"),
+    ("f16", 384, 272, 1344, 5, 64, "mixed"),
+    ("f16", 384, 272, 1360, 5, 64, "mixed"),
+    ("bf16", 190, 272, 144, 3, 128, "mixed"),
+    ("bf16", 200, 272, 144, 3, 128, "mixed"),
+    ("f16", 65, 64, 8224, 6, 16, "mixed"),
+    ("f16", 395, 208, 336, 2, 128, "runs"),
+    ("bf16", 391, 96, 1296, 0, 0, None),
+    ("f16", 410, 656, 1040, 4, 40, "mixed"),
+    ("bf16", 400, 4096, 256, 3, 64, "runs"),
+    ("bf16", 449, 1040, 528, 16, 72, "mixed"),
+    ("f16", 390, 16384, 32, 2, 8, "none"),
+    ("f16", 386, 5152, 32, 3, 64, "mixed"),
 ]
 
 
@@ -238,7 +252,7 @@ def test_large_projection_matches_plain(case):
         assert torch.equal(part, got[first:last])
 
 
-@pytest.mark.parametrize("case", [2, 5, 9, 11, 14])
+@pytest.mark.parametrize("case", [2, 5, 9, 11, 14, 24, 25, 27, 33])
 def test_projection_of_a_row_does_not_depend_on_others(case):
     dtype, args = project_case(PROJECTIONS, case)
     want = call(args, dtype=R.TYPES[dtype])
@@ -383,7 +397,7 @@ def test_copied_pages(heads, d):
     st.st_kv_copy(one, one, lists[0][:0], lists[1][:0])
 
 
-@pytest.mark.parametrize("case", [("bf16", 17, 128, 128, 5, 24), ("f16", 64, 512, 80, 20, 16), ("bf16", 2, 512, 64, 2, 16), ("f16", 130, 208, 144, 4, 40),
+@pytest.mark.parametrize("case", [("bf16", 17, 128, 128, 5, 24), ("f16", 64, 512, 80, 20, 16), ("bf16", 2, 512, 64, 2, 16), ("f16", 130, 208, 144, 4, 40), ("f16", 420, 208, 144, 4, 40),
                                   ("bf16", 600, 96, 272, 9, 16), ("f16", 2100, 128, 5136, 3, 24), ("bf16", 4100, 64, 5152, 30, 8)])
 def test_projection_beside_adapters_that_are_no_numbers(case):
     """Infinities and NaN in one tenant's adapter, another's factor that is none: the other tenants' rows keep their bits."""

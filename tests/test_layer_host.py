@@ -121,7 +121,9 @@ def test_routes_of_projections():
     assert plan(1, 512, 1024) == {"edge": 0, "inner_rows": 0, "order": 0}
     assert plan(1, 4096, 1024, 8, 16) == {"edge": 0, "inner_rows": 1, "order": 0}
     assert plan(64, 512, 1024, 8, 16) == {"edge": 0, "inner_rows": 1, "order": 0}
-    assert plan(65, 512, 1024, 4, 16) == {"edge": 64, "inner_rows": 16, "order": 0}
+    assert plan(384, 512, 1024, 8, 16) == {"edge": 0, "inner_rows": 1, "order": 0}
+    assert plan(192, 512, 1024, 8, 128)["edge"] == 0 and plan(193, 512, 1024, 8, 128)["edge"] == 64
+    assert plan(385, 512, 1024, 4, 16) == plan(65, 512, 8192 + 16, 4, 16) == {"edge": 64, "inner_rows": 16, "order": 0}
     assert plan(1001, 1040, 1296, 5, 8) == {"edge": 64, "inner_rows": 16, "order": 1}
     assert plan(16384, 4096, 5120, 16, 32) == {"edge": 256, "inner_rows": 32, "order": 1}
     assert plan(16384, 4096, 5120) == {"edge": 256, "inner_rows": 0, "order": 0}
