@@ -100,7 +100,7 @@ ProjectPlan project_plan(int32_t n_rows, int32_t n, const st_adapters* adapters)
     if (!adapters) return {0, 0, 0};
     const int64_t values = (int64_t)n_rows * adapters->rank, words = st::round_up((int64_t)n_rows * 4, 256);
     if (project_few(n_rows, n, adapters)) return {st::round_up(values * 4 * st::kInnerParts, 256), 0, 0};
-    return {st::round_up(values * 2, 256), words, project_ordered(n_rows, adapters) ? words : 0};
+    return {st::round_up(values * 4, 256), words, project_ordered(n_rows, adapters) ? words : 0};
 }
 
 // Edge of the tiles of many rows by an estimate of the call's microseconds.  64 (three workgroups to a compute unit): the longer of one

@@ -17,7 +17,7 @@ struct ProjectArgs {
     const uint16_t* b;
     const float* alpha;
     const int32_t* adapter_of;
-    uint16_t* inner;    // [n_rows, rank]: alpha x_scale a x / 2^e, rounded
+    uint16_t* inner;    // [n_rows, 2, rank]: alpha x_scale a x / 2^e, rounded, and what the rounding left, rounded
     float* power;       // [n_rows]: 2^e
     float* parts;       // few rows, in place of inner and power: [kInnerParts, n_rows, rank], a x over a part of k each
     int32_t* order;     // [n_rows]: rows of one adapter side by side; NULL: as they come
@@ -251,6 +251,15 @@ __device__ inline uint32_t project_exponent(uint32_t top)
     return e < 27 || e == 255 ? 127u : min(e, 227u);
 }
 
+// A number as the sum of two 16-bit ones: rounded, and what the rounding left, rounded (nothing beside an infinity).
+template <bool kBf16>
+__device__ inline void two_halves(float v, uint16_t* high, uint16_t* low)
+{
+    *high = one_16<kBf16>(v);
+    const float h = kBf16 ? bf16_float(*high) : f16_float(*high);
+    *low = one_16<kBf16>(fabsf(h) < __builtin_inff() ? v - h : 0.0f);
+}
+
 // The same for many rows: operands come through the LDS, in space of the wavefront's own, kSlots - 1 steps ahead.  A load straight into a
 // lane's operand touches 64 places with 64 lanes, which an address unit takes one by one; rows in the LDS come in by lines.  A step is
 // 64 values of k and two tiles of ranks; the rows come with a chunk's first.
@@ -445,7 +454,10 @@ __global__ __launch_bounds__(kInnerParts * 64) void project_inner_kernel(Project
 #pragma unroll
             for (int c = 0; c < kEach; ++c) {
                 const int r = c * 32 + l;
-                if (r < p.rank) p.inner[row * p.rank + r] = one_16<kBf16>(v[c] * down);
+                if (r < p.rank) {
+                    uint16_t* at = p.inner + row * 2 * p.rank + r;
+                    two_halves<kBf16>(v[c] * down, at, at + p.rank);
+                }
             }
             if (l == 0) p.power[row] = __uint_as_float(e << 23);
         }
@@ -481,11 +493,26 @@ struct ProjectRow {
     float power;  // 2^e
 };
 
-// Eight of a row's inner values, from rank r on; zeros for a row of another adapter and behind the last rank.
-__device__ inline uint4 project_inner_values(const ProjectArgs& p, int row, int r, bool mine)
+// The halves of eight of a row's inner values, from rank r on; zeros for a row of another adapter and behind the last rank.
+struct InnerValues {
+    uint4 high, low;
+};
+__device__ inline InnerValues project_inner_values(const ProjectArgs& p, int row, int r, bool mine)
 {
-    if (mine && r < p.rank) return *(const uint4*)(p.inner + (int64_t)row * p.rank + r);
-    return make_uint4(0, 0, 0, 0);
+    InnerValues v = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (mine && r < p.rank) {
+        const uint16_t* at = p.inner + (int64_t)row * 2 * p.rank + r;
+        v.high = *(const uint4*)at;
+        v.low = *(const uint4*)(at + p.rank);
+    }
+    return v;
+}
+
+// An adapter's products with inner values: with the first halves, and then with the second.
+template <bool kBf16>
+__device__ inline float16v project_inner_products(const uint4& b, const InnerValues& v, const float16v& sum)
+{
+    return mfma_32<kBf16>(b, v.low, mfma_32<kBf16>(b, v.high, sum));
 }
 
 // The weights' scales of a lane's columns.
@@ -548,7 +575,8 @@ __device__ inline void project_add_adapters(const ProjectArgs& p, float16v (&sum
         for (int i = 0; i < kTM; ++i) alone = alone && ballot(of[i] != a) == 0;
         for (int r0 = 0; r0 < p.rank; r0 += 16) {
             const int r = r0 + (lane >> 5) * 8;
-            uint4 v[kTM], b[kTN];
+            InnerValues v[kTM];
+            uint4 b[kTN];
 #pragma unroll
             for (int i = 0; i < kTM; ++i) v[i] = project_inner_values(p, rows[i].row, r, of[i] == a);
 #pragma unroll
@@ -561,13 +589,13 @@ __device__ inline void project_add_adapters(const ProjectArgs& p, float16v (&sum
 #pragma unroll
                 for (int i = 0; i < kTM; ++i)
 #pragma unroll
-                    for (int j = 0; j < kTN; ++j) sum[i][j] = mfma_32<kBf16>(b[j], v[i], sum[i][j]);
+                    for (int j = 0; j < kTN; ++j) sum[i][j] = project_inner_products<kBf16>(b[j], v[i], sum[i][j]);
             } else {
 #pragma unroll
                 for (int i = 0; i < kTM; ++i)
 #pragma unroll
                     for (int j = 0; j < kTN; ++j) {
-                        sum[i][j] = project_with(sum[i][j], mfma_32<kBf16>(b[j], v[i], sum[i][j]), of[i] == a);
+                        sum[i][j] = project_with(sum[i][j], project_inner_products<kBf16>(b[j], v[i], sum[i][j]), of[i] == a);
                         __builtin_amdgcn_sched_barrier(0);  // (one tile's sums twice, not all)
                     }
             }
@@ -818,11 +846,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
     constexpr int kStages = kTM == 1 ? 4 : 5;
     constexpr int kShare = kFewWaves / kTM;   // wavefronts to a tile
     constexpr int kHeld = 4;                  // operands of adapters (16 ranks x 32 columns) that are loaded ahead
-    constexpr int kInner = kStages * kRows * 256, kInnerRow = ST_MAX_RANK + 8, kPower = kInner + 32 * kTM * kInnerRow * 2;
-    constexpr int kParts = kPower + 32 * kTM * 4;
+    // the sums and the inner values (first halves and second halves of a row) take the place of the steps
+    constexpr int kSteps = kStages * kRows * 256, kInner = kFewWaves * kTM * 4096, kLow = ST_MAX_RANK, kInnerRow = 2 * ST_MAX_RANK + 8;
+    static_assert(kInner + 32 * kTM * kInnerRow * 2 <= kSteps, "they fit");
+    constexpr int kPower = kSteps, kParts = kPower + 32 * kTM * 4;
     // (one array for all, read as int4v: beside another, or read as a struct, the compiler has the reads of a step wait for the loads of later ones)
     __shared__ __align__(1024) int8_t lds[kParts + (kWithInner ? kInnerParts * kFusedRanks * 4 : 0)];
-    static_assert(kInner >= kFewWaves * kTM * 4096, "the sums take the place of the steps");
     int32_t(*s_dot)[kTM][1024] = (int32_t(*)[kTM][1024])lds;
     uint16_t(*s_inner)[kInnerRow] = (uint16_t(*)[kInnerRow])(lds + kInner);
     float* s_power = (float*)(lds + kPower);
@@ -955,6 +984,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
         for (int i = 0; i < kTM; ++i) dot[i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv, *(const int4v*)(held + i * 32 * 256), dot[i], 0, 0, 0);
         stage = stage + 1 == kStages ? 0 : stage + 1;
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the steps are read, and nothing is on its way to them
     if (p.a) {
         // the inner values: their parts summed in order, the power of two of the largest, rounding
         const float factor = alpha * part_scale;
@@ -979,10 +1009,16 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
         const float down = __uint_as_float((254u - e) << 23);
 #pragma unroll
         for (int t = 0; t < kTurns; ++t)
-            if (2 * t * kWide < 16 * ranks16) *(uint32_t*)&s_inner[m][2 * (t * kWide + l)] = two_16<kBf16>(v[t].x * down, v[t].y * down);
+            if (2 * t * kWide < 16 * ranks16) {
+                uint16_t h[4];
+                two_halves<kBf16>(v[t].x * down, h, h + 2);
+                two_halves<kBf16>(v[t].y * down, h + 1, h + 3);
+                uint16_t* at = &s_inner[m][2 * (t * kWide + l)];
+                *(uint32_t*)at = h[0] | (uint32_t)h[1] << 16;
+                *(uint32_t*)(at + kLow) = h[2] | (uint32_t)h[3] << 16;
+            }
         if (l == 0) s_power[m] = has ? __uint_as_float(e << 23) : 1.0f;
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the steps are read, and nothing is on its way to them
 #pragma unroll
     for (int i = 0; i < kTM; ++i)
 #pragma unroll
@@ -1004,9 +1040,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
 #pragma unroll
     for (int u = 0; u < 16; ++u) sum[0][u] = (float)s_dot[0][tile][u / 4 * 256 + lane * 4 + u % 4] * down * ws[0][u / 4][u % 4];
     auto add = [&](int a, int at, const uint4& b) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (adapter == a) v = *(const uint4*)&s_inner[row][at * 16 + (lane >> 5) * 8];
-        sum[0] = project_with(sum[0], mfma_32<kBf16>(b, v, sum[0]), adapter == a);
+        InnerValues v = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (adapter == a) {
+            const uint16_t* mine = &s_inner[row][at * 16 + (lane >> 5) * 8];
+            v = {*(const uint4*)mine, *(const uint4*)(mine + kLow)};
+        }
+        sum[0] = project_with(sum[0], project_inner_products<kBf16>(b, v, sum[0]), adapter == a);
     };
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
