@@ -511,9 +511,10 @@ typedef struct st_adapters {
  *   dev_adapter_of  int32 [n_rows]; a number that no adapter has means none.  Rows may be in any order; equal neighbours share loads
  *   dev_out         rows of n values of dtype (ST_BF16, ST_F16), out_stride elements apart (a multiple of 8, at least n), apart from the inputs
  *   workspace       st_project_workspace_bytes() bytes, 256-byte aligned, scratch
- * The first sum is exact (int32).  The inner values of an adapter, dot(a, x), are summed in fp32, divided by the power of two
- * that leaves the largest of a row's in [1, 2) (2^-100 to 2^100; 1 where the largest is below), and held as the sum of two numbers of dtype, by both of which b
- * is multiplied (bf16: off by 2^-16 of an inner value at most; fp16: by 2^-22, and 2^-25 of the row's largest); all else is fp32, and outputs are rounded once.
+ * The first sum is exact (int32).  The inner values of an adapter, dot(a, x), are summed in fp32, divided by a power of two (fp16: the one that leaves the largest
+ * of a row's in [1, 2), from 2^-100 to 2^120, 1 where the largest is below; bf16: 1, but 2 from 2^127 on), and held as the sum of two numbers of dtype, by both
+ * of which b is multiplied (bf16: off by 2^-16 of an inner value at most; fp16: by 2^-22, and 2^-25 of the row's largest); all else is fp32, the two terms are
+ * added where they are divided by that power (fp16: off by 2^-30 at most for it), and outputs are rounded once.  Neither term leaves fp32 for the size of the other.
  * k and n are multiples of 16, k at most ST_MAX_ROW, n at most ST_MAX_OUT, n_rows >= 0.  Arrays 16-byte aligned (dev_x_scale, dev_adapter_of 4).
  * A row's result does not depend on the other rows, nor on adapters that are not its own, whatever these hold.  A row whose x_scale is no
  * number gives none.  Asynchronous, no allocation. */

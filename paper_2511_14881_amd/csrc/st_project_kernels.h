@@ -244,11 +244,16 @@ struct InnerPart {
     }
 };
 
-// The power of two of a row's largest inner value (its bits), kept within what can be inverted; 1 where there is none or it is no number.
+// The exponent (with its bias) of the power of two 2^e that a row's inner values are divided by, and with them what they are added to, from the bits
+// of the largest.  Neither term may leave fp32 for the other's sake.  bf16 has fp32's range: 1, but 2 where rounding up could leave it.  fp16: the
+// largest's own, from 2^-100 (sums of products that leave fp32 by it, from 2^28 on, are beyond fp16 in any case) to 2^120 (they are off by
+// 2^-30 then, 2^-25 being half of fp16's least); 1 where the largest is below or no number.
+template <bool kBf16>
 __device__ inline uint32_t project_exponent(uint32_t top)
 {
     const uint32_t e = top >> 23;
-    return e < 27 || e == 255 ? 127u : min(e, 227u);
+    if (kBf16) return e == 254 ? 128u : 127u;
+    return e < 27 || e == 255 ? 127u : min(e, 247u);
 }
 
 // A number as the sum of two 16-bit ones: rounded, and what the rounding left, rounded (nothing beside an infinity).
@@ -449,7 +454,7 @@ __global__ __launch_bounds__(kInnerParts * 64) void project_inner_kernel(Project
             top = max(top, row_ror<2>(top));
             top = max(top, row_ror<1>(top));
             const auto both = __builtin_amdgcn_permlane16_swap(top, top, false, false);
-            const uint32_t e = project_exponent(max((uint32_t)both[0], (uint32_t)both[1]));
+            const uint32_t e = project_exponent<kBf16>(max((uint32_t)both[0], (uint32_t)both[1]));
             const float down = __uint_as_float((254u - e) << 23);
 #pragma unroll
             for (int c = 0; c < kEach; ++c) {
@@ -489,9 +494,11 @@ __global__ __launch_bounds__(64) void project_parts_kernel(ProjectArgs p)
 // n0 + 8 * (u / 4) + 4 * (l / 32) + u % 4 for u < 16.  The sums of products take on scales and the adapters' part in the same registers.
 struct ProjectRow {
     int row, adapter;
-    float scale;  // x_scale / 2^e
+    float scale;  // x_scale, bf16: divided by 2^e
     float power;  // 2^e
 };
+// 1 / 2^e.  fp16: the sums of products with both scales are divided by it, since x_scale / 2^e by itself could be beyond fp32.
+__device__ inline float project_inverse(float power) { return __uint_as_float(0x7F000000u - __float_as_uint(power)); }
 
 // The halves of eight of a row's inner values, from rank r on; zeros for a row of another adapter and behind the last rank.
 struct InnerValues {
@@ -799,8 +806,9 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
                     mine[i].adapter = of;
                     mine[i].power = __int_as_float(word(kPower, m));
                 }
-                mine[i].scale *= __uint_as_float(0x7F000000u - __float_as_uint(mine[i].power));
             }
+            const float inverse = project_inverse(mine[i].power);
+            if (kBf16) mine[i].scale *= inverse;
 #pragma unroll
             for (int j = 0; j < kTN; ++j)
 #pragma unroll
@@ -809,6 +817,11 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
 #pragma unroll
                     for (int u = 0; u < 4; ++u) sum[i][j][4 * g + u] = (float)dot[i0 + i][j][4 * g + u] * mine[i].scale * __int_as_float(ws[u]);
                 }
+            if (!kBf16 && p.a)
+#pragma unroll
+                for (int j = 0; j < kTN; ++j)
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) sum[i][j][u] *= inverse;
         }
         if (p.a) project_add_adapters<kBf16, kAtOnce, kTN>(p, sum, mine, n0 + wn);
 #pragma unroll
@@ -1005,7 +1018,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
             top = max(top, max(__float_as_uint(v[t].x) & 0x7FFFFFFFu, __float_as_uint(v[t].y) & 0x7FFFFFFFu));
         }
         for (int o = kWide / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-        const uint32_t e = project_exponent(top);
+        const uint32_t e = project_exponent<kBf16>(top);
         const float down = __uint_as_float((254u - e) << 23);
 #pragma unroll
         for (int t = 0; t < kTurns; ++t)
@@ -1035,10 +1048,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void project_few_kernel(ProjectArgs
         *at = d;
     }
     __syncthreads();
-    const float power = p.a ? s_power[row] : 1.0f, down = scale * __uint_as_float(0x7F000000u - __float_as_uint(power));
+    const float power = p.a ? s_power[row] : 1.0f, inverse = project_inverse(power), x_scale = kBf16 ? scale * inverse : scale;
     float16v sum[1];
 #pragma unroll
-    for (int u = 0; u < 16; ++u) sum[0][u] = (float)s_dot[0][tile][u / 4 * 256 + lane * 4 + u % 4] * down * ws[0][u / 4][u % 4];
+    for (int u = 0; u < 16; ++u) sum[0][u] = (float)s_dot[0][tile][u / 4 * 256 + lane * 4 + u % 4] * x_scale * ws[0][u / 4][u % 4] * (kBf16 ? 1.0f : inverse);
     auto add = [&](int a, int at, const uint4& b) {
         InnerValues v = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
         if (adapter == a) {

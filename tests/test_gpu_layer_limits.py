@@ -1,4 +1,5 @@
-"""The operators of a layer around the cached histories where their numbers end: inner values that cancel.
+"""The operators of a layer around the cached histories where their numbers end: inner values that cancel, adapters of any size beside their
+row's own.
 Bounds: layer_reference, or derived here."""
 import numpy as np
 import pytest
@@ -45,3 +46,50 @@ def test_projection_of_inner_values_that_cancel(n_rows, dtype):
         over = np.abs(got[rows] - want) - off - half * (np.abs(want) + off) - R.least(dtype)
         assert not rows.any() or over.max() <= 0, f"{over.max()} over the bound"
     assert (got[of < 0] == 0).all()
+
+
+# ---------------------------------------------------------------- adapters of any size beside their row's own
+FAR = {  # exponents: of the smallest and largest scale of a row, of the weights' scales, of the adapters' factors
+    "bf16": [(6, 20, -14, (-106, -120, -149, -60, 0, 60)), (0, 20, 40, (-106, -120, -149, -60, 0, 60)), (-30, 0, -14, (-106, -120, -149, -60, 0, 60))],
+    "f16": [(6, 20, -35, (-106, -120, -149, -60, -40, -31)), (60, 80, -95, (-106, -120, -149, -100, -95, -91)), (-30, 0, -16, (-106, -120, -149, -60, -30, -9))],
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n_rows", ROUTES)
+def test_projection_with_adapters_far_below_and_above(n_rows, dtype):
+    """Inner values from 2^-130 to 2^100 beside sums of products from 2^-30 to 2^80: neither term leaves fp32 for the other's sake."""
+    say(f"[layer] adapters far below and above, {n_rows} rows, {dtype}")
+    rng = np.random.default_rng(100 + n_rows)
+    k, n, rank, count = 256, 64, 8, 6
+    x, w = torch.full((n_rows, k), 127, dtype=torch.int8), integers(rng, n, k)
+    w[0] = 127
+    a = torch.from_numpy(rng.uniform(0.5, 1.0, (count, rank, k)).astype(np.float32)).to(R.TYPES[dtype])
+    b = torch.from_numpy(rng.normal(0, 1, (count, n, rank)).astype(np.float32)).to(R.TYPES[dtype])
+    of = torch.from_numpy(rng.integers(-1, count, n_rows).astype(np.int32))
+    for low, high, weight, factors in FAR[dtype]:
+        alpha = torch.from_numpy(np.ldexp(1.0, factors).astype(np.float32))
+        xs = torch.from_numpy(np.ldexp(1.0, rng.integers(low, high + 1, n_rows)).astype(np.float32))
+        args = (x, xs, w, torch.full((n,), 2.0 ** weight), a, b, alpha, of)
+        got = call(args).double().cpu().numpy()
+        want, bound = R.project(*args, dtype=dtype)
+        assert np.isfinite(got).all()
+        over = np.abs(got - want) - bound
+        assert over.max() <= 0, f"{over.max()} over the bound, scales 2^{low} to 2^{high}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n_rows", ROUTES)
+def test_projection_beside_an_adapter_that_adds_nothing(n_rows, dtype):
+    """b = 0, as before the first step of its training: the outputs are those without the adapter, however large its inner values are."""
+    say(f"[layer] adapters that add nothing, {n_rows} rows, {dtype}")
+    rng = np.random.default_rng(200 + n_rows)
+    k, n, rank, count = 128, 48, 8, 6
+    x, w = integers(rng, n_rows, k), integers(rng, n, k)
+    xs, ws = torch.full((n_rows,), 2.0 ** -8), torch.full((n,), 2.0 ** -8)
+    a = torch.from_numpy(rng.integers(32, 65, (count, rank, k)).astype(np.float32)).to(R.TYPES[dtype])
+    alpha = torch.from_numpy(np.ldexp(1.0, [-149, -100, 0, 90, 110, 113]).astype(np.float32))
+    of = torch.from_numpy((np.arange(n_rows) % count).astype(np.int32))
+    want = call((x, xs, w, ws), dtype=R.TYPES[dtype])
+    got = call((x, xs, w, ws, a, torch.zeros((count, n, rank), dtype=R.TYPES[dtype]), alpha, of))
+    assert torch.equal(got, want)
