@@ -510,7 +510,7 @@ typedef struct st_adapters {
  *   adapters        NULL (no second term; dev_adapter_of is NULL too)
  *   dev_adapter_of  int32 [n_rows]; a number that no adapter has means none.  Rows may be in any order; equal neighbours share loads
  *   dev_out         rows of n values of dtype (ST_BF16, ST_F16), out_stride elements apart (a multiple of 8, at least n), apart from the inputs
- *   workspace       st_project_workspace_bytes() bytes, 256-byte aligned, scratch
+ *   workspace       st_project_workspace_bytes() bytes (enough for every call of as many rows or fewer), 256-byte aligned, scratch
  * The first sum is exact (int32).  The inner values of an adapter, dot(a, x), are summed in fp32, divided by a power of two (fp16: the one that leaves the largest
  * of a row's in [1, 2), from 2^-100 to 2^120, 1 where the largest is below; bf16: 1, but 2 from 2^127 on), and held as the sum of two numbers of dtype, by both
  * of which b is multiplied (bf16: off by 2^-16 of an inner value at most; fp16: by 2^-22, and 2^-25 of the row's largest); all else is fp32, the two terms are

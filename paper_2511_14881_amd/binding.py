@@ -971,7 +971,7 @@ class Adapters:
 
 
 class ProjectBuffers:
-    """Output and workspace of repeated st_project calls of one shape, one at a time."""
+    """Output and workspace of repeated st_project calls of one shape, one at a time; of fewer rows too where the call names its out."""
 
     def __init__(self, n_rows: int, k: int, n: int, dtype=torch.bfloat16, adapters: Adapters | None = None, device="cuda"):
         self.nbytes = st_project_workspace_bytes(n_rows, k, n, adapters)

@@ -72,11 +72,12 @@ int check_project(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapt
 // of 128 33.0 / 35.5; 128 rows, 512, 4096 6.7 / 7.0, 16.8 / 13.0.  In more than one round: 96 rows, k = 4096, n = 5120 10.6 / 14.8; of more rows:
 // 1024, 4096, 256, 36 adapters of rank 16 24.6 / 36.3.
 constexpr int kFewRows = 64, kFewMost = 384, kFewRanks = 24576;  // of all rows
-bool project_few(int32_t n_rows, int32_t n, const st_adapters* a)
+int32_t project_most_few(int32_t n, const st_adapters* a)
 {
-    if (n_rows <= kFewRows) return true;
-    return n_rows <= kFewMost && (n_rows + kFewRows - 1) / kFewRows * ((n + 31) / 32) <= st::kComputeUnits && (!a || n_rows * a->rank <= kFewRanks);
+    const int32_t most = std::min(kFewMost, st::kComputeUnits / ((n + 31) / 32) * kFewRows);
+    return std::max(kFewRows, a ? std::min(most, kFewRanks / a->rank) : most);
 }
+bool project_few(int32_t n_rows, int32_t n, const st_adapters* a) { return n_rows <= project_most_few(n, a); }
 
 // Rows up to which a workgroup that sums inner values takes 16, beyond 32.  Kernel in us, 16 / 32 / 64: 2048 rows, k = 4096, rank 16 9.9 / 11.7 /
 // 17.4; 4096, 1024, 64 14.5 / 13.9 / 18.7; 16384, 4096, 32 57 / 36 / 39.
@@ -101,6 +102,14 @@ ProjectPlan project_plan(int32_t n_rows, int32_t n, const st_adapters* adapters)
     const int64_t values = (int64_t)n_rows * adapters->rank, words = st::round_up((int64_t)n_rows * 4, 256);
     if (project_few(n_rows, n, adapters)) return {st::round_up(values * 4 * st::kInnerParts, 256), 0, 0};
     return {st::round_up(values * 4, 256), words, project_ordered(n_rows, adapters) ? words : 0};
+}
+
+// Bytes that are enough for every call of up to n_rows rows: the few rows' parts take more to a row than what many rows need, so that the most
+// rows that go that way may need more than n_rows do.
+int64_t project_bytes(int32_t n_rows, int32_t n, const st_adapters* adapters)
+{
+    const int32_t few = std::min(n_rows, project_most_few(n, adapters));
+    return std::max(project_plan(n_rows, n, adapters).bytes(), project_plan(few, n, adapters).bytes());
 }
 
 // Edge of the tiles of many rows by an estimate of the call's microseconds.  64 (three workgroups to a compute unit): the longer of one
@@ -215,7 +224,7 @@ int64_t st_project_workspace_bytes(int32_t n_rows, int32_t k, int32_t n, const s
 {
     int rc;
     if ((rc = check_project(n_rows, k, n, adapters))) return rc;
-    return std::max<int64_t>(256, project_plan(n_rows, n, adapters).bytes());
+    return std::max<int64_t>(256, project_bytes(n_rows, n, adapters));
 }
 
 int st_project(const int8_t* dev_x, const float* dev_x_scale, int32_t n_rows, int32_t k, const int8_t* dev_w,

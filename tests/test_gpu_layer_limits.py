@@ -93,3 +93,20 @@ def test_projection_beside_an_adapter_that_adds_nothing(n_rows, dtype):
     want = call((x, xs, w, ws), dtype=R.TYPES[dtype])
     got = call((x, xs, w, ws, a, torch.zeros((count, n, rank), dtype=R.TYPES[dtype]), alpha, of))
     assert torch.equal(got, want)
+
+
+# ---------------------------------------------------------------- workspaces of more rows
+def test_buffers_of_more_rows_serve_fewer():
+    """192 rows of rank 128 need more than 500 or 2000 do by their own route."""
+    rng = np.random.default_rng(300)
+    k, n, rank, count, rows = 272, 144, 128, 4, 2000
+    args = (integers(rng, rows, k), torch.full((rows,), 2.0 ** -6), integers(rng, n, k), torch.full((n,), 2.0 ** -6),
+            torch.from_numpy(rng.normal(0, 1, (count, rank, k)).astype(np.float32)).bfloat16(),
+            torch.from_numpy(rng.normal(0, 1, (count, n, rank)).astype(np.float32)).bfloat16(), torch.ones(count),
+            torch.from_numpy((np.arange(rows) % count).astype(np.int32)))
+    x, xs, w, ws, a, b, alpha, of = (t.cuda() for t in args)
+    adapters = st.Adapters(a, b, alpha)
+    buffers = st.ProjectBuffers(rows, k, n, torch.bfloat16, adapters)
+    for m in (1, 64, 192, 193, 500, 2000):
+        some = x[:m], xs[:m], w, ws, adapters, of[:m]
+        assert torch.equal(st.st_project(*some, out=buffers.out[:m], buffers=buffers), st.st_project(*some))
