@@ -476,8 +476,8 @@ int st_kv_copy(const st_kv_cache* from, const st_kv_cache* to, const int32_t* de
  *   q     = rint(t / u) kept in [-127, 127]          ties to even, the quotient rounded to fp32; 0 where u is 0
  *   rms   = 1 / sqrt(mean of h * h + eps)            1 where normalise is 0
  *   scale = u * rms,  y = t * rms rounded to dtype
- * The integers do not contain the mean, so that they are bit-exact whatever order its sum has.  Rows with squares beyond fp32's
- * range are formed with h / 2^70 throughout.  A row in which an h or a t is infinite or no number gives q = 0, scale = NaN, y = NaN.
+ * The integers do not contain the mean, so that they are bit-exact whatever order its sum has.  Rows whose squares' sum
+ * reaches 2^120 are formed with h / 2^80 throughout (where normalise is not 0).  A row in which an h or a t is infinite or no number gives q = 0, scale = NaN, y = NaN.
  *   dev_x, dev_residual  rows of d values of dtype (ST_BF16, ST_F16, ST_F32), strides in elements: multiples of 8, at least d
  *   dev_weight           [d] of dtype, or NULL
  *   dev_out_sum          h, rows sum_stride apart, or NULL; may be dev_x or dev_residual with the same stride

@@ -179,18 +179,18 @@ __global__ __launch_bounds__(kLayerThreads) void norm_rows_kernel(NormArgs a)
     if (a.normalise) {
         sum = sum_of_lanes<kLanes>(sum, s_sum);
         float eps = a.eps;
-        if (!(sum < 0x1p120f)) {  // (not for NaN either, which stays one)
+        if (!(sum < 0x1p120f)) {  // (not for NaN either, which stays one); ST_MAX_ROW squares of up to 2^96 are below 2^128
             sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < kVectors; ++i)
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    h[i][u] *= 0x1p-70f;
+                    h[i][u] *= 0x1p-80f;
                     sum += h[i][u] * h[i][u];
                 }
             if (kLanes == 256) __syncthreads();  // the words of the sum before are read
             sum = sum_of_lanes<kLanes>(sum, s_sum);
-            eps = 0.0f;  // (eps / 2^140 beside at least 2^-34)
+            eps = 0.0f;  // (eps / 2^160 beside at least 2^-54)
         }
         rms = 1.0f / __fsqrt_rn(sum / (float)a.d + eps);
     }

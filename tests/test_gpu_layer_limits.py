@@ -1,5 +1,5 @@
 """The operators of a layer around the cached histories where their numbers end: inner values that cancel, adapters of any size beside their
-row's own.
+row's own, rows at the end of a type.
 Bounds: layer_reference, or derived here."""
 import numpy as np
 import pytest
@@ -7,7 +7,7 @@ import torch
 
 from paper_2511_14881_amd import binding as st
 from tests import layer_reference as R
-from tests.test_gpu_layer import call, integers, say
+from tests.test_gpu_layer import call, integers, rows_of, say
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,44 @@ def test_buffers_of_more_rows_serve_fewer():
     for m in (1, 64, 192, 193, 500, 2000):
         some = x[:m], xs[:m], w, ws, adapters, of[:m]
         assert torch.equal(st.st_project(*some, out=buffers.out[:m], buffers=buffers), st.st_project(*some))
+
+
+# ---------------------------------------------------------------- rows at the end of a type
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [2048, 4208, 8192, 16384])
+def test_norm_of_rows_of_the_largest_numbers(d, dtype):
+    """All values near the type's largest, rows in which squares alone leave fp32, and rows on both sides of where they do."""
+    say(f"[layer] norm of the largest numbers, {d}, {dtype}")
+    rng = np.random.default_rng(d)
+    top = float(torch.finfo(R.TYPES[dtype]).max)
+    sign = torch.from_numpy(rng.choice([-1.0, 1.0], (6, d)))
+    x = sign * top
+    x[1] = sign[1] * 2.0 ** 100
+    x[2, 1:] = 0.0
+    x[3] = sign[3] * 2.0 ** 63
+    x[4] = sign[4] * 2.0 ** 52
+    x[5] = torch.from_numpy(rng.uniform(-top, top, d))
+    x = x.to(R.TYPES[dtype])
+    weight = rows_of(rng, 1, d, dtype)[0].contiguous()
+    for w in (None, weight):
+        got = st.st_norm_rows(x.cuda(), None if w is None else w.cuda(), y=True)
+        small = (x.double() * 2.0 ** -50).to(x.dtype)  # exact; beside the squares eps is nothing
+        _, q, unit, _, t = R.norm(small, w, None, 1e-6, True)
+        rms = 1.0 / np.sqrt(np.square(small.double().numpy()).mean(1))
+        assert np.array_equal(got.q.cpu().numpy(), q)
+        off = R.norm_bound(d)
+        assert np.all(np.abs(got.scale.cpu().numpy() - unit * rms) <= off * unit * rms)
+        want = t * rms[:, None]
+        assert np.all(np.abs(got.y.double().cpu().numpy() - want) <= np.abs(want) * (R.half_step(dtype) + 2 * off) + R.least(dtype))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 2064), ("f32", 2064), ("f16", 6160), ("bf16", 16384)])
+def test_norm_in_place_by_256_threads_to_a_row(dtype, d):
+    rng = np.random.default_rng(d)
+    x, r = rows_of(rng, 7, d, dtype), rows_of(rng, 7, d, dtype)
+    weight = rows_of(rng, 1, d, dtype)[0].cuda()
+    want = st.st_norm_rows(x.cuda(), weight, r.cuda())
+    for place in ("x", "residual"):
+        a, b = x.cuda(), r.cuda()
+        got = st.st_norm_rows(a, weight, b, total=a if place == "x" else b)
+        assert torch.equal(got.total, want.total) and torch.equal(got.q, want.q) and torch.equal(got.scale, want.scale)
