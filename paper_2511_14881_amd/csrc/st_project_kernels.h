@@ -322,7 +322,12 @@ struct InnerStream {
 #pragma unroll
         for (int t = 0; t < kGroup; ++t) {
             const int8_t* row = at + kM * 1024 + (t * 16 + (lane & 15)) * 128;
-            const int4v v0 = *(const int4v*)(row + rank_place(lane & 15, 2 * piece) * 16), v1 = *(const int4v*)(row + rank_place(lane & 15, 2 * piece + 1) * 16);
+            int4v v0 = *(const int4v*)(row + rank_place(lane & 15, 2 * piece) * 16), v1 = *(const int4v*)(row + rank_place(lane & 15, 2 * piece + 1) * 16);
+            if (chunk * 64 + 64 > k) {  // (there too: 0 times an infinity is no number)
+                const int in = chunk * 64 + piece * 16 < k ? -1 : 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v0[u] &= in, v1[u] &= in;
+            }
             const uint4 a0 = make_uint4(v0[0], v0[1], v0[2], v0[3]), a1 = make_uint4(v1[0], v1[1], v1[2], v1[3]);
 #pragma unroll
             for (int i = 0; i < kM; ++i) {

@@ -1,5 +1,5 @@
 """The operators of a layer around the cached histories where their numbers end: inner values that cancel, adapters of any size beside their
-row's own, rows at the end of a type.
+row's own, rows at the end of a type, values behind the last of k.
 Bounds: layer_reference, or derived here."""
 import numpy as np
 import pytest
@@ -151,3 +151,25 @@ def test_norm_in_place_by_256_threads_to_a_row(dtype, d):
         a, b = x.cuda(), r.cuda()
         got = st.st_norm_rows(a, weight, b, total=a if place == "x" else b)
         assert torch.equal(got.total, want.total) and torch.equal(got.q, want.q) and torch.equal(got.scale, want.scale)
+
+
+# ---------------------------------------------------------------- values behind the last of k
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rank", [8, 24, 40, 128])
+def test_infinite_adapter_at_the_last_values_of_k(rank, dtype):
+    """A row's bits do not go by the number of rows beside it, where its adapter holds an infinity among the last values of k either."""
+    say(f"[layer] infinity at the last values of k, rank {rank}, {dtype}")
+    rng = np.random.default_rng(rank)
+    k, n, rows = 80, 32, 2100
+    x = integers(rng, rows, k).abs().clamp(1, 127)
+    args = [x, torch.full((rows,), 2.0 ** -6), integers(rng, n, k), torch.full((n,), 2.0 ** -8)]
+    a = torch.from_numpy(rng.normal(0, 1, (3, rank, k)).astype(np.float32)).to(R.TYPES[dtype])
+    a[0, 0, 64], a[1, rank - 1, 71], a[2, 3, 72] = float("inf"), float("-inf"), float("inf")
+    b = torch.from_numpy(rng.uniform(0.5, 1, (3, n, rank)).astype(np.float32)).to(R.TYPES[dtype])
+    of = torch.from_numpy((np.arange(rows) % 3).astype(np.int32))
+    got = call((*args, a, b, torch.ones(3), of))
+    for m in (1, 20, 100, 500):
+        few = call((args[0][:m], args[1][:m], *args[2:], a, b, torch.ones(3), of[:m]))
+        assert torch.equal(few.view(torch.int16), got[:m].view(torch.int16))
+    sign = torch.tensor([1.0, -1.0, 1.0], device="cuda")[of.cuda().long()]
+    assert (got.float() == sign[:, None] * float("inf")).all()
