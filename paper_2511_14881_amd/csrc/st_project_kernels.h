@@ -811,9 +811,8 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
                     mine[i].adapter = of;
                     mine[i].power = __int_as_float(word(kPower, m));
                 }
+                if (kBf16) mine[i].scale *= project_inverse(mine[i].power);
             }
-            const float inverse = project_inverse(mine[i].power);
-            if (kBf16) mine[i].scale *= inverse;
 #pragma unroll
             for (int j = 0; j < kTN; ++j)
 #pragma unroll
@@ -826,7 +825,7 @@ __global__ __launch_bounds__(kWM* kWN * 64) void project_tile_kernel(ProjectArgs
 #pragma unroll
                 for (int j = 0; j < kTN; ++j)
 #pragma unroll
-                    for (int u = 0; u < 16; ++u) sum[i][j][u] *= inverse;
+                    for (int u = 0; u < 16; ++u) sum[i][j][u] *= project_inverse(mine[i].power);
         }
         if (p.a) project_add_adapters<kBf16, kAtOnce, kTN>(p, sum, mine, n0 + wn);
 #pragma unroll
