@@ -38,6 +38,7 @@ class HistoryStore:
         self.mass = torch.zeros((n_users, n_heads, max_blocks), dtype=torch.float32, device="cuda")
         self.free = list(range(n_pages - 1, -1, -1))
         self.shares = np.zeros(n_pages, np.int32)  # histories that hold a page
+        self.forked = False  # whether there may be more than one to a page
 
     def _known(self, users, once: bool = False) -> np.ndarray:
         """The users as an array of indices.  once: none may be named twice, since the call writes to their histories."""
@@ -81,28 +82,33 @@ class HistoryStore:
         if need.size and need.max() > self.max_blocks:
             raise ValueError(f"a history would hold {need.max()} blocks of at most {self.max_blocks}: evict first")
         # where the block that the first event goes to is shared, the history gets a copy of its own; the last holder keeps the page
-        shares, copied = self.shares.copy(), []
-        tails = tables[np.arange(len(users)), np.maximum(have - 1, 0)]
-        for i in np.flatnonzero((lengths % st.ST_KV_BLOCK > 0) & (counts > 0) & (self.shares[tails] > 1)):
-            if shares[tails[i]] > 1:
-                shares[tails[i]] -= 1
-                copied.append((i, tails[i]))
+        left, copied = {}, []  # of such pages, the histories that still hold them
+        if self.forked:
+            tails = tables[np.arange(len(users)), np.maximum(have - 1, 0)]
+            for i in np.flatnonzero((lengths % st.ST_KV_BLOCK > 0) & (counts > 0) & (self.shares[tails] > 1)):
+                holders = left.get(tails[i], self.shares[tails[i]])
+                if holders > 1:
+                    left[tails[i]] = holders - 1
+                    copied.append((i, tails[i]))
         taken = int((need - have).sum()) + len(copied)
         if taken > len(self.free):
             raise ValueError(f"{taken} pages are needed, {len(self.free)} are free: evict first")
-        pages = iter(self.free[len(self.free) - taken:][::-1])
+        new = self.free[len(self.free) - taken:][::-1]
+        pages = iter(new)
         for row, a, b in zip(tables, have, need):
             for block in range(a, b):
                 row[block] = next(pages)
-                shares[row[block]] = 1
         if copied:
             for i, _ in copied:
                 tables[i, have[i] - 1] = next(pages)
-                shares[tables[i, have[i] - 1]] = 1
             self._copy(self.cache, self.cache, [page for _, page in copied], [tables[i, have[i] - 1] for i, _ in copied])
         lengths = (lengths + counts).astype(np.int32)
         st.st_kv_append(self.cache, self._view(tables, lengths, counts), k, v)
-        self.tables[users], self.lengths[users], self.shares = tables, lengths, shares
+        self.tables[users], self.lengths[users] = tables, lengths
+        if new:
+            self.shares[new] = 1
+        for page, holders in left.items():
+            self.shares[page] = holders
         del self.free[len(self.free) - taken:]
 
     def attend(self, users, q, counts, n_sel: int = 0, sink: int = 0, recent: int = 0, causal: bool = False, track: bool = False,
@@ -165,6 +171,7 @@ class HistoryStore:
         self.tables[to], self.lengths[to] = self.tables[users], self.lengths[users]
         held = self.tables[to]
         np.add.at(self.shares, held[held >= 0], 1)
+        self.forked = True
         self.mass[torch.from_numpy(to).cuda()] = self.mass[torch.from_numpy(users).cuda()]
 
     def release(self, users) -> int:
