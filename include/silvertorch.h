@@ -540,7 +540,7 @@ int st_project_host_plan(int32_t n_rows, int32_t k, int32_t n, const st_adapters
  *   dev_freqs       fp64 [pairs], radians to a position, |freq| <= 2 pi
  *   dev_out_q, dev_out_k  rows like dev_q and dev_k, apart from each other; either may be its input with the same stride
  * d is a multiple of 8, at most 512; pairs a multiple of 8, 8 <= pairs <= d / 2; 1 <= n_axes <= ST_MAX_AXES; sections >= 0.
- * Angles are formed and reduced in fp64 (off by |angle| 2^-52 at most), cos and sin are the hardware's with fp32 turns (2^-22 at most; the
+ * Angles are formed and reduced in fp64 (off by 1.3 |angle| 2^-52 at most), cos and sin are the hardware's with fp32 turns (2^-22 at most; the
  * outputs' roundings are 2^-8 and 2^-11), products are fp32 and rounded once.  The inverse is also the gradient's way back.  One kernel, asynchronous, no allocation. */
 #define ST_MAX_AXES 8
 int st_rotate(const void* dev_q, int64_t q_stride, int32_t n_q_heads, const void* dev_k, int64_t k_stride, int32_t n_k_heads,

@@ -1,6 +1,8 @@
 """The operators of a layer around the cached histories where their numbers end: inner values that cancel, adapters of any size beside their
-row's own, rows at the end of a type, values behind the last of k.
+row's own, rows at the end of a type, values behind the last of k, positions far from the first.
 Bounds: layer_reference, or derived here."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -173,3 +175,27 @@ def test_infinite_adapter_at_the_last_values_of_k(rank, dtype):
         assert torch.equal(few.view(torch.int16), got[:m].view(torch.int16))
     sign = torch.tensor([1.0, -1.0, 1.0], device="cuda")[of.cuda().long()]
     assert (got.float() == sign[:, None] * float("inf")).all()
+
+
+# ---------------------------------------------------------------- positions far from the first
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotation_of_far_positions(inverse):
+    """Sines and cosines off by 2^-22, and by 1.3 * 2^-52 of the angle, of which there are up to 2^33.6; angles reduced here in 200 bits."""
+    say("[layer] rotation of far positions")
+    rng = np.random.default_rng(17)
+    n, d, pairs = 96, 64, 32
+    pos = np.concatenate([rng.integers(-2 ** 31, 2 ** 31, n - 34), [2 ** 31 - 1, -2 ** 31], rng.integers(0, 2000, 32)]).astype(np.int32)
+    freqs = np.concatenate([rng.uniform(np.pi, 2 * np.pi, 12), 2 * np.pi / 60 * (60 / 3.2e8) ** (np.arange(20) / 20)])
+    pi = Fraction(314159265358979323846264338327950288419716939937510582097494459, 10 ** 62)
+    angle = np.array([[float(a - 2 * pi * round(a / (2 * pi))) for a in (Fraction(int(p)) * Fraction(f) for f in freqs)] for p in pos])
+    off = 2.0 ** -22 + 1.3 * 2.0 ** -52 * np.abs(pos.astype(np.float64)[:, None] * freqs)
+    x = torch.from_numpy(rng.normal(0, 2, (n, 2, d)).astype(np.float32)).half()
+    x[:, 0, pairs:] = 0  # cosines and sines by themselves
+    got = st.st_rotate(x.cuda(), None, torch.from_numpy(pos[None]).cuda(), torch.from_numpy(freqs).cuda(), (pairs,), inverse=inverse)[0].double().cpu().numpy()
+    cos, sin, off = np.cos(angle)[:, None], np.sin(angle)[:, None] * (-1 if inverse else 1), off[:, None]
+    f = x.double().numpy()
+    one, two = f[..., :pairs], f[..., pairs:]
+    for out, want in ((got[..., :pairs], one * cos - two * sin), (got[..., pairs:], one * sin + two * cos)):
+        bound = (np.abs(one) + np.abs(two)) * (off + 3 * R.F32)
+        bound = bound + R.half_step("f16") * (np.abs(want) + bound) + R.least("f16")
+        assert np.all(np.abs(out - want) <= bound), (np.abs(out - want) - bound).max()
