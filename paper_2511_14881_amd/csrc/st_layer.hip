@@ -67,10 +67,10 @@ int check_project(int32_t n_rows, int32_t k, int32_t n, const st_adapters* adapt
 
 // Rows that a workgroup takes where there are few, and rows up to which there may be several such workgroups to 32 columns: as long as the
 // compute units take all of them at once, they need no more time than one, and the adapters' inner values come in over the whole chip, unless
-// those are many.  Calls in us, tiles / this, mixed rows: k = 4096, n = 896, 96 rows without adapters 9.9 / 8.1, 36 adapters of rank 16
-// 29.9 / 16.9, 8 of 128 58 / 30, 384 rows 10.5 / 8.7, 25.2 / 23.3, 53.2 / 53.9; k = n = 512 7.0 / 6.6, 13.6 / 13.1, 21.0 / 24.5; 229 rows, 752, 1568, 20
-// of 128 33.0 / 35.5; 128 rows, 512, 4096 6.7 / 7.0, 16.8 / 13.0.  In more than one round: 96 rows, k = 4096, n = 5120 10.6 / 14.8; of more rows:
-// 1024, 4096, 256, 36 adapters of rank 16 24.6 / 36.3.
+// those are many.  Calls in us, tiles / this, mixed rows: k = 4096, n = 896, 96 rows without adapters 9.8 / 8.2, 36 adapters of rank 16
+// 30.4 / 17.3, 8 of 128 61 / 31, 192 rows 58 / 38, 384 rows 10.3 / 8.5, 26.0 / 23.2, 54.4 / 53.6; 96 rows, k = n = 512 6.6 / 6.5, 19.9 / 11.8, 28.5 / 19.6;
+// 229 rows, 752, 1568, 20 of 128 32.9 / 35.4; 128 rows, 512, 4096 6.6 / 6.4, 18.6 / 12.3.  In more than one round: 96 rows, k = 4096, n = 5120 10.7 / 14.8;
+// of more rows: 1024, 4096, 256, 36 adapters of rank 16 25.1 / 36.8.
 constexpr int kFewRows = 64, kFewMost = 384, kFewRanks = 24576;  // of all rows
 int32_t project_most_few(int32_t n, const st_adapters* a)
 {
@@ -83,9 +83,10 @@ bool project_few(int32_t n_rows, int32_t n, const st_adapters* a) { return n_row
 // 17.4; 4096, 1024, 64 14.5 / 13.9 / 18.7; 16384, 4096, 32 57 / 36 / 39.
 constexpr int kOneTileRows = 2048;
 // Whether rows are brought into the order of their adapters first: each adapter more in a tile costs loads and products by its rank.
-// Calls in us, as they come / ordered, mixed rows: 256 rows, 32 adapters of rank 16 32 / 30; 1001, 5 of 8 17.5 / 16.7, 2 of 32 14.6 / 18.1; 300, 3
-// of 64 14.5 / 16.6; 2048, 8 of 16 95 / 69; 4096, 2 of 16 47 / 52, 2 of 64 61.3 / 60.8, 3 of 32 58 / 52, 16 of 64 103 / 34; 16384, 3 of 32
-// 180 / 157, 16 of 32 791 / 409.  Rows that come in runs pay for it: 1000, 16 adapters 21.9 / 26.7, 16384 373 / 385.
+// Calls in us, as they come / ordered, mixed rows: k = 4096, n = 5120: 256 rows, 32 adapters of rank 16 37.1 / 30.6, 2048, 2 of 16 59.6 / 63.4, 8 of 16
+// 93 / 64, 16384, 3 of 32 428 / 375, 16 of 32 823 / 389; 1040, 1296: 1001, 5 of 8 16.0 / 15.6, 2 of 32 13.4 / 16.9, 300, 3 of 64 14.7 / 14.6; 2048, 2560:
+// 4096, 2 of 16 39.7 / 43.4, 2 of 64 51.3 / 53.9, 3 of 32 51.6 / 46.0, 16384, 3 of 32 167 / 140; 1024, 1024: 4096, 16 of 64 119 / 34.5.  Rows that come in
+// runs pay for it: 1000, 2048, 2560, 16 of 16 22.1 / 26.5, 16384, 4096, 5120, 16 of 32 366 / 372.
 bool project_ordered(int32_t n_rows, const st_adapters* a)
 {
     return a->n_adapters >= 5 || (n_rows > kOneTileRows && (a->n_adapters - 1) * a->rank >= 64);

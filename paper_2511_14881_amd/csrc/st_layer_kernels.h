@@ -126,8 +126,9 @@ struct NormArgs {
 // eight neighbouring values to a vector and kVectors vectors to a thread, so that everything is read and written once.  With residual
 // and sum, bf16: 65536 x 2048 175 us (5.4 TB/s), 32768 x 4096 158 (5.9), 16384 x 8192 163, 1048576 x 128 161 (5.8); fp32 65536 x 1024 150; a
 // copy reaches 5.04.  The same with other threads to a row: 2048 with 128 or 256 183 and 191, 4096 with 64 or 128 172 and 163, 1024 with 16
-// 228, 128 with 16 and more of a row each 267.  Stores past the caches gain 1 to 3 % with 16-bit rows (8000 x 1008 13.8 to
-// 12.6), lose 4 % with fp32 rows, and whoever reads the rows next misses them (64 x 4096 and the projection behind it 14.1 to 15.4): not used.
+// 228, 128 with 16 and more of a row each 267.  Stores past the caches gain 1 to 3 % with 16-bit rows, 5 to 14 % with
+// calls that a cache would hold (8000 x 1008, fp16, with the norm's output 12.2 to 10.6), lose 3 % with fp32 rows, and whoever reads the rows next misses
+// them (64 x 4096 and the projection behind it 14.1 to 15.4): not used.
 template <int kType, int kLanes, int kVectors>
 __global__ __launch_bounds__(kLayerThreads) void norm_rows_kernel(NormArgs a)
 {

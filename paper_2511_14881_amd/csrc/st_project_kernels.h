@@ -256,7 +256,10 @@ __device__ inline uint32_t project_exponent(uint32_t top)
     return e < 27 || e == 255 ? 127u : min(e, 247u);
 }
 
-// A number as the sum of two 16-bit ones: rounded, and what the rounding left, rounded (nothing beside an infinity).
+// A number as the sum of two 16-bit ones: rounded, and what the rounding left, rounded (nothing beside an infinity).  Inner values are held so, and an
+// adapter's products made twice, since one half alone shows in the outputs (bf16, adapters' part as large as the rest: 2^-9.2 of them, and
+// 2^-14 with both, beside plain sums in fp32).  It costs 2 % of a call with rank 32 (16384 x 4096 x 5120, 16 adapters 362 -> 370 us), 8 % with 128
+// (16384 x 4096 x 4096 374 -> 404), nothing with few rows.
 template <bool kBf16>
 __device__ inline void two_halves(float v, uint16_t* high, uint16_t* low)
 {
@@ -656,10 +659,10 @@ __device__ inline void project_store_lines(const ProjectArgs& p, const uint4 (&o
 //
 // Bound by the matrix units and, with the whole chip at work, by its power: 8192 x 8192 x 8192 takes 512 us (2150 TOP/s), the products
 // alone 334, without loads 423, without reads of the LDS 457 (the clock is at 1.8 GHz then, 2.4 with a tenth of the chip, where a
-// step of 256 x 256 takes 1.02 us and its products 0.85).  16384 x 4096 x 5120: 315 us, 2180 TOP/s, with 16 adapters of rank 32 in runs of rows 365
+// step of 256 x 256 takes 1.02 us and its products 0.85).  16384 x 4096 x 5120: 315 us, 2180 TOP/s, with 16 adapters of rank 32 in runs of rows 370
 // in all.  What follows the products takes some 8 us of a tile of 256 x 256, half of it the stores, which all workgroups begin at once.
 // Its rows' and columns' words therefore come with the first steps, and the adapters' operands with one trip for two rows of tiles (16384 x
-// 4096 x 4096 266 us -> 255; with the adapters above 377 -> 365).  Tried: four wavefronts with 128 x 128 each
+// 4096 x 4096 266 us -> 255; with the adapters above 3 %).  Tried: four wavefronts with 128 x 128 each
 // (345 us for 323; fewer reads, but a SIMD waits with its only wavefront), steps of 64 values with four and five stages (356), tiles of
 // 256 x 128 (498), loads and reads in the first half of the products between which they stand (327); all rows of tiles at once behind
 // the products (registers spill); stores past the caches (417 for 348).
