@@ -18,13 +18,14 @@ ROUTES = [2, 20, 100, 600, 2100]
 
 
 # ---------------------------------------------------------------- inner values that cancel
-@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+# the exponents of an adapter's factor and of b: outputs in fp16's range, with inner values of any size (bf16's own least among them)
+@pytest.mark.parametrize("dtype,size,up", [("bf16", -10, 0), ("f16", -10, 0), ("bf16", -121, 110), ("bf16", 90, -90), ("f16", 2, -12)])
 @pytest.mark.parametrize("n_rows", ROUTES)
-def test_projection_of_inner_values_that_cancel(n_rows, dtype):
+def test_projection_of_inner_values_that_cancel(n_rows, dtype, size, up):
     """Ranks in pairs of nearly the same inner value, with opposite signs behind them: what is left of a pair is some 2^-8 of either.  All sums
     before the rounding to two 16-bit halves are of integers below 2^24, with factors that are powers of two, and so exact; the halves leave
     half a step of half a step (and fp16's smallest numbers, whose half step is 2^-25 beside a row's largest value in [1, 2))."""
-    say(f"[layer] cancelling inner values, {n_rows} rows, {dtype}")
+    say(f"[layer] cancelling inner values, {n_rows} rows, {dtype}, 2^{size}, 2^{up}")
     rng = np.random.default_rng(n_rows)
     k, n, rank, count = 64, 48, 8 if n_rows == 2 else 24, 6
     x = integers(rng, n_rows, k)
@@ -34,7 +35,7 @@ def test_projection_of_inner_values_that_cancel(n_rows, dtype):
     b[:, :, 1::2] = -b[:, :, 0::2]
     of = rng.integers(-1, count, n_rows)
     half = R.half_step(dtype)
-    size = -10  # outputs of fp16's range
+    b = b * 2.0 ** up
     args = (x, torch.full((n_rows,), 2.0 ** -6), torch.zeros((n, k), dtype=torch.int8), torch.ones(n), torch.from_numpy(a).to(R.TYPES[dtype]),
             torch.from_numpy(b).to(R.TYPES[dtype]), torch.full((count,), 2.0 ** size), torch.from_numpy(of.astype(np.int32)))
     got = call(args).double().cpu().numpy()
